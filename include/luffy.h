@@ -57,7 +57,11 @@ typedef enum {
   LUFFY_E_HIP = -4          /* a HIP runtime call or launch failed         */
 } luffy_status;
 
-typedef enum { LUFFY_F32 = 0, LUFFY_BF16 = 1 } luffy_dtype;
+typedef enum {
+  LUFFY_F32 = 0,
+  LUFFY_BF16 = 1,
+  LUFFY_MX4 = 2 /* microscaled 4-bit, see luffy_mx4_quantize; where a call says so */
+} luffy_dtype;
 
 /* Expert activation (Sec. 2.1: an expert is an FFN).
  * GELU is the exact form 0.5 z (1 + erf(z / sqrt 2)); SiLU is z / (1 + e^-z). */
@@ -351,6 +355,90 @@ int luffy_expert_ffn_backward(const void* x, const int32_t* row_index, const int
                               int act, int max_rows, const void* dy_rep, void* dx_rep,
                               void* dw1, void* dw2, int dw_dtype, void* workspace,
                               size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Microscaled 4-bit matrices, for serving the layer: a matrix [groups, rows,
+ * cols] (groups: experts; 1 for activations) in blocks of 32 consecutive
+ * values of a row.  A block is 32 values v_i of {0, 0.5, 1, 1.5, 2, 3, 4, 6}
+ * with a sign (E2M1: codes 0..7, 8..15 negative) and one scale 2^(s - 127)
+ * (E8M0, s = 0..254; s = 255: the block holds no numbers, every value of it
+ * reads as NaN).
+ *   values  q [groups, rows, cols/2] uint8, column 2i in the low half of byte
+ *           i of its row, column 2i + 1 in the high half;
+ *   scales  s [groups, ceil(cols/256), rows, 8] uint8: the scales of 256
+ *           consecutive columns of a row side by side, 0 past the last column
+ *           (luffy_mx4_scale_bytes(groups, rows, cols) bytes in all).
+ * cols is a multiple of 32; q is 16-byte aligned, s 8-byte.
+ *
+ * luffy_mx4_quantize - rounds x [groups * rows, cols] (float32 or bf16) to
+ * such a matrix.  With m the largest |value| of a block its scale is
+ * 2^(floor(log2 m) - 2) (at least 2^-127; s = 0 for a block of zeros), so
+ * that m / scale lies in [4, 8); every value / scale goes to the nearest
+ * representable value, halfway cases to the even code, those above 6 to 6.
+ * A block with an infinity or a NaN gets s = 255.
+ *   row_index  [rows] int32, device, or NULL: row r is x[row_index[r]]
+ *              (groups = 1 only)
+ *
+ * luffy_mx4_dequantize - the values of such a matrix as float32 or bf16
+ * (exact in float32; bf16 has every value but those of scales below 2^-126,
+ * which it rounds).
+ * ---------------------------------------------------------------------- */
+size_t luffy_mx4_scale_bytes(int groups, int rows, int cols);
+int luffy_mx4_quantize(const void* x, const int32_t* row_index, int groups, int rows, int cols, int dtype, void* q,
+                       void* s, void* stream);
+int luffy_mx4_dequantize(const void* q, const void* s, int groups, int rows, int cols, int dtype, void* x,
+                         void* stream);
+
+/* ------------------------------------------------------------------------
+ * luffy_mx4_matmul - products of rows with their expert's matrix, both
+ * microscaled:  y[r] = W_e x_r  for the rows r of expert e.
+ *   xq, xs   [M, K] microscaled rows
+ *   offsets  [E+1] int32, device: expert e has rows offsets[e] ..
+ *            offsets[e+1]-1 (offsets[E] <= M; later rows of y are not
+ *            written); NULL: all M rows are of one expert (E = 1)
+ *   wq, ws   [E, N, K] microscaled weights
+ *   y        [M, N] dtype (float32 or bf16)
+ * Products of two such values are exact in float32; their sums are float32.
+ * K and N multiples of 32, at most 32768; E <= 64.
+ * ---------------------------------------------------------------------- */
+int luffy_mx4_matmul(const void* xq, const void* xs, int M, const int32_t* offsets, int E, int N, int K,
+                     const void* wq, const void* ws, void* y, int dtype, void* stream);
+
+/* ------------------------------------------------------------------------
+ * luffy_mx4_expert_ffn - luffy_expert_ffn on microscaled weights (Sec. 2.1,
+ * Sec. 3), for serving: y_rep[r] = W2_e Q(act(W1_e Q(x_r))), Q the rounding of
+ * luffy_mx4_quantize (the hidden rows are rounded from float32).  bf16 rows
+ * and results; x, row_index, rep_offsets, act, max_rows and y_rep as for
+ * luffy_expert_ffn; w1 [E, d_ff, d] and w2 [E, d, d_ff] microscaled.
+ * ---------------------------------------------------------------------- */
+size_t luffy_mx4_expert_ffn_workspace_size(int max_rows, int E, int d, int d_ff);
+int luffy_mx4_expert_ffn(const void* x, const int32_t* row_index, const int32_t* rep_offsets, int E, int d, int d_ff,
+                         const void* w1q, const void* w1s, const void* w2q, const void* w2s, int act, int max_rows,
+                         void* y_rep, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * luffy_moe_few - a whole layer for a serving step of a few tokens (Sec. 2.1:
+ * gate, top-k, experts, combine), without condensation and without a capacity
+ * limit:
+ *   y_t = sum_j topk_gate[t,j] W2_e act(W1_e x_t),  e = topk_idx[t,j],
+ * experts and gates as luffy_route defines them (its choices, made here on
+ * float64 logits throughout).
+ *   x, w_gate, b_gate (or NULL), T <= LUFFY_FEW_MAX_TOKENS, d, E, k, act
+ *   w1 [E, d_ff, d], w2 [E, d, d_ff] of weight_type: the activations' dtype,
+ *   or LUFFY_MX4 with bf16 activations (w1_scale, w2_scale: their scales;
+ *   NULL otherwise).  Activations are not rounded to 4 bits here: the step is
+ *   bound by reading the weights, and keeps the accuracy.
+ *   topk_idx, topk_gate [T, k], y [T, d] dtype.
+ * Hidden rows and the sum over a token's experts are float32 (bf16: hidden
+ * rows as two bf16 parts, 16 bits of mantissa).  x, w_gate, w1 and w2 must
+ * be 16-byte aligned.  A token's output depends on its own row only.
+ * ---------------------------------------------------------------------- */
+#define LUFFY_FEW_MAX_TOKENS 64
+size_t luffy_moe_few_workspace_size(int T, int d, int E, int k, int d_ff);
+int luffy_moe_few(const void* x, int T, int d, int dtype, const void* w_gate, const float* b_gate, int E, int k,
+                  const void* w1, const void* w1_scale, const void* w2, const void* w2_scale, int weight_type,
+                  int d_ff, int act, int32_t* topk_idx, float* topk_gate, void* y, void* workspace,
+                  size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
  * luffy_adaptive_threshold - the condensation threshold h_t of training

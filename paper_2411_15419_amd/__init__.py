@@ -24,11 +24,15 @@ __all__ = [
     "luffy_combine_backward", "combine_backward_workspace_size", "luffy_expert_ffn_backward",
     "expert_ffn_backward_workspace_size", "luffy_condense_history", "history_size",
     "condense_history_workspace_size", "MoEStack", "CondensationDriver",
+    "LUFFY_MX4", "FEW_MAX_TOKENS", "mx4_scale_bytes", "luffy_mx4_quantize", "luffy_mx4_dequantize",
+    "luffy_mx4_matmul", "luffy_mx4_expert_ffn", "mx4_expert_ffn_workspace_size", "luffy_moe_few",
+    "moe_few_workspace_size",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libluffy.so")
 
-LUFFY_F32, LUFFY_BF16 = 0, 1
+LUFFY_F32, LUFFY_BF16, LUFFY_MX4 = 0, 1, 2
+FEW_MAX_TOKENS = 64   # luffy_moe_few
 LUFFY_ACT_GELU, LUFFY_ACT_SILU = 0, 1
 _ACTS = {"gelu": LUFFY_ACT_GELU, "silu": LUFFY_ACT_SILU}
 
@@ -65,6 +69,16 @@ _SIGS = {
     "luffy_expert_ffn_backward_workspace_size": (_c_size, [_c_int, _c_int, _c_int, _c_int, _c_int]),
     "luffy_expert_ffn_backward": (_c_int, [_vp, _vp, _vp, _c_int, _c_int, _c_int, _c_int, _vp, _vp, _c_int,
                                            _c_int, _vp, _vp, _vp, _vp, _c_int, _vp, _c_size, _vp]),
+    "luffy_mx4_scale_bytes": (_c_size, [_c_int, _c_int, _c_int]),
+    "luffy_mx4_quantize": (_c_int, [_vp, _vp, _c_int, _c_int, _c_int, _c_int, _vp, _vp, _vp]),
+    "luffy_mx4_dequantize": (_c_int, [_vp, _vp, _c_int, _c_int, _c_int, _c_int, _vp, _vp]),
+    "luffy_mx4_matmul": (_c_int, [_vp, _vp, _c_int, _vp, _c_int, _c_int, _c_int, _vp, _vp, _vp, _c_int, _vp]),
+    "luffy_mx4_expert_ffn_workspace_size": (_c_size, [_c_int, _c_int, _c_int, _c_int]),
+    "luffy_mx4_expert_ffn": (_c_int, [_vp, _vp, _vp, _c_int, _c_int, _c_int, _vp, _vp, _vp, _vp, _c_int, _c_int, _vp,
+                                      _vp, _c_size, _vp]),
+    "luffy_moe_few_workspace_size": (_c_size, [_c_int, _c_int, _c_int, _c_int, _c_int]),
+    "luffy_moe_few": (_c_int, [_vp, _c_int, _c_int, _c_int, _vp, _vp, _c_int, _c_int, _vp, _vp, _vp, _vp, _c_int,
+                               _c_int, _c_int, _vp, _vp, _vp, _vp, _c_size, _vp]),
     "luffy_adaptive_threshold": (_c_int, [ctypes.c_double, ctypes.c_double, ctypes.POINTER(ctypes.c_double)]),
     "luffy_profile_kernel": (_c_int, [ctypes.c_char_p]),
     "luffy_profile_read": (_c_int, [ctypes.POINTER(ctypes.c_double), ctypes.POINTER(_c_int)]),
@@ -268,6 +282,121 @@ def luffy_expert_ffn_backward(x, row_index, rep_offsets, w1, w2, act, max_rows, 
         _p(x), _p(row_index), _p(rep_offsets), E, d, d_ff, _dtype_code(x), _p(w1), _p(w2), _ACTS[act],
         max_rows, _p(dy_rep), _p(dx_rep), _p(dw1), _p(dw2), _dtype_code(dw1), _p(workspace), workspace.numel(),
         _stream(stream)), "luffy_expert_ffn_backward")
+
+
+def mx4_scale_bytes(groups: int, rows: int, cols: int) -> int:
+    """Bytes of the scales of a microscaled matrix [groups, rows, cols]."""
+    return int(load_library().luffy_mx4_scale_bytes(int(groups), int(rows), int(cols)))
+
+
+def _mx4_shape(q, s, what):
+    """(groups, rows, cols) of a microscaled matrix, its tensors checked:
+    values [groups, rows, cols/2] or [rows, cols/2], scales
+    [(groups,) ceil(cols/256), rows, 8]."""
+    if q.dtype != torch.uint8 or s.dtype != torch.uint8:
+        raise LuffyError(f"{what}: values and scales must be uint8")
+    if q.dim() not in (2, 3):
+        raise LuffyError(f"{what}: values must be [rows, cols/2] or [groups, rows, cols/2]")
+    groups, rows, cols = (q.shape[0] if q.dim() == 3 else 1), q.shape[-2], 2 * q.shape[-1]
+    want = ((cols + 255) // 256, rows, 8)
+    if tuple(s.shape) != ((groups,) + want if q.dim() == 3 else want):
+        raise LuffyError(f"{what}: scales of values {tuple(q.shape)} must be "
+                         f"{((groups,) + want if q.dim() == 3 else want)}, got {tuple(s.shape)}")
+    return groups, rows, cols
+
+
+def luffy_mx4_quantize(x, q, s, row_index=None, stream=None):
+    """Rounds x [rows, cols] (or [groups, rows, cols]; float32 or bf16) to
+    microscaled 4-bit values q [.., rows, cols/2] with scales s
+    [.., ceil(cols/256), rows, 8] (uint8).  row_index (int32 [rows], 2-D q
+    only): row r is x[row_index[r]]."""
+    groups, rows, cols = _mx4_shape(q, s, "luffy_mx4_quantize")
+    if x.shape[-1] != cols or x.dim() != q.dim() or (row_index is None and x.shape[:-1] != q.shape[:-1]):
+        raise LuffyError(f"luffy_mx4_quantize: x {tuple(x.shape)} does not fit values {tuple(q.shape)}")
+    if row_index is not None and (row_index.dtype != torch.int32 or row_index.numel() != rows):
+        raise LuffyError("luffy_mx4_quantize: row_index must be int32 [rows]")
+    _check(load_library().luffy_mx4_quantize(_p(x), _p(row_index), groups, rows, cols, _dtype_code(x), _p(q), _p(s),
+                                             _stream(stream)), "luffy_mx4_quantize")
+
+
+def luffy_mx4_dequantize(q, s, x, stream=None):
+    """The values of a microscaled matrix into x (float32 or bf16)."""
+    groups, rows, cols = _mx4_shape(q, s, "luffy_mx4_dequantize")
+    if tuple(x.shape) != tuple(q.shape[:-1]) + (cols,):
+        raise LuffyError(f"luffy_mx4_dequantize: x {tuple(x.shape)} does not fit values {tuple(q.shape)}")
+    _check(load_library().luffy_mx4_dequantize(_p(q), _p(s), groups, rows, cols, _dtype_code(x), _p(x),
+                                               _stream(stream)), "luffy_mx4_dequantize")
+
+
+def luffy_mx4_matmul(xq, xs, offsets, wq, ws, y, stream=None):
+    """y[r] = W_e x_r on microscaled rows xq [M, K/2] and weights wq
+    [E, N, K/2]; offsets (int32 [E+1]) buckets the rows by expert, None: one
+    expert.  y [M, N] float32 or bf16."""
+    _, M, K = _mx4_shape(xq, xs, "luffy_mx4_matmul")
+    E, N, Kw = _mx4_shape(wq, ws, "luffy_mx4_matmul")
+    if xq.dim() != 2 or wq.dim() != 3 or K != Kw or tuple(y.shape) != (M, N):
+        raise LuffyError(f"luffy_mx4_matmul: rows {tuple(xq.shape)}, weights {tuple(wq.shape)}, y {tuple(y.shape)}")
+    if offsets is not None and (offsets.dtype != torch.int32 or offsets.numel() != E + 1):
+        raise LuffyError("luffy_mx4_matmul: offsets must be int32 [E + 1]")
+    _check(load_library().luffy_mx4_matmul(_p(xq), _p(xs), M, _p(offsets), E, N, K, _p(wq), _p(ws), _p(y),
+                                           _dtype_code(y), _stream(stream)), "luffy_mx4_matmul")
+
+
+def mx4_expert_ffn_workspace_size(max_rows: int, E: int, d: int, d_ff: int) -> int:
+    return int(load_library().luffy_mx4_expert_ffn_workspace_size(int(max_rows), int(E), int(d), int(d_ff)))
+
+
+def luffy_mx4_expert_ffn(x, row_index, rep_offsets, w1q, w1s, w2q, w2s, act, max_rows, y_rep, workspace, stream=None):
+    """luffy_expert_ffn on microscaled weights w1 [E, d_ff, d] and w2
+    [E, d, d_ff]: the rows of x (bf16) and the hidden rows are rounded to 4 bits
+    on the way."""
+    E, d_ff, d = _mx4_shape(w1q, w1s, "luffy_mx4_expert_ffn")
+    if _mx4_shape(w2q, w2s, "luffy_mx4_expert_ffn") != (E, d, d_ff):
+        raise LuffyError(f"luffy_mx4_expert_ffn: weights {tuple(w1q.shape)} and {tuple(w2q.shape)}")
+    if x.dtype != torch.bfloat16 or y_rep.dtype != torch.bfloat16 or x.shape[-1] != d or y_rep.shape[-1] != d:
+        raise LuffyError("luffy_mx4_expert_ffn: x and y_rep must be bf16 rows of d values")
+    if y_rep.shape[0] < max_rows or (row_index is None and x.shape[0] < max_rows) or rep_offsets.numel() != E + 1:
+        raise LuffyError("luffy_mx4_expert_ffn: x, y_rep and rep_offsets do not fit max_rows and E")
+    _check(load_library().luffy_mx4_expert_ffn(
+        _p(x), _p(row_index), _p(rep_offsets), E, d, d_ff, _p(w1q), _p(w1s), _p(w2q), _p(w2s),
+        _ACTS[act] if isinstance(act, str) else int(act), int(max_rows), _p(y_rep), _p(workspace), workspace.numel(),
+        _stream(stream)), "luffy_mx4_expert_ffn")
+
+
+def moe_few_workspace_size(T: int, d: int, E: int, k: int, d_ff: int) -> int:
+    return int(load_library().luffy_moe_few_workspace_size(int(T), int(d), int(E), int(k), int(d_ff)))
+
+
+def luffy_moe_few(x, w_gate, b_gate, w1, w2, k, act, topk_idx, topk_gate, y, workspace, w1_scale=None,
+                  w2_scale=None, stream=None):
+    """A whole layer (gate, top-k, expert FFN, combine; no condensation, no
+    capacity) for T <= 64 tokens in one call.  Weights of x's dtype, or
+    microscaled (uint8 values with their scales) under bf16 activations."""
+    T, d = x.shape
+    E = w_gate.shape[0]
+    if w1_scale is not None or w2_scale is not None:
+        if w1_scale is None or w2_scale is None:
+            raise LuffyError("luffy_moe_few: microscaled weights need both scales")
+        shape1, shape2 = _mx4_shape(w1, w1_scale, "luffy_moe_few"), _mx4_shape(w2, w2_scale, "luffy_moe_few")
+        wtype = LUFFY_MX4
+    else:
+        shape1, shape2 = tuple(w1.shape), tuple(w2.shape)
+        wtype = _dtype_code(w1)
+        if w2.dtype != w1.dtype:
+            raise LuffyError("luffy_moe_few: w1 and w2 must have the same dtype")
+    if len(shape1) != 3 or shape1[0] != E or shape1[2] != d or shape2 != (E, d, shape1[1]) or w_gate.shape[1] != d:
+        raise LuffyError(f"luffy_moe_few: w_gate {tuple(w_gate.shape)}, w1 {shape1}, w2 {shape2} for d = {d}")
+    if w_gate.dtype != x.dtype or y.dtype != x.dtype or y.shape != x.shape:
+        raise LuffyError("luffy_moe_few: w_gate and y must have x's dtype, y its shape")
+    if b_gate is not None and (b_gate.dtype != torch.float32 or b_gate.numel() != E):
+        raise LuffyError("luffy_moe_few: b_gate must be float32 [E]")
+    if (topk_idx.dtype != torch.int32 or topk_gate.dtype != torch.float32 or topk_idx.numel() != T * k
+            or topk_gate.numel() != T * k):
+        raise LuffyError("luffy_moe_few: topk_idx must be int32 [T, k], topk_gate float32 [T, k]")
+    _check(load_library().luffy_moe_few(
+        _p(x), T, d, _dtype_code(x), _p(w_gate), _p(b_gate), E, k, _p(w1), _p(w1_scale), _p(w2), _p(w2_scale), wtype,
+        shape1[1], _ACTS[act] if isinstance(act, str) else int(act), _p(topk_idx), _p(topk_gate), _p(y),
+        _p(workspace), workspace.numel(), _stream(stream)), "luffy_moe_few")
 
 
 def adaptive_threshold(l_ini: float, l_prev: float) -> float:

@@ -25,7 +25,7 @@ FLAGS = [
     "-Wall", "-Wno-unused-result", "-Wno-unused-command-line-argument",
     f"-I{INCLUDE}", f"-I{CSRC}",
 ]
-SOURCES = ["luffy_api.hip", "route.hip", "condense.hip", "ffn.hip", "combine.hip"]
+SOURCES = ["luffy_api.hip", "route.hip", "condense.hip", "ffn.hip", "combine.hip", "mx4.hip", "few.hip"]
 
 
 def _compile(src: str) -> str:
