@@ -430,8 +430,8 @@ int luffy_mx4_expert_ffn(const void* x, const int32_t* row_index, const int32_t*
  *   bound by reading the weights, and keeps the accuracy.
  *   topk_idx, topk_gate [T, k], y [T, d] dtype.
  * Hidden rows and the sum over a token's experts are float32 (bf16: hidden
- * rows as two bf16 parts, 16 bits of mantissa).  x, w_gate, w1 and w2 must
- * be 16-byte aligned.  A token's output depends on its own row only.
+ * rows as two bf16 parts, 16 bits of mantissa).  x, w_gate, w1, w2 and y
+ * must be 16-byte aligned.  A token's output depends on its own row only.
  * ---------------------------------------------------------------------- */
 #define LUFFY_FEW_MAX_TOKENS 64
 size_t luffy_moe_few_workspace_size(int T, int d, int E, int k, int d_ff);

@@ -7,17 +7,96 @@
 //
 // Three launches: few_gate_kernel (a block a token: logits in float64, top-k,
 // gates), few_product_kernel<.., false> (hidden rows) and <.., true> (second
-// product, whose last block of each column tile adds the tokens' experts).
+// product, whose last block of each row group adds the tokens' experts).
+#include <algorithm>
+
 #include "act.h"
 #include "luffy_common.h"
+#include "mx4_core.h"
 
 namespace luffy {
 namespace {
 
 constexpr int kFewTokens = LUFFY_FEW_MAX_TOKENS;
 constexpr int kGateThreads = 1024;
+constexpr int kFewWaves = 8, kFewThreads = 64 * kFewWaves;
 
 enum FewWeights { kF32 = 0, kBf16 = 1, kMx4 = 2 };
+
+// The tokens' side of the products ("columns") is kept in rows of 128-byte
+// units: BL units for every 128-byte piece of a weight row.
+//   float32           1 unit: the 32 values
+//   bf16, tokens      1 unit: the 64 values
+//   bf16, hidden      2 units: the 64 values' bf16 parts and what those leave
+//                     (also bf16), together 16 bits of every float32 value
+//   4-bit             2 units a term: 256 values as E4M3 with a scale byte per
+//                     32, term t the E4M3 rounding of what the terms before
+//                     leave, at 2^-4t of the scale.  Two terms hold a bf16 token
+//                     exactly (but for values below 2^-13 of their block's
+//                     largest, to 2^-21 of it), three hold a hidden value to
+//                     2^-13 of itself or 2^-25 of its block's largest.  So the
+//                     weights' codes go to the block-scaled MFMA as they are,
+//                     without a conversion to bf16 for every value.
+template <int WT, bool SECOND>
+struct FewLayout {
+  static constexpr int TERMS = SECOND ? 3 : 2;
+  static constexpr int BL = WT == kMx4 ? 2 * TERMS : (WT == kBf16 && SECOND ? 2 : 1);
+  static constexpr int PIECE = WT == kF32 ? 32 : (WT == kBf16 ? 64 : 256);   // values of a piece
+};
+template <int WT, bool SECOND>
+__host__ __device__ constexpr int few_pitch(int K) {
+  return (K + FewLayout<WT, SECOND>::PIECE - 1) / FewLayout<WT, SECOND>::PIECE * FewLayout<WT, SECOND>::BL * 128;
+}
+__host__ __device__ constexpr int few_scale_pitch(int K) { return (K + 255) / 256 * 8; }
+
+// Stores eight consecutive values (unit `u` of eight of a row; the four units
+// of a block of 32 sit in four neighbouring lanes) as TERMS E4M3 terms.  The
+// block-scaled MFMA 16x16x128 takes 8-bit values k = 64 h + 16 g + b from byte
+// 16 h + b of lane quarter g, and the scale of values 32 g.. from quarter g (4-
+// bit values: 32 g.. in quarter g).  The weight blocks a lane holds put block
+// c of a piece at quarter c / 2 of the half c % 2 of a wave's rows, so value i
+// of block c goes to half h = c / 4, eighth 4 (c / 2 % 2) + 2 (i / 16) + c % 2.
+template <int TERMS>
+__device__ __forceinline__ void store_e4m3(float (&v)[8], int u, uint8_t* __restrict__ row, uint8_t* __restrict__ scale) {
+  typedef short s16x2 __attribute__((ext_vector_type(2)));
+  typedef float f32v2 __attribute__((ext_vector_type(2)));
+  uint32_t most = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) most = max(most, __float_as_uint(v[j]) & 0x7fffffffu);
+  most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), 1, 64)));
+  most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), 2, 64)));
+  // largest value in [128, 256) of the first scale; 4 (TERMS - 1) is left below it
+  const uint32_t ex = most >> 23, s0 = ex == 255u ? 255u : max(static_cast<int>(ex) - 7, 8);
+  const int c = u >> 2 & 7, j = u & 3, piece = u >> 5;
+  const int at = 128 * (c >> 2) + 16 * (4 * (c >> 1 & 1) + 2 * (j >> 1) + (c & 1)) + 8 * (j & 1);
+#pragma unroll
+  for (int t = 0; t < TERMS; ++t) {
+    const float sc = __uint_as_float((s0 - 4 * t) << 23);
+    s16x2 q[2] = {{0, 0}, {0, 0}};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      q[i] = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(q[i], v[4 * i], v[4 * i + 1], sc, false);
+      q[i] = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(q[i], v[4 * i + 2], v[4 * i + 3], sc, true);
+    }
+    const int w0 = __builtin_bit_cast(int, q[0]), w1 = __builtin_bit_cast(int, q[1]);
+    if (t + 1 < TERMS) {
+      const f32v2 b0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w0, sc, false);
+      const f32v2 b1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w0, sc, true);
+      const f32v2 b2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w1, sc, false);
+      const f32v2 b3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w1, sc, true);
+      v[0] -= b0.x; v[1] -= b0.y; v[2] -= b1.x; v[3] -= b1.y;
+      v[4] -= b2.x; v[5] -= b2.y; v[6] -= b3.x; v[7] -= b3.y;
+    }
+    const uint2 o = ex == 255u ? make_uint2(0, 0) : make_uint2(w0, w1);
+    *reinterpret_cast<uint2*>(row + (static_cast<size_t>(piece) * 2 * TERMS + 2 * t) * 128 + at) = o;
+  }
+  if (j == 0) scale[piece * 8 + c] = static_cast<uint8_t>(s0);
+}
+
+struct FewTerms {   // 4-bit weights: the tokens' and hidden rows' terms and scales
+  uint8_t *x8, *x8_scale, *h8, *h8_scale;
+  int d_ff;
+};
 
 // One block a token; wave w takes experts w, w + 16, ...  A logit is one
 // float64 sum (products of two bf16 or float32 values are exact there), so a
@@ -25,17 +104,16 @@ enum FewWeights { kF32 = 0, kBf16 = 1, kMx4 = 2 };
 // count below every other; a token without a single finite logit has gates of
 // its own making (NaN, as softmax gives) but valid experts.
 //
-// With xs (4-bit weights) the block also stores its token's values in the
-// order the 4-bit product takes them: of every 256 values (padded with zeros),
-// value 32 c + 8 s + j at 64 s + 8 c + j, so that the eight lanes that hold a
-// row's eight blocks read 128 contiguous bytes.
+// With x8 (4-bit weights) the block also stores its token's values as E4M3
+// terms (store_e4m3), zeros past the last one, and clears the last piece of its
+// hidden rows h8, which the first product may fill only in part.
 template <bool F32>
 __global__ __launch_bounds__(kGateThreads) void few_gate_kernel(const void* __restrict__ x, int d,
                                                                 const void* __restrict__ w_gate,
                                                                 const float* __restrict__ b_gate, int E, int k,
                                                                 int32_t* __restrict__ topk_idx,
                                                                 float* __restrict__ topk_gate,
-                                                                uint16_t* __restrict__ xs, int* __restrict__ done,
+                                                                const FewTerms f, int* __restrict__ done,
                                                                 int n_done) {
   __shared__ double logit[kMaxExperts];
   const int t = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
@@ -67,14 +145,29 @@ __global__ __launch_bounds__(kGateThreads) void few_gate_kernel(const void* __re
     for (int o = 32; o >= 1; o >>= 1) s += __shfl_xor(s, o, 64);
     if (lane == 0) logit[e] = s + (b_gate ? static_cast<double>(b_gate[e]) : 0.0);
   }
-  if (xs) {
-    const int pitch = (d + 255) / 256 * 256;
-    uint16_t* dst = xs + static_cast<size_t>(t) * pitch;
-    for (int i = tid * 8; i < pitch; i += kGateThreads * 8) {
-      const int s = i >> 6 & 3, c = i >> 3 & 7, src = (i & ~255) + 32 * c + 8 * s;
-      uint4 v = make_uint4(0, 0, 0, 0);
-      if (src < d) v = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(x) + row + src);
-      *reinterpret_cast<uint4*>(dst + i) = v;
+  if (f.x8) {
+    uint8_t* dst = f.x8 + static_cast<size_t>(t) * few_pitch<kMx4, false>(d);
+    uint8_t* scale = f.x8_scale + static_cast<size_t>(t) * few_scale_pitch(d);
+    const int units = (d + 255) / 256 * 32;   // a multiple of 32: a block's four lanes stay together
+    for (int u = tid; u < units; u += kGateThreads) {
+      Pack16 a;
+      a.u4 = make_uint4(0, 0, 0, 0);
+      if (u * 8 < d) a.u4 = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(x) + row + u * 8);
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = bf16_to_f32(a.h[i]);
+      store_e4m3<2>(v, u, dst, scale);
+    }
+    if (f.d_ff & 255) {
+      constexpr int words = FewLayout<kMx4, true>::BL * 32;
+      for (int i = tid; i < k * words; i += kGateThreads) {
+        const int slot = t * k + i / words;
+        uint8_t* end = f.h8 + static_cast<size_t>(slot + 1) * few_pitch<kMx4, true>(f.d_ff) - 4 * words;
+        reinterpret_cast<uint32_t*>(end)[i % words] = 0;
+      }
+      if (tid < 2 * k)
+        reinterpret_cast<uint32_t*>(f.h8_scale + static_cast<size_t>(t * k + tid / 2 + 1) * few_scale_pitch(f.d_ff) -
+                                    8)[tid & 1] = 0;
     }
   }
   __syncthreads();
@@ -120,181 +213,368 @@ __global__ __launch_bounds__(kGateThreads) void few_gate_kernel(const void* __re
   }
 }
 
-// Which slots (token t, choice j: t * k + j) expert number `rank` of the
-// experts in use has; block-uniform.  Returns false when fewer are in use.
+__device__ __forceinline__ void lds_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
+
+// The experts in use and their slots (token t, choice j: slot t * k + j).
 struct FewLists {
-  int flag[kMaxExperts];
-  int slot[kFewTokens];
-  int count;
+  int expert[kMaxExperts], first[kMaxExperts + 1];   // by rank among the experts in use
+  int slot[2 * kFewTokens];
+  int used;
+  int at[kMaxExperts];
 };
 
-__device__ __forceinline__ bool few_expert(const int32_t* __restrict__ topk_idx, int slots, int rank, FewLists& l,
-                                           int& e, int& n, int& used) {
-  const int tid = threadIdx.x, lane = tid & 63;
-  if (tid < kMaxExperts) l.flag[tid] = 0;
-  __syncthreads();
-  for (int i = tid; i < slots; i += blockDim.x) l.flag[topk_idx[i]] = 1;
-  __syncthreads();
-  const uint64_t m = __ballot(l.flag[lane] != 0);
-  used = __popcll(m);
-  if (rank >= used) return false;
-  const uint64_t hit = __ballot((m >> lane & 1) && __popcll(m & lanemask_lt()) == rank);
-  e = __builtin_amdgcn_readfirstlane(__builtin_ctzll(hit));
-  if (tid < 64) {
-    int base = 0;
-    for (int s0 = 0; s0 < slots; s0 += 64) {
-      const bool mine = s0 + lane < slots && topk_idx[s0 + lane] == e;
-      const uint64_t b = __ballot(mine);
-      const int at = base + __popcll(b & lanemask_lt());
-      if (mine && at < kFewTokens) l.slot[at] = s0 + lane;   // a token has an expert at most once
-      base += __popcll(b);
-    }
-    if (lane == 0) l.count = base;
+// One wave.  The order of an expert's slots is that of the LDS atomics; it
+// decides which column of the products a slot has and nothing else.
+__device__ __forceinline__ void few_lists(const int32_t* __restrict__ topk_idx, int slots, FewLists& l) {
+  const int lane = threadIdx.x & 63;
+  const int e0 = lane < slots ? topk_idx[lane] : -1;
+  const int e1 = 64 + lane < slots ? topk_idx[64 + lane] : -1;
+  l.at[lane] = 0;
+  lds_order();
+  const int p0 = e0 >= 0 ? atomicAdd(&l.at[e0], 1) : 0;
+  const int p1 = e1 >= 0 ? atomicAdd(&l.at[e1], 1) : 0;
+  lds_order();
+  const int n = l.at[lane];
+  int incl = n;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int v = __shfl_up(incl, o, 64);
+    if (lane >= o) incl += v;
   }
-  __syncthreads();
-  n = min(l.count, kFewTokens);
-  return true;
+  const uint64_t m = __ballot(n > 0);
+  const int rank = __popcll(m & lanemask_lt());
+  if (n > 0) {
+    l.expert[rank] = lane;
+    l.first[rank] = incl - n;
+  }
+  l.at[lane] = incl - n;
+  if (lane == 63) {
+    l.used = __popcll(m);
+    l.first[__popcll(m)] = incl;
+  }
+  lds_order();
+  if (e0 >= 0) l.slot[l.at[e0] + p0] = lane;
+  if (e1 >= 0) l.slot[l.at[e1] + p1] = 64 + lane;
 }
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
-__device__ __forceinline__ bf16x8 mx4_to_bf16(uint32_t q, float scale) {
-  typedef __bf16 bf16v2 __attribute__((ext_vector_type(2)));
-  union { bf16v2 p[4]; bf16x8 v; } r;
-  r.p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, scale, 0);
-  r.p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, scale, 1);
-  r.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, scale, 2);
-  r.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, scale, 3);
-  return r.v;
-}
-
 // The 8 x 8 products of one 128-byte piece of eight weight rows with eight
-// tokens, on 16 x 16 MFMA.  Lane l holds 16 bytes of row l % 8, chunk l / 8 (so
+// columns, on 16 x 16 MFMA.  Lane l holds 16 bytes of row l % 8, chunk l / 8 (so
 // one load instruction reads eight whole 128-byte lines, the pattern that
 // streams fastest: 6.9 TB/s of reads against 6.2 for 64-byte pieces).  Seen as
 // an MFMA operand, rows 0-7 of a lane quarter g hold chunk 2g and rows 8-15
-// the same weight rows' chunk 2g + 1, and the tokens come the same way, so
-//   product of row r, token c  =  D[r][c] + D[r + 8][c + 8];
+// the same weight rows' chunk 2g + 1, and the columns come the same way, so
+//   product of row r, column c  =  D[r][c] + D[r + 8][c + 8];
 // the other two quadrants mix chunks and are not used.
-template <int WT, bool HILO>
-__device__ __forceinline__ void few_mma(u32x4 a, float scale, const u32x4* b, f32x4& acc) {
+template <int WT, int BL>
+__device__ __forceinline__ void few_mma(u32x4 a, int sa, const u32x4 (&b)[BL], int sb, f32x4& acc) {
   if constexpr (WT == kF32) {
     const f32x4 av = __builtin_bit_cast(f32x4, a), bv = __builtin_bit_cast(f32x4, b[0]);
 #pragma unroll
     for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(av[i], bv[i], acc, 0, 0, 0);
   } else if constexpr (WT == kBf16) {
-    const bf16x8 av = __builtin_bit_cast(bf16x8, a);
-    acc = mfma16x16x32(av, __builtin_bit_cast(bf16x8, b[0]), acc);
-    if constexpr (HILO) acc = mfma16x16x32(av, __builtin_bit_cast(bf16x8, b[1]), acc);
-  } else {
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      const bf16x8 av = mx4_to_bf16(a[s], scale);
-      acc = mfma16x16x32(av, __builtin_bit_cast(bf16x8, b[s]), acc);
-      if constexpr (HILO) acc = mfma16x16x32(av, __builtin_bit_cast(bf16x8, b[4 + s]), acc);
+    for (int i = 0; i < BL; ++i)
+      acc = mfma16x16x32(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b[i]), acc);
+  } else {
+    const i32x4 q = __builtin_bit_cast(i32x4, a);
+    const i32x8 av = __builtin_shufflevector(q, q, 0, 1, 2, 3, -1, -1, -1, -1);
+#pragma unroll
+    for (int t = 0; t < BL / 2; ++t) {
+      const i32x4 lo = __builtin_bit_cast(i32x4, b[2 * t]), hi = __builtin_bit_cast(i32x4, b[2 * t + 1]);
+      const i32x8 bv = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(av, bv, acc, 4, 0, 0, sa, 0, sb - 4 * t);
     }
   }
 }
 
 struct FewArgs {
-  const void* w;            // [E, N, K] weights (4-bit: two a byte)
-  const uint8_t* scale;     // [E, ceil(K/256), N, 8] (4-bit weights)
-  const void* in;           // rows of `pitch` bytes: tokens (first product), slots (second)
-  size_t lo;                // second product: byte offset of the low halves of `in`
-  int pitch;
-  int N, K;
-  int T, k;
+  const uint8_t* w;         // [E, N, K] weights
+  const uint8_t* w_scale;   // [E, ceil(K/256), N, 8] (4-bit weights)
+  const uint8_t* in;        // columns: tokens (first product) or slots (second), FewLayout rows
+  const uint8_t* in_scale;
+  int N, K, T, k, split;    // split: waves that share a row's K (1, 2, 4 or 8)
   const int32_t* topk_idx;
   const float* topk_gate;
-  void* h;                  // first product: hidden rows [slot], h_pitch bytes each
-  size_t h_lo;
-  int h_pitch;
+  uint8_t *h, *h_scale;     // first product: hidden rows by slot
   float* part;              // second product: [slot, N]
-  int* done;                // a counter a column tile
+  int* done;                // a counter a row group
   void* y;
 };
 
-// Position of hidden column c in a row of the second product's input.
+// LDS of a block.  Columns come in chunks of K, double-buffered; NBMAX: groups
+// of eight columns that an item may have (an expert has at most T).  With one
+// group the registers allow two blocks a CU, with more one.
+template <int NBMAX, int RT>
+struct FewLds {
+  static constexpr int HALF = (NBMAX == 1 ? 30 : 52) * 1024;      // one chunk's columns
+  static constexpr int SCALES = NBMAX == 1 ? 512 : 1024;          // and their scale bytes (64 a piece and group)
+  static constexpr int RED = NBMAX * 8 * kFewWaves * RT * 8 * 4;  // the waves' sums
+  __attribute__((aligned(16))) uint8_t cols[2 * HALF];
+  __attribute__((aligned(16))) uint8_t scales[2 * SCALES];
+  __attribute__((aligned(16))) float red[RED / 4];
+  FewLists l;
+  int ready;                       // row groups that this block adds up at its end
+  int group[kFewThreads];
+};
+
+// Pieces of each part of K in a chunk of nb column groups.
+template <int WT, bool SECOND, int NBMAX, int RT>
+__host__ __device__ constexpr int few_chunk(int split_log2, int nb_log2) {
+  using S = FewLds<NBMAX, RT>;
+  const int fit = S::HALF / 1024 / FewLayout<WT, SECOND>::BL, scales = S::SCALES / 64;
+  return (WT == kMx4 && scales < fit ? scales : fit) >> (split_log2 + nb_log2);
+}
+// Groups of eight columns that n columns are multiplied as: 1, 2, 4 or 8.
+__host__ __device__ constexpr int few_nb_log2(int n) { return n <= 8 ? 0 : (n <= 16 ? 1 : (n <= 32 ? 2 : 3)); }
+
+// A block's waves are arranged as `split` parts of K by 8 / split row groups of
+// RT * 8 rows; a work item is the RT * 64 / split rows of one expert that the
+// block takes at a time, times all of that expert's columns.
+struct FewItem {
+  const uint8_t *w, *s;          // the expert's weights and scales
+  uint32_t row;                  // this wave's first row
+  int rank, group, first, n;
+  int p0, p1;                    // pieces of K of this wave (none where its rows do not exist)
+  int c1;                        // and the end of those in the first chunk
+};
+
 template <int WT>
-__device__ __forceinline__ int few_hidden_at(int c) {
-  if constexpr (WT == kMx4) return (c & ~255) + 64 * (c >> 3 & 3) + 8 * (c >> 5 & 7) + (c & 7);
-  else return c;
+__device__ __forceinline__ int few_kbytes(int K) { return WT == kF32 ? K * 4 : (WT == kBf16 ? K * 2 : K / 2); }
+
+constexpr uint32_t kFewRange = 0xFFFF0000u;   // an expert's matrix is smaller (checked on the host)
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t few_rsrc(const uint8_t* base) {
+  const uint64_t v = reinterpret_cast<uint64_t>(base);
+  const uint64_t lo = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v)));
+  const uint64_t hi = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v >> 32)));
+  return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>((hi << 32) | lo), static_cast<short>(0),
+                                           static_cast<int>(kFewRange), 0x00020000);
 }
 
-// One block: RT * 8 weight rows of one expert times that expert's tokens, K
-// split over its W waves.  NB: groups of eight tokens a pass over the weights
-// (an expert with more tokens passes over its rows again, from L2).
-template <int WT, int RT, int W, int NB, bool SECOND>
-__device__ __forceinline__ void few_tile(const FewArgs& a, int e, int n0, int first, int n, const int* slot,
-                                         float* red, int act) {
-  constexpr int U = RT >= 4 ? 2 : 4;                     // pieces of 128 bytes in flight a row
-  constexpr bool HILO = SECOND && WT != kF32;
-  constexpr int BP = (WT == kMx4 ? 4 : 1);               // 16-byte loads a lane, group and piece (and half)
-  constexpr int BL = BP * (HILO ? 2 : 1);
+template <int WT, int RT, int NBMAX, bool SECOND>
+__device__ __forceinline__ FewItem few_item(const FewArgs& a, const FewLists& l, int item, int groups) {
+  FewItem t;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  t.rank = __builtin_amdgcn_readfirstlane(item / groups);
+  t.group = item - t.rank * groups;
+  const int e = __builtin_amdgcn_readfirstlane(l.expert[t.rank]);
+  t.first = __builtin_amdgcn_readfirstlane(l.first[t.rank]);
+  t.n = __builtin_amdgcn_readfirstlane(l.first[t.rank + 1]) - t.first;
+  const int kbytes = few_kbytes<WT>(a.K), pieces = (kbytes + 127) / 128, split_log2 = __builtin_ctz(a.split);
+  const int part = w & (a.split - 1);
+  t.row = (t.group * (kFewWaves >> split_log2) + (w >> split_log2)) * (8 * RT);
+  const bool rows = static_cast<int>(t.row) < a.N;
+  t.p0 = rows ? (part * pieces) >> split_log2 : 0;
+  t.p1 = rows ? ((part + 1) * pieces) >> split_log2 : 0;
+  t.c1 = min(t.p1, t.p0 + few_chunk<WT, SECOND, NBMAX, RT>(split_log2, few_nb_log2(t.n)));
+  t.w = a.w + static_cast<size_t>(e) * a.N * kbytes;
+  t.s = WT == kMx4 ? a.w_scale + static_cast<size_t>(e) * pieces * a.N * 8 : nullptr;
+  return t;
+}
+
+// U pieces of the wave's RT row tiles, from piece p on.  The loads are issued
+// whatever p is, and those at or past p1 fetch nothing (their offset is out of
+// the buffer's range; 4-bit: nor do chunks past the row's end): a load behind a
+// branch would leave the number of loads in flight open, and every use of an
+// earlier one would wait for all.
+template <int WT, int RT, int U>
+__device__ __forceinline__ void few_load(const FewArgs& a, const uint8_t* w, const uint8_t* s, uint32_t row, int p,
+                                         int p1, u32x4 (&av)[U][RT], uint8_t (&sv)[U][RT]) {
+  constexpr int kStream = 2;   // non-temporal: read once
+  const int kbytes = few_kbytes<WT>(a.K), lane = threadIdx.x & 63, r = lane & 7, c = lane >> 3;
+  const uint32_t off = static_cast<uint32_t>(r) * kbytes + 16 * c;
+  const __amdgpu_buffer_rsrc_t wr = few_rsrc(w);
+  uint32_t in[U];   // all ones where the piece exists
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    in[u] = static_cast<uint32_t>((p + u - p1) >> 31);
+    uint32_t o = off | (~in[u] & kFewRange);
+    if constexpr (WT == kMx4) o = (p + u) * 128 + 16 * c < kbytes ? o : kFewRange;
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+      av[u][i] = __builtin_amdgcn_raw_buffer_load_b128(wr, o, ((row + 8 * i) * kbytes + (p + u) * 128) & in[u], kStream);
+  }
+  if constexpr (WT == kMx4) {
+    const __amdgpu_buffer_rsrc_t sr = few_rsrc(s);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < RT; ++i)
+        sv[u][i] = __builtin_amdgcn_raw_buffer_load_b8(sr, (8u * r + c) | (~in[u] & kFewRange),
+                                                       (((p + u) * a.N + row + 8 * i) * 8) & in[u], 0);
+  }
+}
+
+// BYTES (4 or 16) a lane from offset off + soff to dst + BYTES * lane,
+// asynchronously.
+template <int BYTES>
+__device__ __forceinline__ void lds_dma(__amdgpu_buffer_rsrc_t r, uint32_t off, int soff,
+                                        __attribute__((address_space(3))) uint8_t* dst) {
+  using lds_ptr = __attribute__((address_space(3))) void*;
+  if constexpr (BYTES == 16) __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr)dst, 16, off, soff, 0, 0);
+  else __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr)dst, 4, off, soff, 0, 0);
+}
+
+// Barrier for data in LDS: waits for this wave's LDS accesses only, so that
+// loads from memory stay in flight across it.
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  raw_barrier();
+}
+
+// What the column buffers hold, and where the next chunk goes (block-uniform).
+struct FewStage {
+  int half;        // of the current chunk
+  int whole;       // rank whose columns the half holds over all of K, -1: none
+  bool behind;     // a step of weight loads follows the chunk's loads (this wave)
+};
+
+// Columns of the chunk of item t that starts at piece c0 of every part, straight
+// into LDS (asynchronous loads, all in flight together): units of 8 columns x
+// 128 bytes, the eighths of a column's line permuted so that the products'
+// reads (eight columns, one eighth) fall on distinct banks.  Pieces past a
+// part's end are left out; nothing reads them.
+template <int WT, int RT, int NB, int NBMAX, bool SECOND>
+__device__ __forceinline__ void few_stage(const FewArgs& a, FewLds<NBMAX, RT>& m, const FewItem& t, int c0,
+                                          int half) {
+  using L = FewLayout<WT, SECOND>;
+  using S = FewLds<NBMAX, RT>;
+  using lds_ptr = __attribute__((address_space(3))) uint8_t*;
+  constexpr int BL = L::BL;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int r = lane & 7, c = lane >> 3;
-  const int kbytes = WT == kF32 ? a.K * 4 : (WT == kBf16 ? a.K * 2 : a.K / 2);
-  const int pieces = (kbytes + 127) / 128;
-  const char* wp = static_cast<const char*>(a.w) + (static_cast<size_t>(e) * a.N + n0 + r) * kbytes + 16 * c;
-  const uint8_t* sp = nullptr;
-  if constexpr (WT == kMx4) sp = a.scale + (static_cast<size_t>(e) * pieces * a.N + n0 + r) * 8 + c;
-  const char* bp[NB];
+  const int pieces = (few_kbytes<WT>(a.K) + 127) / 128, pitch = few_pitch<WT, SECOND>(a.K);
+  const int split_log2 = __builtin_ctz(a.split);
+  const int chunk = few_chunk<WT, SECOND, NBMAX, RT>(split_log2, few_nb_log2(8 * NB));
+  const lds_ptr cols = (lds_ptr)m.cols + half * S::HALF, scales = (lds_ptr)m.scales + half * S::SCALES;
+  const int row = lane >> 3, pos = (lane & 7) ^ row;
+  const __amdgpu_buffer_rsrc_t in = few_rsrc(a.in), ins = few_rsrc(a.in_scale);
+  uint32_t off[NB], soff[NB];   // (the columns of a step are far below 4 GiB)
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
-    const int s = slot[min(first + 8 * b + r, n - 1)];
-    bp[b] = static_cast<const char*>(a.in) + static_cast<size_t>(SECOND ? s : s / a.k) * a.pitch + 16 * c;
+    const int s = m.l.slot[t.first + min(8 * b + row, t.n - 1)];
+    off[b] = static_cast<uint32_t>(SECOND || a.k == 1 ? s : s >> 1) * pitch + 16 * pos;
+    if constexpr (WT == kMx4) {   // eight bytes a column: a dword each for 16 lanes
+      const int s2 = m.l.slot[t.first + min(8 * b + (lane >> 1 & 7), t.n - 1)];
+      soff[b] = static_cast<uint32_t>(SECOND || a.k == 1 ? s2 : s2 >> 1) * few_scale_pitch(a.K) + 4 * (lane & 1);
+    }
   }
+  for (int kp = w & (a.split - 1); kp < a.split; kp += kFewWaves) {
+    const int first = (kp * pieces) >> split_log2, end = ((kp + 1) * pieces) >> split_log2;
+#pragma unroll 1
+    for (int i = w >> split_log2; i < chunk; i += kFewWaves >> split_log2) {
+      const int p = first + c0 + i;
+      if (p >= end) break;
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        const int unit = (kp * chunk + i) * NB + b;
+#pragma unroll
+        for (int j = 0; j < BL; ++j)
+          lds_dma<16>(in, off[b], (p * BL + j) * 128, cols + (unit * BL + j) * 1024);
+        if constexpr (WT == kMx4) {
+          if (lane < 16) lds_dma<4>(ins, soff[b], p * 8, scales + unit * 64);
+        }
+      }
+    }
+  }
+}
+
+// Stages the first chunk of an item.
+template <int WT, int RT, int NBMAX, bool SECOND>
+__device__ __forceinline__ void few_stage_first(const FewArgs& a, FewLds<NBMAX, RT>& m, const FewItem& t,
+                                                int half) {
+  if (NBMAX == 1 || t.n <= 8) few_stage<WT, RT, 1, NBMAX, SECOND>(a, m, t, 0, half);
+  else if (t.n <= 16) few_stage<WT, RT, (NBMAX > 1 ? 2 : 1), NBMAX, SECOND>(a, m, t, 0, half);
+  else if (t.n <= 32) few_stage<WT, RT, (NBMAX > 1 ? 4 : 1), NBMAX, SECOND>(a, m, t, 0, half);
+  else few_stage<WT, RT, (NBMAX > 1 ? 8 : 1), NBMAX, SECOND>(a, m, t, 0, half);
+}
+
+// One work item with NB groups of eight columns.  av holds the item's first
+// pieces on entry and the next item's (`next`, if any) on return, and its first
+// columns are on their way to LDS, so that the weight stream does not stop
+// while an item's sums are added and stored.
+template <int WT, int RT, int NB, int NBMAX, bool SECOND>
+__device__ __forceinline__ void few_run(const FewArgs& a, FewLds<NBMAX, RT>& m, const FewItem& t,
+                                        const FewItem& next, bool more, int act, FewStage& st,
+                                        u32x4 (&av)[8 / RT][RT], uint8_t (&sv)[8 / RT][RT]) {
+  using L = FewLayout<WT, SECOND>;
+  using S = FewLds<NBMAX, RT>;
+  constexpr int U = 8 / RT, BL = L::BL;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int part = w & (a.split - 1), pieces = (few_kbytes<WT>(a.K) + 127) / 128;
+  const int chunk = few_chunk<WT, SECOND, NBMAX, RT>(__builtin_ctz(a.split), few_nb_log2(8 * NB));
+  const int span = (pieces + a.split - 1) >> __builtin_ctz(a.split);   // the longest part
   f32x4 acc[RT][NB];
 #pragma unroll
   for (int i = 0; i < RT; ++i)
 #pragma unroll
     for (int b = 0; b < NB; ++b) acc[i][b] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int p0 = w * pieces / W, p1 = (w + 1) * pieces / W;
-  for (int p = p0; p < p1; p += U) {
-    u32x4 av[U][RT];
-    float sv[U][RT];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-#pragma unroll
-      for (int i = 0; i < RT; ++i) {
-        av[u][i] = u32x4{0, 0, 0, 0};
-        sv[u][i] = 0.f;
-        // chunks past the row's end (K no multiple of 256) hold zeros
-        if (p + u < p1 && (WT != kMx4 || (p + u) * 128 + 16 * c < kbytes)) {
-          av[u][i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(
-              wp + static_cast<size_t>(8 * i) * kbytes + static_cast<size_t>(p + u) * 128));
-          if constexpr (WT == kMx4) {
-            const uint32_t s8 = sp[(static_cast<size_t>(p + u) * a.N + 8 * i) * 8];
-            sv[u][i] = __uint_as_float(s8 << 23);   // only the exponent is read; 255 gives NaN
-          }
-        }
-      }
+  const int lr = lane & 7, lc = lane >> 3;
+#pragma unroll 1
+  for (int c0 = 0; c0 < span; c0 += chunk) {
+    if (c0 > 0 || st.whole != t.rank) {
+      // this wave's columns have landed (all but its newest loads, a step of
+      // weights); then every wave's, and every wave is done with the other half
+      if (st.behind) wait_vmcnt<U * RT * (WT == kMx4 ? 2 : 1)>();
+      else wait_vmcnt<0>();
+      lds_barrier();
+      st.whole = span <= chunk ? t.rank : -1;
     }
+    st.behind = false;
+    if (c0 + chunk < span) {
+      few_stage<WT, RT, NB, NBMAX, SECOND>(a, m, t, c0 + chunk, st.half ^ 1);
+    } else if (more && st.whole != next.rank) {
+      few_stage_first<WT, RT, NBMAX, SECOND>(a, m, next, st.half ^ 1);
+    }
+    const uint8_t* cols = m.cols + st.half * S::HALF;
+    const uint8_t* scales = m.scales + st.half * S::SCALES;
+    // Steps of U pieces in pairs, the registers of one loaded while the other's
+    // are multiplied; an odd number is filled up with a step that loads nothing.
+    const int len = t.p1 - t.p0, end = min(len, c0 + chunk);
+    const bool on = c0 + chunk < len;   // this wave has pieces in the next chunk
+    // Pieces past the end are zeros, multiplied with the last piece's columns:
+    // without branches the compiler knows how many loads are in flight.
+    auto multiply = [&](const u32x4(&av)[U][RT], const uint8_t(&sv)[U][RT], int p) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (p + u < p1) {
+      for (int u = 0; u < U; ++u) {
+        const int at = (part * chunk + min(p + u, end - 1) - c0) * NB;
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
           u32x4 bv[BL];
+          int sb = 0;
 #pragma unroll
-          for (int q = 0; q < BL; ++q) bv[q] = u32x4{0, 0, 0, 0};
-          // (hidden rows have nothing past the last column)
-          if (WT != kMx4 || (p + u) * 128 + 16 * c < kbytes) {
+          for (int j = 0; j < BL; ++j)
+            bv[j] = *reinterpret_cast<const u32x4*>(cols + ((at + b) * BL + j) * 1024 + lr * 128 + 16 * (lc ^ lr));
+          if constexpr (WT == kMx4) sb = scales[(at + b) * 64 + lr * 8 + lc];
 #pragma unroll
-            for (int q = 0; q < BP; ++q) {
-              const char* at = bp[b] + (static_cast<size_t>(p + u) * BP + q) * 128;
-              bv[q] = *reinterpret_cast<const u32x4*>(at);
-              if constexpr (HILO) bv[BP + q] = *reinterpret_cast<const u32x4*>(at + a.lo);
-            }
-          }
-#pragma unroll
-          for (int i = 0; i < RT; ++i) few_mma<WT, HILO>(av[u][i], sv[u][i], bv, acc[i][b]);
+          for (int i = 0; i < RT; ++i) few_mma<WT, BL>(av[u][i], sv[u][i], bv, sb, acc[i][b]);
         }
       }
+    };
+#pragma unroll 1
+    for (int p = c0; p < end; p += 2 * U) {
+      u32x4 bv[U][RT];
+      uint8_t bs[U][RT];
+      few_load<WT, RT, U>(a, t.w, t.s, t.row, t.p0 + p + U, t.p0 + end, bv, bs);
+      multiply(av, sv, p);
+      // then this chunk, the next one, or the next item (none: nothing)
+      const bool here = p + 2 * U < end, mine = here || on;
+      few_load<WT, RT, U>(a, mine ? t.w : next.w, mine ? t.s : next.s, mine ? t.row : next.row,
+                          here ? t.p0 + p + 2 * U : (on ? t.p0 + c0 + chunk : next.p0),
+                          here ? t.p0 + end : (on ? t.p0 + min(len, c0 + 2 * chunk) : (more ? next.c1 : 0)), av, sv);
+      multiply(bv, bs, p + U);
+      st.behind = true;
     }
+    // (the last chunk's half stays the current one if the next item uses it too)
+    if (c0 + chunk < span || (more && st.whole != next.rank)) st.half ^= 1;
   }
-  // D[r][c] (lanes 0-7 and 16-23) + D[r + 8][c + 8] (40 lanes further), then
-  // the waves' parts in wave order
+  // a wave without pieces has not fetched the next item's yet
+  if (t.p1 == t.p0) st.behind = true, few_load<WT, RT, U>(a, next.w, next.s, next.row, next.p0, more ? next.c1 : 0, av, sv);
+  // D[r][c] (lanes 0-7 and 16-23) + D[r + 8][c + 8] (40 lanes further) of every
+  // wave, then the parts of K in order
+  const int rows = RT * 8 * (kFewWaves >> __builtin_ctz(a.split));
+  lds_barrier();   // (every wave is done with the previous item's sums)
 #pragma unroll
   for (int i = 0; i < RT; ++i)
 #pragma unroll
@@ -303,136 +583,217 @@ __device__ __forceinline__ void few_tile(const FewArgs& a, int e, int n0, int fi
       for (int v = 0; v < 4; ++v) {
         const float other = __shfl(acc[i][b][v], (lane + 40) & 63, 64);
         if ((lane & 8) == 0 && lane < 32)
-          red[((w * NB + b) * 8 + (lane & 7)) * (RT * 8) + 8 * i + 4 * (lane >> 4) + v] = acc[i][b][v] + other;
+          m.red[((part * NB + b) * 8 + lr) * rows + (w >> __builtin_ctz(a.split)) * (8 * RT) + 8 * i + 4 * (lane >> 4) + v] =
+              acc[i][b][v] + other;
       }
-  __syncthreads();
-  for (int o = threadIdx.x; o < NB * 8 * RT * 8; o += W * 64) {
-    const int col = o % (RT * 8), tok = o / (RT * 8);
-    if (first + tok < n) {
-      float z = 0.f;
+  lds_barrier();
+  const int n0 = t.group * rows, units_log2 = __builtin_ctz(rows) - 3;   // eight rows of a column a thread
+  const int stride = NB * 8 * rows;
+#pragma unroll 1
+  for (int o = tid; o < t.n << units_log2; o += kFewThreads) {
+    const int tok = o >> units_log2, col = (o & ((1 << units_log2) - 1)) * 8;
+    const bool valid = n0 + col < a.N;
+    float z[8];
 #pragma unroll
-      for (int q = 0; q < W; ++q) z += red[(q * NB * 8 + tok) * (RT * 8) + col];
-      const int s = slot[first + tok];
-      if constexpr (SECOND) {
-        // read by whichever block adds this tile's experts, maybe on another XCD
-        __hip_atomic_store(a.part + static_cast<size_t>(s) * a.N + n0 + col, z * a.topk_gate[s], __ATOMIC_RELAXED,
-                           __HIP_MEMORY_SCOPE_AGENT);
-      } else {
-        const float hv = act == LUFFY_ACT_GELU ? act_f32<LUFFY_ACT_GELU>(z) : act_f32<LUFFY_ACT_SILU>(z);
-        char* dst = static_cast<char*>(a.h) + static_cast<size_t>(s) * a.h_pitch;
-        const int at = few_hidden_at<WT>(n0 + col);
+    for (int i = 0; i < 8; ++i) z[i] = 0.f;
+    for (int q = 0; q < a.split; ++q)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) z[i] += m.red[q * stride + tok * rows + col + i];
+    const int s = m.l.slot[t.first + tok];
+    if constexpr (SECOND) {
+      // read by whichever block adds this group's experts, maybe on another XCD
+      const float g = a.topk_gate[s];
+      float* dst = a.part + static_cast<size_t>(s) * a.N + n0 + col;
+      if (valid)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          __hip_atomic_store(dst + i, z[i] * g, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        z[i] = act == LUFFY_ACT_GELU ? act_f32<LUFFY_ACT_GELU>(z[i]) : act_f32<LUFFY_ACT_SILU>(z[i]);
+      uint8_t* dst = a.h + static_cast<size_t>(s) * few_pitch<WT, true>(a.N);
+      if constexpr (WT == kMx4) {
+        // (rows is a multiple of 32 and N of 64: a block's four lanes agree)
+        if (valid) store_e4m3<3>(z, (n0 + col) / 8, dst, a.h_scale + static_cast<size_t>(s) * few_scale_pitch(a.N));
+      } else if (valid) {
         if constexpr (WT == kF32) {
-          reinterpret_cast<float*>(dst)[at] = hv;
+          float4* f = reinterpret_cast<float4*>(dst + (n0 + col) * 4);
+          f[0] = make_float4(z[0], z[1], z[2], z[3]);
+          f[1] = make_float4(z[4], z[5], z[6], z[7]);
         } else {
-          // hidden rows stay float32 in effect: two bf16 halves whose sum is
-          // within 2^-17 of the value, multiplied one after the other
-          const uint32_t hi = pack_bf16x2(hv, 0.f) & 0xFFFFu;
-          float rest = hv - __uint_as_float(hi << 16);
-          if (!(fabsf(rest) < HUGE_VALF)) rest = 0.f;   // an infinite or NaN value is all in its high half
-          reinterpret_cast<uint16_t*>(dst)[at] = static_cast<uint16_t>(hi);
-          reinterpret_cast<uint16_t*>(dst + a.h_lo)[at] = static_cast<uint16_t>(pack_bf16x2(rest, 0.f) & 0xFFFFu);
+          uint32_t hi[4], lo[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            hi[i] = pack_bf16x2(z[2 * i], z[2 * i + 1]);
+            float r0 = z[2 * i] - __uint_as_float(hi[i] << 16), r1 = z[2 * i + 1] - __uint_as_float(hi[i] & 0xFFFF0000u);
+            // an infinite or NaN value is all in its first part
+            if (!(fabsf(r0) < HUGE_VALF)) r0 = 0.f;
+            if (!(fabsf(r1) < HUGE_VALF)) r1 = 0.f;
+            lo[i] = pack_bf16x2(r0, r1);
+          }
+          const int c = n0 + col;
+          uint8_t* f = dst + (c >> 6) * 256 + (c & 63) * 2;
+          *reinterpret_cast<uint4*>(f) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+          *reinterpret_cast<uint4*>(f + 128) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
         }
       }
     }
   }
-  __syncthreads();
 }
 
-template <int WT, int RT, int W, bool SECOND>
-__global__ __launch_bounds__(W * 64) void few_product_kernel(const FewArgs a, int act) {
-  __shared__ FewLists lists;
-  __shared__ float red[W * 4 * 8 * RT * 8];
-  __shared__ int last;
-  const int tiles = a.N / (RT * 8), tile = blockIdx.x % tiles;
-  int e, n, used;
-  if (!few_expert(a.topk_idx, a.T * a.k, blockIdx.x / tiles, lists, e, n, used)) return;
-  const int n0 = tile * RT * 8;
-  for (int first = 0; first < n; first += 32) {
-    const int left = n - first;
-    if (left <= 8) few_tile<WT, RT, W, 1, SECOND>(a, e, n0, first, n, lists.slot, red, act);
-    else if (left <= 16) few_tile<WT, RT, W, 2, SECOND>(a, e, n0, first, n, lists.slot, red, act);
-    else few_tile<WT, RT, W, 4, SECOND>(a, e, n0, first, n, lists.slot, red, act);
+template <int WT, int RT, int NBMAX, bool SECOND>
+__global__ __launch_bounds__(kFewThreads, NBMAX == 1 ? 4 : 2) void few_product_kernel(const FewArgs a, int act) {
+  __shared__ FewLds<NBMAX, RT> m;
+  constexpr int U = 8 / RT;
+  const int rows = RT * 8 * (kFewWaves >> __builtin_ctz(a.split)), groups = (a.N + rows - 1) / rows;
+  if (threadIdx.x < 64) few_lists(a.topk_idx, a.T * a.k, m.l);
+  __syncthreads();
+  // contiguous items a block, neighbouring blocks of an XCD on neighbouring items
+  const int used = __builtin_amdgcn_readfirstlane(m.l.used);
+  const long long items = static_cast<long long>(used) * groups;
+  const int vb = xcd_virtual_block();
+  int item = __builtin_amdgcn_readfirstlane(static_cast<int>(vb * items / gridDim.x));
+  const int end = __builtin_amdgcn_readfirstlane(static_cast<int>((vb + 1) * items / gridDim.x));
+  if (item >= end) return;
+  u32x4 av[U][RT];
+  uint8_t sv[U][RT];
+  const int begin = item;
+  FewItem t = few_item<WT, RT, NBMAX, SECOND>(a, m.l, item, groups);
+  FewStage st = {0, -1, true};
+  few_stage_first<WT, RT, NBMAX, SECOND>(a, m, t, 0);
+  few_load<WT, RT, U>(a, t.w, t.s, t.row, t.p0, t.c1, av, sv);
+#pragma unroll 1
+  for (; item < end; ++item) {
+    const bool more = item + 1 < end;
+    const FewItem next = few_item<WT, RT, NBMAX, SECOND>(a, m.l, more ? item + 1 : item, groups);
+    if (NBMAX == 1 || t.n <= 8) few_run<WT, RT, 1, NBMAX, SECOND>(a, m, t, next, more, act, st, av, sv);
+    else if (t.n <= 16) few_run<WT, RT, (NBMAX > 1 ? 2 : 1), NBMAX, SECOND>(a, m, t, next, more, act, st, av, sv);
+    else if (t.n <= 32) few_run<WT, RT, (NBMAX > 1 ? 4 : 1), NBMAX, SECOND>(a, m, t, next, more, act, st, av, sv);
+    else few_run<WT, RT, (NBMAX > 1 ? 8 : 1), NBMAX, SECOND>(a, m, t, next, more, act, st, av, sv);
+    t = next;
   }
   if constexpr (SECOND) {
-    // every wave waits for its own partial results, then the block counts
-    // itself done; the last of a tile's experts adds them in slot order
+    // Partial results are stored past the caches (agent scope), every wave waits
+    // until its own have arrived, then the block counts its items done, one
+    // thread an item; it adds the experts of every row group whose last item it
+    // had, reading past the caches.  No cache has to be written back or emptied
+    // for that: a release for each item took 79 us in place of 51 of a second
+    // product of 1024 blocks.
+    if (threadIdx.x == 0) m.ready = 0;
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    if (threadIdx.x == 0)
-      last = __hip_atomic_fetch_add(a.done + tile, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == used - 1;
-    __syncthreads();
-    if (!last) return;
-    for (int o = threadIdx.x; o < a.T * RT * 8; o += W * 64) {
-      const int t = o / (RT * 8), col = n0 + o % (RT * 8);
-      float v = 0.f;
-      for (int j = 0; j < a.k; ++j)
-        v += __hip_atomic_load(a.part + static_cast<size_t>(t * a.k + j) * a.N + col, __ATOMIC_RELAXED,
-                               __HIP_MEMORY_SCOPE_AGENT);
-      if constexpr (WT == kF32) static_cast<float*>(a.y)[static_cast<size_t>(t) * a.N + col] = v;
-      else static_cast<uint16_t*>(a.y)[static_cast<size_t>(t) * a.N + col] =
-          static_cast<uint16_t>(pack_bf16x2(v, 0.f) & 0xFFFFu);
+    for (int i0 = begin; i0 < end; i0 += kFewThreads) {
+      const int i = i0 + static_cast<int>(threadIdx.x);
+      if (i < end) {
+        const int g = i % groups;
+        if (__hip_atomic_fetch_add(a.done + g, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == used - 1)
+          m.group[atomicAdd(&m.ready, 1)] = g;
+      }
+      __syncthreads();
+      const int ready = m.ready;
+      for (int o = threadIdx.x; o < ready * a.T * (rows / 4); o += kFewThreads) {
+        const int col = (o % (rows / 4)) * 4, u = o / (rows / 4), tok = u % a.T;
+        const int n = m.group[u / a.T] * rows + col;
+        if (n >= a.N) continue;
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < a.k; ++j)
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            v[q] += __hip_atomic_load(a.part + static_cast<size_t>(tok * a.k + j) * a.N + n + q, __ATOMIC_RELAXED,
+                                      __HIP_MEMORY_SCOPE_AGENT);
+        if constexpr (WT == kF32) {
+          *reinterpret_cast<float4*>(static_cast<float*>(a.y) + static_cast<size_t>(tok) * a.N + n) =
+              make_float4(v[0], v[1], v[2], v[3]);
+        } else {
+          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.y) + static_cast<size_t>(tok) * a.N + n) =
+              make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+        }
+      }
+      __syncthreads();
+      if (threadIdx.x == 0) m.ready = 0;
+      __syncthreads();
     }
   }
 }
 
 struct FewWs {
-  uint16_t* xs;    // 4-bit weights: tokens in the product's order
-  char* h;         // hidden rows, then (bf16, 4-bit) their low halves
+  FewTerms f;
+  uint8_t* h;      // hidden rows
   float* part;
   int* done;
 };
 
-// rows padded to whole 256 values, so one layout serves every weight type
+// one layout serves every weight type: 4 bytes a hidden value (4-bit weights: 3
+// and the scales)
 FewWs carve_few(Carver& c, int T, int d, int k, int d_ff) {
-  const size_t dp = align_up(d, 256), fp = align_up(d_ff, 256);
+  const size_t slots = static_cast<size_t>(T) * k;
   FewWs w;
-  w.xs = c.take<uint16_t>(static_cast<size_t>(T) * dp);
-  w.h = c.take<char>(static_cast<size_t>(T) * k * fp * 4);
-  w.part = c.take<float>(static_cast<size_t>(T) * k * d);
+  w.f.x8 = c.take<uint8_t>(static_cast<size_t>(T) * few_pitch<kMx4, false>(d));
+  w.f.x8_scale = c.take<uint8_t>(static_cast<size_t>(T) * few_scale_pitch(d));
+  w.h = c.take<uint8_t>(slots * align_up(d_ff, 256) * 4);
+  w.f.h8 = w.h;
+  w.f.h8_scale = c.take<uint8_t>(slots * few_scale_pitch(d_ff));
+  w.f.d_ff = d_ff;
+  w.part = c.take<float>(slots * d);
   w.done = c.take<int>(d / 8);
   return w;
 }
 
-template <int WT, int RT, bool SECOND>
-void launch_few(const FewArgs& a, int experts, int act, hipStream_t s) {
-  launch(SECOND ? "few_ffn2" : "few_ffn1", few_product_kernel<WT, RT, 4, SECOND>, experts * (a.N / (RT * 8)), 256, 0,
-         s, a, act);
+template <int WT, int NBMAX, bool SECOND>
+void launch_few_nb(FewArgs a, int act, hipStream_t s) {
+  constexpr int RT = 2;
+  // most parts of K whose columns (an expert has at most T) fit the buffer
+  while (few_chunk<WT, SECOND, NBMAX, RT>(__builtin_ctz(a.split), few_nb_log2(a.T)) < 1) a.split /= 2;
+  const int grid = persistent_grid() * (NBMAX == 1 ? 2 : 1);
+  launch(SECOND ? "few_ffn2" : "few_ffn1", few_product_kernel<WT, RT, NBMAX, SECOND>, grid, kFewThreads, 0, s, a, act);
+}
+
+template <int WT, bool SECOND>
+void launch_few(FewArgs a, int used, int act, hipStream_t s) {
+#ifdef FEW_SPLIT1
+  a.split = SECOND ? FEW_SPLIT2 : FEW_SPLIT1;
+#else
+  a.split = 2;
+#endif
+  if (WT == kMx4 && !SECOND) a.split = std::min(a.split, 4);   // whole blocks of 32 hidden values
+  if (a.T <= 8) launch_few_nb<WT, 1, SECOND>(a, act, s);
+  else launch_few_nb<WT, 8, SECOND>(a, act, s);
 }
 
 template <int WT>
 void run_few(const void* x, int T, int d, const void* w_gate, const float* b_gate, int E, int k, const void* w1,
-             const uint8_t* s1, const void* w2, const uint8_t* s2, int d_ff, int act, int32_t* topk_idx,
+             const void* s1, const void* w2, const void* s2, int d_ff, int act, int32_t* topk_idx,
              float* topk_gate, void* y, const FewWs& ws, hipStream_t s) {
+  FewTerms f = ws.f;
+  if (WT != kMx4) f.x8 = nullptr;
   launch("few_gate", few_gate_kernel<WT == kF32>, T, kGateThreads, 0, s, x, d, w_gate, b_gate, E, k, topk_idx,
-         topk_gate, WT == kMx4 ? ws.xs : nullptr, ws.done, d / 8);
-  const int experts = E < T * k ? E : T * k;
-  const size_t fp = align_up(d_ff, 256);
+         topk_gate, f, ws.done, d / 8);
+  const int used = E < T * k ? E : T * k;
   FewArgs a = {};
   a.T = T;
   a.k = k;
   a.topk_idx = topk_idx;
   a.topk_gate = topk_gate;
-  a.w = w1;
-  a.scale = s1;
-  a.in = WT == kMx4 ? static_cast<const void*>(ws.xs) : x;
-  a.pitch = WT == kF32 ? d * 4 : (WT == kBf16 ? d * 2 : static_cast<int>(align_up(d, 256)) * 2);
+  a.w = static_cast<const uint8_t*>(w1);
+  a.w_scale = static_cast<const uint8_t*>(s1);
+  a.in = WT == kMx4 ? ws.f.x8 : static_cast<const uint8_t*>(x);
+  a.in_scale = ws.f.x8_scale;
   a.N = d_ff;
   a.K = d;
   a.h = ws.h;
-  a.h_pitch = static_cast<int>(WT == kF32 ? fp * 4 : fp * 2);
-  a.h_lo = static_cast<size_t>(T) * k * fp * 2;
-  launch_few<WT, 2, false>(a, experts, act, s);
-  a.w = w2;
-  a.scale = s2;
+  a.h_scale = ws.f.h8_scale;
+  launch_few<WT, false>(a, used, act, s);
+  a.w = static_cast<const uint8_t*>(w2);
+  a.w_scale = static_cast<const uint8_t*>(s2);
   a.in = ws.h;
-  a.pitch = a.h_pitch;
-  a.lo = a.h_lo;
+  a.in_scale = ws.f.h8_scale;
   a.N = d;
   a.K = d_ff;
   a.part = ws.part;
   a.done = ws.done;
   a.y = y;
-  launch_few<WT, 2, true>(a, experts, act, s);
+  launch_few<WT, true>(a, used, act, s);
 }
 
 bool few_misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
@@ -472,21 +833,21 @@ extern "C" int luffy_moe_few(const void* x, int T, int d, int dtype, const void*
   if (E > kMaxExperts) return fail(LUFFY_E_UNSUPPORTED, "luffy_moe_few: E=%d > %d", E, kMaxExperts);
   if (d % 64 != 0 || d_ff % 64 != 0 || d > 32768 || d_ff > 32768)
     return fail(LUFFY_E_UNSUPPORTED, "luffy_moe_few: d=%d d_ff=%d must be multiples of 64 and at most 32768", d, d_ff);
-  if (few_misaligned(x) || few_misaligned(w_gate) || few_misaligned(w1) || few_misaligned(w2))
-    return fail(LUFFY_E_INVALID, "luffy_moe_few: x, w_gate, w1 and w2 must be 16-byte aligned");
+  if (few_misaligned(x) || few_misaligned(w_gate) || few_misaligned(w1) || few_misaligned(w2) || few_misaligned(y))
+    return fail(LUFFY_E_INVALID, "luffy_moe_few: x, w_gate, w1, w2 and y must be 16-byte aligned");
+  if (weight_type != LUFFY_MX4 && static_cast<long long>(d) * d_ff * elem_bytes(dtype) > 0xFFFF0000ll)
+    return fail(LUFFY_E_UNSUPPORTED, "luffy_moe_few: one expert's weights exceed 4 GiB - 64 KiB");
   const size_t need = luffy_moe_few_workspace_size(T, d, E, k, d_ff);
   if (workspace_bytes < need || !workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u))
     return fail(LUFFY_E_WORKSPACE, "luffy_moe_few: workspace needs %zu bytes, 256-aligned", need);
   hipStream_t s = static_cast<hipStream_t>(stream);
   Carver c(workspace);
   const FewWs ws = carve_few(c, T, d, k, d_ff);
-  const auto* s1 = static_cast<const uint8_t*>(w1_scale);
-  const auto* s2 = static_cast<const uint8_t*>(w2_scale);
   if (weight_type == LUFFY_F32)
-    run_few<kF32>(x, T, d, w_gate, b_gate, E, k, w1, s1, w2, s2, d_ff, act, topk_idx, topk_gate, y, ws, s);
+    run_few<kF32>(x, T, d, w_gate, b_gate, E, k, w1, w1_scale, w2, w2_scale, d_ff, act, topk_idx, topk_gate, y, ws, s);
   else if (weight_type == LUFFY_BF16)
-    run_few<kBf16>(x, T, d, w_gate, b_gate, E, k, w1, s1, w2, s2, d_ff, act, topk_idx, topk_gate, y, ws, s);
+    run_few<kBf16>(x, T, d, w_gate, b_gate, E, k, w1, w1_scale, w2, w2_scale, d_ff, act, topk_idx, topk_gate, y, ws, s);
   else
-    run_few<kMx4>(x, T, d, w_gate, b_gate, E, k, w1, s1, w2, s2, d_ff, act, topk_idx, topk_gate, y, ws, s);
+    run_few<kMx4>(x, T, d, w_gate, b_gate, E, k, w1, w1_scale, w2, w2_scale, d_ff, act, topk_idx, topk_gate, y, ws, s);
   return check_launch("luffy_moe_few");
 }
