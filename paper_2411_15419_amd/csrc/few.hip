@@ -295,6 +295,8 @@ struct FewArgs {
   const uint8_t* in;        // columns: tokens (first product) or slots (second), FewLayout rows
   const uint8_t* in_scale;
   int N, K, T, k, split;    // split: waves that share a row's K (1, 2, 4 or 8)
+  int groups;               // row groups of N: ceil(N / rows of an item)
+  float per_group, per_block;   // 1 / groups, 1 / blocks
   const int32_t* topk_idx;
   const float* topk_gate;
   uint8_t *h, *h_scale;     // first product: hidden rows by slot
@@ -303,31 +305,66 @@ struct FewArgs {
   void* y;
 };
 
+// BYTES (4 or 16) a lane from offset off + soff to dst + BYTES * lane,
+// asynchronously.
+template <int BYTES>
+__device__ __forceinline__ void lds_dma(__amdgpu_buffer_rsrc_t r, uint32_t off, int soff,
+                                        __attribute__((address_space(3))) uint8_t* dst) {
+  using lds_ptr = __attribute__((address_space(3))) void*;
+  if constexpr (BYTES == 16) __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr)dst, 16, off, soff, 0, 0);
+  else __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr)dst, 4, off, soff, 0, 0);
+}
+
+// Barrier for data in LDS: waits for this wave's LDS accesses only, so that
+// loads from memory stay in flight across it.
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  raw_barrier();
+}
+
 // LDS of a block.  Columns come in chunks of K, double-buffered; NBMAX: groups
 // of eight columns that an item may have (an expert has at most T).  With one
 // group the registers allow two blocks a CU, with more one.
 template <int NBMAX, int RT>
 struct FewLds {
-  static constexpr int HALF = (NBMAX == 1 ? 30 : 52) * 1024;      // one chunk's columns
-  static constexpr int SCALES = NBMAX == 1 ? 512 : 1024;          // and their scale bytes (64 a piece and group)
+  static constexpr int HALF = (NBMAX == 1 ? 24 : 48) * 1024;      // one chunk's columns
+  static constexpr int SCALES = NBMAX == 1 ? 1024 : 2048;         // and their scale bytes (8 a piece and column)
   static constexpr int RED = NBMAX * 8 * kFewWaves * RT * 8 * 4;  // the waves' sums
   __attribute__((aligned(16))) uint8_t cols[2 * HALF];
   __attribute__((aligned(16))) uint8_t scales[2 * SCALES];
+  __attribute__((aligned(16))) uint8_t wscale[kFewWaves][2][1024];   // 4-bit weights: each wave's scales
   __attribute__((aligned(16))) float red[RED / 4];
   FewLists l;
   int ready;                       // row groups that this block adds up at its end
   int group[kFewThreads];
 };
 
-// Pieces of each part of K in a chunk of nb column groups.
-template <int WT, bool SECOND, int NBMAX, int RT>
-__host__ __device__ constexpr int few_chunk(int split_log2, int nb_log2) {
-  using S = FewLds<NBMAX, RT>;
-  const int fit = S::HALF / 1024 / FewLayout<WT, SECOND>::BL, scales = S::SCALES / 64;
-  return (WT == kMx4 && scales < fit ? scales : fit) >> (split_log2 + nb_log2);
+// Columns that n columns are kept as, log2: 1, 2, 4 or 8 in the one group, else
+// whole groups (2, 4 or 8 of them).
+__host__ __device__ constexpr int few_cols_log2(int n) {
+  return n <= 1 ? 0 : (n <= 2 ? 1 : (n <= 4 ? 2 : (n <= 8 ? 3 : (n <= 16 ? 4 : (n <= 32 ? 5 : 6)))));
 }
-// Groups of eight columns that n columns are multiplied as: 1, 2, 4 or 8.
-__host__ __device__ constexpr int few_nb_log2(int n) { return n <= 8 ? 0 : (n <= 16 ? 1 : (n <= 32 ? 2 : 3)); }
+// A half's bytes for each part of K (whole DMA instructions), and the pieces of
+// a part in a chunk.
+template <int NBMAX, int RT>
+__host__ __device__ constexpr int few_part_bytes(int split_log2) {
+  return (FewLds<NBMAX, RT>::HALF >> split_log2) & ~1023;
+}
+template <int WT, bool SECOND, int NBMAX, int RT>
+__host__ __device__ constexpr int few_chunk(int split_log2, int cols_log2) {
+  const int fit = few_part_bytes<NBMAX, RT>(split_log2) / (128 * FewLayout<WT, SECOND>::BL) >> cols_log2;
+  const int scales = FewLds<NBMAX, RT>::SCALES / 8 >> (split_log2 + cols_log2);
+  return WT == kMx4 && scales < fit ? scales : fit;
+}
+// With K in one part every number of columns fits (the loops over chunks would
+// not advance otherwise).
+template <int NBMAX, int COLS_LOG2>
+constexpr bool few_fits() {
+  return few_chunk<kF32, true, NBMAX, 2>(0, COLS_LOG2) >= 1 && few_chunk<kBf16, true, NBMAX, 2>(0, COLS_LOG2) >= 1 &&
+         few_chunk<kMx4, false, NBMAX, 2>(0, COLS_LOG2) >= 1 && few_chunk<kMx4, true, NBMAX, 2>(0, COLS_LOG2) >= 1;
+}
+static_assert(few_fits<1, 3>() && few_fits<8, 6>(), "a piece of every column in LDS");
+static_assert(sizeof(FewLds<8, 2>) <= 160 * 1024 && 2 * sizeof(FewLds<1, 2>) <= 160 * 1024, "LDS");
 
 // A block's waves are arranged as `split` parts of K by 8 / split row groups of
 // RT * 8 rows; a work item is the RT * 64 / split rows of one expert that the
@@ -354,11 +391,15 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t few_rsrc(const uint8_t* base) 
 }
 
 template <int WT, int RT, int NBMAX, bool SECOND>
-__device__ __forceinline__ FewItem few_item(const FewArgs& a, const FewLists& l, int item, int groups) {
+__device__ __forceinline__ FewItem few_item(const FewArgs& a, const FewLists& l, int item) {
   FewItem t;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  t.rank = __builtin_amdgcn_readfirstlane(item / groups);
-  t.group = item - t.rank * groups;
+  // item / groups: the product is off by less than one (items < 2^23)
+  int rank = static_cast<int>(static_cast<float>(item) * a.per_group);
+  if (rank * a.groups > item) --rank;
+  if ((rank + 1) * a.groups <= item) ++rank;
+  t.rank = __builtin_amdgcn_readfirstlane(rank);
+  t.group = item - t.rank * a.groups;
   const int e = __builtin_amdgcn_readfirstlane(l.expert[t.rank]);
   t.first = __builtin_amdgcn_readfirstlane(l.first[t.rank]);
   t.n = __builtin_amdgcn_readfirstlane(l.first[t.rank + 1]) - t.first;
@@ -368,7 +409,7 @@ __device__ __forceinline__ FewItem few_item(const FewArgs& a, const FewLists& l,
   const bool rows = static_cast<int>(t.row) < a.N;
   t.p0 = rows ? (part * pieces) >> split_log2 : 0;
   t.p1 = rows ? ((part + 1) * pieces) >> split_log2 : 0;
-  t.c1 = min(t.p1, t.p0 + few_chunk<WT, SECOND, NBMAX, RT>(split_log2, few_nb_log2(t.n)));
+  t.c1 = min(t.p1, t.p0 + few_chunk<WT, SECOND, NBMAX, RT>(split_log2, few_cols_log2(t.n)));
   t.w = a.w + static_cast<size_t>(e) * a.N * kbytes;
   t.s = WT == kMx4 ? a.w_scale + static_cast<size_t>(e) * pieces * a.N * 8 : nullptr;
   return t;
@@ -376,52 +417,37 @@ __device__ __forceinline__ FewItem few_item(const FewArgs& a, const FewLists& l,
 
 // U pieces of the wave's RT row tiles, from piece p on.  The loads are issued
 // whatever p is, and those at or past p1 fetch nothing (their offset is out of
-// the buffer's range; 4-bit: nor do chunks past the row's end): a load behind a
-// branch would leave the number of loads in flight open, and every use of an
-// earlier one would wait for all.
+// the buffer's range; 4-bit: nor do chunks past the row's end) and give zeros:
+// a load behind a branch would leave the number of loads in flight open, and
+// every use of an earlier one would wait for all.
 template <int WT, int RT, int U>
-__device__ __forceinline__ void few_load(const FewArgs& a, const uint8_t* w, const uint8_t* s, uint32_t row, int p,
-                                         int p1, u32x4 (&av)[U][RT], uint8_t (&sv)[U][RT]) {
+__device__ __forceinline__ void few_load(const FewArgs& a, const uint8_t* w, uint32_t row, int p, int p1,
+                                         u32x4 (&av)[U][RT]) {
   constexpr int kStream = 2;   // non-temporal: read once
   const int kbytes = few_kbytes<WT>(a.K), lane = threadIdx.x & 63, r = lane & 7, c = lane >> 3;
   const uint32_t off = static_cast<uint32_t>(r) * kbytes + 16 * c;
   const __amdgpu_buffer_rsrc_t wr = few_rsrc(w);
-  uint32_t in[U];   // all ones where the piece exists
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    in[u] = static_cast<uint32_t>((p + u - p1) >> 31);
-    uint32_t o = off | (~in[u] & kFewRange);
+    const uint32_t in = static_cast<uint32_t>((p + u - p1) >> 31);   // all ones where the piece exists
+    uint32_t o = off | (~in & kFewRange);
     if constexpr (WT == kMx4) o = (p + u) * 128 + 16 * c < kbytes ? o : kFewRange;
 #pragma unroll
     for (int i = 0; i < RT; ++i)
-      av[u][i] = __builtin_amdgcn_raw_buffer_load_b128(wr, o, ((row + 8 * i) * kbytes + (p + u) * 128) & in[u], kStream);
-  }
-  if constexpr (WT == kMx4) {
-    const __amdgpu_buffer_rsrc_t sr = few_rsrc(s);
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int i = 0; i < RT; ++i)
-        sv[u][i] = __builtin_amdgcn_raw_buffer_load_b8(sr, (8u * r + c) | (~in[u] & kFewRange),
-                                                       (((p + u) * a.N + row + 8 * i) * 8) & in[u], 0);
+      av[u][i] = __builtin_amdgcn_raw_buffer_load_b128(wr, o, ((row + 8 * i) * kbytes + (p + u) * 128) & in, kStream);
   }
 }
 
-// BYTES (4 or 16) a lane from offset off + soff to dst + BYTES * lane,
-// asynchronously.
-template <int BYTES>
-__device__ __forceinline__ void lds_dma(__amdgpu_buffer_rsrc_t r, uint32_t off, int soff,
-                                        __attribute__((address_space(3))) uint8_t* dst) {
-  using lds_ptr = __attribute__((address_space(3))) void*;
-  if constexpr (BYTES == 16) __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr)dst, 16, off, soff, 0, 0);
-  else __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr)dst, 4, off, soff, 0, 0);
-}
-
-// Barrier for data in LDS: waits for this wave's LDS accesses only, so that
-// loads from memory stay in flight across it.
-__device__ __forceinline__ void lds_barrier() {
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-  raw_barrier();
+// The scale bytes of the wave's 16 rows in eight pieces from piece p on, 128
+// bytes a piece, into the wave's own LDS: one instruction in place of sixteen
+// byte loads beside the weights' sixteen (pieces at or past p1: not fetched).
+template <int RT>
+__device__ __forceinline__ void few_load_scales(const FewArgs& a, const uint8_t* s, uint32_t row, int p, int p1,
+                                                __attribute__((address_space(3))) uint8_t* dst) {
+  static_assert(RT == 2, "16 rows of 8 bytes, a lane quarter of 8 lanes each 16 bytes");
+  const int lane = threadIdx.x & 63, u = lane >> 3;
+  const uint32_t off = (static_cast<uint32_t>(u) * a.N + 2 * (lane & 7)) * 8;
+  lds_dma<16>(few_rsrc(s), p + u < p1 ? off : kFewRange, p < p1 ? (p * a.N + row) * 8 : 0, dst);
 }
 
 // What the column buffers hold, and where the next chunk goes (block-uniform).
@@ -429,53 +455,55 @@ struct FewStage {
   int half;        // of the current chunk
   int whole;       // rank whose columns the half holds over all of K, -1: none
   bool behind;     // a step of weight loads follows the chunk's loads (this wave)
+  int slot;        // of the current scales (this wave)
 };
 
 // Columns of the chunk of item t that starts at piece c0 of every part, straight
-// into LDS (asynchronous loads, all in flight together): units of 8 columns x
-// 128 bytes, the eighths of a column's line permuted so that the products'
-// reads (eight columns, one eighth) fall on distinct banks.  Pieces past a
-// part's end are left out; nothing reads them.
+// into LDS (asynchronous loads, all in flight together): for every 128-byte
+// unit of a part's pieces one line a column, a line's eighths permuted so that
+// the products' reads (eight columns, one eighth) fall on distinct banks.  A
+// DMA instruction fills eight lines.  Lines past the part's end are not
+// fetched; nothing reads them.  The scale bytes of a column's chunk are one run.
 template <int WT, int RT, int NB, int NBMAX, bool SECOND>
-__device__ __forceinline__ void few_stage(const FewArgs& a, FewLds<NBMAX, RT>& m, const FewItem& t, int c0,
-                                          int half) {
-  using L = FewLayout<WT, SECOND>;
+__device__ __forceinline__ void few_stage(const FewArgs& a, FewLds<NBMAX, RT>& m, const FewItem& t, int c0, int half) {
   using S = FewLds<NBMAX, RT>;
   using lds_ptr = __attribute__((address_space(3))) uint8_t*;
-  constexpr int BL = L::BL;
+  constexpr int BL = FewLayout<WT, SECOND>::BL;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int pieces = (few_kbytes<WT>(a.K) + 127) / 128, pitch = few_pitch<WT, SECOND>(a.K);
-  const int split_log2 = __builtin_ctz(a.split);
-  const int chunk = few_chunk<WT, SECOND, NBMAX, RT>(split_log2, few_nb_log2(8 * NB));
-  const lds_ptr cols = (lds_ptr)m.cols + half * S::HALF, scales = (lds_ptr)m.scales + half * S::SCALES;
-  const int row = lane >> 3, pos = (lane & 7) ^ row;
-  const __amdgpu_buffer_rsrc_t in = few_rsrc(a.in), ins = few_rsrc(a.in_scale);
-  uint32_t off[NB], soff[NB];   // (the columns of a step are far below 4 GiB)
+  const int split_log2 = __builtin_ctz(a.split), cols_log2 = few_cols_log2(NB > 1 ? 8 * NB : t.n);
+  const int chunk = few_chunk<WT, SECOND, NBMAX, RT>(split_log2, cols_log2);
+  const __amdgpu_buffer_rsrc_t in = few_rsrc(a.in);   // (a step's columns are far below 4 GiB)
+  // this wave's part of K, one of the 8 / split waves that have it
+  const int kp = w & (a.split - 1), first = ((kp * pieces) >> split_log2) + c0;
+  const int len = min(chunk, (((kp + 1) * pieces) >> split_log2) - first), lines = len * BL << cols_log2;
+  const lds_ptr cols = (lds_ptr)m.cols + half * S::HALF + kp * few_part_bytes<NBMAX, RT>(split_log2);
+  const int line = lane >> 3;
+  uint32_t off[NB];
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
-    const int s = m.l.slot[t.first + min(8 * b + row, t.n - 1)];
-    off[b] = static_cast<uint32_t>(SECOND || a.k == 1 ? s : s >> 1) * pitch + 16 * pos;
-    if constexpr (WT == kMx4) {   // eight bytes a column: a dword each for 16 lanes
-      const int s2 = m.l.slot[t.first + min(8 * b + (lane >> 1 & 7), t.n - 1)];
-      soff[b] = static_cast<uint32_t>(SECOND || a.k == 1 ? s2 : s2 >> 1) * few_scale_pitch(a.K) + 4 * (lane & 1);
-    }
+    const int col = 8 * b + (line & ((1 << cols_log2) - 1));
+    const int s = m.l.slot[t.first + min(col, t.n - 1)];
+    off[b] = static_cast<uint32_t>(SECOND || a.k == 1 ? s : s >> 1) * pitch + 16 * ((lane & 7) ^ (col & 7));
+    if (NB == 1) off[b] += (line >> cols_log2) * 128;
   }
-  for (int kp = w & (a.split - 1); kp < a.split; kp += kFewWaves) {
-    const int first = (kp * pieces) >> split_log2, end = ((kp + 1) * pieces) >> split_log2;
 #pragma unroll 1
-    for (int i = w >> split_log2; i < chunk; i += kFewWaves >> split_log2) {
-      const int p = first + c0 + i;
-      if (p >= end) break;
+  for (int l0 = (w >> split_log2) * (8 * NB); l0 < lines; l0 += (kFewWaves >> split_log2) * (8 * NB)) {
+    const int soff = (first * BL + (l0 >> cols_log2)) * 128;
 #pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        const int unit = (kp * chunk + i) * NB + b;
-#pragma unroll
-        for (int j = 0; j < BL; ++j)
-          lds_dma<16>(in, off[b], (p * BL + j) * 128, cols + (unit * BL + j) * 1024);
-        if constexpr (WT == kMx4) {
-          if (lane < 16) lds_dma<4>(ins, soff[b], p * 8, scales + unit * 64);
-        }
-      }
+    for (int b = 0; b < NB; ++b)
+      lds_dma<16>(in, NB > 1 || l0 + line < lines ? off[b] : kFewRange, soff, cols + (l0 + 8 * b) * 128);
+  }
+  if constexpr (WT == kMx4) {
+    const __amdgpu_buffer_rsrc_t ins = few_rsrc(a.in_scale);
+    const lds_ptr scales = (lds_ptr)m.scales + half * S::SCALES;
+#pragma unroll 1
+    for (int col = w >> split_log2; col < 1 << cols_log2; col += kFewWaves >> split_log2) {
+      const int s = __builtin_amdgcn_readfirstlane(m.l.slot[t.first + min(col, t.n - 1)]);
+      const uint32_t row = static_cast<uint32_t>(SECOND || a.k == 1 ? s : s >> 1) * few_scale_pitch(a.K) + first * 8;
+      for (int d = 0; d < 2 * len; d += 64)
+        if (d + lane < 2 * len)
+          lds_dma<4>(ins, 4 * lane, row + 4 * d, scales + ((kp << cols_log2) + col) * chunk * 8 + 4 * d);
     }
   }
 }
@@ -497,26 +525,28 @@ __device__ __forceinline__ void few_stage_first(const FewArgs& a, FewLds<NBMAX, 
 template <int WT, int RT, int NB, int NBMAX, bool SECOND>
 __device__ __forceinline__ void few_run(const FewArgs& a, FewLds<NBMAX, RT>& m, const FewItem& t,
                                         const FewItem& next, bool more, int act, FewStage& st,
-                                        u32x4 (&av)[8 / RT][RT], uint8_t (&sv)[8 / RT][RT]) {
+                                        u32x4 (&av)[8 / RT][RT]) {
   using L = FewLayout<WT, SECOND>;
   using S = FewLds<NBMAX, RT>;
   constexpr int U = 8 / RT, BL = L::BL;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int part = w & (a.split - 1), pieces = (few_kbytes<WT>(a.K) + 127) / 128;
-  const int chunk = few_chunk<WT, SECOND, NBMAX, RT>(__builtin_ctz(a.split), few_nb_log2(8 * NB));
+  const int split_log2 = __builtin_ctz(a.split), cols_log2 = few_cols_log2(NB > 1 ? 8 * NB : t.n);
+  const int chunk = few_chunk<WT, SECOND, NBMAX, RT>(split_log2, cols_log2);
   const int span = (pieces + a.split - 1) >> __builtin_ctz(a.split);   // the longest part
   f32x4 acc[RT][NB];
 #pragma unroll
   for (int i = 0; i < RT; ++i)
 #pragma unroll
     for (int b = 0; b < NB; ++b) acc[i][b] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int lr = lane & 7, lc = lane >> 3;
+  using lds_ptr = __attribute__((address_space(3))) uint8_t*;
+  const int lr = lane & 7, lc = lane >> 3, lane_scale = 8 * lr + lc;
 #pragma unroll 1
   for (int c0 = 0; c0 < span; c0 += chunk) {
     if (c0 > 0 || st.whole != t.rank) {
       // this wave's columns have landed (all but its newest loads, a step of
       // weights); then every wave's, and every wave is done with the other half
-      if (st.behind) wait_vmcnt<U * RT * (WT == kMx4 ? 2 : 1)>();
+      if (st.behind) wait_vmcnt<U * RT>();
       else wait_vmcnt<0>();
       lds_barrier();
       st.whole = span <= chunk ? t.rank : -1;
@@ -527,50 +557,70 @@ __device__ __forceinline__ void few_run(const FewArgs& a, FewLds<NBMAX, RT>& m, 
     } else if (more && st.whole != next.rank) {
       few_stage_first<WT, RT, NBMAX, SECOND>(a, m, next, st.half ^ 1);
     }
-    const uint8_t* cols = m.cols + st.half * S::HALF;
-    const uint8_t* scales = m.scales + st.half * S::SCALES;
     // Steps of U pieces in pairs, the registers of one loaded while the other's
     // are multiplied; an odd number is filled up with a step that loads nothing.
     const int len = t.p1 - t.p0, end = min(len, c0 + chunk);
     const bool on = c0 + chunk < len;   // this wave has pieces in the next chunk
+    // this lane's column in each group, and where its lines start
+    const int lcol = lr & ((1 << cols_log2) - 1);
+    const uint8_t* cols = m.cols + st.half * S::HALF + part * few_part_bytes<NBMAX, RT>(split_log2) + lcol * 128 +
+                          16 * (lc ^ (lcol & 7));
+    const uint8_t* scales = m.scales + st.half * S::SCALES + ((part << cols_log2) + lcol) * chunk * 8 + lc;
     // Pieces past the end are zeros, multiplied with the last piece's columns:
     // without branches the compiler knows how many loads are in flight.
-    auto multiply = [&](const u32x4(&av)[U][RT], const uint8_t(&sv)[U][RT], int p) {
+    auto multiply = [&](const u32x4(&av)[U][RT], int p, const uint8_t* ws) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int at = (part * chunk + min(p + u, end - 1) - c0) * NB;
+        const int at = min(p + u, end - 1) - c0;
+        int sa[RT];
+#pragma unroll
+        for (int i = 0; i < RT; ++i) sa[i] = WT == kMx4 ? ws[128 * u + 64 * i] & ((p + u - end) >> 31) : 0;
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
           u32x4 bv[BL];
           int sb = 0;
 #pragma unroll
           for (int j = 0; j < BL; ++j)
-            bv[j] = *reinterpret_cast<const u32x4*>(cols + ((at + b) * BL + j) * 1024 + lr * 128 + 16 * (lc ^ lr));
-          if constexpr (WT == kMx4) sb = scales[(at + b) * 64 + lr * 8 + lc];
+            bv[j] = *reinterpret_cast<const u32x4*>(cols + (((at * BL + j) << cols_log2) + 8 * b) * 128);
+          if constexpr (WT == kMx4) sb = scales[8 * b * chunk * 8 + at * 8];
 #pragma unroll
-          for (int i = 0; i < RT; ++i) few_mma<WT, BL>(av[u][i], sv[u][i], bv, sb, acc[i][b]);
+          for (int i = 0; i < RT; ++i) few_mma<WT, BL>(av[u][i], sa[i], bv, sb, acc[i][b]);
         }
       }
     };
 #pragma unroll 1
     for (int p = c0; p < end; p += 2 * U) {
-      u32x4 bv[U][RT];
-      uint8_t bs[U][RT];
-      few_load<WT, RT, U>(a, t.w, t.s, t.row, t.p0 + p + U, t.p0 + end, bv, bs);
-      multiply(av, sv, p);
-      // then this chunk, the next one, or the next item (none: nothing)
+      // what comes next: this chunk, the next one, or the next item (none: nothing)
       const bool here = p + 2 * U < end, mine = here || on;
-      few_load<WT, RT, U>(a, mine ? t.w : next.w, mine ? t.s : next.s, mine ? t.row : next.row,
-                          here ? t.p0 + p + 2 * U : (on ? t.p0 + c0 + chunk : next.p0),
-                          here ? t.p0 + end : (on ? t.p0 + min(len, c0 + 2 * chunk) : (more ? next.c1 : 0)), av, sv);
-      multiply(bv, bs, p + U);
+      const uint32_t row = mine ? t.row : next.row;
+      const int q = here ? t.p0 + p + 2 * U : (on ? t.p0 + c0 + chunk : next.p0);
+      const int q1 = here ? t.p0 + end : (on ? t.p0 + min(len, c0 + 2 * chunk) : (more ? next.c1 : 0));
+      const uint8_t* ws = m.wscale[w][st.slot] + lane_scale;
+      if constexpr (WT == kMx4) {
+        wait_vmcnt<U * RT>();   // this pair's scales (older than the step of weights in flight) have landed
+        asm volatile("" ::: "memory");
+        few_load_scales<RT>(a, mine ? t.s : next.s, row, q, q1, (lds_ptr)m.wscale[w][st.slot ^ 1]);
+        st.slot ^= 1;
+      }
+      u32x4 bv[U][RT];
+      few_load<WT, RT, U>(a, t.w, t.row, t.p0 + p + U, t.p0 + end, bv);
+      multiply(av, p, ws);
+      few_load<WT, RT, U>(a, mine ? t.w : next.w, row, q, q1, av);
+      multiply(bv, p + U, ws + 128 * U);
       st.behind = true;
     }
     // (the last chunk's half stays the current one if the next item uses it too)
     if (c0 + chunk < span || (more && st.whole != next.rank)) st.half ^= 1;
   }
   // a wave without pieces has not fetched the next item's yet
-  if (t.p1 == t.p0) st.behind = true, few_load<WT, RT, U>(a, next.w, next.s, next.row, next.p0, more ? next.c1 : 0, av, sv);
+  if (t.p1 == t.p0) {
+    if constexpr (WT == kMx4) {
+      st.slot ^= 1;
+      few_load_scales<RT>(a, next.s, next.row, next.p0, more ? next.c1 : 0, (lds_ptr)m.wscale[w][st.slot]);
+    }
+    few_load<WT, RT, U>(a, next.w, next.row, next.p0, more ? next.c1 : 0, av);
+    st.behind = true;
+  }
   // D[r][c] (lanes 0-7 and 16-23) + D[r + 8][c + 8] (40 lanes further) of every
   // wave, then the parts of K in order
   const int rows = RT * 8 * (kFewWaves >> __builtin_ctz(a.split));
@@ -587,55 +637,49 @@ __device__ __forceinline__ void few_run(const FewArgs& a, FewLds<NBMAX, RT>& m, 
               acc[i][b][v] + other;
       }
   lds_barrier();
-  const int n0 = t.group * rows, units_log2 = __builtin_ctz(rows) - 3;   // eight rows of a column a thread
+  // V rows of a column a thread: 4-bit weights' hidden rows are rounded eight at
+  // a time, everything else goes out in pairs (more threads at work)
+  constexpr int V = WT == kMx4 && !SECOND ? 8 : 2;
+  const int n0 = t.group * rows, units_log2 = __builtin_ctz(rows) - __builtin_ctz(V);
   const int stride = NB * 8 * rows;
 #pragma unroll 1
   for (int o = tid; o < t.n << units_log2; o += kFewThreads) {
-    const int tok = o >> units_log2, col = (o & ((1 << units_log2) - 1)) * 8;
-    const bool valid = n0 + col < a.N;
-    float z[8];
+    const int tok = o >> units_log2, col = (o & ((1 << units_log2) - 1)) * V, n = n0 + col;
+    const bool valid = n < a.N;
+    float z[V];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) z[i] = 0.f;
+    for (int i = 0; i < V; ++i) z[i] = 0.f;
     for (int q = 0; q < a.split; ++q)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) z[i] += m.red[q * stride + tok * rows + col + i];
+      for (int i = 0; i < V; ++i) z[i] += m.red[q * stride + tok * rows + col + i];
     const int s = m.l.slot[t.first + tok];
     if constexpr (SECOND) {
       // read by whichever block adds this group's experts, maybe on another XCD
       const float g = a.topk_gate[s];
-      float* dst = a.part + static_cast<size_t>(s) * a.N + n0 + col;
+      const uint64_t v = static_cast<uint64_t>(__float_as_uint(z[1] * g)) << 32 | __float_as_uint(z[0] * g);
       if (valid)
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          __hip_atomic_store(dst + i, z[i] * g, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(reinterpret_cast<uint64_t*>(a.part + static_cast<size_t>(s) * a.N + n), v,
+                           __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
+      for (int i = 0; i < V; ++i)
         z[i] = act == LUFFY_ACT_GELU ? act_f32<LUFFY_ACT_GELU>(z[i]) : act_f32<LUFFY_ACT_SILU>(z[i]);
       uint8_t* dst = a.h + static_cast<size_t>(s) * few_pitch<WT, true>(a.N);
       if constexpr (WT == kMx4) {
         // (rows is a multiple of 32 and N of 64: a block's four lanes agree)
-        if (valid) store_e4m3<3>(z, (n0 + col) / 8, dst, a.h_scale + static_cast<size_t>(s) * few_scale_pitch(a.N));
+        if (valid) store_e4m3<3>(z, n / 8, dst, a.h_scale + static_cast<size_t>(s) * few_scale_pitch(a.N));
       } else if (valid) {
         if constexpr (WT == kF32) {
-          float4* f = reinterpret_cast<float4*>(dst + (n0 + col) * 4);
-          f[0] = make_float4(z[0], z[1], z[2], z[3]);
-          f[1] = make_float4(z[4], z[5], z[6], z[7]);
+          *reinterpret_cast<float2*>(dst + n * 4) = make_float2(z[0], z[1]);
         } else {
-          uint32_t hi[4], lo[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            hi[i] = pack_bf16x2(z[2 * i], z[2 * i + 1]);
-            float r0 = z[2 * i] - __uint_as_float(hi[i] << 16), r1 = z[2 * i + 1] - __uint_as_float(hi[i] & 0xFFFF0000u);
-            // an infinite or NaN value is all in its first part
-            if (!(fabsf(r0) < HUGE_VALF)) r0 = 0.f;
-            if (!(fabsf(r1) < HUGE_VALF)) r1 = 0.f;
-            lo[i] = pack_bf16x2(r0, r1);
-          }
-          const int c = n0 + col;
-          uint8_t* f = dst + (c >> 6) * 256 + (c & 63) * 2;
-          *reinterpret_cast<uint4*>(f) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-          *reinterpret_cast<uint4*>(f + 128) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+          const uint32_t hi = pack_bf16x2(z[0], z[1]);
+          float r0 = z[0] - __uint_as_float(hi << 16), r1 = z[1] - __uint_as_float(hi & 0xFFFF0000u);
+          // an infinite or NaN value is all in its first part
+          if (!(fabsf(r0) < HUGE_VALF)) r0 = 0.f;
+          if (!(fabsf(r1) < HUGE_VALF)) r1 = 0.f;
+          uint8_t* f = dst + (n >> 6) * 256 + (n & 63) * 2;
+          *reinterpret_cast<uint32_t*>(f) = hi;
+          *reinterpret_cast<uint32_t*>(f + 128) = pack_bf16x2(r0, r1);
         }
       }
     }
@@ -646,31 +690,37 @@ template <int WT, int RT, int NBMAX, bool SECOND>
 __global__ __launch_bounds__(kFewThreads, NBMAX == 1 ? 4 : 2) void few_product_kernel(const FewArgs a, int act) {
   __shared__ FewLds<NBMAX, RT> m;
   constexpr int U = 8 / RT;
-  const int rows = RT * 8 * (kFewWaves >> __builtin_ctz(a.split)), groups = (a.N + rows - 1) / rows;
+  const int rows = RT * 8 * (kFewWaves >> __builtin_ctz(a.split));
   if (threadIdx.x < 64) few_lists(a.topk_idx, a.T * a.k, m.l);
   __syncthreads();
   // contiguous items a block, neighbouring blocks of an XCD on neighbouring items
   const int used = __builtin_amdgcn_readfirstlane(m.l.used);
-  const long long items = static_cast<long long>(used) * groups;
-  const int vb = xcd_virtual_block();
-  int item = __builtin_amdgcn_readfirstlane(static_cast<int>(vb * items / gridDim.x));
-  const int end = __builtin_amdgcn_readfirstlane(static_cast<int>((vb + 1) * items / gridDim.x));
+  const int items = used * a.groups, vb = xcd_virtual_block();
+  const float share = static_cast<float>(items) * a.per_block;
+  int item = __builtin_amdgcn_readfirstlane(static_cast<int>(static_cast<float>(vb) * share));
+  const int end = vb + 1 == static_cast<int>(gridDim.x)
+                      ? items
+                      : __builtin_amdgcn_readfirstlane(min(items, static_cast<int>(static_cast<float>(vb + 1) * share)));
   if (item >= end) return;
   u32x4 av[U][RT];
-  uint8_t sv[U][RT];
   const int begin = item;
-  FewItem t = few_item<WT, RT, NBMAX, SECOND>(a, m.l, item, groups);
-  FewStage st = {0, -1, true};
+  FewItem t = few_item<WT, RT, NBMAX, SECOND>(a, m.l, item);
+  FewStage st = {0, -1, true, 0};
   few_stage_first<WT, RT, NBMAX, SECOND>(a, m, t, 0);
-  few_load<WT, RT, U>(a, t.w, t.s, t.row, t.p0, t.c1, av, sv);
+  if constexpr (WT == kMx4) {
+    using lds_ptr = __attribute__((address_space(3))) uint8_t*;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    few_load_scales<RT>(a, t.s, t.row, t.p0, t.c1, (lds_ptr)m.wscale[w][0]);
+  }
+  few_load<WT, RT, U>(a, t.w, t.row, t.p0, t.c1, av);
 #pragma unroll 1
   for (; item < end; ++item) {
     const bool more = item + 1 < end;
-    const FewItem next = few_item<WT, RT, NBMAX, SECOND>(a, m.l, more ? item + 1 : item, groups);
-    if (NBMAX == 1 || t.n <= 8) few_run<WT, RT, 1, NBMAX, SECOND>(a, m, t, next, more, act, st, av, sv);
-    else if (t.n <= 16) few_run<WT, RT, (NBMAX > 1 ? 2 : 1), NBMAX, SECOND>(a, m, t, next, more, act, st, av, sv);
-    else if (t.n <= 32) few_run<WT, RT, (NBMAX > 1 ? 4 : 1), NBMAX, SECOND>(a, m, t, next, more, act, st, av, sv);
-    else few_run<WT, RT, (NBMAX > 1 ? 8 : 1), NBMAX, SECOND>(a, m, t, next, more, act, st, av, sv);
+    const FewItem next = few_item<WT, RT, NBMAX, SECOND>(a, m.l, more ? item + 1 : item);
+    if (NBMAX == 1 || t.n <= 8) few_run<WT, RT, 1, NBMAX, SECOND>(a, m, t, next, more, act, st, av);
+    else if (t.n <= 16) few_run<WT, RT, (NBMAX > 1 ? 2 : 1), NBMAX, SECOND>(a, m, t, next, more, act, st, av);
+    else if (t.n <= 32) few_run<WT, RT, (NBMAX > 1 ? 4 : 1), NBMAX, SECOND>(a, m, t, next, more, act, st, av);
+    else few_run<WT, RT, (NBMAX > 1 ? 8 : 1), NBMAX, SECOND>(a, m, t, next, more, act, st, av);
     t = next;
   }
   if constexpr (SECOND) {
@@ -686,22 +736,29 @@ __global__ __launch_bounds__(kFewThreads, NBMAX == 1 ? 4 : 2) void few_product_k
     for (int i0 = begin; i0 < end; i0 += kFewThreads) {
       const int i = i0 + static_cast<int>(threadIdx.x);
       if (i < end) {
-        const int g = i % groups;
+        const int g = i % a.groups;
         if (__hip_atomic_fetch_add(a.done + g, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == used - 1)
           m.group[atomicAdd(&m.ready, 1)] = g;
       }
       __syncthreads();
       const int ready = m.ready;
       for (int o = threadIdx.x; o < ready * a.T * (rows / 4); o += kFewThreads) {
-        const int col = (o % (rows / 4)) * 4, u = o / (rows / 4), tok = u % a.T;
+        const int col = (o & (rows / 4 - 1)) * 4, u = o >> (__builtin_ctz(rows) - 2), tok = u % a.T;
         const int n = m.group[u / a.T] * rows + col;
         if (n >= a.N) continue;
-        float v[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int j = 0; j < a.k; ++j)
+        uint64_t p[2][2] = {{0, 0}, {0, 0}};
+        const uint64_t* src = reinterpret_cast<const uint64_t*>(a.part + static_cast<size_t>(tok * a.k) * a.N + n);
 #pragma unroll
-          for (int q = 0; q < 4; ++q)
-            v[q] += __hip_atomic_load(a.part + static_cast<size_t>(tok * a.k + j) * a.N + n + q, __ATOMIC_RELAXED,
-                                      __HIP_MEMORY_SCOPE_AGENT);
+        for (int j = 0; j < 2; ++j)
+          if (j < a.k)
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+              p[j][q] = __hip_atomic_load(src + j * (a.N / 2) + q, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        float v[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          v[q] = __uint_as_float(static_cast<uint32_t>(p[0][q >> 1] >> (32 * (q & 1)))) +
+                 __uint_as_float(static_cast<uint32_t>(p[1][q >> 1] >> (32 * (q & 1))));
         if constexpr (WT == kF32) {
           *reinterpret_cast<float4*>(static_cast<float*>(a.y) + static_cast<size_t>(tok) * a.N + n) =
               make_float4(v[0], v[1], v[2], v[3]);
@@ -744,17 +801,33 @@ template <int WT, int NBMAX, bool SECOND>
 void launch_few_nb(FewArgs a, int act, hipStream_t s) {
   constexpr int RT = 2;
   // most parts of K whose columns (an expert has at most T) fit the buffer
-  while (few_chunk<WT, SECOND, NBMAX, RT>(__builtin_ctz(a.split), few_nb_log2(a.T)) < 1) a.split /= 2;
+  while (a.split > 1 && few_chunk<WT, SECOND, NBMAX, RT>(__builtin_ctz(a.split), few_cols_log2(a.T)) < 1) a.split /= 2;
   const int grid = persistent_grid() * (NBMAX == 1 ? 2 : 1);
+  const int rows = 8 * RT * kFewWaves / a.split;
+  a.groups = (a.N + rows - 1) / rows;
+  a.per_group = 1.0f / a.groups;
+  a.per_block = 1.0f / grid;
   launch(SECOND ? "few_ffn2" : "few_ffn1", few_product_kernel<WT, RT, NBMAX, SECOND>, grid, kFewThreads, 0, s, a, act);
 }
 
+// Rows of an item.  More rows take their columns to LDS less often; fewer give
+// every CU an item and split K over more waves.  So: the fewest parts of K with
+// an item a CU, and eight where no number of parts gives that.  61 tokens on 16
+// experts of 1024 x 4096 (bf16), second product: 1, 2 and 4 parts (128, 256,
+// 512 items) 48, 41 and 40 us; 64 tokens on 8 experts of 4096 x 11008: 1 and 2
+// parts (256, 512 items) 141 and 151 us; one token on two experts of 1024 x
+// 4096: 1, 2, 4 and 8 parts (16 to 128 items) 62, 35, 24 and 16 us.
 template <int WT, bool SECOND>
-void launch_few(FewArgs a, int used, int act, hipStream_t s) {
+void launch_few(FewArgs a, int E, int act, hipStream_t s) {
+  // experts in use, expected at an even load
+  double idle = 1.0;
+  for (int t = 0; t < a.T; ++t) idle *= 1.0 - static_cast<double>(a.k) / E;
+  const double used = std::max(1.0, E * (1.0 - idle));
+  constexpr int kRows = 8 * 2 * kFewWaves;
+  a.split = 1;
+  while (a.split < kFewWaves && used * ((a.N * a.split + kRows - 1) / kRows) < persistent_grid()) a.split *= 2;
 #ifdef FEW_SPLIT1
   a.split = SECOND ? FEW_SPLIT2 : FEW_SPLIT1;
-#else
-  a.split = 2;
 #endif
   if (WT == kMx4 && !SECOND) a.split = std::min(a.split, 4);   // whole blocks of 32 hidden values
   if (a.T <= 8) launch_few_nb<WT, 1, SECOND>(a, act, s);
@@ -769,7 +842,6 @@ void run_few(const void* x, int T, int d, const void* w_gate, const float* b_gat
   if (WT != kMx4) f.x8 = nullptr;
   launch("few_gate", few_gate_kernel<WT == kF32>, T, kGateThreads, 0, s, x, d, w_gate, b_gate, E, k, topk_idx,
          topk_gate, f, ws.done, d / 8);
-  const int used = E < T * k ? E : T * k;
   FewArgs a = {};
   a.T = T;
   a.k = k;
@@ -783,7 +855,7 @@ void run_few(const void* x, int T, int d, const void* w_gate, const float* b_gat
   a.K = d;
   a.h = ws.h;
   a.h_scale = ws.f.h8_scale;
-  launch_few<WT, false>(a, used, act, s);
+  launch_few<WT, false>(a, E, act, s);
   a.w = static_cast<const uint8_t*>(w2);
   a.w_scale = static_cast<const uint8_t*>(s2);
   a.in = ws.h;
@@ -793,7 +865,7 @@ void run_few(const void* x, int T, int d, const void* w_gate, const float* b_gat
   a.part = ws.part;
   a.done = ws.done;
   a.y = y;
-  launch_few<WT, true>(a, used, act, s);
+  launch_few<WT, true>(a, E, act, s);
 }
 
 bool few_misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
