@@ -133,8 +133,10 @@ def _p(t: Optional[torch.Tensor]):
 
 
 def _stream(stream) -> Optional[int]:
+    # the current stream's handle without a Stream object: 0.3 us instead of
+    # 2.7, of about 7 for a whole call
     if stream is None:
-        stream = torch.cuda.current_stream()
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return stream.cuda_stream
 
 

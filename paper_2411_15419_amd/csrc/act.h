@@ -1,18 +1,56 @@
-// Expert activations in float32, for results that are rounded once at the end
-// (the bf16 FFN's cheaper forms, whose error hides under its hidden rows'
-// rounding, are its own).
+// Expert activations.
 #pragma once
 
 #include "luffy_common.h"
 
 namespace luffy {
 
+// Exact to float32 (the device math library), for results that stay in it.
 template <int ACT>
 __device__ __forceinline__ float act_f32(float z) {
   if constexpr (ACT == LUFFY_ACT_GELU) {
     return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
   } else {
     return z / (1.0f + expf(-z));
+  }
+}
+
+// Activation code of a plain product (no activation), used by the backward.
+constexpr int kActNone = 2;
+
+// For results that are rounded to bf16 (relative step 2^-8) or to 4 bits: a
+// dozen VALU operations instead of the library erf, which dominated the
+// epilogue of the first product.
+//   GELU: erf from Abramowitz & Stegun 7.1.26 (Hastings' rational
+//   approximation), erf(u) = 1 - q(u), q(u) = t (a1 + t (a2 + ... + t a5))
+//   e^{-u^2}, t = 1 / (1 + p u), u >= 0, |error| <= 1.5e-7.  With
+//   u = |z| / sqrt(2): GELU(z) = z (1 - q/2) for z >= 0 and z q/2 for z < 0,
+//   evaluated as |z| (1 - q) / 2 + z / 2.
+//   SiLU: z / (1 + 2^{-z log2 e}).
+// The hardware exp2 and reciprocal are accurate to about 1 ulp.
+template <int ACT>
+__device__ __forceinline__ float act_fast(float z) {
+  if constexpr (ACT == kActNone) {
+    return z;
+  } else if constexpr (ACT == LUFFY_ACT_GELU) {
+    // Hastings' erf(u) = 1 - t (a1 + a2 t + ... + a5 t^4) e^{-u^2},
+    // t = 1 / (1 + p u), u = |z| / sqrt(2), with the a_i halved here so
+    // that w = 1/2 - t e P(t) = erf(u) / 2.  Then z Phi(z) = |z| w + z / 2
+    // for either sign of z (Phi(z) = 1/2 + sign(z) erf(u) / 2): 10 vector
+    // operations and two transcendentals per element.
+    constexpr float kPs = 0.3275911f * 0.70710678118654752f;   // p / sqrt(2)
+    constexpr float kB1 = 0.5f * 0.254829592f, kB2 = 0.5f * -0.284496736f, kB3 = 0.5f * 1.421413741f;
+    constexpr float kB4 = 0.5f * -1.453152027f, kB5 = 0.5f * 1.061405429f;
+    constexpr float kHalfLog2e = -0.72134752044448170f;   // -log2(e) / 2
+    const float a = fabsf(z);
+    const float t = __builtin_amdgcn_rcpf(fmaf(kPs, a, 1.0f));
+    const float pt = fmaf(t, fmaf(t, fmaf(t, fmaf(t, kB5, kB4), kB3), kB2), kB1);
+    const float e = __builtin_amdgcn_exp2f(z * z * kHalfLog2e);   // e^{-u^2}
+    const float w = fmaf(-(t * e), pt, 0.5f);
+    return fmaf(a, w, 0.5f * z);
+  } else {
+    constexpr float kNegLog2e = -1.44269504088896341f;
+    return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * kNegLog2e));
   }
 }
 

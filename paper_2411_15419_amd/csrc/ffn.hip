@@ -12,61 +12,12 @@
 // float32: 64 x 64 or 32 x 32 tiles of float32 MFMA.
 #include <type_traits>
 
+#include "act.h"
 #include "gemm_core.h"
 #include "luffy_common.h"
 
 namespace luffy {
 namespace {
-
-// Activations of the float32 path: exact erf-GELU and SiLU from the device
-// math library.
-template <int ACT>
-__device__ __forceinline__ float act_fn(float z) {
-  if constexpr (ACT == LUFFY_ACT_GELU) {
-    return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
-  } else {
-    return z / (1.0f + expf(-z));
-  }
-}
-
-// Activations of the bf16 path, whose results are rounded to bf16 (relative
-// step 2^-8): a dozen VALU operations instead of the library erf, which
-// dominated the epilogue of the first product.
-//   GELU: erf from Abramowitz & Stegun 7.1.26 (Hastings' rational
-//   approximation), erf(u) = 1 - q(u), q(u) = t (a1 + t (a2 + ... + t a5))
-//   e^{-u^2}, t = 1 / (1 + p u), u >= 0, |error| <= 1.5e-7.  With
-//   u = |z| / sqrt(2): GELU(z) = z (1 - q/2) for z >= 0 and z q/2 for z < 0,
-//   evaluated as |z| (1 - q) / 2 + z / 2.
-//   SiLU: z / (1 + 2^{-z log2 e}).
-// The hardware exp2 and reciprocal are accurate to about 1 ulp.
-// Activation code of a plain product (no activation), used by the backward.
-constexpr int kActNone = 2;
-
-template <int ACT>
-__device__ __forceinline__ float act_fast(float z) {
-  if constexpr (ACT == kActNone) {
-    return z;
-  } else if constexpr (ACT == LUFFY_ACT_GELU) {
-    // Hastings' erf(u) = 1 - t (a1 + a2 t + ... + a5 t^4) e^{-u^2},
-    // t = 1 / (1 + p u), u = |z| / sqrt(2), with the a_i halved here so
-    // that w = 1/2 - t e P(t) = erf(u) / 2.  Then z Phi(z) = |z| w + z / 2
-    // for either sign of z (Phi(z) = 1/2 + sign(z) erf(u) / 2): 10 vector
-    // operations and two transcendentals per element.
-    constexpr float kPs = 0.3275911f * 0.70710678118654752f;   // p / sqrt(2)
-    constexpr float kB1 = 0.5f * 0.254829592f, kB2 = 0.5f * -0.284496736f, kB3 = 0.5f * 1.421413741f;
-    constexpr float kB4 = 0.5f * -1.453152027f, kB5 = 0.5f * 1.061405429f;
-    constexpr float kHalfLog2e = -0.72134752044448170f;   // -log2(e) / 2
-    const float a = fabsf(z);
-    const float t = __builtin_amdgcn_rcpf(fmaf(kPs, a, 1.0f));
-    const float pt = fmaf(t, fmaf(t, fmaf(t, fmaf(t, kB5, kB4), kB3), kB2), kB1);
-    const float e = __builtin_amdgcn_exp2f(z * z * kHalfLog2e);   // e^{-u^2}
-    const float w = fmaf(-(t * e), pt, 0.5f);
-    return fmaf(a, w, 0.5f * z);
-  } else {
-    constexpr float kNegLog2e = -1.44269504088896341f;
-    return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * kNegLog2e));
-  }
-}
 
 // Derivative of the activation, with the approximations of act_fast (the
 // result is rounded to bf16): GELU'(z) = Phi(z) + z phi(z), Phi from the
@@ -618,7 +569,7 @@ __device__ __forceinline__ void store_block_f32(const f32x16& acc, int row0, int
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       z[q] = acc[4 * g + q];
-      if constexpr (FIRST) z[q] = act_fn<ACT>(z[q]);
+      if constexpr (FIRST) z[q] = act_f32<ACT>(z[q]);
     }
     *reinterpret_cast<float4*>(dst + 8 * g) = make_float4(z[0], z[1], z[2], z[3]);
   }
@@ -712,7 +663,7 @@ __global__ __launch_bounds__(GemmF32::THREADS, kF32Blocks) void ffn_kernel_f32(
         for (int q = 0; q < 4; ++q) {
           const float* p = part + (4 * w + q) * 64 + lane;
           z[q] = ((p[0] + p[16 * 64]) + p[32 * 64]) + p[48 * 64];
-          if constexpr (FIRST) z[q] = act_fn<ACT>(z[q]);
+          if constexpr (FIRST) z[q] = act_f32<ACT>(z[q]);
         }
         *reinterpret_cast<float4*>(out + static_cast<size_t>(r0 + (lane & 31)) * N + col0 + 8 * w + 4 * (lane >> 5)) =
             make_float4(z[0], z[1], z[2], z[3]);

@@ -127,11 +127,24 @@ __global__ __launch_bounds__(kQuantThreads) void mx4_dequantize_kernel(const uin
 // ------------------------------------------------------------- the product
 enum Mx4Out { kOutF32 = 0, kOutBf16 = 1, kOutMx4Gelu = 2, kOutMx4Silu = 3 };
 
-using Mx4Gemm = Mx4Core<128, 128, 2, 2, 3>;
+// Two tile shapes.  Four waves either way, two blocks a CU (one block's
+// epilogue under the other's products).  128 x 128 reads an operand half as
+// often as 128 x 64 does, which counts once the matrix cores are busy; with few
+// rows an expert most of its second 64 rows are empty, the weights are read
+// once in either shape, and three stages in flight beat two.  On 32 experts of
+// 2048 -> 4096 -> 2048 (FFN, us, 128 x 64 | 128 x 128): 500 rows 71 | 85, 1500
+// rows 97 | 99, 4000 rows 133 | 140, 6000 rows 163 | 157; one 4096 x 4096
+// matrix on 4096 rows 66 | 50.  256 x 256 (one block a CU) was 8 % faster
+// on 16384 rows of 4096 -> 11008, 10 % slower on 8192 rows of 4096 -> 8192 and
+// slower everywhere below, and was not kept.
+using Mx4Wide = Mx4Core<128, 128, 2, 2, 2>;
+using Mx4Narrow = Mx4Core<128, 64, 4, 1, 3>;
+constexpr int kNarrowRows = 96;   // average rows an expert up to which Mx4Narrow runs
 
 // Tile t of the grouped product -> expert, first row, rows, first column: the
-// tiles expert by expert (one expert's counts a lane), column tiles in groups
-// of 4 with the row tiles fastest inside a group.
+// tiles expert by expert (one expert's counts a lane), in blocks of 8 row tiles
+// by 4 column tiles, which an XCD's 32 CUs run together: 12 operand panels in
+// its L2 for 32 tiles.
 struct Mx4Tiles {
   int lo, hi, mt, incl, NT, tiles;
   __device__ __forceinline__ Mx4Tiles(const int32_t* __restrict__ offsets, int E, int M, int N, int bm, int bn) {
@@ -139,7 +152,7 @@ struct Mx4Tiles {
     NT = (N + bm - 1) / bm;
     lo = hi = 0;
     if (lane < E) {
-      lo = offsets ? min(offsets[lane], M) : 0;
+      lo = offsets ? min(max(offsets[lane], 0), M) : 0;
       hi = offsets ? min(offsets[lane + 1], M) : M;
     }
     mt = hi > lo ? (hi - lo + bn - 1) / bn : 0;
@@ -156,11 +169,12 @@ struct Mx4Tiles {
     e = __popcll(__ballot(lane < E && incl <= t));
     const int me = __shfl(mt, e, 64);
     const int r = t - (__shfl(incl, e, 64) - me * NT);
-    const int g = min(r / (4 * me), (NT + 3) / 4 - 1);
-    const int r2 = r - 4 * g * me;
-    row0 = __builtin_amdgcn_readfirstlane(__shfl(lo, e, 64) + r2 % me * bn);
+    const int g = min(r / (4 * me), (NT + 3) / 4 - 1), cols = min(4, NT - 4 * g);
+    const int r2 = r - 4 * g * me, rg = min(r2 / (8 * cols), (me + 7) / 8 - 1);
+    const int r3 = r2 - 8 * cols * rg, nr = min(8, me - 8 * rg);
+    row0 = __builtin_amdgcn_readfirstlane(__shfl(lo, e, 64) + (8 * rg + r3 % nr) * bn);
     rows = __builtin_amdgcn_readfirstlane(min(bn, __shfl(hi, e, 64) - row0));
-    n0 = __builtin_amdgcn_readfirstlane((4 * g + r2 / me) * bm);
+    n0 = __builtin_amdgcn_readfirstlane((4 * g + r3 / nr) * bm);
   }
 };
 
@@ -192,7 +206,7 @@ __device__ __forceinline__ void store_block(const f32x16& acc, bool valid, size_
     uint32_t most = 0;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      v[i] = act_f32<ACT>(acc[i]);
+      v[i] = act_fast<ACT>(acc[i]);
       most = max(most, abs_bits(v[i]));
     }
     most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), 32, 64)));
@@ -223,12 +237,11 @@ __device__ __forceinline__ void store_block(const f32x16& acc, bool valid, size_
   }
 }
 
-template <int OUT>
-__global__ __launch_bounds__(Mx4Gemm::THREADS) void mx4_product_kernel(
+template <class G, int OUT>
+__global__ __launch_bounds__(G::THREADS) void mx4_product_kernel(
     const uint8_t* __restrict__ xq, const uint8_t* __restrict__ xs, int M, const int32_t* __restrict__ offsets, int E,
     int N, int K, const uint8_t* __restrict__ wq, const uint8_t* __restrict__ ws, void* __restrict__ out,
     uint8_t* __restrict__ out_scale) {
-  using G = Mx4Gemm;
   __shared__ __attribute__((aligned(16))) uint8_t lds[G::LDS_BYTES];
   const Mx4Tiles map(offsets, E, M, N, G::BM, G::BN);
   const int t = xcd_virtual_block();
@@ -246,27 +259,38 @@ __global__ __launch_bounds__(Mx4Gemm::THREADS) void mx4_product_kernel(
   tile.ps_stage = static_cast<size_t>(N) * 8;
   tile.qs_stage = static_cast<size_t>(M) * 8;
   tile.kbytes = kbytes;
+  typename G::Pipe pipe;
+  G::prefetch(tile, pipe, lds);
+  const int lane = threadIdx.x & 63, w = G::wave(), wm = G::wave_m(w), wn = G::wave_n(w);
   typename G::Acc acc;
-  G::run(tile, lds, acc);
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, wm = w / G::WN, wn = w % G::WN;
+  G::zero(acc);
+  G::run_nq(G::active_q(wn, rows), tile, pipe, lds, acc);
 #pragma unroll
   for (int i = 0; i < G::FM; ++i)
 #pragma unroll
     for (int j = 0; j < G::FN; ++j) {
-      const int n = n0 + wm * G::WTM + 32 * i, r = wn * G::WTN + 32 * j + (lane & 31);
+      const int n = n0 + wm * G::WTM + 32 * i, r = G::q_row(wn, j) + (lane & 31);
       if (n < N) store_block<OUT>(acc[i][j], r < rows, static_cast<size_t>(row0) + r, M, n, N, out, out_scale);
     }
+}
+
+template <class G, int OUT>
+void launch_shape(const char* name, const uint8_t* xq, const uint8_t* xs, int M, const int32_t* offsets, int E, int N,
+                  int K, const uint8_t* wq, const uint8_t* ws, void* out, uint8_t* out_scale, hipStream_t s) {
+  // every expert may add one partial row tile
+  const long long row_tiles = (M + G::BN - 1) / G::BN + (offsets ? E - 1 : 0);
+  const long long tiles = row_tiles * ((N + G::BM - 1) / G::BM);
+  launch(name, mx4_product_kernel<G, OUT>, static_cast<int>((tiles + 7) / 8 * 8), G::THREADS, 0, s, xq, xs, M, offsets,
+         E, N, K, wq, ws, out, out_scale);
 }
 
 template <int OUT>
 void launch_product(const char* name, const uint8_t* xq, const uint8_t* xs, int M, const int32_t* offsets, int E,
                     int N, int K, const uint8_t* wq, const uint8_t* ws, void* out, uint8_t* out_scale, hipStream_t s) {
-  using G = Mx4Gemm;
-  // every expert may add one partial row tile
-  const long long row_tiles = (M + G::BN - 1) / G::BN + (offsets ? E - 1 : 0);
-  const long long tiles = row_tiles * ((N + G::BM - 1) / G::BM);
-  launch(name, mx4_product_kernel<OUT>, static_cast<int>((tiles + 7) / 8 * 8), G::THREADS, 0, s, xq, xs, M, offsets, E,
-         N, K, wq, ws, out, out_scale);
+  if (M <= kNarrowRows * E)
+    launch_shape<Mx4Narrow, OUT>(name, xq, xs, M, offsets, E, N, K, wq, ws, out, out_scale, s);
+  else
+    launch_shape<Mx4Wide, OUT>(name, xq, xs, M, offsets, E, N, K, wq, ws, out, out_scale, s);
 }
 
 void launch_quantize(const void* x, const int32_t* row_index, const int32_t* count, int rows, long long total_rows,

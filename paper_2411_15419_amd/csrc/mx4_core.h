@@ -125,71 +125,208 @@ struct Mx4Core {
     }
   }
 
-  template <int STEP>
-  static __device__ __forceinline__ void step(lds_ptr prow, lds_ptr qrow, int half, int sw, const int (&sa)[FM],
-                                              const int (&sb)[FN], Acc& acc) {
-    const int at = ((4 * half + STEP) ^ sw) * 16;
-    i32x4 a[FM], b[FN];
-#pragma unroll
-    for (int i = 0; i < FM; ++i)
-      a[i] = *reinterpret_cast<const __attribute__((address_space(3))) i32x4*>(prow + 32 * i * 128 + at);
-#pragma unroll
-    for (int j = 0; j < FN; ++j)
-      b[j] = *reinterpret_cast<const __attribute__((address_space(3))) i32x4*>(qrow + 32 * j * 128 + at);
-#pragma unroll
-    for (int i = 0; i < FM; ++i)
-#pragma unroll
-      for (int j = 0; j < FN; ++j) acc[i][j] = mfma32x32x64_f4<STEP>(a[i], b[j], acc[i][j], sa[i], sb[j]);
+  // Wave w: P rows wave_m(w) WTM.., Q blocks of 32 rows wave_n(w), wave_n(w) +
+  // WN, ... (a tile with few Q rows keeps every wave equally busy: active_q).
+  static __device__ __forceinline__ int wave_m(int w) { return w % WM; }
+  static __device__ __forceinline__ int wave_n(int w) { return w / WM; }
+  static __device__ __forceinline__ int q_row(int wn, int fn) { return 32 * (wn + WN * fn); }
+  static __device__ __forceinline__ int active_q(int wn, int rows) {
+    return min(max((rows - 32 * wn + 32 * WN - 1) / (32 * WN), 0), FN);
   }
 
-  // The whole product of a tile.  Result layout: acc[i][j][v] of lane l of wave
-  // w is P row (w / WN) WTM + 32 i + 8 (v / 4) + 4 (l / 32) + v % 4 and Q row
-  // (w % WN) WTN + 32 j + l % 32.  Ends with a barrier after which the LDS may
-  // be used again.
-  static __device__ __forceinline__ void run(const Tile& t, uint8_t* lds_generic, Acc& acc) {
+  struct Frags {
+    i32x4 a[FM], b[FN];
+  };
+  struct Scales {
+    int a[FM], b[FN];
+  };
+  struct Addr {
+    int prow, qrow, half, sw, ps, qs;   // fragment rows and scales in a stage
+  };
+  static __device__ __forceinline__ Addr addr(int wm, int wn) {
+    const int lane = opaque_tid() & 63;
+    Addr a;
+    a.half = lane >> 5;
+    a.sw = swz(lane & 31);
+    a.prow = (wm * WTM + (lane & 31)) * 128;
+    a.qrow = BM * 128 + (32 * wn + (lane & 31)) * 128;
+    a.ps = SCALE_AT + (wm * WTM + (lane & 31)) * 8 + 4 * a.half;
+    a.qs = SCALE_Q_AT + (32 * wn + (lane & 31)) * 8 + 4 * a.half;
+    return a;
+  }
+  // fragments of step `step` of the stage at st, first NQ Q blocks
+  template <int NQ>
+  static __device__ __forceinline__ void read_step(lds_ptr st, const Addr& ad, int step, Frags& f) {
+    const int at = ((4 * ad.half + step) ^ ad.sw) * 16;
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+      f.a[i] = *reinterpret_cast<const __attribute__((address_space(3))) i32x4*>(st + ad.prow + 32 * i * 128 + at);
+#pragma unroll
+    for (int j = 0; j < NQ; ++j)
+      f.b[j] = *reinterpret_cast<const __attribute__((address_space(3))) i32x4*>(st + ad.qrow + 32 * WN * j * 128 + at);
+  }
+  template <int NQ>
+  static __device__ __forceinline__ void read_scales(lds_ptr st, const Addr& ad, Scales& s) {
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+      s.a[i] = *reinterpret_cast<const __attribute__((address_space(3))) int*>(st + ad.ps + 32 * i * 8);
+#pragma unroll
+    for (int j = 0; j < NQ; ++j)
+      s.b[j] = *reinterpret_cast<const __attribute__((address_space(3))) int*>(st + ad.qs + 32 * WN * j * 8);
+  }
+  template <int NQ, int STEP>
+  static __device__ __forceinline__ void mma_step(const Frags& f, const Scales& s, Acc& acc) {
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < NQ; ++j) acc[i][j] = mfma32x32x64_f4<STEP>(f.a[i], f.b[j], acc[i][j], s.a[i], s.b[j]);
+  }
+
+  // Instruction order of a step: the next step's LDS reads two after an MFMA
+  // from the first on, so they have landed when the next step starts.
+  template <int NQ>
+  static __device__ __forceinline__ void interleave_reads() {
+    constexpr int NMF = FM * NQ, NDS = FM + NQ;
+#pragma unroll
+    for (int i = 0; i < NMF; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);   // MFMA
+      if (2 * i + 1 < NDS) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);   // DS read
+      else if (2 * i < NDS) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    if constexpr (NDS > 2 * NMF) __builtin_amdgcn_sched_group_barrier(0x100, NDS - 2 * NMF, 0);
+  }
+  // The step after the barrier: the next stage's DMA goes out first, one after
+  // an MFMA; then the reads (fragments and scales).
+  template <int NQ>
+  static __device__ __forceinline__ void interleave_loads() {
+    constexpr int NMF = FM * NQ, NDS = 2 * (FM + NQ);
+    constexpr int PV = NMF < LOADS ? NMF : LOADS;
+#pragma unroll
+    for (int i = 0; i < PV; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);   // MFMA
+      __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);   // VMEM read
+    }
+    if constexpr (NMF > PV) __builtin_amdgcn_sched_group_barrier(0x008, NMF - PV, 0);
+    if constexpr (LOADS > PV) __builtin_amdgcn_sched_group_barrier(0x020, LOADS - PV, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, NDS, 0);
+  }
+
+  // waits until at most n stages of this wave's DMA are outstanding
+  static __device__ __forceinline__ void wait_stages(int n) {
+    if constexpr (STAGES > 3) {
+      if (n >= 2) { wait_vmcnt<2 * LOADS>(); return; }
+    }
+    if (n >= 1) wait_vmcnt<LOADS>();
+    else wait_vmcnt<0>();
+  }
+
+  template <int NQ>
+  static __device__ __forceinline__ void stage_steps(lds_ptr cur, const Addr& ad, const Scales& sc, Frags (&f)[2],
+                                                     Acc& acc, bool sched) {
+    if (sched) __builtin_amdgcn_sched_barrier(0);
+    read_step<NQ>(cur, ad, 1, f[1]);
+    mma_step<NQ, 0>(f[0], sc, acc);
+    if (sched) interleave_reads<NQ>();
+    if (sched) __builtin_amdgcn_sched_barrier(0);
+    read_step<NQ>(cur, ad, 2, f[0]);
+    mma_step<NQ, 1>(f[1], sc, acc);
+    if (sched) interleave_reads<NQ>();
+    if (sched) __builtin_amdgcn_sched_barrier(0);
+    read_step<NQ>(cur, ad, 3, f[1]);
+    mma_step<NQ, 2>(f[0], sc, acc);
+    if (sched) interleave_reads<NQ>();
+  }
+
+  // Issues the first stages of a tile.
+  static __device__ __forceinline__ void prefetch(const Tile& t, Pipe& s, uint8_t* lds_generic) {
     const lds_ptr lds = (lds_ptr)lds_generic;
-    const int lane = opaque_tid() & 63, w = wave(), wm = w / WN, wn = w % WN;
-    Pipe s;
     setup(t, s);
     const int nk = __builtin_amdgcn_readfirstlane((t.kbytes + 127) / 128);
+#pragma unroll
+    for (int k = 0; k < STAGES; ++k)
+      if (k < nk) issue(t, s, k, lds + k * STAGE_BYTES);
+  }
+
+  // The product of a tile whose first stages are on their way; the wave
+  // multiplies its first NQ Q blocks, but takes part in every load and barrier.
+  // Result layout: acc[i][j][v] of lane l of wave w is P row wave_m(w) WTM +
+  // 32 i + 8 (v / 4) + 4 (l / 32) + v % 4 and Q row q_row(wave_n(w), j) +
+  // l % 32.  Ends with a barrier after which the LDS may be used again.
+  //
+  // Fragments are double-buffered a step: while the MFMAs of step s run, step
+  // s + 1 is read; after the last read of a stage every wave waits for the next
+  // stage's DMA, one barrier frees the stage's buffer, and the DMA of the stage
+  // after the ring goes into it under the last step's MFMAs.
+  template <int NQ>
+  static __device__ __forceinline__ void run(const Tile& t, const Pipe& s, uint8_t* lds_generic, Acc& acc) {
+    const lds_ptr lds = (lds_ptr)lds_generic;
+    const int w = wave();
+    const int nk = __builtin_amdgcn_readfirstlane((t.kbytes + 127) / 128);
+    wait_stages(min(nk, STAGES) - 1);
+    raw_barrier();
+    const Addr ad = addr(wave_m(w), wave_n(w));
+    Frags f[2];
+    Scales sc;
+    read_scales<NQ>(lds, ad, sc);
+    read_step<NQ>(lds, ad, 0, f[0]);
+    int kt = 0, cb = 0;
+    // steady state: stage kt + STAGES exists
+    for (; kt + STAGES < nk; ++kt) {
+      const lds_ptr cur = lds + cb * STAGE_BYTES;
+      cb = cb + 1 == STAGES ? 0 : cb + 1;
+      const lds_ptr nxt = lds + cb * STAGE_BYTES;
+      stage_steps<NQ>(cur, ad, sc, f, acc, true);
+      __builtin_amdgcn_sched_barrier(0);
+      wait_vmcnt<(STAGES - 2) * LOADS>();   // stage kt + 1 has landed (this wave's part)
+      __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0): own reads of stage kt are done
+      raw_barrier();
+      __builtin_amdgcn_sched_barrier(0);
+      issue(t, s, kt + STAGES, cur);
+      Scales ns;
+      read_scales<NQ>(nxt, ad, ns);
+      read_step<NQ>(nxt, ad, 0, f[0]);
+      mma_step<NQ, 3>(f[1], sc, acc);
+      interleave_loads<NQ>();
+      __builtin_amdgcn_sched_barrier(0);
+      sc = ns;
+    }
+    for (; kt < nk; ++kt) {
+      const lds_ptr cur = lds + cb * STAGE_BYTES;
+      cb = cb + 1 == STAGES ? 0 : cb + 1;
+      stage_steps<NQ>(cur, ad, sc, f, acc, false);
+      Scales ns = sc;
+      if (kt + 1 < nk) {
+        wait_stages(nk - 2 - kt);
+        __builtin_amdgcn_s_waitcnt(0xC07F);
+        raw_barrier();
+        read_scales<NQ>(lds + cb * STAGE_BYTES, ad, ns);
+        read_step<NQ>(lds + cb * STAGE_BYTES, ad, 0, f[0]);
+      }
+      mma_step<NQ, 3>(f[1], sc, acc);
+      sc = ns;
+    }
+    __syncthreads();
+  }
+
+  static __device__ __forceinline__ void zero(Acc& acc) {
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
       for (int j = 0; j < FN; ++j)
 #pragma unroll
         for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
-#pragma unroll
-    for (int k = 0; k < STAGES - 1; ++k)
-      if (k < nk) issue(t, s, k, lds + k * STAGE_BYTES);
-    const int half = lane >> 5, sw = swz(lane & 31);
-    const int prow = (wm * WTM + (lane & 31)) * 128, qrow = BM * 128 + (wn * WTN + (lane & 31)) * 128;
-    const int psc = SCALE_AT + (wm * WTM + (lane & 31)) * 8 + 4 * half;
-    const int qsc = SCALE_Q_AT + (wn * WTN + (lane & 31)) * 8 + 4 * half;
-    int buf = 0;
-    for (int kt = 0; kt < nk; ++kt) {
-      // stage kt has landed (this wave's part); then every wave's, and every
-      // wave is done with the buffer of stage kt - 1
-      if (kt + STAGES - 2 < nk) wait_vmcnt<(STAGES - 2) * LOADS>();
-      else wait_vmcnt<0>();
-      __builtin_amdgcn_s_waitcnt(0xC07F);
-      raw_barrier();
-      const int free_buf = buf == 0 ? STAGES - 1 : buf - 1;
-      if (kt + STAGES - 1 < nk) issue(t, s, kt + STAGES - 1, lds + free_buf * STAGE_BYTES);
-      const lds_ptr st = lds + buf * STAGE_BYTES;
-      int sa[FM], sb[FN];
-#pragma unroll
-      for (int i = 0; i < FM; ++i)
-        sa[i] = *reinterpret_cast<const __attribute__((address_space(3))) int*>(st + psc + 32 * 8 * i);
-#pragma unroll
-      for (int j = 0; j < FN; ++j)
-        sb[j] = *reinterpret_cast<const __attribute__((address_space(3))) int*>(st + qsc + 32 * 8 * j);
-      step<0>(st + prow, st + qrow, half, sw, sa, sb, acc);
-      step<1>(st + prow, st + qrow, half, sw, sa, sb, acc);
-      step<2>(st + prow, st + qrow, half, sw, sa, sb, acc);
-      step<3>(st + prow, st + qrow, half, sw, sa, sb, acc);
-      buf = buf + 1 == STAGES ? 0 : buf + 1;
+  }
+
+  // prefetch() and run() with the number of Q blocks that hold a valid row
+  // (a wave without one: no MFMAs).
+  template <int N = FN>
+  static __device__ __forceinline__ void run_nq(int nq, const Tile& t, const Pipe& s, uint8_t* lds, Acc& acc) {
+    if constexpr (N == 0) {
+      run<0>(t, s, lds, acc);
+    } else {
+      if (nq >= N) run<N>(t, s, lds, acc);
+      else run_nq<N - 1>(nq, t, s, lds, acc);
     }
-    __syncthreads();
   }
 };
 
