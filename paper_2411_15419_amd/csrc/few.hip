@@ -6,8 +6,9 @@
 // are small beside them.
 //
 // Three launches: few_gate_kernel (a block a token: logits in float64, top-k,
-// gates), few_product_kernel<.., false> (hidden rows) and <.., true> (second
-// product, whose last block of each row group adds the tokens' experts).
+// gates), the hidden rows, and the second product, which also adds the tokens'
+// experts; the products by few_product_kernel, or by few_direct_kernel for the
+// fewest tokens.
 #include <algorithm>
 
 #include "act.h"
@@ -20,6 +21,7 @@ namespace {
 constexpr int kFewTokens = LUFFY_FEW_MAX_TOKENS;
 constexpr int kGateThreads = 1024;
 constexpr int kFewWaves = 8, kFewThreads = 64 * kFewWaves;
+constexpr int kDirectSlots = 8;   // up to which few_direct_kernel runs
 
 enum FewWeights { kF32 = 0, kBf16 = 1, kMx4 = 2 };
 
@@ -450,6 +452,39 @@ __device__ __forceinline__ void few_load_scales(const FewArgs& a, const uint8_t*
   lds_dma<16>(few_rsrc(s), p + u < p1 ? off : kFewRange, p < p1 ? (p * a.N + row) * 8 : 0, dst);
 }
 
+// Values a thread finishes at a time: 4-bit weights' hidden rows are rounded
+// eight at a time, everything else goes out in pairs (more threads at work).
+template <int WT, bool SECOND>
+constexpr int kFewValues = WT == kMx4 && !SECOND ? 8 : 2;
+
+// Hidden values n, n + 1, ... of slot s from their sums z.
+template <int WT>
+__device__ __forceinline__ void few_store_hidden(const FewArgs& a, int act, int s, int n, bool valid,
+                                                 float (&z)[kFewValues<WT, false>]) {
+#pragma unroll
+  for (int i = 0; i < kFewValues<WT, false>; ++i)
+    z[i] = act == LUFFY_ACT_GELU ? act_f32<LUFFY_ACT_GELU>(z[i]) : act_f32<LUFFY_ACT_SILU>(z[i]);
+  uint8_t* dst = a.h + static_cast<size_t>(s) * few_pitch<WT, true>(a.N);
+  if constexpr (WT == kMx4) {
+    // (a block's four lanes agree on valid: a block of waves has a multiple of
+    // 32 rows and N is one of 64)
+    if (valid) store_e4m3<3>(z, n / 8, dst, a.h_scale + static_cast<size_t>(s) * few_scale_pitch(a.N));
+  } else if (valid) {
+    if constexpr (WT == kF32) {
+      *reinterpret_cast<float2*>(dst + n * 4) = make_float2(z[0], z[1]);
+    } else {
+      const uint32_t hi = pack_bf16x2(z[0], z[1]);
+      float r0 = z[0] - __uint_as_float(hi << 16), r1 = z[1] - __uint_as_float(hi & 0xFFFF0000u);
+      // an infinite or NaN value is all in its first part
+      if (!(fabsf(r0) < HUGE_VALF)) r0 = 0.f;
+      if (!(fabsf(r1) < HUGE_VALF)) r1 = 0.f;
+      uint8_t* f = dst + (n >> 6) * 256 + (n & 63) * 2;
+      *reinterpret_cast<uint32_t*>(f) = hi;
+      *reinterpret_cast<uint32_t*>(f + 128) = pack_bf16x2(r0, r1);
+    }
+  }
+}
+
 // What the column buffers hold, and where the next chunk goes (block-uniform).
 struct FewStage {
   int half;        // of the current chunk
@@ -637,9 +672,7 @@ __device__ __forceinline__ void few_run(const FewArgs& a, FewLds<NBMAX, RT>& m, 
               acc[i][b][v] + other;
       }
   lds_barrier();
-  // V rows of a column a thread: 4-bit weights' hidden rows are rounded eight at
-  // a time, everything else goes out in pairs (more threads at work)
-  constexpr int V = WT == kMx4 && !SECOND ? 8 : 2;
+  constexpr int V = kFewValues<WT, SECOND>;
   const int n0 = t.group * rows, units_log2 = __builtin_ctz(rows) - __builtin_ctz(V);
   const int stride = NB * 8 * rows;
 #pragma unroll 1
@@ -661,27 +694,7 @@ __device__ __forceinline__ void few_run(const FewArgs& a, FewLds<NBMAX, RT>& m, 
         __hip_atomic_store(reinterpret_cast<uint64_t*>(a.part + static_cast<size_t>(s) * a.N + n), v,
                            __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     } else {
-#pragma unroll
-      for (int i = 0; i < V; ++i)
-        z[i] = act == LUFFY_ACT_GELU ? act_f32<LUFFY_ACT_GELU>(z[i]) : act_f32<LUFFY_ACT_SILU>(z[i]);
-      uint8_t* dst = a.h + static_cast<size_t>(s) * few_pitch<WT, true>(a.N);
-      if constexpr (WT == kMx4) {
-        // (rows is a multiple of 32 and N of 64: a block's four lanes agree)
-        if (valid) store_e4m3<3>(z, n / 8, dst, a.h_scale + static_cast<size_t>(s) * few_scale_pitch(a.N));
-      } else if (valid) {
-        if constexpr (WT == kF32) {
-          *reinterpret_cast<float2*>(dst + n * 4) = make_float2(z[0], z[1]);
-        } else {
-          const uint32_t hi = pack_bf16x2(z[0], z[1]);
-          float r0 = z[0] - __uint_as_float(hi << 16), r1 = z[1] - __uint_as_float(hi & 0xFFFF0000u);
-          // an infinite or NaN value is all in its first part
-          if (!(fabsf(r0) < HUGE_VALF)) r0 = 0.f;
-          if (!(fabsf(r1) < HUGE_VALF)) r1 = 0.f;
-          uint8_t* f = dst + (n >> 6) * 256 + (n & 63) * 2;
-          *reinterpret_cast<uint32_t*>(f) = hi;
-          *reinterpret_cast<uint32_t*>(f + 128) = pack_bf16x2(r0, r1);
-        }
-      }
+      few_store_hidden<WT>(a, act, s, n, valid, z);
     }
   }
 }
@@ -774,6 +787,180 @@ __global__ __launch_bounds__(kFewThreads, NBMAX == 1 ? 4 : 2) void few_product_k
   }
 }
 
+// Up to eight slots (tokens times choices): the same products and sums, bit for
+// bit, with nothing before the first load of weights that can be left out.  With
+// so few columns latency is all there is, so a block has one item (second
+// product: the same rows of every expert, one after the other, so that it can
+// add a token's experts itself), its columns come straight into registers, and
+// no list is built: lane s knows slot s's expert and which slots share it.
+// Seven tokens on 4 experts of 256 x 1024 (float32): 13.4 and 16.3 us by the
+// kernel above, 8.8 and 10.3 here; one token on two of 1024 x 4096 (bf16): 12.8
+// and 15.3, 10.2 and 13.2; on one of 4096 x 11008 (4 bits), second: 19.8, 15.4.
+template <int WT, int RT, bool SECOND>
+struct DirectStep {
+  static constexpr int BL = FewLayout<WT, SECOND>::BL, U = BL == 1 ? 4 : (BL <= 4 ? 2 : 1);   // pieces of K
+  u32x4 w[U][RT], col[U][BL];
+  int sw[U][RT], sc[U];
+};
+
+template <int WT, int RT, bool SECOND>
+__global__ __launch_bounds__(SECOND ? 2 * kFewThreads : kFewThreads, 4) void few_direct_kernel(const FewArgs a, int act) {
+  using Step = DirectStep<WT, RT, SECOND>;
+  constexpr int U = Step::U, BL = Step::BL, V = kFewValues<WT, SECOND>;
+  __shared__ float red[kDirectSlots * 8 * RT * kFewWaves];   // [part][slot][row]
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int w = wave % kFewWaves;
+  const int slots = a.T * a.k, lr = lane & 7, lc = lane >> 3;
+  const int es = lane < slots ? a.topk_idx[lane] : -1;
+  uint32_t same = 0;
+#pragma unroll
+  for (int j = 0; j < kDirectSlots; ++j) {
+    const uint32_t m = static_cast<uint32_t>(__ballot(lane < slots && es == __builtin_amdgcn_readlane(es, j)));
+    if (lane == j) same = m;
+  }
+  // the first slot of every expert in use
+  uint32_t todo = static_cast<uint32_t>(__ballot(lane < slots && __builtin_ctz(same | 1u << 31) == lane));
+  int group = blockIdx.x;
+  if constexpr (!SECOND) {
+    const int rank = blockIdx.x / a.groups;
+    group -= rank * a.groups;
+    for (int r = 0; r < rank; ++r) todo &= todo - 1;
+    if (todo == 0) return;
+    todo &= -todo;
+  }
+  const int kbytes = few_kbytes<WT>(a.K), pieces = (kbytes + 127) / 128, split_log2 = __builtin_ctz(a.split);
+  const int part = w & (a.split - 1), rows = 8 * RT * kFewWaves >> split_log2, in_block = (w >> split_log2) * (8 * RT);
+  const uint32_t row = group * rows + in_block;
+  const int p0 = (part * pieces) >> split_log2;
+  const int p1 = static_cast<int>(row) < a.N ? ((part + 1) * pieces) >> split_log2 : p0;
+  const int steps = (((pieces + a.split - 1) >> split_log2) + U - 1) / U;   // of the longest part
+  const int pitch = few_pitch<WT, SECOND>(a.K), scale_pitch = few_scale_pitch(a.K);
+  const __amdgpu_buffer_rsrc_t in = few_rsrc(a.in), ins = few_rsrc(WT == kMx4 ? a.in_scale : a.in);
+  // the slot of this lane's column under a mask of slots (those past the last
+  // repeat it; their products are not used)
+  auto slot_of = [&](uint32_t mask) {
+    for (int i = 0; i < lr; ++i)
+      if (mask & (mask - 1)) mask &= mask - 1;
+    return __builtin_ctz(mask);
+  };
+  // what does not exist is not fetched and reads as zeros
+  auto load = [&](int e, uint32_t mask, int step, bool on, Step& s) {
+    const __amdgpu_buffer_rsrc_t wr = few_rsrc(a.w + static_cast<size_t>(e) * a.N * kbytes);
+    const int slot = slot_of(mask);
+    const uint32_t column = SECOND || a.k == 1 ? slot : slot >> 1;
+    const int first = p0 + step * U;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int p = first + u;
+      const bool here = on && p < p1 && p * 128 + 16 * lc < kbytes;
+#pragma unroll
+      for (int i = 0; i < RT; ++i)
+        s.w[u][i] = __builtin_amdgcn_raw_buffer_load_b128(
+            wr, here ? (row + 8 * i + lr) * kbytes + p * 128 + 16 * lc : kFewRange, 0, 2);
+    }
+    if constexpr (WT == kMx4) {
+      const __amdgpu_buffer_rsrc_t sr = few_rsrc(a.w_scale + static_cast<size_t>(e) * pieces * a.N * 8);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int p = first + u;
+        const bool here = on && p < p1;
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+          s.sw[u][i] = __builtin_amdgcn_raw_buffer_load_b8(
+              sr, here ? (p * a.N + row + 8 * i + lr) * 8 + lc : kFewRange, 0, 0);
+        s.sc[u] = __builtin_amdgcn_raw_buffer_load_b8(ins, here ? column * scale_pitch + p * 8 + lc : kFewRange, 0, 0);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int p = first + u;
+#pragma unroll
+      for (int j = 0; j < BL; ++j)
+        s.col[u][j] = __builtin_amdgcn_raw_buffer_load_b128(
+            in, on && p < p1 ? column * pitch + (p * BL + j) * 128 + 16 * lc : kFewRange, 0, 0);
+    }
+  };
+  // second product: a block of 16 waves takes two experts at a time
+  const int teams = SECOND ? blockDim.x / kFewThreads : 1;
+  if (SECOND && wave >= kFewWaves) todo &= todo - 1;
+  int step = 0, first = todo ? __builtin_ctz(todo) : 0;
+  uint32_t mask = __builtin_amdgcn_readlane(same, first);
+  Step cur;
+  load(__builtin_amdgcn_readlane(es, first), mask, 0, todo != 0, cur);
+  f32x4 acc[RT];
+#pragma unroll
+  for (int i = 0; i < RT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  while (todo) {
+    const uint32_t at = mask;
+    const bool last = ++step == steps;   // of this expert
+    if (last) {
+      step = 0;
+      todo &= todo - 1;
+      if (teams > 1) todo &= todo - 1;
+    }
+    const bool more = todo != 0;
+    if (more) first = __builtin_ctz(todo);
+    mask = __builtin_amdgcn_readlane(same, first);
+    Step next;
+    load(__builtin_amdgcn_readlane(es, first), mask, step, more, next);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < RT; ++i)
+        few_mma<WT, BL>(cur.w[u][i], WT == kMx4 ? cur.sw[u][i] : 0, cur.col[u], WT == kMx4 ? cur.sc[u] : 0, acc[i]);
+    if (last) {
+      const int slot = slot_of(at), n = __builtin_popcount(at);
+#pragma unroll
+      for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const float other = __shfl(acc[i][v], (lane + 40) & 63, 64);
+          if ((lane & 8) == 0 && lane < 32 && lr < n)
+            red[(part * kDirectSlots + slot) * rows + in_block + 8 * i + 4 * (lane >> 4) + v] = acc[i][v] + other;
+          acc[i][v] = 0.f;
+        }
+    }
+    cur = next;
+  }
+  __syncthreads();
+  const int units = rows / V;
+  auto sums = [&](int slot, int col, float (&z)[V]) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) z[i] = 0.f;
+    for (int q = 0; q < a.split; ++q)
+#pragma unroll
+      for (int i = 0; i < V; ++i) z[i] += red[(q * kDirectSlots + slot) * rows + col + i];
+  };
+  for (int o = tid; o < (SECOND ? a.T : slots) * units; o += blockDim.x) {
+    const int s = o / units, col = (o - s * units) * V, n = group * rows + col;
+    const bool valid = n < a.N;
+    if constexpr (SECOND) {
+#pragma clang fp contract(off)   // each expert's part is rounded, as where they are added from memory
+      float y[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) y[i] = 0.f;
+      for (int j = 0; j < a.k; ++j) {
+        float z[V];
+        sums(s * a.k + j, col, z);
+        const float g = a.topk_gate[s * a.k + j];
+#pragma unroll
+        for (int i = 0; i < V; ++i) y[i] = j == 0 ? z[i] * g : y[i] + z[i] * g;
+      }
+      if (!valid) continue;
+      if constexpr (WT == kF32)
+        *reinterpret_cast<float2*>(static_cast<float*>(a.y) + static_cast<size_t>(s) * a.N + n) = make_float2(y[0], y[1]);
+      else
+        *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.y) + static_cast<size_t>(s) * a.N + n) =
+            pack_bf16x2(y[0], y[1]);
+    } else {
+      if (!(mask >> s & 1)) continue;
+      float z[V];
+      sums(s, col, z);
+      few_store_hidden<WT>(a, act, s, n, valid, z);
+    }
+  }
+}
+
 struct FewWs {
   FewTerms f;
   uint8_t* h;      // hidden rows
@@ -826,10 +1013,22 @@ void launch_few(FewArgs a, int E, int act, hipStream_t s) {
   constexpr int kRows = 8 * 2 * kFewWaves;
   a.split = 1;
   while (a.split < kFewWaves && used * ((a.N * a.split + kRows - 1) / kRows) < persistent_grid()) a.split *= 2;
-#ifdef FEW_SPLIT1
-  a.split = SECOND ? FEW_SPLIT2 : FEW_SPLIT1;
-#endif
   if (WT == kMx4 && !SECOND) a.split = std::min(a.split, 4);   // whole blocks of 32 hidden values
+  const int slots = a.T * a.k;
+  bool direct = slots <= kDirectSlots;
+  // (4-bit tokens, four units a piece: 17.9 us against 14.9 through LDS for one
+  // token of 4096 -> 11008)
+  if constexpr (WT == kMx4 && !SECOND) direct = false;
+  else if (direct) {
+    // half the rows a wave where a block a CU needs it
+    const int experts = SECOND ? 1 : std::min(slots, E), threads = SECOND && slots > 1 ? 2 * kFewThreads : kFewThreads;
+    const bool half = static_cast<long long>(a.N) * a.split * experts < static_cast<long long>(kRows) * persistent_grid();
+    const int rows = (half ? kRows / 2 : kRows) / a.split;
+    a.groups = (a.N + rows - 1) / rows;
+    launch(SECOND ? "few_ffn2" : "few_ffn1", half ? few_direct_kernel<WT, 1, SECOND> : few_direct_kernel<WT, 2, SECOND>,
+           a.groups * experts, threads, 0, s, a, act);
+  }
+  if (direct) return;
   if (a.T <= 8) launch_few_nb<WT, 1, SECOND>(a, act, s);
   else launch_few_nb<WT, 8, SECOND>(a, act, s);
 }
@@ -838,10 +1037,11 @@ template <int WT>
 void run_few(const void* x, int T, int d, const void* w_gate, const float* b_gate, int E, int k, const void* w1,
              const void* s1, const void* w2, const void* s2, int d_ff, int act, int32_t* topk_idx,
              float* topk_gate, void* y, const FewWs& ws, hipStream_t s) {
+  const bool direct = T * k <= kDirectSlots;
   FewTerms f = ws.f;
   if (WT != kMx4) f.x8 = nullptr;
   launch("few_gate", few_gate_kernel<WT == kF32>, T, kGateThreads, 0, s, x, d, w_gate, b_gate, E, k, topk_idx,
-         topk_gate, f, ws.done, d / 8);
+         topk_gate, f, ws.done, direct ? 0 : d / 8);
   FewArgs a = {};
   a.T = T;
   a.k = k;
