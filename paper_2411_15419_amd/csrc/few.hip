@@ -21,7 +21,7 @@ namespace {
 constexpr int kFewTokens = LUFFY_FEW_MAX_TOKENS;
 constexpr int kGateThreads = 1024;
 constexpr int kFewWaves = 8, kFewThreads = 64 * kFewWaves;
-constexpr int kDirectSlots = 8;   // up to which few_direct_kernel runs
+constexpr int kDirectSlots = 8;   // few_direct_kernel's most
 
 enum FewWeights { kF32 = 0, kBf16 = 1, kMx4 = 2 };
 
@@ -36,7 +36,7 @@ enum FewWeights { kF32 = 0, kBf16 = 1, kMx4 = 2 };
 //                     leave, at 2^-4t of the scale.  Two terms hold a bf16 token
 //                     exactly (but for values below 2^-13 of their block's
 //                     largest, to 2^-21 of it), three hold a hidden value to
-//                     2^-13 of itself or 2^-25 of its block's largest.  So the
+//                     2^-12 of itself or 2^-25 of its block's largest.  So the
 //                     weights' codes go to the block-scaled MFMA as they are,
 //                     without a conversion to bf16 for every value.
 template <int WT, bool SECOND>
@@ -380,7 +380,7 @@ struct FewItem {
 };
 
 template <int WT>
-__device__ __forceinline__ int few_kbytes(int K) { return WT == kF32 ? K * 4 : (WT == kBf16 ? K * 2 : K / 2); }
+__host__ __device__ __forceinline__ int few_kbytes(int K) { return WT == kF32 ? K * 4 : (WT == kBf16 ? K * 2 : K / 2); }
 
 constexpr uint32_t kFewRange = 0xFFFF0000u;   // an expert's matrix is smaller (checked on the host)
 
@@ -1014,10 +1014,16 @@ void launch_few(FewArgs a, int E, int act, hipStream_t s) {
   a.split = 1;
   while (a.split < kFewWaves && used * ((a.N * a.split + kRows - 1) / kRows) < persistent_grid()) a.split *= 2;
   if (WT == kMx4 && !SECOND) a.split = std::min(a.split, 4);   // whole blocks of 32 hidden values
-  const int slots = a.T * a.k;
-  bool direct = slots <= kDirectSlots;
+  // Without LDS columns: up to two slots, or eight on experts of 32 MB together
+  // (the second product takes a block's experts one after the other).  Whole
+  // calls, us, few_product_kernel | few_direct_kernel: bf16, 1024 x 4096 of 16,
+  // k = 2, one token 29.1 | 25.2, two 32.4 | 32.0, four (56 MB) 37.6 | 45.3; 4096
+  // x 11008 of 8, k = 2, three tokens 191 | 250; float32, 256 x 1024 of 4, seven
+  // tokens 28.6 | 20.7, 1024 x 1024 of 4, eight (17 MB) 32.2 | 22.3.
   // (4-bit tokens, four units a piece: 17.9 us against 14.9 through LDS for one
   // token of 4096 -> 11008)
+  const int slots = a.T * a.k;
+  bool direct = slots <= 2 || (slots <= kDirectSlots && used * a.N * few_kbytes<WT>(a.K) <= 32e6);
   if constexpr (WT == kMx4 && !SECOND) direct = false;
   else if (direct) {
     // half the rows a wave where a block a CU needs it
@@ -1037,11 +1043,10 @@ template <int WT>
 void run_few(const void* x, int T, int d, const void* w_gate, const float* b_gate, int E, int k, const void* w1,
              const void* s1, const void* w2, const void* s2, int d_ff, int act, int32_t* topk_idx,
              float* topk_gate, void* y, const FewWs& ws, hipStream_t s) {
-  const bool direct = T * k <= kDirectSlots;
   FewTerms f = ws.f;
   if (WT != kMx4) f.x8 = nullptr;
   launch("few_gate", few_gate_kernel<WT == kF32>, T, kGateThreads, 0, s, x, d, w_gate, b_gate, E, k, topk_idx,
-         topk_gate, f, ws.done, direct ? 0 : d / 8);
+         topk_gate, f, ws.done, d / 8);
   FewArgs a = {};
   a.T = T;
   a.k = k;
