@@ -380,8 +380,7 @@ int luffy_expert_ffn_backward(const void* x, const int32_t* row_index, const int
  *              (groups = 1 only)
  *
  * luffy_mx4_dequantize - the values of such a matrix as float32 or bf16
- * (exact in float32; bf16 has every value but those of scales below 2^-126,
- * which it rounds).
+ * (exact in both; 6 * 2^127 and the like, beyond either type, give infinity).
  * ---------------------------------------------------------------------- */
 size_t luffy_mx4_scale_bytes(int groups, int rows, int cols);
 int luffy_mx4_quantize(const void* x, const int32_t* row_index, int groups, int rows, int cols, int dtype, void* q,
@@ -429,9 +428,13 @@ int luffy_mx4_expert_ffn(const void* x, const int32_t* row_index, const int32_t*
  *   NULL otherwise).  Activations are not rounded to 4 bits here: the step is
  *   bound by reading the weights, and keeps the accuracy.
  *   topk_idx, topk_gate [T, k], y [T, d] dtype.
- * Hidden rows and the sum over a token's experts are float32 (bf16: hidden
- * rows as two bf16 parts, 16 bits of mantissa).  x, w_gate, w1, w2 and y
- * must be 16-byte aligned.  A token's output depends on its own row only.
+ * Sums, hidden values and the sum over a token's experts are float32; between
+ * the products hidden values are kept as float32 (float32 weights), as two bf16
+ * parts (bf16: 16 bits of mantissa) or as three E4M3 parts (4-bit weights: 12
+ * bits, relative to the value).  x, w_gate, w1, w2 and y must be 16-byte
+ * aligned; d and d_ff multiples of 64, at most 32768; one expert's w1 at most
+ * 4 GiB - 64 KiB.  A token's output depends on its own row only, up to the
+ * order of its sums: K is split by the number of tokens and of experts.
  * ---------------------------------------------------------------------- */
 #define LUFFY_FEW_MAX_TOKENS 64
 size_t luffy_moe_few_workspace_size(int T, int d, int E, int k, int d_ff);
@@ -470,7 +473,8 @@ int luffy_adaptive_threshold(double l_ini, double l_prev, double* h_out);
  * greedy_finish, rep_local, rep_finalize, gather, ffn_queue, ffn1, ffn2,
  * ffn2_reduce, combine; backward: cbwd_group, cbwd_rows, cbwd_gate,
  * bwd_z, bwd_da, bwd_dx, bwd_dx_reduce, bwd_gather, bwd_dw2,
- * bwd_dw1.
+ * bwd_dw1; serving: mx4_quantize, mx4_dequantize, mx4_matmul, mx4_ffn1,
+ * mx4_ffn2, few_gate, few_ffn1, few_ffn2.
  * ---------------------------------------------------------------------- */
 int luffy_profile_kernel(const char* name);
 int luffy_profile_read(double* total_ms, int* launches);

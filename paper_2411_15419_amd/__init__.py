@@ -26,7 +26,7 @@ __all__ = [
     "condense_history_workspace_size", "MoEStack", "CondensationDriver",
     "LUFFY_MX4", "FEW_MAX_TOKENS", "mx4_scale_bytes", "luffy_mx4_quantize", "luffy_mx4_dequantize",
     "luffy_mx4_matmul", "luffy_mx4_expert_ffn", "mx4_expert_ffn_workspace_size", "luffy_moe_few",
-    "moe_few_workspace_size",
+    "moe_few_workspace_size", "mx4_weights", "ServingLayer",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libluffy.so")
@@ -321,6 +321,16 @@ def luffy_mx4_quantize(x, q, s, row_index=None, stream=None):
                                              _stream(stream)), "luffy_mx4_quantize")
 
 
+def mx4_weights(w, stream=None):
+    """(values, scales) of weights w [groups, rows, cols] (float32 or bf16) in
+    microscaled 4 bits, in tensors of their own."""
+    groups, rows, cols = w.shape
+    q = torch.empty(groups, rows, cols // 2, dtype=torch.uint8, device=w.device)
+    s = torch.empty(groups, (cols + 255) // 256, rows, 8, dtype=torch.uint8, device=w.device)
+    luffy_mx4_quantize(w, q, s, stream=stream)
+    return q, s
+
+
 def luffy_mx4_dequantize(q, s, x, stream=None):
     """The values of a microscaled matrix into x (float32 or bf16)."""
     groups, rows, cols = _mx4_shape(q, s, "luffy_mx4_dequantize")
@@ -604,6 +614,58 @@ class MoELayer:
         self.expert_ffn(x, stream)
         self.combine(stream)
         return self.buf.y
+
+
+class ServingLayer(MoELayer):
+    """A layer that answers rather than learns.  __call__ runs T tokens (a
+    prompt, a batch of prompts) through route, condense, expert FFN and combine;
+    step runs up to FEW_MAX_TOKENS tokens (one of every stream being decoded)
+    through luffy_moe_few, where condensation and a capacity would find nothing
+    to do.
+
+    microscaled (default): the weights are rounded to microscaled 4 bits here,
+    once, and only that form is kept (4.25 bits a weight); activations are bf16.
+    """
+
+    def __init__(self, w_gate, b_gate, w1, w2, *, microscaled: bool = True, **layer):
+        super().__init__(w_gate, b_gate, w1, w2, **layer)
+        if microscaled and self.dtype != torch.bfloat16:
+            raise LuffyError("ServingLayer: microscaled weights take bf16 activations")
+        dev = w1.device
+        self.w1_scale = self.w2_scale = None
+        if microscaled:
+            self.w1, self.w1_scale = mx4_weights(w1)
+            self.w2, self.w2_scale = mx4_weights(w2)
+            self.buf.ws_ffn = _workspace(
+                mx4_expert_ffn_workspace_size(self.T * self.k, self.E, self.d, self.d_ff), dev)
+        n = FEW_MAX_TOKENS
+        self.step_idx = torch.empty(n, self.k, dtype=torch.int32, device=dev)
+        self.step_gate = torch.empty(n, self.k, dtype=torch.float32, device=dev)
+        self.step_y = torch.empty(n, self.d, dtype=self.dtype, device=dev)
+        self.ws_step = _workspace(moe_few_workspace_size(n, self.d, self.E, self.k, self.d_ff), dev)
+
+    def expert_ffn(self, x, stream=None):
+        if self.w1_scale is None:
+            return super().expert_ffn(x, stream)
+        b = self.buf
+        src, idx = (x, b.rep_token) if b.x_rep is None else (b.x_rep, None)
+        luffy_mx4_expert_ffn(src, idx, b.rep_offsets, self.w1, self.w1_scale, self.w2, self.w2_scale, self.act,
+                             self.T * self.k, b.y_rep, self.buf.ws_ffn, stream)
+
+    def backward(self, x, dy, stream=None, dw_dtype=torch.float32):
+        raise LuffyError("ServingLayer has no backward")
+
+    def step(self, x, stream=None):
+        """y [n, d] of n <= FEW_MAX_TOKENS tokens x [n, d], valid until the next
+        step; their experts and gates are step_idx[:n] and step_gate[:n]."""
+        n = x.shape[0]
+        if x.dim() != 2 or not 0 < n <= FEW_MAX_TOKENS:
+            raise LuffyError(f"ServingLayer.step: x {tuple(x.shape)}, takes 1 to {FEW_MAX_TOKENS} tokens")
+        y = self.step_y[:n]
+        luffy_moe_few(x, self.w_gate, self.b_gate, self.w1, self.w2, self.k, self.act, self.step_idx[:n],
+                      self.step_gate[:n], y, self.ws_step, w1_scale=self.w1_scale, w2_scale=self.w2_scale,
+                      stream=stream)
+        return y
 
 
 class MoEStack:
