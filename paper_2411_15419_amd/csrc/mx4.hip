@@ -127,16 +127,22 @@ __global__ __launch_bounds__(kQuantThreads) void mx4_dequantize_kernel(const uin
 // ------------------------------------------------------------- the product
 enum Mx4Out { kOutF32 = 0, kOutBf16 = 1, kOutMx4Gelu = 2, kOutMx4Silu = 3 };
 
-// Two tile shapes.  Four waves either way, two blocks a CU (one block's
-// epilogue under the other's products).  128 x 128 reads an operand half as
-// often as 128 x 64 does, which counts once the matrix cores are busy; with few
-// rows an expert most of its second 64 rows are empty, the weights are read
-// once in either shape, and three stages in flight beat two.  On 32 experts of
-// 2048 -> 4096 -> 2048 (FFN, us, 128 x 64 | 128 x 128): 500 rows 71 | 85, 1500
-// rows 97 | 99, 4000 rows 133 | 140, 6000 rows 163 | 157; one 4096 x 4096
-// matrix on 4096 rows 66 | 50.  256 x 256 (one block a CU) was 8 % faster
-// on 16384 rows of 4096 -> 11008, 10 % slower on 8192 rows of 4096 -> 8192 and
-// slower everywhere below, and was not kept.
+// Three tile shapes.  128 x 128 and 128 x 64: four waves, two blocks a CU (one
+// block's epilogue under the other's products).  256 x 256: eight waves, one
+// block a CU, half the operand bytes from L2, which is what bounds the others (a
+// copy of the kernel without MFMAs takes nine tenths of its time).
+//   With few rows an expert most of a 128 x 128 tile's second 64 rows are empty,
+// the weights are read once in either shape, and three stages in flight beat two.
+// FFN on 32 experts of 2048 x 4096 (us, 128 x 64 | 128 x 128): 500 rows 71 | 85,
+// 1500 rows 97 | 99, 4000 rows 133 | 140, 6000 rows 163 | 157.
+//   256 x 256 exposes its first loads and its epilogue, so it takes one matrix
+// whose tiles fill whole rounds of the CUs, and rows of more than eight stages.
+// Rows x N x K, bf16 results (us, 128 x 128 | 256 x 256): 8192 x 4096 x 4096 97 |
+// 82, 16384 x 11008 x 4096 464 | 410, 16384 x 4096 x 8192 309 | 266; K = 1088 and
+// float32 results, 5003 x 2880 23.6 | 25.8, 16384 x 2880 68 | 72; of rounds 0.8
+// full, 6000 x 11008 x 4096 169 | 172; 0.67 full, 3000 x 11008 x 4096 95 | 99; FFN
+// of 16384 rows on 16 experts of 1024 x 4096 157 | 184.
+using Mx4Large = Mx4Core<256, 256, 2, 4, 2>;
 using Mx4Wide = Mx4Core<128, 128, 2, 2, 2>;
 using Mx4Narrow = Mx4Core<128, 64, 4, 1, 3>;
 constexpr int kNarrowRows = 96;   // average rows an expert up to which Mx4Narrow runs
@@ -178,62 +184,95 @@ struct Mx4Tiles {
   }
 };
 
-// Stores one 32 x 32 block of accumulators: lane l has row l % 32 of the block
-// and, in value v, column 8 (v / 4) + 4 (l / 32) + v % 4.
-template <int OUT>
-__device__ __forceinline__ void store_block(const f32x16& acc, bool valid, size_t row, int M, int n, int N, void* out,
-                                            uint8_t* out_scale) {
+// A wave's results of 32 rows (accumulators of one Q block: lane l has row
+// l % 32 and, in value v of block i, column 32 i + 8 (v / 4) + 4 (l / 32) + v %
+// 4) as float32 or bf16.  They turn in LDS, so that a store writes whole lines
+// of a row, past the caches' operands (non-temporal).  A product with 16384 x
+// 11008 bf16 results: 498 us with 8-byte stores straight from the registers, 32
+// rows each, 470 by way of LDS, 461 non-temporal (and 557 non-temporal without
+// whole lines).  The 16-byte chunks of a row are permuted by the row, so that
+// both sides fall on distinct banks.
+template <class G, bool F32>
+__device__ __forceinline__ void store_rows(const f32x16 (&acc)[G::FM], int rows, size_t row, int n, int N,
+                                           void* __restrict__ out, uint8_t* lds) {
+  constexpr int BYTES = F32 ? 4 : 2, PITCH = G::WTM * BYTES, CHUNKS = PITCH / 16, PER = 64 / CHUNKS;
+  constexpr int MASK = CHUNKS < 8 ? CHUNKS - 1 : 7, SHIFT = CHUNKS < 8 ? 1 : 0;
+  static_assert(CHUNKS == 4 || CHUNKS == 8 || CHUNKS == 16 || CHUNKS == 32, "chunk permutation");
+  const int lane = threadIdx.x & 63, half = lane >> 5, r = lane & 31, sw = (r >> SHIFT) & MASK;
+  uint8_t* mine = lds + r * PITCH;
+#pragma unroll
+  for (int i = 0; i < G::FM; ++i) {
+    if constexpr (F32) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<float4*>(mine + 16 * ((8 * i + 2 * g + half) ^ sw)) =
+            make_float4(acc[i][4 * g], acc[i][4 * g + 1], acc[i][4 * g + 2], acc[i][4 * g + 3]);
+    } else {
+      // lanes l and l ^ 32 exchange halves of two groups of four columns, so
+      // that each has eight consecutive ones
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        const uint32_t x0 = pack_bf16x2(acc[i][8 * g], acc[i][8 * g + 1]);
+        const uint32_t y0 = pack_bf16x2(acc[i][8 * g + 2], acc[i][8 * g + 3]);
+        const uint32_t x1 = pack_bf16x2(acc[i][8 * g + 4], acc[i][8 * g + 5]);
+        const uint32_t y1 = pack_bf16x2(acc[i][8 * g + 6], acc[i][8 * g + 7]);
+        const auto x = __builtin_amdgcn_permlane32_swap(x0, x1, false, false);
+        const auto y = __builtin_amdgcn_permlane32_swap(y0, y1, false, false);
+        *reinterpret_cast<uint4*>(mine + 16 * ((4 * i + 2 * g + half) ^ sw)) = make_uint4(x[0], y[0], x[1], y[1]);
+      }
+    }
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // the rows' other lanes are of this wave
+  const int c = lane % CHUNKS, cn = n + c * (16 / BYTES);
+#pragma unroll
+  for (int q = 0; q < 32 / PER; ++q) {
+    const int t = q * PER + lane / CHUNKS;
+    const i32x4 v = *reinterpret_cast<const i32x4*>(lds + t * PITCH + 16 * (c ^ ((t >> SHIFT) & MASK)));
+    if (t < rows && cn < N)
+      __builtin_nontemporal_store(v, reinterpret_cast<i32x4*>(static_cast<uint8_t*>(out) + ((row + t) * N + cn) * BYTES));
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
+// One 32 x 32 block of accumulators (layout as above) through the activation
+// and rounded to 4 bits.
+template <int ACT>
+__device__ __forceinline__ void store_mx4(const f32x16& acc, bool valid, size_t row, int M, int n, int N,
+                                          uint8_t* __restrict__ out, uint8_t* __restrict__ out_scale) {
   const int half = (threadIdx.x >> 5) & 1;
-  if constexpr (OUT == kOutF32) {
-    if (!valid) return;
-    float* dst = static_cast<float*>(out) + row * N + n + 4 * half;
+  // the activation, then the rounding to 4 bits: the 32 columns of a row are
+  // one block, half of it in lane l and half in lane l ^ 32
+  float v[16];
+  uint32_t most = 0;
 #pragma unroll
-    for (int g = 0; g < 4; ++g)
-      *reinterpret_cast<float4*>(dst + 8 * g) =
-          make_float4(acc[4 * g], acc[4 * g + 1], acc[4 * g + 2], acc[4 * g + 3]);
-  } else if constexpr (OUT == kOutBf16) {
-    if (!valid) return;
-    uint16_t* dst = static_cast<uint16_t*>(out) + row * N + n + 4 * half;
+  for (int i = 0; i < 16; ++i) {
+    v[i] = act_fast<ACT>(acc[i]);
+    most = max(most, abs_bits(v[i]));
+  }
+  most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), 32, 64)));
+  const uint32_t ex = mx4_exponent(most);
+  const float scale = __uint_as_float(ex << 23);
+  uint32_t c[2] = {0, 0};   // columns 0-3 and 8-11, 16-19 and 24-27 (+ 4 in the upper half)
 #pragma unroll
-    for (int g = 0; g < 4; ++g)
-      *reinterpret_cast<uint2*>(dst + 8 * g) = make_uint2(pack_bf16x2(acc[4 * g], acc[4 * g + 1]),
-                                                          pack_bf16x2(acc[4 * g + 2], acc[4 * g + 3]));
-  } else {
-    // the activation, then the rounding to 4 bits: the 32 columns of a row are
-    // one block, half of it in lane l and half in lane l ^ 32
-    constexpr int ACT = OUT == kOutMx4Gelu ? LUFFY_ACT_GELU : LUFFY_ACT_SILU;
-    float v[16];
-    uint32_t most = 0;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      v[i] = act_fast<ACT>(acc[i]);
-      most = max(most, abs_bits(v[i]));
-    }
-    most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), 32, 64)));
-    const uint32_t ex = mx4_exponent(most);
-    const float scale = __uint_as_float(ex << 23);
-    uint32_t c[2] = {0, 0};   // columns 0-3 and 8-11, 16-19 and 24-27 (+ 4 in the upper half)
-#pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      c[g] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c[g], v[8 * g], v[8 * g + 1], scale, 0);
-      c[g] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c[g], v[8 * g + 2], v[8 * g + 3], scale, 1);
-      c[g] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c[g], v[8 * g + 4], v[8 * g + 5], scale, 2);
-      c[g] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c[g], v[8 * g + 6], v[8 * g + 7], scale, 3);
-      if (ex == 255u) c[g] = 0;
-    }
-    // the lower half stores columns 0-15, the upper one 16-31
-    const uint32_t got = static_cast<uint32_t>(__shfl_xor(static_cast<int>(half ? c[0] : c[1]), 32, 64));
-    const uint32_t a = half ? got : c[0], b = half ? c[1] : got;   // columns +0..3 and +4..7 of each eight
-    if (!valid) return;
-    *reinterpret_cast<uint2*>(static_cast<uint8_t*>(out) + row * (N / 2) + n / 2 + 8 * half) =
-        make_uint2((a & 0xFFFFu) | (b << 16), (a >> 16) | (b & 0xFFFF0000u));
-    if (half == 0) {
-      uint8_t* dst = out_scale + (static_cast<size_t>(n >> 8) * M + row) * 8;
-      const int blk = n >> 5 & 7;
-      dst[blk] = static_cast<uint8_t>(ex);
-      if (n + 32 == N)
-        for (int z = blk + 1; z < 8; ++z) dst[z] = 0;
-    }
+  for (int g = 0; g < 2; ++g) {
+    c[g] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c[g], v[8 * g], v[8 * g + 1], scale, 0);
+    c[g] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c[g], v[8 * g + 2], v[8 * g + 3], scale, 1);
+    c[g] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c[g], v[8 * g + 4], v[8 * g + 5], scale, 2);
+    c[g] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c[g], v[8 * g + 6], v[8 * g + 7], scale, 3);
+    if (ex == 255u) c[g] = 0;
+  }
+  // the lower half stores columns 0-15, the upper one 16-31
+  const uint32_t got = static_cast<uint32_t>(__shfl_xor(static_cast<int>(half ? c[0] : c[1]), 32, 64));
+  const uint32_t a = half ? got : c[0], b = half ? c[1] : got;   // columns +0..3 and +4..7 of each eight
+  if (!valid) return;
+  *reinterpret_cast<uint2*>(out + row * (N / 2) + n / 2 + 8 * half) =
+      make_uint2((a & 0xFFFFu) | (b << 16), (a >> 16) | (b & 0xFFFF0000u));
+  if (half == 0) {
+    uint8_t* dst = out_scale + (static_cast<size_t>(n >> 8) * M + row) * 8;
+    const int blk = n >> 5 & 7;
+    dst[blk] = static_cast<uint8_t>(ex);
+    if (n + 32 == N)
+      for (int z = blk + 1; z < 8; ++z) dst[z] = 0;
   }
 }
 
@@ -265,13 +304,28 @@ __global__ __launch_bounds__(G::THREADS) void mx4_product_kernel(
   typename G::Acc acc;
   G::zero(acc);
   G::run_nq(G::active_q(wn, rows), tile, pipe, lds, acc);
+  const int n = n0 + wm * G::WTM;
 #pragma unroll
-  for (int i = 0; i < G::FM; ++i)
+  for (int j = 0; j < G::FN; ++j) {
+    const int q = G::q_row(wn, j);
+    if (q >= rows) break;
+    const size_t row = static_cast<size_t>(row0) + q;
+    if constexpr (OUT == kOutF32 || OUT == kOutBf16) {
+      constexpr bool F32 = OUT == kOutF32;
+      f32x16 a[G::FM];
 #pragma unroll
-    for (int j = 0; j < G::FN; ++j) {
-      const int n = n0 + wm * G::WTM + 32 * i, r = G::q_row(wn, j) + (lane & 31);
-      if (n < N) store_block<OUT>(acc[i][j], r < rows, static_cast<size_t>(row0) + r, M, n, N, out, out_scale);
+      for (int i = 0; i < G::FM; ++i) a[i] = acc[i][j];
+      static_assert(G::NWAVES * 32 * G::WTM * 4 <= G::LDS_BYTES, "results turn in the operands' LDS");
+      store_rows<G, F32>(a, rows - q, row, n, N, out, lds + w * 32 * G::WTM * (F32 ? 4 : 2));
+    } else {
+      constexpr int ACT = OUT == kOutMx4Gelu ? LUFFY_ACT_GELU : LUFFY_ACT_SILU;
+#pragma unroll
+      for (int i = 0; i < G::FM; ++i)
+        if (n + 32 * i < N)
+          store_mx4<ACT>(acc[i][j], q + (lane & 31) < rows, row + (lane & 31), M, n + 32 * i, N,
+                         static_cast<uint8_t*>(out), out_scale);
     }
+  }
 }
 
 template <class G, int OUT>
@@ -287,6 +341,15 @@ void launch_shape(const char* name, const uint8_t* xq, const uint8_t* xs, int M,
 template <int OUT>
 void launch_product(const char* name, const uint8_t* xq, const uint8_t* xs, int M, const int32_t* offsets, int E,
                     int N, int K, const uint8_t* wq, const uint8_t* ws, void* out, uint8_t* out_scale, hipStream_t s) {
+  if constexpr (OUT == kOutF32 || OUT == kOutBf16) {
+    const long long tiles = static_cast<long long>((M + Mx4Large::BN - 1) / Mx4Large::BN) *
+                            ((N + Mx4Large::BM - 1) / Mx4Large::BM);
+    const int cus = persistent_grid();
+    if (E == 1 && K > 2048 && 10 * tiles >= 9 * ((tiles + cus - 1) / cus * cus)) {
+      launch_shape<Mx4Large, OUT>(name, xq, xs, M, offsets, E, N, K, wq, ws, out, out_scale, s);
+      return;
+    }
+  }
   if (M <= kNarrowRows * E)
     launch_shape<Mx4Narrow, OUT>(name, xq, xs, M, offsets, E, N, K, wq, ws, out, out_scale, s);
   else

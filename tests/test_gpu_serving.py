@@ -157,3 +157,22 @@ def test_matmul_over_many_tiles(rows):
     xv = M.values(xc, xs)
     want = np.concatenate([xv[a:b] @ M.values(c, s).T for a, b, c, s in zip(off[:-1], off[1:], wc, ws)])
     assert np.array_equal(y.double().cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("R,N", [(4001, 3840), (3900, 4064)])
+def test_one_matrix_that_fills_the_cus(dtype, R, N):
+    """Sizes of the largest tiles (about 16 by 16 of them, the last ones ragged);
+    small integers, exact in float32 (and their sums' nearest bf16)."""
+    import torch
+    import paper_2411_15419_amd as L
+    rng = np.random.default_rng(R)
+    K = 2144
+    xc, wc = (rng.integers(0, 16, (r, K)).astype(np.uint8) for r in (R, N))
+    xs, ws = (rng.integers(127, 129, (r, K // 32)).astype(np.uint8) for r in (R, N))
+    (xq, xsc), (wq, wsc) = M.pack(xc, xs), M.pack(wc, ws)
+    t = torch.float32 if dtype == "f32" else torch.bfloat16
+    y = torch.full((R, N), -7.0, dtype=t, device="cuda")
+    L.luffy_mx4_matmul(gpu(xq), gpu(xsc), None, gpu(wq[None]), gpu(wsc[None]), y)
+    want = torch.from_numpy(M.values(xc, xs)).cuda() @ torch.from_numpy(M.values(wc, ws)).cuda().t()
+    assert torch.equal(y, want.to(t))
