@@ -100,6 +100,29 @@ struct FewTerms {   // 4-bit weights: the tokens' and hidden rows' terms and sca
   int d_ff;
 };
 
+template <int CTRL>
+__device__ __forceinline__ double add_dpp(double v) {
+  const int2 a = __builtin_bit_cast(int2, v);
+  const int2 b = make_int2(__builtin_amdgcn_update_dpp(0, a.x, CTRL, 0xf, 0xf, true),
+                           __builtin_amdgcn_update_dpp(0, a.y, CTRL, 0xf, 0xf, true));
+  return v + __builtin_bit_cast(double, b);
+}
+// Sum over a wave, in every lane, without going through LDS: neighbours, pairs,
+// fours and eights by row permutations, rows of 16 and halves by swaps.
+__device__ __forceinline__ double sum64(double v) {
+  v = add_dpp<0xB1>(v);    // lane ^ 1
+  v = add_dpp<0x4E>(v);    // lane ^ 2
+  v = add_dpp<0x141>(v);   // mirrored in 8
+  v = add_dpp<0x140>(v);   // mirrored in 16
+  uint2 a = __builtin_bit_cast(uint2, v);
+  auto x = __builtin_amdgcn_permlane16_swap(a.x, a.x, false, false), y = __builtin_amdgcn_permlane16_swap(a.y, a.y, false, false);
+  v = __builtin_bit_cast(double, make_uint2(x[0], y[0])) + __builtin_bit_cast(double, make_uint2(x[1], y[1]));
+  a = __builtin_bit_cast(uint2, v);
+  x = __builtin_amdgcn_permlane32_swap(a.x, a.x, false, false);
+  y = __builtin_amdgcn_permlane32_swap(a.y, a.y, false, false);
+  return __builtin_bit_cast(double, make_uint2(x[0], y[0])) + __builtin_bit_cast(double, make_uint2(x[1], y[1]));
+}
+
 // One block a token; wave w takes experts w, w + 16, ...  A logit is one
 // float64 sum (products of two bf16 or float32 values are exact there), so a
 // choice needs no second look at close calls.  Logits that are no number
@@ -143,8 +166,7 @@ __global__ __launch_bounds__(kGateThreads) void few_gate_kernel(const void* __re
           s = fma(static_cast<double>(bf16_to_f32(a.h[i])), static_cast<double>(bf16_to_f32(b.h[i])), s);
       }
     }
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) s += __shfl_xor(s, o, 64);
+    s = sum64(s);
     if (lane == 0) logit[e] = s + (b_gate ? static_cast<double>(b_gate[e]) : 0.0);
   }
   if (f.x8) {
@@ -175,29 +197,22 @@ __global__ __launch_bounds__(kGateThreads) void few_gate_kernel(const void* __re
   __syncthreads();
   if (w != 0) return;
   const double mine = lane < E ? logit[lane] : 0.0;
-  const bool num = lane < E && !isnan(mine);
-  double v0 = 0.0, v1 = 0.0;
-  int i0 = 0, i1 = 0;
-  // largest first, ties to the lower index; taken marks experts already chosen
-  uint64_t taken = 0;
-  for (int j = 0; j < k; ++j) {
-    const bool open = lane < E && !(taken >> lane & 1);
-    double best = open && num ? mine : -HUGE_VAL;
-    int at = open ? lane : kMaxExperts;
-    bool bn = open && num;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const double ob = __shfl_xor(best, o, 64);
-      const int oa = __shfl_xor(at, o, 64);
-      const bool on = __shfl_xor(static_cast<int>(bn), o, 64);
-      const bool take = oa < kMaxExperts &&
-                        (at == kMaxExperts || (on != bn ? on : (ob > best || (ob == best && oa < at))));
-      if (take) { best = ob; at = oa; bn = on; }
-    }
-    taken |= 1ull << at;
-    const double v = logit[at];
-    if (j == 0) { i0 = at; v0 = v; } else { i1 = at; v1 = v; }
+  // An expert's rank: how many come before it (larger first, ties to the lower
+  // index, no number last).  Its logit becomes an integer of the same order, 0
+  // for no number, and every lane compares its own with each in turn.
+  const uint64_t bits = __builtin_bit_cast(uint64_t, mine + 0.0);   // (-0 + 0 = +0: the two are a tie)
+  const uint64_t sign = 1ull << 63;
+  const uint64_t key = isnan(mine) ? 0 : (bits & sign ? ~bits : bits | sign);
+  int rank = 0;
+#pragma unroll 4
+  for (int e = 0; e < E; ++e) {
+    const uint64_t o = static_cast<uint64_t>(__builtin_amdgcn_readlane(static_cast<int>(key >> 32), e)) << 32 |
+                       static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(key), e));
+    rank += o >= key + (e >= lane ? 1 : 0) ? 1 : 0;
   }
+  const int i0 = __ffsll(__ballot(lane < E && rank == 0)) - 1;
+  const int i1 = k > 1 ? __ffsll(__ballot(lane < E && rank == 1)) - 1 : i0;
+  const double v0 = logit[i0], v1 = logit[i1];
   if (k == 1) {
     float den = lane < E ? expf(static_cast<float>(mine - v0)) : 0.f;
 #pragma unroll
