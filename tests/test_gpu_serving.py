@@ -176,3 +176,76 @@ def test_one_matrix_that_fills_the_cus(dtype, R, N):
     L.luffy_mx4_matmul(gpu(xq), gpu(xsc), None, gpu(wq[None]), gpu(wsc[None]), y)
     want = torch.from_numpy(M.values(xc, xs)).cuda() @ torch.from_numpy(M.values(wc, ws)).cuda().t()
     assert torch.equal(y, want.to(t))
+
+
+def test_rows_past_4_gib():
+    """Values, scales, rows and results whose offsets pass 32 bits: the last rows
+    are what they are on their own."""
+    import torch
+    import paper_2411_15419_amd as L
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    rows, cols = 2 ** 18 + 37, 32768          # q just past 4 GiB, bf16 values past 16
+    x = torch.empty(rows, cols, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    q = torch.empty(rows, cols // 2, dtype=torch.uint8, device="cuda")
+    s = torch.empty(cols // 256, rows, 8, dtype=torch.uint8, device="cuda")
+    L.luffy_mx4_quantize(x, q, s)
+    tail = x[-41:].clone()
+    tq, ts = torch.empty_like(q[-41:]), torch.empty(cols // 256, 41, 8, dtype=torch.uint8, device="cuda")
+    L.luffy_mx4_quantize(tail, tq, ts)
+    assert torch.equal(q[-41:], tq) and torch.equal(s[:, -41:], ts)
+    L.luffy_mx4_dequantize(q, s, x)
+    back = torch.empty_like(tail)
+    L.luffy_mx4_dequantize(tq, ts, back)
+    assert torch.equal(x[-41:], back)
+    del x
+    wq, ws = L.mx4_weights(torch.empty(1, 64, cols, dtype=torch.bfloat16, device="cuda").normal_(generator=gen))
+    y, ty = torch.empty(rows, 64, device="cuda"), torch.empty(41, 64, device="cuda")
+    L.luffy_mx4_matmul(q, s, None, wq, ws, y)
+    L.luffy_mx4_matmul(tq, ts, None, wq, ws, ty)
+    v = torch.empty(1, 64, cols, device="cuda")
+    L.luffy_mx4_dequantize(wq, ws, v)
+    # 32768 float32 additions in some order
+    bound = 32768 * 2.0 ** -24 * (back.double().abs() @ v[0].double().abs().t())
+    for got in (ty, y[-41:]):
+        assert ((got.double() - back.double() @ v[0].double().t()).abs() <= bound).all()
+
+
+@pytest.mark.parametrize("w,E,d,d_ff", [("bf16", 64, 4096, 11008), ("mx4", 9, 32768, 32768)])
+def test_experts_past_4_gib(w, E, d, d_ff):
+    """The last expert's weights lie past 4 GiB; the same weights as the first
+    expert give the same bits."""
+    import torch
+    import paper_2411_15419_amd as L
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    if w == "bf16":
+        w1, w2 = (torch.empty(E, *m, dtype=torch.bfloat16, device="cuda").normal_(0, 0.02, generator=gen)
+                  for m in ((d_ff, d), (d, d_ff)))
+        scales = [None, None]
+        tensors = [w1, w2]
+    else:
+        w1, w2 = (torch.randint(0, 256, (E, a, b // 2), dtype=torch.uint8, device="cuda", generator=gen)
+                  for a, b in ((d_ff, d), (d, d_ff)))
+        scales = [torch.randint(112, 120, (E, b // 256, a, 8), dtype=torch.uint8, device="cuda", generator=gen)
+                  for a, b in ((d_ff, d), (d, d_ff))]
+        tensors = [w1, w2] + scales
+    assert (E - 1) * w1[0].numel() * w1.element_size() >= 2 ** 32
+    w_gate = torch.zeros(E, d, dtype=torch.bfloat16, device="cuda")
+    for T in (1, 9):
+        x = torch.empty(T, d, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+        out = []
+        for e in (E - 1, 0):
+            if e == 0:
+                for t in tensors:
+                    t[0].copy_(t[E - 1])
+            b_gate = torch.full((E,), -50.0, device="cuda")
+            b_gate[e] = 50.0
+            idx, gate = torch.empty(T, 1, dtype=torch.int32, device="cuda"), torch.empty(T, 1, device="cuda")
+            y = torch.empty_like(x)
+            ws = torch.empty(L.moe_few_workspace_size(T, d, E, 1, d_ff), dtype=torch.uint8, device="cuda")
+            L.luffy_moe_few(x, w_gate, b_gate, w1, w2, 1, "gelu", idx, gate, y, ws, w1_scale=scales[0],
+                            w2_scale=scales[1])
+            assert (idx == e).all()
+            out.append(y)
+        assert torch.isfinite(out[0]).all() and out[0].abs().max() > 0
+        assert torch.equal(out[0], out[1])
+        tensors[0][0].zero_()
