@@ -290,48 +290,62 @@ __global__ __launch_bounds__(G::THREADS) void mx4_product_kernel(
     uint8_t* __restrict__ out_scale) {
   __shared__ __attribute__((aligned(16))) uint8_t lds[G::LDS_BYTES];
   const Mx4Tiles map(offsets, E, M, N, G::BM, G::BN);
-  const int t = xcd_virtual_block();
+  int t = xcd_virtual_block();
   if (t >= map.tiles) return;
-  int e, row0, rows, n0;
-  map.decode(t, E, G::BM, G::BN, e, row0, rows, n0);
   const int kbytes = K / 2, kstages = (K + 255) / 256;
   typename G::Tile tile;
-  tile.p = wq + (static_cast<size_t>(e) * N + n0) * kbytes;
-  tile.q = xq + static_cast<size_t>(row0) * kbytes;
-  tile.ps = ws + (static_cast<size_t>(e) * kstages * N + n0) * 8;
-  tile.qs = xs + static_cast<size_t>(row0) * 8;
-  tile.pvalid = min(G::BM, N - n0);
-  tile.qvalid = rows;
+  typename G::Pipe pipe;
   tile.ps_stage = static_cast<size_t>(N) * 8;
   tile.qs_stage = static_cast<size_t>(M) * 8;
   tile.kbytes = kbytes;
-  typename G::Pipe pipe;
-  G::prefetch(tile, pipe, lds);
+  int row0, rows, n0;
+  // tile t's place, and its first stages on their way
+  auto start = [&]() {
+    int e;
+    map.decode(t, E, G::BM, G::BN, e, row0, rows, n0);
+    tile.p = wq + (static_cast<size_t>(e) * N + n0) * kbytes;
+    tile.q = xq + static_cast<size_t>(row0) * kbytes;
+    tile.ps = ws + (static_cast<size_t>(e) * kstages * N + n0) * 8;
+    tile.qs = xs + static_cast<size_t>(row0) * 8;
+    tile.pvalid = min(G::BM, N - n0);
+    tile.qvalid = rows;
+    G::prefetch(tile, pipe, lds);
+  };
+  start();
   const int lane = threadIdx.x & 63, w = G::wave(), wm = G::wave_m(w), wn = G::wave_n(w);
-  typename G::Acc acc;
-  G::zero(acc);
-  G::run_nq(G::active_q(wn, rows), tile, pipe, lds, acc);
-  const int n = n0 + wm * G::WTM;
-#pragma unroll
-  for (int j = 0; j < G::FN; ++j) {
-    const int q = G::q_row(wn, j);
-    if (q >= rows) break;
-    const size_t row = static_cast<size_t>(row0) + q;
-    if constexpr (OUT == kOutF32 || OUT == kOutBf16) {
-      constexpr bool F32 = OUT == kOutF32;
-      f32x16 a[G::FM];
-#pragma unroll
-      for (int i = 0; i < G::FM; ++i) a[i] = acc[i][j];
-      static_assert(G::NWAVES * 32 * G::WTM * 4 <= G::LDS_BYTES, "results turn in the operands' LDS");
-      store_rows<G, F32>(a, rows - q, row, n, N, out, lds + w * 32 * G::WTM * (F32 ? 4 : 2));
-    } else {
-      constexpr int ACT = OUT == kOutMx4Gelu ? LUFFY_ACT_GELU : LUFFY_ACT_SILU;
-#pragma unroll
-      for (int i = 0; i < G::FM; ++i)
-        if (n + 32 * i < N)
-          store_mx4<ACT>(acc[i][j], q + (lane & 31) < rows, row + (lane & 31), M, n + 32 * i, N,
-                         static_cast<uint8_t*>(out), out_scale);
+  while (true) {
+    typename G::Acc acc;
+    G::zero(acc);
+    G::run_nq(G::active_q(wn, rows), tile, pipe, lds, acc);
+    const int out_row0 = row0, out_rows = rows, n = n0 + wm * G::WTM;
+    bool more = false;
+    if constexpr (OUT == kOutMx4Gelu || OUT == kOutMx4Silu) {
+      t += gridDim.x;
+      more = t < map.tiles;
+      if (more) start();
     }
+#pragma unroll
+    for (int j = 0; j < G::FN; ++j) {
+      const int q = G::q_row(wn, j);
+      if (q >= out_rows) break;
+      const size_t row = static_cast<size_t>(out_row0) + q;
+      if constexpr (OUT == kOutF32 || OUT == kOutBf16) {
+        constexpr bool F32 = OUT == kOutF32;
+        f32x16 a[G::FM];
+#pragma unroll
+        for (int i = 0; i < G::FM; ++i) a[i] = acc[i][j];
+        static_assert(G::NWAVES * 32 * G::WTM * 4 <= G::LDS_BYTES, "results turn in the operands' LDS");
+        store_rows<G, F32>(a, out_rows - q, row, n, N, out, lds + w * 32 * G::WTM * (F32 ? 4 : 2));
+      } else {
+        constexpr int ACT = OUT == kOutMx4Gelu ? LUFFY_ACT_GELU : LUFFY_ACT_SILU;
+#pragma unroll
+        for (int i = 0; i < G::FM; ++i)
+          if (n + 32 * i < N)
+            store_mx4<ACT>(acc[i][j], q + (lane & 31) < out_rows, row + (lane & 31), M, n + 32 * i, N,
+                           static_cast<uint8_t*>(out), out_scale);
+      }
+    }
+    if (!more) break;
   }
 }
 
@@ -340,7 +354,8 @@ void launch_shape(const char* name, const uint8_t* xq, const uint8_t* xs, int M,
                   int K, const uint8_t* wq, const uint8_t* ws, void* out, uint8_t* out_scale, hipStream_t s) {
   // every expert may add one partial row tile
   const long long row_tiles = (M + G::BN - 1) / G::BN + (offsets ? E - 1 : 0);
-  const long long tiles = row_tiles * ((N + G::BM - 1) / G::BM);
+  long long tiles = row_tiles * ((N + G::BM - 1) / G::BM);
+  if (OUT == kOutMx4Gelu || OUT == kOutMx4Silu) tiles = std::min(tiles, 2ll * persistent_grid());
   launch(name, mx4_product_kernel<G, OUT>, static_cast<int>((tiles + 7) / 8 * 8), G::THREADS, 0, s, xq, xs, M, offsets,
          E, N, K, wq, ws, out, out_scale);
 }
