@@ -282,7 +282,17 @@ __device__ __forceinline__ void store_mx4(const f32x16& acc, bool valid, size_t 
 // MFMA busy 52 % of the cycles, the rest is the first loads and the epilogue of
 // a CU's one block.  The first product of an FFN is bound by its epilogue: about
 // 23 vector instructions a hidden value, two of them transcendental (8653 rows on
-// 32 experts of 2048 x 8192: 190 us, 160 without fetching operands).
+// 32 experts of 2048 x 8192: 170 us; MFMA busy 22 %, vector unit half).
+// Whether a block takes one tile after the other, the next one's first loads
+// under the epilogue: all shapes with two blocks a CU.  (FFN of 8653 rows on 32
+// experts of 2048 x 8192: first product 190 -> 170 us, second 150 -> 134; of 2000
+// rows on 32 of 2048 x 4096 102 -> 66.)  256 x 256 has no registers left for it: 93
+// spilled, 402 -> 498 us on 16384 x 11008 x 4096.
+template <class G>
+constexpr bool mx4_stays() {
+  return 2 * G::LDS_BYTES <= 160 * 1024;
+}
+
 template <class G, int OUT>
 __global__ __launch_bounds__(G::THREADS) void mx4_product_kernel(
     const uint8_t* __restrict__ xq, const uint8_t* __restrict__ xs, int M, const int32_t* __restrict__ offsets, int E,
@@ -299,6 +309,13 @@ __global__ __launch_bounds__(G::THREADS) void mx4_product_kernel(
   tile.qs_stage = static_cast<size_t>(M) * 8;
   tile.kbytes = kbytes;
   int row0, rows, n0;
+  // Results turn in LDS behind the first stage, which may already hold the next
+  // tile's by then; 4-bit results need no LDS, and all first stages go out.
+  constexpr bool MX4 = OUT == kOutMx4Gelu || OUT == kOutMx4Silu;
+  constexpr int TURN = G::NWAVES * 32 * G::WTM * (OUT == kOutF32 ? 4 : 2);
+  constexpr bool STAY = mx4_stays<G>();
+  constexpr int EARLY = MX4 ? G::STAGES : 1;
+  static_assert(MX4 || TURN <= (G::STAGES - STAY) * G::STAGE_BYTES, "results turn in the operands' LDS");
   // tile t's place, and its first stages on their way
   auto start = [&]() {
     int e;
@@ -309,17 +326,18 @@ __global__ __launch_bounds__(G::THREADS) void mx4_product_kernel(
     tile.qs = xs + static_cast<size_t>(row0) * 8;
     tile.pvalid = min(G::BM, N - n0);
     tile.qvalid = rows;
-    G::prefetch(tile, pipe, lds);
+    G::template prefetch<0, EARLY>(tile, pipe, lds);
   };
   start();
   const int lane = threadIdx.x & 63, w = G::wave(), wm = G::wave_m(w), wn = G::wave_n(w);
   while (true) {
+    G::template prefetch<EARLY, G::STAGES>(tile, pipe, lds);
     typename G::Acc acc;
     G::zero(acc);
     G::run_nq(G::active_q(wn, rows), tile, pipe, lds, acc);
     const int out_row0 = row0, out_rows = rows, n = n0 + wm * G::WTM;
     bool more = false;
-    if constexpr (OUT == kOutMx4Gelu || OUT == kOutMx4Silu) {
+    if constexpr (STAY) {
       t += gridDim.x;
       more = t < map.tiles;
       if (more) start();
@@ -334,8 +352,7 @@ __global__ __launch_bounds__(G::THREADS) void mx4_product_kernel(
         f32x16 a[G::FM];
 #pragma unroll
         for (int i = 0; i < G::FM; ++i) a[i] = acc[i][j];
-        static_assert(G::NWAVES * 32 * G::WTM * 4 <= G::LDS_BYTES, "results turn in the operands' LDS");
-        store_rows<G, F32>(a, out_rows - q, row, n, N, out, lds + w * 32 * G::WTM * (F32 ? 4 : 2));
+        store_rows<G, F32>(a, out_rows - q, row, n, N, out, lds + (STAY ? G::STAGE_BYTES : 0) + w * (TURN / G::NWAVES));
       } else {
         constexpr int ACT = OUT == kOutMx4Gelu ? LUFFY_ACT_GELU : LUFFY_ACT_SILU;
 #pragma unroll
@@ -346,6 +363,10 @@ __global__ __launch_bounds__(G::THREADS) void mx4_product_kernel(
       }
     }
     if (!more) break;
+    if constexpr (!MX4) {   // every wave is done turning before the other stages go out
+      __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
+      raw_barrier();
+    }
   }
 }
 
@@ -355,7 +376,7 @@ void launch_shape(const char* name, const uint8_t* xq, const uint8_t* xs, int M,
   // every expert may add one partial row tile
   const long long row_tiles = (M + G::BN - 1) / G::BN + (offsets ? E - 1 : 0);
   long long tiles = row_tiles * ((N + G::BM - 1) / G::BM);
-  if (OUT == kOutMx4Gelu || OUT == kOutMx4Silu) tiles = std::min(tiles, 2ll * persistent_grid());
+  if (mx4_stays<G>()) tiles = std::min(tiles, 2ll * persistent_grid());
   launch(name, mx4_product_kernel<G, OUT>, static_cast<int>((tiles + 7) / 8 * 8), G::THREADS, 0, s, xq, xs, M, offsets,
          E, N, K, wq, ws, out, out_scale);
 }

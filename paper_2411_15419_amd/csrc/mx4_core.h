@@ -237,13 +237,14 @@ struct Mx4Core {
     if (sched) interleave_reads<NQ>();
   }
 
-  // Issues the first stages of a tile.
+  // Issues stages FROM .. TO - 1 of a tile (of its first STAGES; FROM = 0 first).
+  template <int FROM, int TO>
   static __device__ __forceinline__ void prefetch(const Tile& t, Pipe& s, uint8_t* lds_generic) {
     const lds_ptr lds = (lds_ptr)lds_generic;
-    setup(t, s);
+    if constexpr (FROM == 0) setup(t, s);
     const int nk = __builtin_amdgcn_readfirstlane((t.kbytes + 127) / 128);
 #pragma unroll
-    for (int k = 0; k < STAGES; ++k)
+    for (int k = FROM; k < TO; ++k)
       if (k < nk) issue(t, s, k, lds + k * STAGE_BYTES);
   }
 
