@@ -134,19 +134,20 @@ enum Mx4Out { kOutF32 = 0, kOutBf16 = 1, kOutMx4Gelu = 2, kOutMx4Silu = 3 };
 // copy of the kernel without MFMAs takes nine tenths of its time).
 //   With few rows an expert most of a 128 x 128 tile's second 64 rows are empty,
 // the weights are read once in either shape, and three stages in flight beat two.
-// FFN on 32 experts of 2048 x 4096 (us, 128 x 64 | 128 x 128): 500 rows 71 | 85,
-// 1500 rows 97 | 99, 4000 rows 133 | 140, 6000 rows 163 | 157.
+// FFN on 32 experts of 2048 x 4096 (us, 128 x 64 | 128 x 128): 500 rows 56 | 61,
+// 2000 rows 66 | 70, 2500 rows 87 | 76, 4000 rows 101 | 88; on 16 of 1024 x 4096:
+// 200 rows 26 | 31, 1000 rows 31.6 | 32.6, 1200 rows 36.6 | 35.8.
 //   256 x 256 exposes its first loads and its epilogue, so it takes one matrix
 // whose tiles fill whole rounds of the CUs, and rows of more than eight stages.
 // Rows x N x K, bf16 results (us, 128 x 128 | 256 x 256): 8192 x 4096 x 4096 97 |
 // 82, 16384 x 11008 x 4096 464 | 410, 16384 x 4096 x 8192 309 | 266; K = 1088 and
 // float32 results, 5003 x 2880 23.6 | 25.8, 16384 x 2880 68 | 72; of rounds 0.8
 // full, 6000 x 11008 x 4096 169 | 172; 0.67 full, 3000 x 11008 x 4096 95 | 99; FFN
-// of 16384 rows on 16 experts of 1024 x 4096 157 | 184.
+// of 16384 rows on 16 experts of 1024 x 4096 139 | 184.
 using Mx4Large = Mx4Core<256, 256, 2, 4, 2>;
 using Mx4Wide = Mx4Core<128, 128, 2, 2, 2>;
 using Mx4Narrow = Mx4Core<128, 64, 4, 1, 3>;
-constexpr int kNarrowRows = 96;   // average rows an expert up to which Mx4Narrow runs
+constexpr int kNarrowRows = 64;   // average rows an expert up to which Mx4Narrow runs
 
 // Tile t of the grouped product -> expert, first row, rows, first column: the
 // tiles expert by expert (one expert's counts a lane), in blocks of 8 row tiles
@@ -282,11 +283,11 @@ __device__ __forceinline__ void store_mx4(const f32x16& acc, bool valid, size_t 
 // MFMA busy 52 % of the cycles, the rest is the first loads and the epilogue of
 // a CU's one block.  The first product of an FFN is bound by its epilogue: about
 // 23 vector instructions a hidden value, two of them transcendental (8653 rows on
-// 32 experts of 2048 x 8192: 170 us; MFMA busy 22 %, vector unit half).
+// 32 experts of 2048 x 8192: 170 us; vector units half busy).
 // Whether a block takes one tile after the other, the next one's first loads
 // under the epilogue: all shapes with two blocks a CU.  (FFN of 8653 rows on 32
 // experts of 2048 x 8192: first product 190 -> 170 us, second 150 -> 134; of 2000
-// rows on 32 of 2048 x 4096 102 -> 66.)  256 x 256 has no registers left for it: 93
+// rows on 32 of 2048 x 4096 82 -> 66 for both.)  256 x 256 has no registers left for it: 93
 // spilled, 402 -> 498 us on 16384 x 11008 x 4096.
 template <class G>
 constexpr bool mx4_stays() {
