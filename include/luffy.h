@@ -406,8 +406,9 @@ int luffy_mx4_matmul(const void* xq, const void* xs, int M, const int32_t* offse
 /* ------------------------------------------------------------------------
  * luffy_mx4_expert_ffn - luffy_expert_ffn on microscaled weights (Sec. 2.1,
  * Sec. 3), for serving: y_rep[r] = W2_e Q(act(W1_e Q(x_r))), Q the rounding of
- * luffy_mx4_quantize (the hidden rows are rounded from float32).  bf16 rows
- * and results; x, row_index, rep_offsets, act, max_rows and y_rep as for
+ * luffy_mx4_quantize (the hidden rows are rounded from float32, where act has a
+ * relative error of at most 10^-6 (1 + z^2) down to z = -13 for GELU, and for
+ * SiLU down to z = -87, below which it is 0).  bf16 rows and results; x, row_index, rep_offsets, act, max_rows and y_rep as for
  * luffy_expert_ffn; w1 [E, d_ff, d] and w2 [E, d, d_ff] microscaled.
  * ---------------------------------------------------------------------- */
 size_t luffy_mx4_expert_ffn_workspace_size(int max_rows, int E, int d, int d_ff);

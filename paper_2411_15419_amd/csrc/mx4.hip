@@ -248,7 +248,7 @@ __device__ __forceinline__ void store_mx4(const f32x16& acc, bool valid, size_t 
   uint32_t most = 0;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    v[i] = act_fast<ACT>(acc[i]);
+    v[i] = act_relative<ACT>(acc[i]);
     most = max(most, abs_bits(v[i]));
   }
   most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), 32, 64)));
