@@ -408,8 +408,9 @@ int luffy_mx4_matmul(const void* xq, const void* xs, int M, const int32_t* offse
  * Sec. 3), for serving: y_rep[r] = W2_e Q(act(W1_e Q(x_r))), Q the rounding of
  * luffy_mx4_quantize (the hidden rows are rounded from float32, where act has a
  * relative error of at most 10^-6 (1 + z^2) down to z = -13 for GELU, and for
- * SiLU down to z = -87, below which it is 0).  bf16 rows and results; x, row_index, rep_offsets, act, max_rows and y_rep as for
- * luffy_expert_ffn; w1 [E, d_ff, d] and w2 [E, d, d_ff] microscaled.
+ * SiLU down to z = -87, below which it is 0).  bf16 rows and results; x,
+ * row_index, rep_offsets, act, max_rows and y_rep as for luffy_expert_ffn; w1
+ * [E, d_ff, d] and w2 [E, d, d_ff] microscaled.
  * ---------------------------------------------------------------------- */
 size_t luffy_mx4_expert_ffn_workspace_size(int max_rows, int E, int d, int d_ff);
 int luffy_mx4_expert_ffn(const void* x, const int32_t* row_index, const int32_t* rep_offsets, int E, int d, int d_ff,
@@ -432,7 +433,8 @@ int luffy_mx4_expert_ffn(const void* x, const int32_t* row_index, const int32_t*
  * Sums, hidden values and the sum over a token's experts are float32; between
  * the products hidden values are kept as float32 (float32 weights), as two bf16
  * parts (bf16: 16 bits of mantissa) or as three E4M3 parts (4-bit weights: 12
- * bits, relative to the value).  x, w_gate, w1, w2 and y must be 16-byte
+ * bits, relative to the value), and act has a relative error of a few
+ * 2^-24 (1 + z^2).  x, w_gate, w1, w2 and y must be 16-byte
  * aligned; d and d_ff multiples of 64, at most 32768; one expert's w1 at most
  * 4 GiB - 64 KiB.  A token's output depends on its own row only, up to the
  * order of its sums: K is split by the number of tokens and of experts.

@@ -480,7 +480,7 @@ __device__ __forceinline__ void few_store_hidden(const FewArgs& a, int act, int 
                                                  float (&z)[kFewValues<WT, false>]) {
 #pragma unroll
   for (int i = 0; i < kFewValues<WT, false>; ++i)
-    z[i] = act == LUFFY_ACT_GELU ? act_f32<LUFFY_ACT_GELU>(z[i]) : act_f32<LUFFY_ACT_SILU>(z[i]);
+    z[i] = act == LUFFY_ACT_GELU ? act_f32_relative<LUFFY_ACT_GELU>(z[i]) : act_f32_relative<LUFFY_ACT_SILU>(z[i]);
   uint8_t* dst = a.h + static_cast<size_t>(s) * few_pitch<WT, true>(a.N);
   if constexpr (WT == kMx4) {
     // (a block's four lanes agree on valid: a block of waves has a multiple of

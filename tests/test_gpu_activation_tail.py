@@ -79,3 +79,42 @@ def test_blocks_of_tail_values_get_their_codes(act):
     bad = whole & ~((got >= np.minimum(low, high)) & (got <= np.maximum(low, high)))
     assert not bad.any(), (np.argwhere(bad)[:4], z[bad][:4], got[bad][:4], h[bad][:4])
     assert (got[whole & (h != 0)] != 0).mean() > 0.5
+
+
+@pytest.mark.parametrize("w", ["f32", "bf16", "mx4"])
+@pytest.mark.parametrize("act", ["gelu", "silu"])
+@pytest.mark.parametrize("T", [7, 40])
+def test_a_step_keeps_tail_values(T, act, w):
+    """luffy_moe_few with one expert and W2 the identity: the results are the
+    hidden values as the second product holds them."""
+    import torch
+    import paper_2411_15419_amd as L
+    d = 320
+    x, w1 = tail_layer(T, d)
+    z = x @ w1.T
+    h = act64(z, act)
+    t = torch.float32 if w == "f32" else torch.bfloat16
+    w2 = np.eye(d)
+    scales = [None, None]
+    if w == "mx4":
+        (g1, s1), (g2, s2) = M.pack(*M.quantize(w1)), M.pack(*M.quantize(w2))
+        g1, g2, scales = gpu(g1[None]), gpu(g2[None]), [gpu(s1[None]), gpu(s2[None])]
+    else:
+        g1, g2 = gpu(w1[None], t), gpu(w2[None], t)
+    idx, gate = torch.empty(T, 1, dtype=torch.int32, device="cuda"), torch.empty(T, 1, device="cuda")
+    y = torch.empty(T, d, dtype=t, device="cuda")
+    ws = torch.empty(L.moe_few_workspace_size(T, d, 1, 1, d), dtype=torch.uint8, device="cuda")
+    L.luffy_moe_few(gpu(x, t), torch.zeros(1, d, dtype=t, device="cuda"), None, g1, g2, 1, act, idx, gate, y, ws,
+                    w1_scale=scales[0], w2_scale=scales[1])
+    got = y.double().cpu().numpy()
+    # erfcf's and expf's argument rounded, a few units in the last place; then
+    # what the hidden values are kept as, for 4 bits also 2^-25 of their block's
+    # largest; then the result's own rounding
+    tol = (2.0 * z * z + 16.0) * 2.0 ** -24 + {"f32": 0.0, "bf16": 2.0 ** -17, "mx4": 2.0 ** -12}[w]
+    slack = 2.0 ** -126 * np.ones_like(h)
+    if w == "mx4":
+        slack += 2.0 ** -25 * np.abs(h).reshape(T, -1, 32).max(-1).repeat(32, axis=1)
+    low, high = h - tol * np.abs(h) - slack, h + tol * np.abs(h) + slack
+    low, high = (torch.from_numpy(v).to(t).double().numpy() for v in (low, high))
+    bad = (z >= -12.5) & ~((got >= low) & (got <= high))
+    assert not bad.any(), (np.argwhere(bad)[:4], z[bad][:4], got[bad][:4], h[bad][:4])
