@@ -618,22 +618,27 @@ __device__ __forceinline__ void few_run(const FewArgs& a, FewLds<NBMAX, RT>& m, 
     const uint8_t* cols = m.cols + st.half * S::HALF + part * few_part_bytes<NBMAX, RT>(split_log2) + lcol * 128 +
                           16 * (lc ^ (lcol & 7));
     const uint8_t* scales = m.scales + st.half * S::SCALES + ((part << cols_log2) + lcol) * chunk * 8 + lc;
-    // Pieces past the end are zeros, multiplied with the last piece's columns:
-    // without branches the compiler knows how many loads are in flight.
+    // Pieces past the end are zeros, multiplied with the last piece's columns as
+    // zeros (an infinity there must not meet a zero; 4-bit weights: a column's
+    // block without numbers has made its result NaN already): without branches
+    // the compiler knows how many loads are in flight.
     auto multiply = [&](const u32x4(&av)[U][RT], int p, const uint8_t* ws) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int at = min(p + u, end - 1) - c0;
+        const uint32_t exists = static_cast<uint32_t>((p + u - end) >> 31);   // all ones or none
         int sa[RT];
 #pragma unroll
-        for (int i = 0; i < RT; ++i) sa[i] = WT == kMx4 ? ws[128 * u + 64 * i] & ((p + u - end) >> 31) : 0;
+        for (int i = 0; i < RT; ++i) sa[i] = WT == kMx4 ? ws[128 * u + 64 * i] & exists : 0;
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
           u32x4 bv[BL];
           int sb = 0;
 #pragma unroll
-          for (int j = 0; j < BL; ++j)
+          for (int j = 0; j < BL; ++j) {
             bv[j] = *reinterpret_cast<const u32x4*>(cols + (((at * BL + j) << cols_log2) + 8 * b) * 128);
+            if constexpr (WT != kMx4) bv[j] &= exists;
+          }
           if constexpr (WT == kMx4) sb = scales[8 * b * chunk * 8 + at * 8];
 #pragma unroll
           for (int i = 0; i < RT; ++i) few_mma<WT, BL>(av[u][i], sa[i], bv, sb, acc[i][b]);
