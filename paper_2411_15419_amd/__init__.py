@@ -369,6 +369,10 @@ def luffy_mx4_expert_ffn(x, row_index, rep_offsets, w1q, w1s, w2q, w2s, act, max
         raise LuffyError("luffy_mx4_expert_ffn: x and y_rep must be bf16 rows of d values")
     if y_rep.shape[0] < max_rows or (row_index is None and x.shape[0] < max_rows) or rep_offsets.numel() != E + 1:
         raise LuffyError("luffy_mx4_expert_ffn: x, y_rep and rep_offsets do not fit max_rows and E")
+    if rep_offsets.dtype != torch.int32:
+        raise LuffyError("luffy_mx4_expert_ffn: rep_offsets must be int32 [E + 1]")
+    if row_index is not None and (row_index.dtype != torch.int32 or row_index.numel() < max_rows):
+        raise LuffyError("luffy_mx4_expert_ffn: row_index must be int32 [max_rows]")
     _check(load_library().luffy_mx4_expert_ffn(
         _p(x), _p(row_index), _p(rep_offsets), E, d, d_ff, _p(w1q), _p(w1s), _p(w2q), _p(w2s),
         _ACTS[act] if isinstance(act, str) else int(act), int(max_rows), _p(y_rep), _p(workspace), workspace.numel(),
