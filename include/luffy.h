@@ -435,9 +435,10 @@ int luffy_mx4_expert_ffn(const void* x, const int32_t* row_index, const int32_t*
  * parts (bf16: 16 bits of mantissa) or as three E4M3 parts (4-bit weights: 12
  * bits, relative to the value), and act has a relative error of a few
  * 2^-24 (1 + z^2).  x, w_gate, w1, w2 and y must be 16-byte
- * aligned; d and d_ff multiples of 64, at most 32768; one expert's w1 at most
- * 4 GiB - 64 KiB.  A token's output depends on its own row only, up to the
- * order of its sums: K is split by the number of tokens and of experts.
+ * aligned, scales 8-byte; d and d_ff multiples of 64, at most 32768; one
+ * expert's w1 at most 4 GiB - 64 KiB.  A token's output depends on its own row
+ * only, up to the order of its sums: K is split by the number of tokens and of
+ * experts.
  * ---------------------------------------------------------------------- */
 #define LUFFY_FEW_MAX_TOKENS 64
 size_t luffy_moe_few_workspace_size(int T, int d, int E, int k, int d_ff);

@@ -1138,6 +1138,9 @@ extern "C" int luffy_moe_few(const void* x, int T, int d, int dtype, const void*
     return fail(LUFFY_E_UNSUPPORTED, "luffy_moe_few: d=%d d_ff=%d must be multiples of 64 and at most 32768", d, d_ff);
   if (few_misaligned(x) || few_misaligned(w_gate) || few_misaligned(w1) || few_misaligned(w2) || few_misaligned(y))
     return fail(LUFFY_E_INVALID, "luffy_moe_few: x, w_gate, w1, w2 and y must be 16-byte aligned");
+  if (weight_type == LUFFY_MX4 &&
+      ((reinterpret_cast<uintptr_t>(w1_scale) | reinterpret_cast<uintptr_t>(w2_scale)) & 7u) != 0)
+    return fail(LUFFY_E_INVALID, "luffy_moe_few: scales must be 8-byte aligned");
   if (weight_type != LUFFY_MX4 && static_cast<long long>(d) * d_ff * elem_bytes(dtype) > 0xFFFF0000ll)
     return fail(LUFFY_E_UNSUPPORTED, "luffy_moe_few: one expert's weights exceed 4 GiB - 64 KiB");
   const size_t need = luffy_moe_few_workspace_size(T, d, E, k, d_ff);

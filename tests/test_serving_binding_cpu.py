@@ -38,3 +38,18 @@ def test_expert_ffn_takes_32_bit_offsets_and_indices():
         L.luffy_mx4_expert_ffn(**dict(good, row_index=good["row_index"].long()))
     with pytest.raises(L.LuffyError, match="row_index must be int32"):
         L.luffy_mx4_expert_ffn(**dict(good, row_index=torch.zeros(3, dtype=torch.int32)))
+
+
+def test_moe_few_refuses_misaligned_scales(lib):
+    """Scales at an odd byte; 8-byte alignment is enough (the call then stops at
+    its workspace, one byte short)."""
+    import ctypes
+    fake, eight, byte = ctypes.c_void_p(256), ctypes.c_void_p(264), ctypes.c_void_p(257)
+    need = lib.luffy_moe_few_workspace_size(4, 64, 4, 2, 128)
+
+    def call(s1, s2):
+        return lib.luffy_moe_few(fake, 4, 64, 1, fake, None, 4, 2, fake, s1, fake, s2, 2, 128, 0, fake, fake, fake,
+                                 fake, need - 1, None)
+    assert call(byte, fake) == -1 and b"aligned" in lib.luffy_last_error()
+    assert call(fake, byte) == -1 and b"aligned" in lib.luffy_last_error()
+    assert call(eight, eight) == -3
