@@ -349,6 +349,8 @@ struct FewLds {
   static constexpr int HALF = (NBMAX == 1 ? 24 : 48) * 1024;      // one chunk's columns
   static constexpr int SCALES = NBMAX == 1 ? 1024 : 2048;         // and their scale bytes (8 a piece and column)
   static constexpr int RED = NBMAX * 8 * kFewWaves * RT * 8 * 4;  // the waves' sums
+  // float32 and bf16: the scales' place holds zeros for a piece of every column
+  static constexpr int ZEROS_AT = 2 * HALF, ZEROS = NBMAX * 8 * 128 * 2;
   __attribute__((aligned(16))) uint8_t cols[2 * HALF];
   __attribute__((aligned(16))) uint8_t scales[2 * SCALES];
   __attribute__((aligned(16))) uint8_t wscale[kFewWaves][2][1024];   // 4-bit weights: each wave's scales
@@ -382,6 +384,12 @@ constexpr bool few_fits() {
   return few_chunk<kF32, true, NBMAX, 2>(0, COLS_LOG2) >= 1 && few_chunk<kBf16, true, NBMAX, 2>(0, COLS_LOG2) >= 1 &&
          few_chunk<kMx4, false, NBMAX, 2>(0, COLS_LOG2) >= 1 && few_chunk<kMx4, true, NBMAX, 2>(0, COLS_LOG2) >= 1;
 }
+using FewLdsOne = FewLds<1, 2>;
+using FewLdsMore = FewLds<8, 2>;
+static_assert(offsetof(FewLdsOne, scales) == FewLdsOne::ZEROS_AT && offsetof(FewLdsMore, scales) == FewLdsMore::ZEROS_AT &&
+                  FewLdsOne::ZEROS_AT + FewLdsOne::ZEROS <= offsetof(FewLdsOne, red) &&
+                  FewLdsMore::ZEROS_AT + FewLdsMore::ZEROS <= offsetof(FewLdsMore, red),
+              "zeros in the scales' place");
 static_assert(few_fits<1, 3>() && few_fits<8, 6>(), "a piece of every column in LDS");
 static_assert(sizeof(FewLds<8, 2>) <= 160 * 1024 && 2 * sizeof(FewLds<1, 2>) <= 160 * 1024, "LDS");
 
@@ -615,30 +623,28 @@ __device__ __forceinline__ void few_run(const FewArgs& a, FewLds<NBMAX, RT>& m, 
     const bool on = c0 + chunk < len;   // this wave has pieces in the next chunk
     // this lane's column in each group, and where its lines start
     const int lcol = lr & ((1 << cols_log2) - 1);
-    const uint8_t* cols = m.cols + st.half * S::HALF + part * few_part_bytes<NBMAX, RT>(split_log2) + lcol * 128 +
-                          16 * (lc ^ (lcol & 7));
+    const uint8_t* cols = reinterpret_cast<const uint8_t*>(&m) + lcol * 128 + 16 * (lc ^ (lcol & 7));
+    const int cols_at = st.half * S::HALF + part * few_part_bytes<NBMAX, RT>(split_log2);
     const uint8_t* scales = m.scales + st.half * S::SCALES + ((part << cols_log2) + lcol) * chunk * 8 + lc;
-    // Pieces past the end are zeros, multiplied with the last piece's columns as
-    // zeros (an infinity there must not meet a zero; 4-bit weights: a column's
-    // block without numbers has made its result NaN already): without branches
-    // the compiler knows how many loads are in flight.
+    // Pieces past the end are zeros, multiplied with zero columns (an infinity must
+    // not meet a zero; 4-bit weights: with the last piece's columns under a zero
+    // scale, where a block without numbers has made the result NaN already):
+    // without branches the compiler knows how many loads are in flight.
     auto multiply = [&](const u32x4(&av)[U][RT], int p, const uint8_t* ws) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int at = min(p + u, end - 1) - c0;
-        const uint32_t exists = static_cast<uint32_t>((p + u - end) >> 31);   // all ones or none
+        const int line = WT == kMx4 || p + u < end ? cols_at + ((at * BL) << cols_log2) * 128 : S::ZEROS_AT;
         int sa[RT];
 #pragma unroll
-        for (int i = 0; i < RT; ++i) sa[i] = WT == kMx4 ? ws[128 * u + 64 * i] & exists : 0;
+        for (int i = 0; i < RT; ++i) sa[i] = WT == kMx4 ? ws[128 * u + 64 * i] & ((p + u - end) >> 31) : 0;
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
           u32x4 bv[BL];
           int sb = 0;
 #pragma unroll
-          for (int j = 0; j < BL; ++j) {
-            bv[j] = *reinterpret_cast<const u32x4*>(cols + (((at * BL + j) << cols_log2) + 8 * b) * 128);
-            if constexpr (WT != kMx4) bv[j] &= exists;
-          }
+          for (int j = 0; j < BL; ++j)
+            bv[j] = *reinterpret_cast<const u32x4*>(cols + line + ((j << cols_log2) + 8 * b) * 128);
           if constexpr (WT == kMx4) sb = scales[8 * b * chunk * 8 + at * 8];
 #pragma unroll
           for (int i = 0; i < RT; ++i) few_mma<WT, BL>(av[u][i], sa[i], bv, sb, acc[i][b]);
@@ -731,6 +737,11 @@ __global__ __launch_bounds__(kFewThreads, NBMAX == 1 ? 4 : 2) void few_product_k
   constexpr int U = 8 / RT;
   const int rows = RT * 8 * (kFewWaves >> __builtin_ctz(a.split));
   if (threadIdx.x < 64) few_lists(a.topk_idx, a.T * a.k, m.l);
+  if constexpr (WT != kMx4) {
+    using S = FewLds<NBMAX, RT>;
+    for (int i = threadIdx.x * 16; i < S::ZEROS; i += kFewThreads * 16)
+      *reinterpret_cast<u32x4*>(reinterpret_cast<uint8_t*>(&m) + S::ZEROS_AT + i) = u32x4{0, 0, 0, 0};
+  }
   __syncthreads();
   // contiguous items a block, neighbouring blocks of an XCD on neighbouring items
   const int used = __builtin_amdgcn_readfirstlane(m.l.used);
