@@ -16,6 +16,15 @@
 
 namespace luffy {
 
+// Keeps the loads before it (plain ones and DMA to LDS) before those after it.  A
+// counted wait (all but the n newest loads of this wave have landed) is right
+// only for the order it was counted on, and to the compiler plain loads and DMA
+// to LDS are independent.
+__device__ __forceinline__ void load_order() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(1);   // arithmetic may cross
+}
+
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 template <int STEP>
@@ -244,8 +253,10 @@ struct Mx4Core {
     if constexpr (FROM == 0) setup(t, s);
     const int nk = __builtin_amdgcn_readfirstlane((t.kbytes + 127) / 128);
 #pragma unroll
-    for (int k = FROM; k < TO; ++k)
+    for (int k = FROM; k < TO; ++k) {
       if (k < nk) issue(t, s, k, lds + k * STAGE_BYTES);
+      load_order();
+    }
   }
 
   // The product of a tile whose first stages are on their way; the wave
