@@ -22,6 +22,7 @@ constexpr int kFewTokens = LUFFY_FEW_MAX_TOKENS;
 constexpr int kGateThreads = 1024;
 constexpr int kFewWaves = 8, kFewThreads = 64 * kFewWaves;
 constexpr int kDirectSlots = 8;   // few_direct_kernel's most
+constexpr int kTiles = 2;         // few_product_kernel: tiles of eight rows that a wave has
 
 enum FewWeights { kF32 = 0, kBf16 = 1, kMx4 = 2 };
 
@@ -344,11 +345,11 @@ __device__ __forceinline__ void lds_barrier() {
 // LDS of a block.  Columns come in chunks of K, double-buffered; NBMAX: groups
 // of eight columns that an item may have (an expert has at most T).  With one
 // group the registers allow two blocks a CU, with more one.
-template <int NBMAX, int RT>
+template <int NBMAX>
 struct FewLds {
   static constexpr int HALF = (NBMAX == 1 ? 24 : 48) * 1024;      // one chunk's columns
   static constexpr int SCALES = NBMAX == 1 ? 1024 : 2048;         // and their scale bytes (8 a piece and column)
-  static constexpr int RED = NBMAX * 8 * kFewWaves * RT * 8 * 4;  // the waves' sums
+  static constexpr int RED = NBMAX * 8 * kFewWaves * kTiles * 8 * 4;  // the waves' sums
   // float32 and bf16: the scales' place holds zeros for a piece of every column
   static constexpr int ZEROS_AT = 2 * HALF, ZEROS = NBMAX * 8 * 128 * 2;
   __attribute__((aligned(16))) uint8_t cols[2 * HALF];
@@ -367,35 +368,35 @@ __host__ __device__ constexpr int few_cols_log2(int n) {
 }
 // A half's bytes for each part of K (whole DMA instructions), and the pieces of
 // a part in a chunk.
-template <int NBMAX, int RT>
+template <int NBMAX>
 __host__ __device__ constexpr int few_part_bytes(int split_log2) {
-  return (FewLds<NBMAX, RT>::HALF >> split_log2) & ~1023;
+  return (FewLds<NBMAX>::HALF >> split_log2) & ~1023;
 }
-template <int WT, bool SECOND, int NBMAX, int RT>
+template <int WT, bool SECOND, int NBMAX>
 __host__ __device__ constexpr int few_chunk(int split_log2, int cols_log2) {
-  const int fit = few_part_bytes<NBMAX, RT>(split_log2) / (128 * FewLayout<WT, SECOND>::BL) >> cols_log2;
-  const int scales = FewLds<NBMAX, RT>::SCALES / 8 >> (split_log2 + cols_log2);
+  const int fit = few_part_bytes<NBMAX>(split_log2) / (128 * FewLayout<WT, SECOND>::BL) >> cols_log2;
+  const int scales = FewLds<NBMAX>::SCALES / 8 >> (split_log2 + cols_log2);
   return WT == kMx4 && scales < fit ? scales : fit;
 }
 // With K in one part every number of columns fits (the loops over chunks would
 // not advance otherwise).
 template <int NBMAX, int COLS_LOG2>
 constexpr bool few_fits() {
-  return few_chunk<kF32, true, NBMAX, 2>(0, COLS_LOG2) >= 1 && few_chunk<kBf16, true, NBMAX, 2>(0, COLS_LOG2) >= 1 &&
-         few_chunk<kMx4, false, NBMAX, 2>(0, COLS_LOG2) >= 1 && few_chunk<kMx4, true, NBMAX, 2>(0, COLS_LOG2) >= 1;
+  return few_chunk<kF32, true, NBMAX>(0, COLS_LOG2) >= 1 && few_chunk<kBf16, true, NBMAX>(0, COLS_LOG2) >= 1 &&
+         few_chunk<kMx4, false, NBMAX>(0, COLS_LOG2) >= 1 && few_chunk<kMx4, true, NBMAX>(0, COLS_LOG2) >= 1;
 }
-using FewLdsOne = FewLds<1, 2>;
-using FewLdsMore = FewLds<8, 2>;
+using FewLdsOne = FewLds<1>;
+using FewLdsMore = FewLds<8>;
 static_assert(offsetof(FewLdsOne, scales) == FewLdsOne::ZEROS_AT && offsetof(FewLdsMore, scales) == FewLdsMore::ZEROS_AT &&
                   FewLdsOne::ZEROS_AT + FewLdsOne::ZEROS <= offsetof(FewLdsOne, red) &&
                   FewLdsMore::ZEROS_AT + FewLdsMore::ZEROS <= offsetof(FewLdsMore, red),
               "zeros in the scales' place");
 static_assert(few_fits<1, 3>() && few_fits<8, 6>(), "a piece of every column in LDS");
-static_assert(sizeof(FewLds<8, 2>) <= 160 * 1024 && 2 * sizeof(FewLds<1, 2>) <= 160 * 1024, "LDS");
+static_assert(sizeof(FewLds<8>) <= 160 * 1024 && 2 * sizeof(FewLds<1>) <= 160 * 1024, "LDS");
 
 // A block's waves are arranged as `split` parts of K by 8 / split row groups of
-// RT * 8 rows; a work item is the RT * 64 / split rows of one expert that the
-// block takes at a time, times all of that expert's columns.
+// 16 rows (kTiles tiles); a work item is the 128 / split rows of one expert that
+// the block takes at a time, times all of that expert's columns.
 struct FewItem {
   const uint8_t *w, *s;          // the expert's weights and scales
   uint32_t row;                  // this wave's first row
@@ -417,7 +418,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t few_rsrc(const uint8_t* base) 
                                            static_cast<int>(kFewRange), 0x00020000);
 }
 
-template <int WT, int RT, int NBMAX, bool SECOND>
+template <int WT, int NBMAX, bool SECOND>
 __device__ __forceinline__ FewItem few_item(const FewArgs& a, const FewLists& l, int item) {
   FewItem t;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -432,24 +433,24 @@ __device__ __forceinline__ FewItem few_item(const FewArgs& a, const FewLists& l,
   t.n = __builtin_amdgcn_readfirstlane(l.first[t.rank + 1]) - t.first;
   const int kbytes = few_kbytes<WT>(a.K), pieces = (kbytes + 127) / 128, split_log2 = __builtin_ctz(a.split);
   const int part = w & (a.split - 1);
-  t.row = (t.group * (kFewWaves >> split_log2) + (w >> split_log2)) * (8 * RT);
+  t.row = (t.group * (kFewWaves >> split_log2) + (w >> split_log2)) * (8 * kTiles);
   const bool rows = static_cast<int>(t.row) < a.N;
   t.p0 = rows ? (part * pieces) >> split_log2 : 0;
   t.p1 = rows ? ((part + 1) * pieces) >> split_log2 : 0;
-  t.c1 = min(t.p1, t.p0 + few_chunk<WT, SECOND, NBMAX, RT>(split_log2, few_cols_log2(t.n)));
+  t.c1 = min(t.p1, t.p0 + few_chunk<WT, SECOND, NBMAX>(split_log2, few_cols_log2(t.n)));
   t.w = a.w + static_cast<size_t>(e) * a.N * kbytes;
   t.s = WT == kMx4 ? a.w_scale + static_cast<size_t>(e) * pieces * a.N * 8 : nullptr;
   return t;
 }
 
-// U pieces of the wave's RT row tiles, from piece p on.  The loads are issued
+// U pieces of the wave's kTiles row tiles, from piece p on.  The loads are issued
 // whatever p is, and those at or past p1 fetch nothing (their offset is out of
 // the buffer's range; 4-bit: nor do chunks past the row's end) and give zeros:
 // a load behind a branch would leave the number of loads in flight open, and
 // every use of an earlier one would wait for all.
-template <int WT, int RT, int U>
+template <int WT, int U>
 __device__ __forceinline__ void few_load(const FewArgs& a, const uint8_t* w, uint32_t row, int p, int p1,
-                                         u32x4 (&av)[U][RT]) {
+                                         u32x4 (&av)[U][kTiles]) {
   constexpr int kStream = 2;   // non-temporal: read once
   const int kbytes = few_kbytes<WT>(a.K), lane = threadIdx.x & 63, r = lane & 7, c = lane >> 3;
   const uint32_t off = static_cast<uint32_t>(r) * kbytes + 16 * c;
@@ -460,7 +461,7 @@ __device__ __forceinline__ void few_load(const FewArgs& a, const uint8_t* w, uin
     uint32_t o = off | (~in & kFewRange);
     if constexpr (WT == kMx4) o = (p + u) * 128 + 16 * c < kbytes ? o : kFewRange;
 #pragma unroll
-    for (int i = 0; i < RT; ++i)
+    for (int i = 0; i < kTiles; ++i)
       av[u][i] = __builtin_amdgcn_raw_buffer_load_b128(wr, o, ((row + 8 * i) * kbytes + (p + u) * 128) & in, kStream);
   }
 }
@@ -468,10 +469,9 @@ __device__ __forceinline__ void few_load(const FewArgs& a, const uint8_t* w, uin
 // The scale bytes of the wave's 16 rows in eight pieces from piece p on, 128
 // bytes a piece, into the wave's own LDS: one instruction in place of sixteen
 // byte loads beside the weights' sixteen (pieces at or past p1: not fetched).
-template <int RT>
 __device__ __forceinline__ void few_load_scales(const FewArgs& a, const uint8_t* s, uint32_t row, int p, int p1,
                                                 __attribute__((address_space(3))) uint8_t* dst) {
-  static_assert(RT == 2, "16 rows of 8 bytes, a lane quarter of 8 lanes each 16 bytes");
+  static_assert(kTiles == 2, "16 rows of 8 bytes, a lane quarter of 8 lanes each 16 bytes");
   const int lane = threadIdx.x & 63, u = lane >> 3;
   const uint32_t off = (static_cast<uint32_t>(u) * a.N + 2 * (lane & 7)) * 8;
   lds_dma<16>(few_rsrc(s), p + u < p1 ? off : kFewRange, p < p1 ? (p * a.N + row) * 8 : 0, dst);
@@ -525,20 +525,20 @@ struct FewStage {
 // the products' reads (eight columns, one eighth) fall on distinct banks.  A
 // DMA instruction fills eight lines.  Lines past the part's end are not
 // fetched; nothing reads them.  The scale bytes of a column's chunk are one run.
-template <int WT, int RT, int NB, int NBMAX, bool SECOND>
-__device__ __forceinline__ void few_stage(const FewArgs& a, FewLds<NBMAX, RT>& m, const FewItem& t, int c0, int half) {
-  using S = FewLds<NBMAX, RT>;
+template <int WT, int NB, int NBMAX, bool SECOND>
+__device__ __forceinline__ void few_stage(const FewArgs& a, FewLds<NBMAX>& m, const FewItem& t, int c0, int half) {
+  using S = FewLds<NBMAX>;
   using lds_ptr = __attribute__((address_space(3))) uint8_t*;
   constexpr int BL = FewLayout<WT, SECOND>::BL;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int pieces = (few_kbytes<WT>(a.K) + 127) / 128, pitch = few_pitch<WT, SECOND>(a.K);
   const int split_log2 = __builtin_ctz(a.split), cols_log2 = few_cols_log2(NB > 1 ? 8 * NB : t.n);
-  const int chunk = few_chunk<WT, SECOND, NBMAX, RT>(split_log2, cols_log2);
+  const int chunk = few_chunk<WT, SECOND, NBMAX>(split_log2, cols_log2);
   const __amdgpu_buffer_rsrc_t in = few_rsrc(a.in);   // (a step's columns are far below 4 GiB)
   // this wave's part of K, one of the 8 / split waves that have it
   const int kp = w & (a.split - 1), first = ((kp * pieces) >> split_log2) + c0;
   const int len = min(chunk, (((kp + 1) * pieces) >> split_log2) - first), lines = len * BL << cols_log2;
-  const lds_ptr cols = (lds_ptr)m.cols + half * S::HALF + kp * few_part_bytes<NBMAX, RT>(split_log2);
+  const lds_ptr cols = (lds_ptr)m.cols + half * S::HALF + kp * few_part_bytes<NBMAX>(split_log2);
   const int line = lane >> 3;
   uint32_t off[NB];
 #pragma unroll
@@ -571,34 +571,34 @@ __device__ __forceinline__ void few_stage(const FewArgs& a, FewLds<NBMAX, RT>& m
 }
 
 // Stages the first chunk of an item.
-template <int WT, int RT, int NBMAX, bool SECOND>
-__device__ __forceinline__ void few_stage_first(const FewArgs& a, FewLds<NBMAX, RT>& m, const FewItem& t,
+template <int WT, int NBMAX, bool SECOND>
+__device__ __forceinline__ void few_stage_first(const FewArgs& a, FewLds<NBMAX>& m, const FewItem& t,
                                                 int half) {
-  if (NBMAX == 1 || t.n <= 8) few_stage<WT, RT, 1, NBMAX, SECOND>(a, m, t, 0, half);
-  else if (t.n <= 16) few_stage<WT, RT, (NBMAX > 1 ? 2 : 1), NBMAX, SECOND>(a, m, t, 0, half);
-  else if (t.n <= 32) few_stage<WT, RT, (NBMAX > 1 ? 4 : 1), NBMAX, SECOND>(a, m, t, 0, half);
-  else few_stage<WT, RT, (NBMAX > 1 ? 8 : 1), NBMAX, SECOND>(a, m, t, 0, half);
+  if (NBMAX == 1 || t.n <= 8) few_stage<WT, 1, NBMAX, SECOND>(a, m, t, 0, half);
+  else if (t.n <= 16) few_stage<WT, (NBMAX > 1 ? 2 : 1), NBMAX, SECOND>(a, m, t, 0, half);
+  else if (t.n <= 32) few_stage<WT, (NBMAX > 1 ? 4 : 1), NBMAX, SECOND>(a, m, t, 0, half);
+  else few_stage<WT, (NBMAX > 1 ? 8 : 1), NBMAX, SECOND>(a, m, t, 0, half);
 }
 
 // One work item with NB groups of eight columns.  av holds the item's first
 // pieces on entry and the next item's (`next`, if any) on return, and its first
 // columns are on their way to LDS, so that the weight stream does not stop
 // while an item's sums are added and stored.
-template <int WT, int RT, int NB, int NBMAX, bool SECOND>
-__device__ __forceinline__ void few_run(const FewArgs& a, FewLds<NBMAX, RT>& m, const FewItem& t,
+template <int WT, int NB, int NBMAX, bool SECOND>
+__device__ __forceinline__ void few_run(const FewArgs& a, FewLds<NBMAX>& m, const FewItem& t,
                                         const FewItem& next, bool more, int act, FewStage& st,
-                                        u32x4 (&av)[8 / RT][RT]) {
+                                        u32x4 (&av)[8 / kTiles][kTiles]) {
   using L = FewLayout<WT, SECOND>;
-  using S = FewLds<NBMAX, RT>;
-  constexpr int U = 8 / RT, BL = L::BL;
+  using S = FewLds<NBMAX>;
+  constexpr int U = 8 / kTiles, BL = L::BL;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int part = w & (a.split - 1), pieces = (few_kbytes<WT>(a.K) + 127) / 128;
   const int split_log2 = __builtin_ctz(a.split), cols_log2 = few_cols_log2(NB > 1 ? 8 * NB : t.n);
-  const int chunk = few_chunk<WT, SECOND, NBMAX, RT>(split_log2, cols_log2);
+  const int chunk = few_chunk<WT, SECOND, NBMAX>(split_log2, cols_log2);
   const int span = (pieces + a.split - 1) >> __builtin_ctz(a.split);   // the longest part
-  f32x4 acc[RT][NB];
+  f32x4 acc[kTiles][NB];
 #pragma unroll
-  for (int i = 0; i < RT; ++i)
+  for (int i = 0; i < kTiles; ++i)
 #pragma unroll
     for (int b = 0; b < NB; ++b) acc[i][b] = f32x4{0.f, 0.f, 0.f, 0.f};
   using lds_ptr = __attribute__((address_space(3))) uint8_t*;
@@ -609,16 +609,16 @@ __device__ __forceinline__ void few_run(const FewArgs& a, FewLds<NBMAX, RT>& m, 
       // this wave's columns have landed (all but its newest loads, a step of
       // weights); then every wave's, and every wave is done with the other half
       load_order();
-      if (st.behind) wait_vmcnt<U * RT>();
+      if (st.behind) wait_vmcnt<U * kTiles>();
       else wait_vmcnt<0>();
       lds_barrier();
       st.whole = span <= chunk ? t.rank : -1;
     }
     st.behind = false;
     if (c0 + chunk < span) {
-      few_stage<WT, RT, NB, NBMAX, SECOND>(a, m, t, c0 + chunk, st.half ^ 1);
+      few_stage<WT, NB, NBMAX, SECOND>(a, m, t, c0 + chunk, st.half ^ 1);
     } else if (more && st.whole != next.rank) {
-      few_stage_first<WT, RT, NBMAX, SECOND>(a, m, next, st.half ^ 1);
+      few_stage_first<WT, NBMAX, SECOND>(a, m, next, st.half ^ 1);
     }
     // Steps of U pieces in pairs, the registers of one loaded while the other's
     // are multiplied; an odd number is filled up with a step that loads nothing.
@@ -627,20 +627,20 @@ __device__ __forceinline__ void few_run(const FewArgs& a, FewLds<NBMAX, RT>& m, 
     // this lane's column in each group, and where its lines start
     const int lcol = lr & ((1 << cols_log2) - 1);
     const uint8_t* cols = reinterpret_cast<const uint8_t*>(&m) + lcol * 128 + 16 * (lc ^ (lcol & 7));
-    const int cols_at = st.half * S::HALF + part * few_part_bytes<NBMAX, RT>(split_log2);
+    const int cols_at = st.half * S::HALF + part * few_part_bytes<NBMAX>(split_log2);
     const uint8_t* scales = m.scales + st.half * S::SCALES + ((part << cols_log2) + lcol) * chunk * 8 + lc;
     // Pieces past the end are zeros, multiplied with zero columns (an infinity must
     // not meet a zero; 4-bit weights: with the last piece's columns under a zero
     // scale, where a block without numbers has made the result NaN already):
     // without branches the compiler knows how many loads are in flight.
-    auto multiply = [&](const u32x4(&av)[U][RT], int p, const uint8_t* ws) {
+    auto multiply = [&](const u32x4(&av)[U][kTiles], int p, const uint8_t* ws) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int at = min(p + u, end - 1) - c0;
         const int line = WT == kMx4 || p + u < end ? cols_at + ((at * BL) << cols_log2) * 128 : S::ZEROS_AT;
-        int sa[RT];
+        int sa[kTiles];
 #pragma unroll
-        for (int i = 0; i < RT; ++i) sa[i] = WT == kMx4 ? ws[128 * u + 64 * i] & ((p + u - end) >> 31) : 0;
+        for (int i = 0; i < kTiles; ++i) sa[i] = WT == kMx4 ? ws[128 * u + 64 * i] & ((p + u - end) >> 31) : 0;
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
           u32x4 bv[BL];
@@ -650,7 +650,7 @@ __device__ __forceinline__ void few_run(const FewArgs& a, FewLds<NBMAX, RT>& m, 
             bv[j] = *reinterpret_cast<const u32x4*>(cols + line + ((j << cols_log2) + 8 * b) * 128);
           if constexpr (WT == kMx4) sb = scales[8 * b * chunk * 8 + at * 8];
 #pragma unroll
-          for (int i = 0; i < RT; ++i) few_mma<WT, BL>(av[u][i], sa[i], bv, sb, acc[i][b]);
+          for (int i = 0; i < kTiles; ++i) few_mma<WT, BL>(av[u][i], sa[i], bv, sb, acc[i][b]);
         }
       }
     };
@@ -668,16 +668,16 @@ __device__ __forceinline__ void few_run(const FewArgs& a, FewLds<NBMAX, RT>& m, 
       const uint8_t* ws = m.wscale[w][st.slot] + lane_scale;
       if constexpr (WT == kMx4) {
         load_order();
-        wait_vmcnt<U * RT>();   // this pair's scales (older than the step of weights in flight) have landed
+        wait_vmcnt<U * kTiles>();   // this pair's scales (older than the step of weights in flight) have landed
         load_order();
-        few_load_scales<RT>(a, mine ? t.s : next.s, row, q, q1, (lds_ptr)m.wscale[w][st.slot ^ 1]);
+        few_load_scales(a, mine ? t.s : next.s, row, q, q1, (lds_ptr)m.wscale[w][st.slot ^ 1]);
         st.slot ^= 1;
       }
-      u32x4 bv[U][RT];
-      few_load<WT, RT, U>(a, t.w, t.row, t.p0 + p + U, t.p0 + end, bv);
+      u32x4 bv[U][kTiles];
+      few_load<WT, U>(a, t.w, t.row, t.p0 + p + U, t.p0 + end, bv);
       if constexpr (kAhead) load_order();
       multiply(av, p, ws);
-      few_load<WT, RT, U>(a, mine ? t.w : next.w, row, q, q1, av);
+      few_load<WT, U>(a, mine ? t.w : next.w, row, q, q1, av);
       if constexpr (kAhead) load_order();
       multiply(bv, p + U, ws + 128 * U);
       st.behind = true;
@@ -689,24 +689,24 @@ __device__ __forceinline__ void few_run(const FewArgs& a, FewLds<NBMAX, RT>& m, 
   if (t.p1 == t.p0) {
     if constexpr (WT == kMx4) {
       st.slot ^= 1;
-      few_load_scales<RT>(a, next.s, next.row, next.p0, more ? next.c1 : 0, (lds_ptr)m.wscale[w][st.slot]);
+      few_load_scales(a, next.s, next.row, next.p0, more ? next.c1 : 0, (lds_ptr)m.wscale[w][st.slot]);
     }
-    few_load<WT, RT, U>(a, next.w, next.row, next.p0, more ? next.c1 : 0, av);
+    few_load<WT, U>(a, next.w, next.row, next.p0, more ? next.c1 : 0, av);
     st.behind = true;
   }
   // D[r][c] (lanes 0-7 and 16-23) + D[r + 8][c + 8] (40 lanes further) of every
   // wave, then the parts of K in order
-  const int rows = RT * 8 * (kFewWaves >> __builtin_ctz(a.split));
+  const int rows = kTiles * 8 * (kFewWaves >> __builtin_ctz(a.split));
   lds_barrier();   // (every wave is done with the previous item's sums)
 #pragma unroll
-  for (int i = 0; i < RT; ++i)
+  for (int i = 0; i < kTiles; ++i)
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
         const float other = __shfl(acc[i][b][v], (lane + 40) & 63, 64);
         if ((lane & 8) == 0 && lane < 32)
-          m.red[((part * NB + b) * 8 + lr) * rows + (w >> __builtin_ctz(a.split)) * (8 * RT) + 8 * i + 4 * (lane >> 4) + v] =
+          m.red[((part * NB + b) * 8 + lr) * rows + (w >> __builtin_ctz(a.split)) * (8 * kTiles) + 8 * i + 4 * (lane >> 4) + v] =
               acc[i][b][v] + other;
       }
   lds_barrier();
@@ -741,14 +741,14 @@ __device__ __forceinline__ void few_run(const FewArgs& a, FewLds<NBMAX, RT>& m, 
 // items.  Bound by the stream of weights: 64 tokens on 8 experts of 4096 x 11008
 // (bf16, 0.72 GB a product) 135 us, 5.3 TB/s, and 152 us, 4.7 TB/s; 32 tokens on
 // 32 experts of 2048 x 8192 (4 bits, 0.25 GB) 55 and 60 us, 4.5 and 4.2 TB/s.
-template <int WT, int RT, int NBMAX, bool SECOND>
+template <int WT, int NBMAX, bool SECOND>
 __global__ __launch_bounds__(kFewThreads, NBMAX == 1 ? 4 : 2) void few_product_kernel(const FewArgs a, int act) {
-  __shared__ FewLds<NBMAX, RT> m;
-  constexpr int U = 8 / RT;
-  const int rows = RT * 8 * (kFewWaves >> __builtin_ctz(a.split));
+  __shared__ FewLds<NBMAX> m;
+  constexpr int U = 8 / kTiles;
+  const int rows = kTiles * 8 * (kFewWaves >> __builtin_ctz(a.split));
   if (threadIdx.x < 64) few_lists(a.topk_idx, a.T * a.k, m.l);
   if constexpr (WT != kMx4) {
-    using S = FewLds<NBMAX, RT>;
+    using S = FewLds<NBMAX>;
     for (int i = threadIdx.x * 16; i < S::ZEROS; i += kFewThreads * 16)
       *reinterpret_cast<u32x4*>(reinterpret_cast<uint8_t*>(&m) + S::ZEROS_AT + i) = u32x4{0, 0, 0, 0};
   }
@@ -762,25 +762,25 @@ __global__ __launch_bounds__(kFewThreads, NBMAX == 1 ? 4 : 2) void few_product_k
                       ? items
                       : __builtin_amdgcn_readfirstlane(min(items, static_cast<int>(static_cast<float>(vb + 1) * share)));
   if (item >= end) return;
-  u32x4 av[U][RT];
+  u32x4 av[U][kTiles];
   const int begin = item;
-  FewItem t = few_item<WT, RT, NBMAX, SECOND>(a, m.l, item);
+  FewItem t = few_item<WT, NBMAX, SECOND>(a, m.l, item);
   FewStage st = {0, -1, true, 0};
-  few_stage_first<WT, RT, NBMAX, SECOND>(a, m, t, 0);
+  few_stage_first<WT, NBMAX, SECOND>(a, m, t, 0);
   if constexpr (WT == kMx4) {
     using lds_ptr = __attribute__((address_space(3))) uint8_t*;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    few_load_scales<RT>(a, t.s, t.row, t.p0, t.c1, (lds_ptr)m.wscale[w][0]);
+    few_load_scales(a, t.s, t.row, t.p0, t.c1, (lds_ptr)m.wscale[w][0]);
   }
-  few_load<WT, RT, U>(a, t.w, t.row, t.p0, t.c1, av);
+  few_load<WT, U>(a, t.w, t.row, t.p0, t.c1, av);
 #pragma unroll 1
   for (; item < end; ++item) {
     const bool more = item + 1 < end;
-    const FewItem next = few_item<WT, RT, NBMAX, SECOND>(a, m.l, more ? item + 1 : item);
-    if (NBMAX == 1 || t.n <= 8) few_run<WT, RT, 1, NBMAX, SECOND>(a, m, t, next, more, act, st, av);
-    else if (t.n <= 16) few_run<WT, RT, (NBMAX > 1 ? 2 : 1), NBMAX, SECOND>(a, m, t, next, more, act, st, av);
-    else if (t.n <= 32) few_run<WT, RT, (NBMAX > 1 ? 4 : 1), NBMAX, SECOND>(a, m, t, next, more, act, st, av);
-    else few_run<WT, RT, (NBMAX > 1 ? 8 : 1), NBMAX, SECOND>(a, m, t, next, more, act, st, av);
+    const FewItem next = few_item<WT, NBMAX, SECOND>(a, m.l, more ? item + 1 : item);
+    if (NBMAX == 1 || t.n <= 8) few_run<WT, 1, NBMAX, SECOND>(a, m, t, next, more, act, st, av);
+    else if (t.n <= 16) few_run<WT, (NBMAX > 1 ? 2 : 1), NBMAX, SECOND>(a, m, t, next, more, act, st, av);
+    else if (t.n <= 32) few_run<WT, (NBMAX > 1 ? 4 : 1), NBMAX, SECOND>(a, m, t, next, more, act, st, av);
+    else few_run<WT, (NBMAX > 1 ? 8 : 1), NBMAX, SECOND>(a, m, t, next, more, act, st, av);
     t = next;
   }
   if constexpr (SECOND) {
@@ -1033,15 +1033,14 @@ FewWs carve_few(Carver& c, int T, int d, int k, int d_ff) {
 
 template <int WT, int NBMAX, bool SECOND>
 void launch_few_nb(FewArgs a, int act, hipStream_t s) {
-  constexpr int RT = 2;
   // most parts of K whose columns (an expert has at most T) fit the buffer
-  while (a.split > 1 && few_chunk<WT, SECOND, NBMAX, RT>(__builtin_ctz(a.split), few_cols_log2(a.T)) < 1) a.split /= 2;
+  while (a.split > 1 && few_chunk<WT, SECOND, NBMAX>(__builtin_ctz(a.split), few_cols_log2(a.T)) < 1) a.split /= 2;
   const int grid = persistent_grid() * (NBMAX == 1 ? 2 : 1);
-  const int rows = 8 * RT * kFewWaves / a.split;
+  const int rows = 8 * kTiles * kFewWaves / a.split;
   a.groups = (a.N + rows - 1) / rows;
   a.per_group = 1.0f / a.groups;
   a.per_block = 1.0f / grid;
-  launch(SECOND ? "few_ffn2" : "few_ffn1", few_product_kernel<WT, RT, NBMAX, SECOND>, grid, kFewThreads, 0, s, a, act);
+  launch(SECOND ? "few_ffn2" : "few_ffn1", few_product_kernel<WT, NBMAX, SECOND>, grid, kFewThreads, 0, s, a, act);
 }
 
 // Rows of an item.  More rows take their columns to LDS less often; fewer give

@@ -220,11 +220,8 @@ struct Mx4Core {
     __builtin_amdgcn_sched_group_barrier(0x100, NDS, 0);
   }
 
-  // waits until at most n stages of this wave's DMA are outstanding
+  // waits until at most min(n, 1) stages of this wave's DMA are outstanding
   static __device__ __forceinline__ void wait_stages(int n) {
-    if constexpr (STAGES > 3) {
-      if (n >= 2) { wait_vmcnt<2 * LOADS>(); return; }
-    }
     if (n >= 1) wait_vmcnt<LOADS>();
     else wait_vmcnt<0>();
   }
