@@ -428,17 +428,19 @@ int luffy_mx4_expert_ffn(const void* x, const int32_t* row_index, const int32_t*
  *   w1 [E, d_ff, d], w2 [E, d, d_ff] of weight_type: the activations' dtype,
  *   or LUFFY_MX4 with bf16 activations (w1_scale, w2_scale: their scales;
  *   NULL otherwise).  Activations are not rounded to 4 bits here: the step is
- *   bound by reading the weights, and keeps the accuracy.
+ *   bound by reading the weights, and keeps the accuracy (4-bit weights: a token's
+ *   values as two E4M3 parts, exact but for those below 2^-13 of the largest of
+ *   their 32, which are kept to 2^-21 of it).
  *   topk_idx, topk_gate [T, k], y [T, d] dtype.
  * Sums, hidden values and the sum over a token's experts are float32; between
  * the products hidden values are kept as float32 (float32 weights), as two bf16
  * parts (bf16: 16 bits of mantissa) or as three E4M3 parts (4-bit weights: 12
- * bits, relative to the value), and act has a relative error of a few
- * 2^-24 (1 + z^2).  x, w_gate, w1, w2 and y must be 16-byte
- * aligned, scales 8-byte; d and d_ff multiples of 64, at most 32768; one
- * expert's w1 at most 4 GiB - 64 KiB.  A token's output depends on its own row
- * only, up to the order of its sums: K is split by the number of tokens and of
- * experts.
+ * bits relative to the value, or 2^-25 of the largest of its 32; an infinity
+ * makes the token's results NaN).  act has a relative error of a few 2^-24
+ * (1 + z^2).  x, w_gate, w1, w2 and y must be 16-byte aligned, scales 8-byte; d
+ * and d_ff multiples of 64, at most 32768; one expert's w1 at most 4 GiB - 64
+ * KiB.  A token's output depends on its own row only, up to the order of its
+ * sums: K is split by the number of tokens and of experts.
  * ---------------------------------------------------------------------- */
 #define LUFFY_FEW_MAX_TOKENS 64
 size_t luffy_moe_few_workspace_size(int T, int d, int E, int k, int d_ff);

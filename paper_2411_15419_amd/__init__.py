@@ -624,8 +624,8 @@ class ServingLayer(MoELayer):
     """A layer that answers rather than learns.  __call__ runs T tokens (a
     prompt, a batch of prompts) through route, condense, expert FFN and combine;
     step runs up to FEW_MAX_TOKENS tokens (one of every stream being decoded)
-    through luffy_moe_few, where condensation and a capacity would find nothing
-    to do.
+    through luffy_moe_few, where condensation would find nothing to do.  A
+    capacity_factor is for prompts alone: step never drops a token's expert.
 
     microscaled (default): the weights are rounded to microscaled 4 bits here,
     once, and only that form is kept (4.25 bits a weight); activations are bf16.

@@ -739,8 +739,11 @@ __device__ __forceinline__ void few_run(const FewArgs& a, FewLds<NBMAX>& m, cons
 
 // The products of a step: persistent blocks, each with a run of neighbouring
 // items.  Bound by the stream of weights: 64 tokens on 8 experts of 4096 x 11008
-// (bf16, 0.72 GB a product) 135 us, 5.3 TB/s, and 152 us, 4.7 TB/s; 32 tokens on
-// 32 experts of 2048 x 8192 (4 bits, 0.25 GB) 55 and 60 us, 4.5 and 4.2 TB/s.
+// (bf16, 0.72 GB a product) 135 us, 5.3 TB/s, and 151 us, 4.8 TB/s; 32 tokens on
+// 32 experts of 2048 x 8192 (4 bits, 0.25 GB) 56 and 60 us, 4.4 and 4.1 TB/s.  With
+// more columns an expert 4-bit weights are bound by the terms' LDS reads and
+// products, and by chunks of one or a few pieces: 64 tokens on 8 experts of 4096 x
+// 11008 (0.19 GB) 54 and 69 us for k = 1, 129 and 195 us for k = 2.
 template <int WT, int NBMAX, bool SECOND>
 __global__ __launch_bounds__(kFewThreads, NBMAX == 1 ? 4 : 2) void few_product_kernel(const FewArgs a, int act) {
   __shared__ FewLds<NBMAX> m;

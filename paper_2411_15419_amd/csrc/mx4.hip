@@ -147,6 +147,8 @@ enum Mx4Out { kOutF32 = 0, kOutBf16 = 1, kOutMx4Gelu = 2, kOutMx4Silu = 3 };
 using Mx4Large = Mx4Core<256, 256, 2, 4, 2>;
 using Mx4Wide = Mx4Core<128, 128, 2, 2, 2>;
 using Mx4Narrow = Mx4Core<128, 64, 4, 1, 3>;
+// Rows are the caller's bound on them (M, max_rows), which the host knows; the
+// offsets on the device may hold fewer.
 constexpr int kNarrowRows = 64;   // average rows an expert up to which Mx4Narrow runs
 
 // Tile t of the grouped product -> expert, first row, rows, first column: the
@@ -279,11 +281,13 @@ __device__ __forceinline__ void store_mx4(const f32x16& acc, bool valid, size_t 
 }
 
 // y[r] = W_e x_r for the rows of every expert, a block a tile.  16384 x 11008 x
-// 4096 in 385 us, 3840 TFLOP/s: half of what the 4-bit MFMA does alone (7380);
-// MFMA busy 52 % of the cycles, the rest is the first loads and the epilogue of
-// a CU's one block.  The first product of an FFN is bound by its epilogue: about
-// 23 vector instructions a hidden value, two of them transcendental (8653 rows on
-// 32 experts of 2048 x 8192: 170 us; vector units half busy).
+// 4096 in 435 us on average over 30 calls on their own (382 to 498; 380 to 395 a
+// call in longer runs), 3400 TFLOP/s: half of what the 4-bit MFMA does alone
+// (7380); MFMA busy 52 % of the cycles, the rest is the first loads and the
+// epilogue of a CU's one block.  The first product of an FFN is bound by its
+// epilogue: about 25 vector instructions a hidden value, two of them
+// transcendental (8653 rows on 32 experts of 2048 x 8192: 170 us; vector units
+// half busy).
 // Whether a block takes one tile after the other, the next one's first loads
 // under the epilogue: all shapes with two blocks a CU.  (FFN of 8653 rows on 32
 // experts of 2048 x 8192: first product 190 -> 170 us, second 150 -> 134; of 2000
