@@ -67,6 +67,12 @@ typedef enum {
  * GELU is the exact form 0.5 z (1 + erf(z / sqrt 2)); SiLU is z / (1 + e^-z). */
 typedef enum { LUFFY_ACT_GELU = 0, LUFFY_ACT_SILU = 1 } luffy_act;
 
+/* Norms of luffy_block_norm: of the values, or of their deviations from the mean. */
+typedef enum { LUFFY_NORM_RMS = 0, LUFFY_NORM_LAYER = 1 } luffy_norm;
+
+/* Gates of luffy_block_norm: none, float32 [d] for every token, [T, d] dtype. */
+typedef enum { LUFFY_GATE_NONE = 0, LUFFY_GATE_CHANNEL = 1, LUFFY_GATE_TOKEN = 2 } luffy_gate;
+
 int luffy_abi_version(void);
 const char* luffy_status_string(int status);
 const char* luffy_last_error(void);
@@ -355,6 +361,43 @@ int luffy_expert_ffn_backward(const void* x, const int32_t* row_index, const int
                               int act, int max_rows, const void* dy_rep, void* dx_rep,
                               void* dw1, void* dw2, int dw_dtype, void* workspace,
                               size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * luffy_block_norm - the residual stream around a layer: the layer's output
+ * normed, gated and added to the stream, and the norm before the next layer.
+ *   N(a; w, b) = (a - m) / sqrt(mean((a - m)^2) + eps) * w + b  over a row,
+ *   m = mean(a) (LUFFY_NORM_LAYER) or 0 (LUFFY_NORM_RMS)
+ *   o_t = res_scale x_t + g_t * N(y_t; w_post, b_post)
+ *   u_t = N(o_t; w_pre, b_pre), of o_t as it is stored: the same bits as a call
+ *         that is given o alone
+ *   x, y, o, u [T, d] dtype; w_post, b_post, w_pre, b_pre [d] float32
+ *   y, o   both NULL: o_t is x_t and is not written (the norm before a first
+ *          layer); w_post, b_post, gate and res_scale (1) belong to y
+ *   w_post NULL: y_t itself in N's place; b_post, b_pre NULL: zeros
+ *   gate   by gate_kind: none (NULL), float32 [d], or [T, d] dtype
+ *   w_pre, u  both NULL: o alone (behind a last layer)
+ * d a multiple of 64, at most 32768; every pointer 16-byte aligned.  Sums are
+ * float32.  With eps = 0 a row without variance gives NaN.
+ *
+ * luffy_block_norm_backward - its gradients, for dout = dL/do (from the rest of
+ * the stream; NULL: zeros) and du = dL/du (NULL: zeros; one of the two is
+ * given).  y, o, gate and the weights as the forward had and left them (y NULL:
+ * o is what it was given as x; o and w_pre are read with du only):
+ *   dx [T, d], dy [T, d] (written where y is given) dtype
+ *   dgate  of a channel gate float32 [d], of a token gate [T, d] dtype, or NULL
+ *   dw_post, db_post, dw_pre, db_pre [d] float32, each may be NULL
+ * Sums over rows are float32 in a fixed order.  Workspace:
+ * luffy_block_norm_backward_workspace_size(T, d) bytes.
+ * ---------------------------------------------------------------------- */
+int luffy_block_norm(const void* x, const void* y, int T, int d, int dtype, int norm, float eps, const float* w_post,
+                     const float* b_post, const void* gate, int gate_kind, float res_scale, const float* w_pre,
+                     const float* b_pre, void* o, void* u, void* stream);
+size_t luffy_block_norm_backward_workspace_size(int T, int d);
+int luffy_block_norm_backward(const void* y, const void* o, int T, int d, int dtype, int norm, float eps,
+                              const float* w_post, const float* b_post, const void* gate, int gate_kind,
+                              float res_scale, const float* w_pre, const void* dout, const void* du, void* dx,
+                              void* dy, void* dgate, float* dw_post, float* db_post, float* dw_pre, float* db_pre,
+                              void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
  * Microscaled 4-bit matrices, for serving the layer: a matrix [groups, rows,

@@ -27,6 +27,7 @@ __all__ = [
     "LUFFY_MX4", "FEW_MAX_TOKENS", "mx4_scale_bytes", "luffy_mx4_quantize", "luffy_mx4_dequantize",
     "luffy_mx4_matmul", "luffy_mx4_expert_ffn", "mx4_expert_ffn_workspace_size", "luffy_moe_few",
     "moe_few_workspace_size", "mx4_weights", "ServingLayer",
+    "luffy_block_norm", "luffy_block_norm_backward", "block_norm_backward_workspace_size",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libluffy.so")
@@ -35,6 +36,9 @@ LUFFY_F32, LUFFY_BF16, LUFFY_MX4 = 0, 1, 2
 FEW_MAX_TOKENS = 64   # luffy_moe_few
 LUFFY_ACT_GELU, LUFFY_ACT_SILU = 0, 1
 _ACTS = {"gelu": LUFFY_ACT_GELU, "silu": LUFFY_ACT_SILU}
+LUFFY_NORM_RMS, LUFFY_NORM_LAYER = 0, 1
+_NORMS = {"rms": LUFFY_NORM_RMS, "layer": LUFFY_NORM_LAYER}
+LUFFY_GATE_NONE, LUFFY_GATE_CHANNEL, LUFFY_GATE_TOKEN = 0, 1, 2
 
 _c_int, _c_float, _c_size, _vp = ctypes.c_int, ctypes.c_float, ctypes.c_size_t, ctypes.c_void_p
 
@@ -79,6 +83,12 @@ _SIGS = {
     "luffy_moe_few_workspace_size": (_c_size, [_c_int, _c_int, _c_int, _c_int, _c_int]),
     "luffy_moe_few": (_c_int, [_vp, _c_int, _c_int, _c_int, _vp, _vp, _c_int, _c_int, _vp, _vp, _vp, _vp, _c_int,
                                _c_int, _c_int, _vp, _vp, _vp, _vp, _c_size, _vp]),
+    "luffy_block_norm": (_c_int, [_vp, _vp, _c_int, _c_int, _c_int, _c_int, _c_float, _vp, _vp, _vp, _c_int, _c_float,
+                                  _vp, _vp, _vp, _vp, _vp]),
+    "luffy_block_norm_backward_workspace_size": (_c_size, [_c_int, _c_int]),
+    "luffy_block_norm_backward": (_c_int, [_vp, _vp, _c_int, _c_int, _c_int, _c_int, _c_float, _vp, _vp, _vp, _c_int,
+                                           _c_float, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _c_size,
+                                           _vp]),
     "luffy_adaptive_threshold": (_c_int, [ctypes.c_double, ctypes.c_double, ctypes.POINTER(ctypes.c_double)]),
     "luffy_profile_kernel": (_c_int, [ctypes.c_char_p]),
     "luffy_profile_read": (_c_int, [ctypes.POINTER(ctypes.c_double), ctypes.POINTER(_c_int)]),
@@ -413,6 +423,104 @@ def luffy_moe_few(x, w_gate, b_gate, w1, w2, k, act, topk_idx, topk_gate, y, wor
         _p(x), T, d, _dtype_code(x), _p(w_gate), _p(b_gate), E, k, _p(w1), _p(w1_scale), _p(w2), _p(w2_scale), wtype,
         shape1[1], _ACTS[act] if isinstance(act, str) else int(act), _p(topk_idx), _p(topk_gate), _p(y),
         _p(workspace), workspace.numel(), _stream(stream)), "luffy_moe_few")
+
+
+def _named(table, value, what, name):
+    if isinstance(value, str):
+        if value not in table:
+            raise LuffyError(f"{what}: {name} {value!r} is none of {', '.join(table)}")
+        return table[value]
+    return int(value)
+
+
+def _fits(what, name, t, shape, dtype):
+    """t (a tensor or None) has this shape and dtype."""
+    if t is not None and (t.dtype != dtype or t.shape != shape):
+        raise LuffyError(f"{what}: {name} must be {str(dtype)[6:]} {list(shape)}, got {str(t.dtype)[6:]} "
+                         f"{list(t.shape)}")
+
+
+def _device_ptrs(what, *tensors):
+    """Pointers of contiguous tensors on the current device (None stays None):
+    the launch goes to the current device's stream."""
+    device = torch.cuda.current_device() if any(t is not None and t.is_cuda for t in tensors) else -1
+    out = []
+    for t in tensors:
+        if t is not None:
+            if not t.is_cuda:
+                raise LuffyError(f"{what}: tensor must be on the GPU")
+            if t.get_device() != device:
+                raise LuffyError(f"{what}: tensor on device {t.get_device()}, the current one is {device}")
+            if not t.is_contiguous():
+                raise LuffyError(f"{what}: tensor must be contiguous")
+            t = t.data_ptr()
+        out.append(t)
+    return out
+
+
+def _block_gate(what, gate, T, d, dtype):
+    """Kind of a block's gate: none, float32 [d], or [T, d] of dtype."""
+    if gate is None:
+        return LUFFY_GATE_NONE
+    if gate.dim() == 1:
+        _fits(what, "a channel gate", gate, (d,), torch.float32)
+        return LUFFY_GATE_CHANNEL
+    _fits(what, "a token gate", gate, (T, d), dtype)
+    return LUFFY_GATE_TOKEN
+
+
+def luffy_block_norm(x, y, o, u, *, norm="rms", eps=1e-6, res_scale=1.0, w_post=None, b_post=None, gate=None,
+                     w_pre=None, b_pre=None, stream=None):
+    """The residual stream around a layer: o = res_scale x + gate N(y; w_post,
+    b_post) and u = N(o; w_pre, b_pre), rows [T, d] float32 or bf16, N the "rms"
+    or "layer" norm.  y and o None: u of x.  w_pre and u None: o alone.  w_post
+    None: y as it is.  gate: None, float32 [d], or [T, d] of x's dtype; weights
+    and biases float32 [d]."""
+    what = "luffy_block_norm"
+    if x.dim() != 2:
+        raise LuffyError(f"{what}: x must be [T, d], got {list(x.shape)}")
+    T, d = x.shape
+    for name, t in (("y", y), ("o", o), ("u", u)):
+        _fits(what, name, t, x.shape, x.dtype)
+    for name, t in (("w_post", w_post), ("b_post", b_post), ("w_pre", w_pre), ("b_pre", b_pre)):
+        _fits(what, name, t, (d,), torch.float32)
+    kind = _block_gate(what, gate, T, d, x.dtype)
+    dt = _dtype_code(x)
+    x, y, w_post, b_post, gate, w_pre, b_pre, o, u = _device_ptrs(what, x, y, w_post, b_post, gate, w_pre, b_pre, o, u)
+    _check(load_library().luffy_block_norm(x, y, T, d, dt, _named(_NORMS, norm, what, "norm"), eps, w_post, b_post, gate,
+                                           kind, res_scale, w_pre, b_pre, o, u, _stream(stream)), what)
+
+
+def block_norm_backward_workspace_size(T: int, d: int) -> int:
+    return int(load_library().luffy_block_norm_backward_workspace_size(int(T), int(d)))
+
+
+def luffy_block_norm_backward(y, o, dout, du, dx, dy, workspace, *, norm="rms", eps=1e-6, res_scale=1.0, w_post=None,
+                              b_post=None, gate=None, w_pre=None, dgate=None, dw_post=None, db_post=None, dw_pre=None,
+                              db_pre=None, stream=None):
+    """Gradients of luffy_block_norm for dout = dL/do and du = dL/du (one of them
+    may be None): dx, dy (None where y is), and those asked for of dgate (the
+    gate's shape and dtype), dw_post, db_post, dw_pre and db_pre (float32 [d]).
+    y, o, gate and weights as the forward had and left them."""
+    what = "luffy_block_norm_backward"
+    if dx.dim() != 2:
+        raise LuffyError(f"{what}: dx must be [T, d], got {list(dx.shape)}")
+    T, d = dx.shape
+    for name, t in (("y", y), ("o", o), ("dout", dout), ("du", du), ("dy", dy)):
+        _fits(what, name, t, dx.shape, dx.dtype)
+    for name, t in (("w_post", w_post), ("b_post", b_post), ("w_pre", w_pre), ("dw_post", dw_post),
+                    ("db_post", db_post), ("dw_pre", dw_pre), ("db_pre", db_pre)):
+        _fits(what, name, t, (d,), torch.float32)
+    kind = _block_gate(what, gate, T, d, dx.dtype)
+    if gate is not None:
+        _fits(what, "dgate", dgate, gate.shape, gate.dtype)
+    dt, ws_bytes = _dtype_code(dx), workspace.numel() * workspace.element_size()
+    (y, o, w_post, b_post, gate, w_pre, dout, du, dx, dy, dgate, dw_post, db_post, dw_pre, db_pre,
+     workspace) = _device_ptrs(what, y, o, w_post, b_post, gate, w_pre, dout, du, dx, dy, dgate, dw_post, db_post,
+                               dw_pre, db_pre, workspace)
+    _check(load_library().luffy_block_norm_backward(
+        y, o, T, d, dt, _named(_NORMS, norm, what, "norm"), eps, w_post, b_post, gate, kind, res_scale, w_pre, dout,
+        du, dx, dy, dgate, dw_post, db_post, dw_pre, db_pre, workspace, ws_bytes, _stream(stream)), what)
 
 
 def adaptive_threshold(l_ini: float, l_prev: float) -> float:

@@ -25,7 +25,8 @@ FLAGS = [
     "-Wall", "-Wno-unused-result", "-Wno-unused-command-line-argument",
     f"-I{INCLUDE}", f"-I{CSRC}",
 ]
-SOURCES = ["luffy_api.hip", "route.hip", "condense.hip", "ffn.hip", "combine.hip", "mx4.hip", "few.hip"]
+SOURCES = ["luffy_api.hip", "route.hip", "condense.hip", "ffn.hip", "combine.hip", "mx4.hip", "few.hip",
+           "block_norm.hip"]
 
 
 def _compile(src: str) -> str:
