@@ -73,6 +73,9 @@ typedef enum { LUFFY_NORM_RMS = 0, LUFFY_NORM_LAYER = 1 } luffy_norm;
 /* Gates of luffy_block_norm: none, float32 [d] for every token, [T, d] dtype. */
 typedef enum { LUFFY_GATE_NONE = 0, LUFFY_GATE_CHANNEL = 1, LUFFY_GATE_TOKEN = 2 } luffy_gate;
 
+/* Scores of luffy_route_scored: softmax over the experts, or 1 / (1 + e^-l). */
+typedef enum { LUFFY_SCORE_SOFTMAX = 0, LUFFY_SCORE_SIGMOID = 1 } luffy_score;
+
 int luffy_abi_version(void);
 const char* luffy_status_string(int status);
 const char* luffy_last_error(void);
@@ -133,6 +136,53 @@ int luffy_route_noalloc(const void* x, int T, int d, int dtype,
                         int32_t* topk_idx, float* topk_gate, int32_t* slot_pos,
                         int32_t* perm_token, int32_t* offsets, float* inv_norm,
                         void* stream);
+
+/* ------------------------------------------------------------------------
+ * luffy_route_scored - luffy_route with softmax or sigmoid scores, a bias for
+ * balance, groups of experts and 1 <= k <= 8 experts a token:
+ *   l_t = W_g x_t + b_gate,  s = softmax(l) or 1 / (1 + e^-l)
+ *   c_e = s_e + balance_e decides, and only decides: gates are made of s.
+ *         Without a balance (NULL) c_e is l_e, the same order.
+ *   groups  expert e is in group e / (E / groups).  With top_groups < groups
+ *           (groups <= 16 then) a token's experts are taken from its top_groups
+ *           best groups alone, a group's value being its largest c (group_best 1)
+ *           or the sum of its two largest (2; without a balance of its two
+ *           largest s); the lower group first among equal ones
+ *   topk_idx [T, k] the k largest c, best first, the lower expert first among
+ *           equal ones; k <= top_groups * E / groups.  A c that is no number
+ *           counts as -infinity; balance may be -infinity (an expert that is
+ *           chosen only where nothing else is left), not +infinity
+ *   topk_gate [T, k] scale * s, or scale * s / (sum of the k chosen s) with
+ *           renormalise
+ *   logits  [T, E] float or NULL: l, for luffy_route_scored_backward
+ * Choices are those of exact logits: float32 sums decide where their error bound
+ * allows, the other tokens are decided in float64.  Everything else (capacity,
+ * slot_pos, perm_token, offsets, inv_norm) as for luffy_route; workspace:
+ * luffy_route_workspace_size(T, E, k) bytes.  x and w_gate 16-byte aligned.
+ *
+ * luffy_route_scored_backward - gradients with the choices held fixed, for dgate
+ * = dL/dtopk_gate (as luffy_combine_backward gives it: 0 for dropped slots) and
+ * dlogits [T, E] float or NULL (the gradient of an auxiliary loss in l):
+ *   dw_gate [E, d] float32, db_gate [E] float32 or NULL
+ *   dx [T, d] dtype: dl_t W_g, and with dx_rep (the experts' input gradients of
+ *      the representatives, luffy_expert_ffn_backward's dx_rep) the rows of those
+ *      representatives that are token t itself: dx_rep[rep_row[p]] for p =
+ *      slot_pos[t, j] with rep_of_pos[p] = p.  dx is then the whole gradient of the
+ *      layer's input.  dx_rep NULL: the router's share alone
+ * Sums are float32, dx is rounded once.  An index in topk_idx outside 0..E-1 is
+ * ignored.  x, w_gate, dx_rep, dx and dw_gate 16-byte aligned.
+ * ---------------------------------------------------------------------- */
+int luffy_route_scored(const void* x, int T, int d, int dtype, const void* w_gate, const float* b_gate, int E, int k,
+                       int score, const float* balance, int groups, int top_groups, int group_best, int renormalise,
+                       float scale, double capacity_factor, int32_t* topk_idx, float* topk_gate, float* logits,
+                       int32_t* slot_pos, int32_t* perm_token, int32_t* offsets, float* inv_norm, void* workspace,
+                       size_t workspace_bytes, void* stream);
+size_t luffy_route_scored_backward_workspace_size(int T, int d, int E);
+int luffy_route_scored_backward(const void* x, int T, int d, int dtype, const void* w_gate, int E, int k, int score,
+                                int renormalise, float scale, const float* logits, const int32_t* topk_idx,
+                                const float* dgate, const float* dlogits, const void* dx_rep, const int32_t* slot_pos,
+                                const int32_t* rep_of_pos, const int32_t* rep_row, void* dx, float* dw_gate,
+                                float* db_gate, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Per-expert slot capacity used by luffy_route: ceil(cf*k*T/E - 1e-9),
  * evaluated in double precision left to right (the 1e-9 keeps a product that

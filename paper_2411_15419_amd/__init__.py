@@ -28,6 +28,7 @@ __all__ = [
     "luffy_mx4_matmul", "luffy_mx4_expert_ffn", "mx4_expert_ffn_workspace_size", "luffy_moe_few",
     "moe_few_workspace_size", "mx4_weights", "ServingLayer",
     "luffy_block_norm", "luffy_block_norm_backward", "block_norm_backward_workspace_size",
+    "luffy_route_scored", "luffy_route_scored_backward", "route_scored_backward_workspace_size",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libluffy.so")
@@ -38,6 +39,8 @@ LUFFY_ACT_GELU, LUFFY_ACT_SILU = 0, 1
 _ACTS = {"gelu": LUFFY_ACT_GELU, "silu": LUFFY_ACT_SILU}
 LUFFY_NORM_RMS, LUFFY_NORM_LAYER = 0, 1
 _NORMS = {"rms": LUFFY_NORM_RMS, "layer": LUFFY_NORM_LAYER}
+LUFFY_SCORE_SOFTMAX, LUFFY_SCORE_SIGMOID = 0, 1
+_SCORES = {"softmax": LUFFY_SCORE_SOFTMAX, "sigmoid": LUFFY_SCORE_SIGMOID}
 LUFFY_GATE_NONE, LUFFY_GATE_CHANNEL, LUFFY_GATE_TOKEN = 0, 1, 2
 
 _c_int, _c_float, _c_size, _vp = ctypes.c_int, ctypes.c_float, ctypes.c_size_t, ctypes.c_void_p
@@ -83,6 +86,13 @@ _SIGS = {
     "luffy_moe_few_workspace_size": (_c_size, [_c_int, _c_int, _c_int, _c_int, _c_int]),
     "luffy_moe_few": (_c_int, [_vp, _c_int, _c_int, _c_int, _vp, _vp, _c_int, _c_int, _vp, _vp, _vp, _vp, _c_int,
                                _c_int, _c_int, _vp, _vp, _vp, _vp, _c_size, _vp]),
+    "luffy_route_scored": (_c_int, [_vp, _c_int, _c_int, _c_int, _vp, _vp, _c_int, _c_int, _c_int, _vp, _c_int, _c_int,
+                                    _c_int, _c_int, _c_float, ctypes.c_double, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
+                                    _c_size, _vp]),
+    "luffy_route_scored_backward_workspace_size": (_c_size, [_c_int, _c_int, _c_int]),
+    "luffy_route_scored_backward": (_c_int, [_vp, _c_int, _c_int, _c_int, _vp, _c_int, _c_int, _c_int, _c_int, _c_float,
+                                             _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _c_size,
+                                             _vp]),
     "luffy_block_norm": (_c_int, [_vp, _vp, _c_int, _c_int, _c_int, _c_int, _c_float, _vp, _vp, _vp, _c_int, _c_float,
                                   _vp, _vp, _vp, _vp, _vp]),
     "luffy_block_norm_backward_workspace_size": (_c_size, [_c_int, _c_int]),
@@ -521,6 +531,83 @@ def luffy_block_norm_backward(y, o, dout, du, dx, dy, workspace, *, norm="rms", 
     _check(load_library().luffy_block_norm_backward(
         y, o, T, d, dt, _named(_NORMS, norm, what, "norm"), eps, w_post, b_post, gate, kind, res_scale, w_pre, dout,
         du, dx, dy, dgate, dw_post, db_post, dw_pre, db_pre, workspace, ws_bytes, _stream(stream)), what)
+
+
+def _router_shapes(what, x, w_gate):
+    if x.dim() != 2 or w_gate.dim() != 2 or w_gate.shape[1] != x.shape[1] or w_gate.dtype != x.dtype:
+        raise LuffyError(f"{what}: x [T, d] and w_gate [E, d] of one dtype, got {list(x.shape)} and "
+                         f"{list(w_gate.shape)}")
+    return x.shape[0], x.shape[1], w_gate.shape[0]
+
+
+def luffy_route_scored(x, w_gate, b_gate, k, score, capacity_factor, topk_idx, topk_gate, logits, slot_pos, perm_token,
+                       offsets, workspace, *, balance=None, groups=1, top_groups=1, group_best=1, renormalise=True,
+                       scale=1.0, inv_norm=None, stream=None):
+    """luffy_route with "softmax" or "sigmoid" scores, a bias for balance
+    (float32 [E], in the choice alone), the experts of the top_groups best of
+    `groups` groups, and up to 8 experts a token.  logits (float32 [T, E] or None)
+    are what luffy_route_scored_backward needs."""
+    what = "luffy_route_scored"
+    T, d, E = _router_shapes(what, x, w_gate)
+    f32, i32 = torch.float32, torch.int32
+    _fits(what, "b_gate", b_gate, (E,), f32)
+    _fits(what, "balance", balance, (E,), f32)
+    _fits(what, "topk_idx", topk_idx, (T, k), i32)
+    _fits(what, "topk_gate", topk_gate, (T, k), f32)
+    _fits(what, "logits", logits, (T, E), f32)
+    _fits(what, "slot_pos", slot_pos, (T, k), i32)
+    _fits(what, "perm_token", perm_token, (T * k,), i32)
+    _fits(what, "offsets", offsets, (E + 1,), i32)
+    _fits(what, "inv_norm", inv_norm, (T,), f32)
+    dt, ws_bytes = _dtype_code(x), workspace.numel() * workspace.element_size()
+    (x, w_gate, b_gate, balance, topk_idx, topk_gate, logits, slot_pos, perm_token, offsets, inv_norm,
+     workspace) = _device_ptrs(what, x, w_gate, b_gate, balance, topk_idx, topk_gate, logits, slot_pos, perm_token,
+                               offsets, inv_norm, workspace)
+    _check(load_library().luffy_route_scored(
+        x, T, d, dt, w_gate, b_gate, E, k, _named(_SCORES, score, what, "score"), balance, groups, top_groups,
+        group_best, bool(renormalise), scale, float(capacity_factor), topk_idx, topk_gate, logits, slot_pos,
+        perm_token, offsets, inv_norm, workspace, ws_bytes, _stream(stream)), what)
+
+
+def route_scored_backward_workspace_size(T: int, d: int, E: int) -> int:
+    return int(load_library().luffy_route_scored_backward_workspace_size(int(T), int(d), int(E)))
+
+
+def luffy_route_scored_backward(x, w_gate, score, logits, topk_idx, dgate, dx, dw_gate, db_gate, workspace, *,
+                                renormalise=True, scale=1.0, dlogits=None, dx_rep=None, slot_pos=None,
+                                rep_of_pos=None, rep_row=None, stream=None):
+    """Gradients of luffy_route_scored's gates with its choices held fixed: dx
+    [T, d], dw_gate [E, d] and db_gate [E] (float32; the last may be None) from
+    dgate [T, k] and, where given, dlogits [T, E] of an auxiliary loss.  With
+    dx_rep (and slot_pos, rep_of_pos, rep_row) the representatives' input
+    gradients are added to their tokens' rows of dx."""
+    what = "luffy_route_scored_backward"
+    T, d, E = _router_shapes(what, x, w_gate)
+    f32, i32 = torch.float32, torch.int32
+    if topk_idx.dim() != 2:
+        raise LuffyError(f"{what}: topk_idx must be [T, k], got {list(topk_idx.shape)}")
+    k = topk_idx.shape[1]
+    _fits(what, "topk_idx", topk_idx, (T, k), i32)
+    _fits(what, "logits", logits, (T, E), f32)
+    _fits(what, "dgate", dgate, (T, k), f32)
+    _fits(what, "dlogits", dlogits, (T, E), f32)
+    _fits(what, "dx", dx, x.shape, x.dtype)
+    _fits(what, "dw_gate", dw_gate, (E, d), f32)
+    _fits(what, "db_gate", db_gate, (E,), f32)
+    if dx_rep is not None:
+        if dx_rep.dim() != 2 or dx_rep.shape[1] != d or dx_rep.dtype != x.dtype:
+            raise LuffyError(f"{what}: dx_rep must be rows of {d} values of x's dtype, got {list(dx_rep.shape)}")
+        _fits(what, "slot_pos", slot_pos, (T, k), i32)
+        _fits(what, "rep_of_pos", rep_of_pos, (T * k,), i32)
+        _fits(what, "rep_row", rep_row, (T * k,), i32)
+    dt, ws_bytes = _dtype_code(x), workspace.numel() * workspace.element_size()
+    (x, w_gate, logits, topk_idx, dgate, dlogits, dx_rep, slot_pos, rep_of_pos, rep_row, dx, dw_gate, db_gate,
+     workspace) = _device_ptrs(what, x, w_gate, logits, topk_idx, dgate, dlogits, dx_rep, slot_pos, rep_of_pos,
+                               rep_row, dx, dw_gate, db_gate, workspace)
+    _check(load_library().luffy_route_scored_backward(
+        x, T, d, dt, w_gate, E, k, _named(_SCORES, score, what, "score"), bool(renormalise), scale, logits, topk_idx,
+        dgate, dlogits, dx_rep, slot_pos, rep_of_pos, rep_row, dx, dw_gate, db_gate, workspace, ws_bytes,
+        _stream(stream)), what)
 
 
 def adaptive_threshold(l_ini: float, l_prev: float) -> float:

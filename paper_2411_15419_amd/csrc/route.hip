@@ -20,6 +20,7 @@
 #include <type_traits>
 
 #include "luffy_common.h"
+#include "route.h"
 
 // Scratch of luffy_route_noalloc (the per-chunk slot counts of one call):
 // one copy per GPU for the life of the process.  In host code the name only
@@ -762,11 +763,7 @@ __global__ __launch_bounds__(256) void slot_scatter_kernel(
   }
 }
 
-struct RouteWs {
-  int32_t* hist;
-  int* totals;
-  int* done;
-};
+}  // namespace
 
 RouteWs carve_route(Carver& c, int T, int E, int k) {
   RouteWs w;
@@ -778,8 +775,6 @@ RouteWs carve_route(Carver& c, int T, int E, int k) {
   return w;
 }
 
-}  // namespace
-
 // ceil(cf*k*T/E - 1e-9) in double precision, evaluated left to right; the
 // 1e-9 keeps a product that is an integer up to the rounding of a decimal
 // factor (cf = 1.1, k*T/E = 1000) at that integer.
@@ -787,6 +782,17 @@ int capacity_slots(int T, int k, int E, double cf) {
   if (!(cf > 0.0)) return 0;
   const double c = std::ceil(cf * k * T / E - 1e-9);
   return c >= 2147483647.0 ? 2147483647 : static_cast<int>(c);
+}
+
+void route_buckets_enqueue(const int32_t* topk_idx, int T, int E, int k, double capacity_factor, int tok,
+                           int32_t* slot_pos, int32_t* perm_token, int32_t* offsets, const RouteWs& ws,
+                           hipStream_t s) {
+  const int C = capacity_slots(T, k, E, capacity_factor);
+  const int nch = k * ((T + tok - 1) / tok);
+  const long long S = static_cast<long long>(T) * k;
+  launch("slot_scan", slot_scan_kernel, E, 1024, 0, s, ws.hist, nch, E, C, offsets, ws.totals, ws.done);
+  launch("slot_scatter", slot_scatter_kernel, static_cast<int>((S + 255) / 256), 256, 0, s, topk_idx, ws.hist,
+         offsets, T, k, E, C, tok, slot_pos, perm_token);
 }
 
 }  // namespace luffy
@@ -827,14 +833,11 @@ int route_check(const char* fn, const void* x, int T, int d, int dtype, const vo
 void route_enqueue(const void* x, int T, int d, int dtype, const void* w_gate, const float* b_gate, int E, int k,
                    double capacity_factor, int32_t* topk_idx, float* topk_gate, int32_t* slot_pos,
                    int32_t* perm_token, int32_t* offsets, float* inv_norm, const RouteWs& ws, hipStream_t s) {
-  const int C = capacity_slots(T, k, E, capacity_factor);
-  const long long S = static_cast<long long>(T) * k;
   // the streaming gate when every wave of its persistent grid has a chunk
   const bool stream = gate_stream_ok(dtype, E, d) &&
                       (T + kGateStreamTok - 1) / kGateStreamTok >= kGateStreamWaves * persistent_grid();
   const int tok = stream ? kGateStreamTok : gate_tokens(T);
   const int gblocks = (T + tok - 1) / tok;
-  const int nch = k * gblocks;
   if (stream) {
     const int grid = std::max(1, std::min(persistent_grid(), (gblocks + kGateStreamWaves - 1) / kGateStreamWaves));
 #define LUFFY_GATE_S(NEB) launch("gate", gate_stream_kernel<NEB>, grid, kGateStreamWaves * 64, 0, s,                  \
@@ -858,9 +861,7 @@ void route_enqueue(const void* x, int T, int d, int dtype, const void* w_gate, c
     }
 #undef LUFFY_GATE_ARGS
   }
-  launch("slot_scan", slot_scan_kernel, E, 1024, 0, s, ws.hist, nch, E, C, offsets, ws.totals, ws.done);
-  launch("slot_scatter", slot_scatter_kernel, static_cast<int>((S + 255) / 256), 256, 0, s, topk_idx, ws.hist,
-         offsets, T, k, E, C, tok, slot_pos, perm_token);
+  route_buckets_enqueue(topk_idx, T, E, k, capacity_factor, tok, slot_pos, perm_token, offsets, ws, s);
 }
 
 constexpr int kMaxDevices = 64;
