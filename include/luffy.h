@@ -413,6 +413,50 @@ int luffy_expert_ffn_backward(const void* x, const int32_t* row_index, const int
                               size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
+ * Activations kept in 8 bits between the forward and the backward: matrices of
+ * microscaled 8-bit integers.  A block of 32 consecutive values of a row is 32
+ * int8 v_i (-127..127) under one scale 2^(s - 127) (s = 0..248; s = 255: the block
+ * holds no numbers, every value of it reads as NaN).
+ *   values  q [rows, cols] int8; scales s [ceil(cols/256), rows, 8] uint8: those of
+ *           256 consecutive columns of a row side by side, 0 past the last column
+ *           (luffy_mx4_scale_bytes(1, rows, cols) bytes)
+ * cols is a multiple of 32, at most 32768; x and q 16-byte, s 8-byte aligned.
+ *
+ * luffy_mx8_quantize - rounds x [rows, cols] (float32 or bf16).  With m the largest
+ * |value| of a block its scale is 2^(floor(log2 m) - 6) (at least 2^-127), so that
+ * m / scale lies in [64, 128); every value / scale goes to the nearest integer,
+ * halfway cases to the even one, above 127 to 127.  A block with an infinity or a
+ * NaN gets s = 255.
+ * luffy_mx8_dequantize - the values as float32 or bf16 (exact in both).
+ *
+ * luffy_expert_ffn_keep - luffy_expert_ffn (bf16), which also leaves its first
+ * product Z = X W1_e^T in zq [max_rows, d_ff], zs, rounded from the float32 sums
+ * (the rows in use; y_rep has the bits of luffy_expert_ffn's).  Workspace:
+ * luffy_expert_ffn_workspace_size(max_rows, E, d_ff, LUFFY_BF16) bytes.
+ *
+ * luffy_expert_ffn_backward_kept - luffy_expert_ffn_backward with the kept values
+ * in the place of Z: four products instead of five, and neither Z nor x is needed
+ * in bf16.
+ *   x, x_scale  rows of x for dW1: bf16 (x_scale NULL), or values and scales of a
+ *               matrix [x_rows, d] of luffy_mx8_quantize; read through row_index
+ *               where it is given
+ * max_rows as for luffy_expert_ffn_keep; the rest as for
+ * luffy_expert_ffn_backward.  dx_rep's rows behind the last one in use stay as they
+ * are.
+ * ---------------------------------------------------------------------- */
+int luffy_mx8_quantize(const void* x, int rows, int cols, int dtype, void* q, void* s, void* stream);
+int luffy_mx8_dequantize(const void* q, const void* s, int rows, int cols, int dtype, void* x, void* stream);
+int luffy_expert_ffn_keep(const void* x, const int32_t* row_index, const int32_t* rep_offsets, int E, int d, int d_ff,
+                          const void* w1, const void* w2, int act, int max_rows, void* zq, void* zs, void* y_rep,
+                          void* workspace, size_t workspace_bytes, void* stream);
+size_t luffy_expert_ffn_backward_kept_workspace_size(int max_rows, int E, int d, int d_ff);
+int luffy_expert_ffn_backward_kept(const void* x, const void* x_scale, int x_rows, const int32_t* row_index,
+                                   const int32_t* rep_offsets, int E, int d, int d_ff, const void* w1, const void* w2,
+                                   int act, int max_rows, const void* zq, const void* zs, const void* dy_rep,
+                                   void* dx_rep, void* dw1, void* dw2, int dw_dtype, void* workspace,
+                                   size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
  * luffy_block_norm - the residual stream around a layer: the layer's output
  * normed, gated and added to the stream, and the norm before the next layer.
  *   N(a; w, b) = (a - m) / sqrt(mean((a - m)^2) + eps) * w + b  over a row,

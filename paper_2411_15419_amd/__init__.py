@@ -29,6 +29,8 @@ __all__ = [
     "moe_few_workspace_size", "mx4_weights", "ServingLayer",
     "luffy_block_norm", "luffy_block_norm_backward", "block_norm_backward_workspace_size",
     "luffy_route_scored", "luffy_route_scored_backward", "route_scored_backward_workspace_size",
+    "luffy_mx8_quantize", "luffy_mx8_dequantize", "luffy_expert_ffn_keep", "luffy_expert_ffn_backward_kept",
+    "expert_ffn_backward_kept_workspace_size",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libluffy.so")
@@ -86,6 +88,13 @@ _SIGS = {
     "luffy_moe_few_workspace_size": (_c_size, [_c_int, _c_int, _c_int, _c_int, _c_int]),
     "luffy_moe_few": (_c_int, [_vp, _c_int, _c_int, _c_int, _vp, _vp, _c_int, _c_int, _vp, _vp, _vp, _vp, _c_int,
                                _c_int, _c_int, _vp, _vp, _vp, _vp, _c_size, _vp]),
+    "luffy_mx8_quantize": (_c_int, [_vp, _c_int, _c_int, _c_int, _vp, _vp, _vp]),
+    "luffy_mx8_dequantize": (_c_int, [_vp, _vp, _c_int, _c_int, _c_int, _vp, _vp]),
+    "luffy_expert_ffn_keep": (_c_int, [_vp, _vp, _vp, _c_int, _c_int, _c_int, _vp, _vp, _c_int, _c_int, _vp, _vp, _vp,
+                                       _vp, _c_size, _vp]),
+    "luffy_expert_ffn_backward_kept_workspace_size": (_c_size, [_c_int, _c_int, _c_int, _c_int]),
+    "luffy_expert_ffn_backward_kept": (_c_int, [_vp, _vp, _c_int, _vp, _vp, _c_int, _c_int, _c_int, _vp, _vp, _c_int,
+                                                _c_int, _vp, _vp, _vp, _vp, _vp, _vp, _c_int, _vp, _c_size, _vp]),
     "luffy_route_scored": (_c_int, [_vp, _c_int, _c_int, _c_int, _vp, _vp, _c_int, _c_int, _c_int, _vp, _c_int, _c_int,
                                     _c_int, _c_int, _c_float, ctypes.c_double, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
                                     _c_size, _vp]),
@@ -531,6 +540,107 @@ def luffy_block_norm_backward(y, o, dout, du, dx, dy, workspace, *, norm="rms", 
     _check(load_library().luffy_block_norm_backward(
         y, o, T, d, dt, _named(_NORMS, norm, what, "norm"), eps, w_post, b_post, gate, kind, res_scale, w_pre, dout,
         du, dx, dy, dgate, dw_post, db_post, dw_pre, db_pre, workspace, ws_bytes, _stream(stream)), what)
+
+
+def _mx8_shape(what, q, s):
+    """(rows, cols) of a microscaled 8-bit matrix, its tensors checked: values
+    int8 [rows, cols], scales uint8 [ceil(cols/256), rows, 8]."""
+    if q.dim() != 2 or q.dtype != torch.int8:
+        raise LuffyError(f"{what}: 8-bit values must be int8 [rows, cols], got {str(q.dtype)[6:]} {list(q.shape)}")
+    rows, cols = q.shape
+    _fits(what, "their scales", s, ((cols + 255) // 256, rows, 8), torch.uint8)
+    return rows, cols
+
+
+def luffy_mx8_quantize(x, q, s, stream=None):
+    """Rounds x [rows, cols] (float32 or bf16) to microscaled 8-bit integers: int8
+    values q [rows, cols] with scales s [ceil(cols/256), rows, 8] (uint8)."""
+    what = "luffy_mx8_quantize"
+    rows, cols = _mx8_shape(what, q, s)
+    if x.shape != q.shape:
+        raise LuffyError(f"{what}: x {list(x.shape)} does not fit values {list(q.shape)}")
+    dt = _dtype_code(x)
+    x, q, s = _device_ptrs(what, x, q, s)
+    _check(load_library().luffy_mx8_quantize(x, rows, cols, dt, q, s, _stream(stream)), what)
+
+
+def luffy_mx8_dequantize(q, s, x, stream=None):
+    """The values of a microscaled 8-bit matrix into x (float32 or bf16)."""
+    what = "luffy_mx8_dequantize"
+    rows, cols = _mx8_shape(what, q, s)
+    if x.shape != q.shape:
+        raise LuffyError(f"{what}: x {list(x.shape)} does not fit values {list(q.shape)}")
+    dt = _dtype_code(x)
+    x, q, s = _device_ptrs(what, x, q, s)
+    _check(load_library().luffy_mx8_dequantize(q, s, rows, cols, dt, x, _stream(stream)), what)
+
+
+def _ffn_shapes(what, x_rows, x_cols, row_index, rep_offsets, w1, w2, max_rows, zq, zs):
+    """(E, d, d_ff), the tensors of an FFN that keeps Z checked."""
+    bf, i32 = torch.bfloat16, torch.int32
+    if w1.dim() != 3:
+        raise LuffyError(f"{what}: w1 must be [E, d_ff, d], got {list(w1.shape)}")
+    E, d_ff, d = w1.shape
+    _fits(what, "w1", w1, (E, d_ff, d), bf)
+    _fits(what, "w2", w2, (E, d, d_ff), bf)
+    _fits(what, "rep_offsets", rep_offsets, (E + 1,), i32)
+    if _mx8_shape(what, zq, zs) != (max_rows, d_ff):
+        raise LuffyError(f"{what}: the kept values must be [{max_rows}, {d_ff}], got {list(zq.shape)}")
+    if x_cols != d or (row_index is None and x_rows < max_rows):
+        raise LuffyError(f"{what}: x [{x_rows}, {x_cols}] does not fit {max_rows} rows of {d}")
+    if row_index is not None and (row_index.dtype != i32 or row_index.dim() != 1 or row_index.numel() < max_rows):
+        raise LuffyError(f"{what}: row_index must be int32 [max_rows]")
+    return E, d, d_ff
+
+
+def luffy_expert_ffn_keep(x, row_index, rep_offsets, w1, w2, act, max_rows, zq, zs, y_rep, workspace, stream=None):
+    """luffy_expert_ffn (bf16) that leaves its first product, before the
+    activation, in microscaled 8 bits: zq int8 [max_rows, d_ff], zs uint8
+    [ceil(d_ff/256), max_rows, 8], for luffy_expert_ffn_backward_kept.  Workspace:
+    expert_ffn_workspace_size."""
+    what = "luffy_expert_ffn_keep"
+    _fits(what, "x", x, x.shape, torch.bfloat16)
+    E, d, d_ff = _ffn_shapes(what, x.shape[0], x.shape[-1], row_index, rep_offsets, w1, w2, max_rows, zq, zs)
+    _fits(what, "y_rep", y_rep, (y_rep.shape[0], d), torch.bfloat16)
+    if y_rep.shape[0] < max_rows:
+        raise LuffyError(f"{what}: y_rep has {y_rep.shape[0]} rows of {max_rows}")
+    ws_bytes, code = workspace.numel() * workspace.element_size(), _named(_ACTS, act, what, "act")
+    x, row_index, rep_offsets, w1, w2, zq, zs, y_rep, workspace = _device_ptrs(
+        what, x, row_index, rep_offsets, w1, w2, zq, zs, y_rep, workspace)
+    _check(load_library().luffy_expert_ffn_keep(x, row_index, rep_offsets, E, d, d_ff, w1, w2, code, max_rows, zq, zs,
+                                                y_rep, workspace, ws_bytes, _stream(stream)), what)
+
+
+def expert_ffn_backward_kept_workspace_size(max_rows: int, E: int, d: int, d_ff: int) -> int:
+    return int(load_library().luffy_expert_ffn_backward_kept_workspace_size(int(max_rows), int(E), int(d), int(d_ff)))
+
+
+def luffy_expert_ffn_backward_kept(x, x_scale, row_index, rep_offsets, w1, w2, act, max_rows, zq, zs, dy_rep, dx_rep,
+                                   dw1, dw2, workspace, stream=None):
+    """luffy_expert_ffn_backward from luffy_expert_ffn_keep's zq, zs.  x: bf16 rows
+    (x_scale None), or the int8 values of luffy_mx8_quantize with their scales;
+    read through row_index where it is given."""
+    what = "luffy_expert_ffn_backward_kept"
+    bf = torch.bfloat16
+    if x_scale is None:
+        _fits(what, "x", x, x.shape, bf)
+        x_rows, x_cols = x.shape
+    else:
+        x_rows, x_cols = _mx8_shape(what, x, x_scale)
+    E, d, d_ff = _ffn_shapes(what, x_rows, x_cols, row_index, rep_offsets, w1, w2, max_rows, zq, zs)
+    for name, t in (("dy_rep", dy_rep), ("dx_rep", dx_rep)):
+        _fits(what, name, t, (t.shape[0], d), bf)
+        if t.shape[0] < max_rows:
+            raise LuffyError(f"{what}: {name} has {t.shape[0]} rows of {max_rows}")
+    _fits(what, "dw1", dw1, w1.shape, dw1.dtype)
+    _fits(what, "dw2", dw2, w2.shape, dw1.dtype)
+    dw, code = _dtype_code(dw1), _named(_ACTS, act, what, "act")
+    ws_bytes = workspace.numel() * workspace.element_size()
+    x, x_scale, row_index, rep_offsets, w1, w2, zq, zs, dy_rep, dx_rep, dw1, dw2, workspace = _device_ptrs(
+        what, x, x_scale, row_index, rep_offsets, w1, w2, zq, zs, dy_rep, dx_rep, dw1, dw2, workspace)
+    _check(load_library().luffy_expert_ffn_backward_kept(
+        x, x_scale, x_rows, row_index, rep_offsets, E, d, d_ff, w1, w2, code, max_rows, zq, zs, dy_rep, dx_rep, dw1,
+        dw2, dw, workspace, ws_bytes, _stream(stream)), what)
 
 
 def _router_shapes(what, x, w_gate):

@@ -26,7 +26,7 @@ FLAGS = [
     f"-I{INCLUDE}", f"-I{CSRC}",
 ]
 SOURCES = ["luffy_api.hip", "route.hip", "condense.hip", "ffn.hip", "combine.hip", "mx4.hip", "few.hip",
-           "block_norm.hip", "route_scored.hip"]
+           "block_norm.hip", "route_scored.hip", "mx8.hip"]
 
 
 def _compile(src: str) -> str:

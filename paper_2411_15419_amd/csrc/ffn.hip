@@ -10,11 +10,13 @@
 // each as one 8-byte word.  The last row tile of an expert usually holds
 // fewer rows; its waves skip the MFMAs of the missing rows.
 // float32: 64 x 64 or 32 x 32 tiles of float32 MFMA.
+#include <initializer_list>
 #include <type_traits>
 
 #include "act.h"
 #include "gemm_core.h"
 #include "luffy_common.h"
+#include "mx8.h"
 
 namespace luffy {
 namespace {
@@ -50,6 +52,12 @@ constexpr int kActDzGelu = 3, kActDzSilu = 4;
 // Epilogue codes of the backward's Z product: store Z to the output and
 // act(Z), taken on the rounded Z, to the second buffer.
 constexpr int kActZaGelu = 5, kActZaSilu = 6;
+// Epilogue codes of a first product that keeps Z: act(Z) to the output, Z in
+// microscaled 8 bits (from the float32 sums) beside it.
+constexpr int kActKeepGelu = 7, kActKeepSilu = 8;
+// Epilogue codes of the backward's dA product on a kept Z: dZ to the output,
+// act(Z) to the second buffer.
+constexpr int kActDz8Gelu = 9, kActDz8Silu = 10;
 
 // Tile shapes of the bf16 products: 256 output columns (weight rows, the P
 // operand) by up to 256 token rows (FfnGemm), or by up to 320 token rows
@@ -228,6 +236,35 @@ __device__ __forceinline__ void store_pair_row(const uint32_t (&pk)[4][2], int h
   }
 }
 
+// The 32 columns nb.. of row r, half of them in lane l and half in l + 32: Z in
+// microscaled 8 bits (they are one block) and act(Z) as bf16.  Returns the block's
+// scale byte.
+template <int ACT>
+__device__ __forceinline__ uint32_t keep_block(const f32x16& z, int r, int nb, int N, int hi,
+                                               uint16_t* __restrict__ out, uint8_t* __restrict__ kq) {
+  uint32_t most = 0;
+#pragma unroll
+  for (int v = 0; v < 16; ++v) most = max(most, __float_as_uint(z[v]) & 0x7FFFFFFFu);
+  most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), 32, 64)));
+  const uint32_t ex = mx8_exponent(most);
+  const float inv = mx8_inverse(min(ex, 248u));
+  uint32_t q8[4], pk[4][2];
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    q8[g] = ex == 255u ? 0u : mx8_pack(z[4 * g], z[4 * g + 1], z[4 * g + 2], z[4 * g + 3], inv);
+    pk[g][0] = pack_bf16x2(act_fast<ACT>(z[4 * g]), act_fast<ACT>(z[4 * g + 1]));
+    pk[g][1] = pack_bf16x2(act_fast<ACT>(z[4 * g + 2]), act_fast<ACT>(z[4 * g + 3]));
+  }
+  const size_t at = static_cast<size_t>(r) * N + nb + 16 * hi;
+  // 16 consecutive columns a lane: the low lane's last two words go to the high
+  // lane, the high lane's first two to the low one
+  const uint32_t r0 = static_cast<uint32_t>(__shfl_xor(static_cast<int>(hi ? q8[0] : q8[2]), 32, 64));
+  const uint32_t r1 = static_cast<uint32_t>(__shfl_xor(static_cast<int>(hi ? q8[1] : q8[3]), 32, 64));
+  *reinterpret_cast<uint4*>(kq + at) = hi ? make_uint4(r0, q8[2], r1, q8[3]) : make_uint4(q8[0], r0, q8[1], r1);
+  store_pair_row(pk, hi, out + at);
+  return ex;
+}
+
 // One output tile (or one K part of it) of shape G: rows row0.. of A
 // (through row_index when given) times the weight rows n0.. of We over K
 // range [k0, k1).  Stores bf16 (activation applied when FIRST), or, when
@@ -237,9 +274,13 @@ template <class G, int ACT, bool FIRST>
 __device__ __forceinline__ void ffn_tile(const uint16_t* __restrict__ A, const int32_t* __restrict__ row_index,
                                          const uint16_t* __restrict__ We, int K, int N, int k0, int k1, int row0,
                                          int rows, int n0, uint16_t* __restrict__ out, float* __restrict__ slot,
-                                         uint16_t* __restrict__ aux, uint8_t* lds) {
+                                         uint16_t* __restrict__ aux, const Kept8& kept, uint8_t* lds) {
   static_assert(G::FN <= 5, "ragged dispatch instantiates FN + 1 main loops");
   constexpr bool ZA = ACT == kActZaGelu || ACT == kActZaSilu;
+  constexpr bool KEEP = ACT == kActKeepGelu || ACT == kActKeepSilu, DZ8 = ACT == kActDz8Gelu || ACT == kActDz8Silu;
+  constexpr int kAct = ACT == kActKeepGelu || ACT == kActDz8Gelu   ? LUFFY_ACT_GELU
+                       : ACT == kActKeepSilu || ACT == kActDz8Silu ? LUFFY_ACT_SILU
+                                                                   : ACT;
   const int tid = opaque_tid(), lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = G::wave_m(w), wn = G::wave_n(w);
   uint32_t poff[G::LP], qoff[G::LQ];
@@ -263,12 +304,46 @@ __device__ __forceinline__ void ffn_tile(const uint16_t* __restrict__ A, const i
   if constexpr (ACT != kActDzGelu && ACT != kActDzSilu) {
     if (!slot) {
       const int hi = lane >> 5;
+      [[maybe_unused]] uint32_t scales[G::FN] = {};   // KEEP: the FM blocks' of a row
 #pragma unroll
       for (int fm = 0; fm < G::FM; ++fm) {
 #pragma unroll
         for (int fn = 0; fn < G::FN; ++fn) {
           const int ml = G::q_row(wn, fn) + (lane & 31);
           const int nb = n0 + wm * G::WTM + 32 * fm;
+          if constexpr (KEEP) {
+            if (ml < rows && nb < N)
+              scales[fn] |= keep_block<kAct>(acc[fm][fn], row0 + ml, nb, N, hi, out, kept.q) << (8 * fm);
+            continue;
+          }
+          if constexpr (DZ8) {
+            if (ml >= rows || nb >= N) continue;
+            const uint4 zw = *reinterpret_cast<const uint4*>(kept.q + static_cast<size_t>(row0 + ml) * N + nb + 16 * hi);
+            const float f =
+                mx8_scale(kept.s[(static_cast<size_t>(n0 >> 8) * kept.rows + row0 + ml) * 8 + ((nb >> 5) & 7)]);
+            const uint32_t r0 = static_cast<uint32_t>(__shfl_xor(static_cast<int>(hi ? zw.x : zw.y), 32, 64));
+            const uint32_t r1 = static_cast<uint32_t>(__shfl_xor(static_cast<int>(hi ? zw.z : zw.w), 32, 64));
+            const uint32_t z8[4] = {hi ? r0 : zw.x, hi ? r1 : zw.z, hi ? zw.y : r0, hi ? zw.w : r1};
+            uint32_t pd[4][2], pa[4][2];
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+              float z[4], dz[4];
+              mx8_unpack(z8[g], f, z);
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {
+                dz[q] = acc[fm][fn][4 * g + q] * act_grad<kAct>(z[q]);
+                z[q] = act_fast<kAct>(z[q]);
+              }
+              pd[g][0] = pack_bf16x2(dz[0], dz[1]);
+              pd[g][1] = pack_bf16x2(dz[2], dz[3]);
+              pa[g][0] = pack_bf16x2(z[0], z[1]);
+              pa[g][1] = pack_bf16x2(z[2], z[3]);
+            }
+            const size_t at = static_cast<size_t>(row0 + ml) * N + nb + 16 * hi;
+            store_pair_row(pd, hi, out + at);
+            store_pair_row(pa, hi, aux + at);
+            continue;
+          }
           if (ml >= rows || nb >= N) continue;
           uint32_t pk[4][2];
 #pragma unroll
@@ -277,7 +352,7 @@ __device__ __forceinline__ void ffn_tile(const uint16_t* __restrict__ A, const i
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
               z[q] = acc[fm][fn][4 * g + q];
-              if constexpr (FIRST && !ZA) z[q] = act_fast<ACT>(z[q]);
+              if constexpr (FIRST && !ZA && !DZ8) z[q] = act_fast<kAct>(z[q]);
             }
             pk[g][0] = pack_bf16x2(z[0], z[1]);
             pk[g][1] = pack_bf16x2(z[2], z[3]);
@@ -294,6 +369,19 @@ __device__ __forceinline__ void ffn_tile(const uint16_t* __restrict__ A, const i
                                        act_fast<A>(__uint_as_float(pk[g][q] & 0xFFFF0000u)));
             store_pair_row(pk, hi, aux + at);
           }
+        }
+      }
+      if constexpr (KEEP) {
+        // a tile is 256 columns, a wave's FM blocks of a row side by side (zeros past
+        // the last column); stored when the sums are done with: the addresses beside
+        // them made the kernel spill
+        static_assert(G::FM == 2 && G::WTM == 64 && G::BM == 256, "two scale bytes a row and wave");
+#pragma unroll
+        for (int fn = 0; fn < G::FN; ++fn) {
+          const int ml = G::q_row(wn, fn) + (lane & 31);
+          if (hi || ml >= rows) continue;
+          uint8_t* sc = kept.s + (static_cast<size_t>(n0 >> 8) * kept.rows + row0 + ml) * 8 + 2 * wm;
+          *reinterpret_cast<uint16_t*>(sc) = static_cast<uint16_t>(scales[fn]);
         }
       }
       return;
@@ -333,7 +421,7 @@ __device__ __forceinline__ void ffn_tile(const uint16_t* __restrict__ A, const i
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             z[q] = acc[fm][fn][4 * g + q];
-            if constexpr (FIRST && !ZA) z[q] = act_fast<ACT>(z[q]);
+            if constexpr (FIRST && !ZA) z[q] = act_fast<kAct>(z[q]);
           }
         }
         *reinterpret_cast<uint2*>(orow + n) = make_uint2(pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3]));
@@ -357,7 +445,7 @@ __global__ __launch_bounds__(FfnGemm::THREADS) void ffn_kernel_bf16(
     const uint16_t* __restrict__ A, const int32_t* __restrict__ row_index,
     const int32_t* __restrict__ rep_offsets, int E, int K, int N,
     const uint16_t* __restrict__ W, uint16_t* __restrict__ out, float* __restrict__ split_slots,
-    uint16_t* __restrict__ aux, int* __restrict__ tail) {
+    uint16_t* __restrict__ aux, int* __restrict__ tail, Kept8 kept) {
   // one LDS array: the operand ring, then the block's current tail item (a
   // second LDS variable would cost the K loop its DMA overlap)
   __shared__ __attribute__((aligned(16))) uint8_t lds[kFfnLds + 16];
@@ -399,11 +487,11 @@ __global__ __launch_bounds__(FfnGemm::THREADS) void ffn_kernel_bf16(
     using GW = std::conditional_t<WT, FfnGemmWideT, FfnGemmWide>;
     using GS = std::conditional_t<WT, FfnGemmSmallT, FfnGemmSmall>;
     if (shape == kShapeWide)
-      ffn_tile<GW, ACT, FIRST>(A, row_index, We, K, N, k0, k1, row0, rows, n0, out, slot, aux, lds);
+      ffn_tile<GW, ACT, FIRST>(A, row_index, We, K, N, k0, k1, row0, rows, n0, out, slot, aux, kept, lds);
     else if (shape == kShapeSmall)
-      ffn_tile<GS, ACT, FIRST>(A, row_index, We, K, N, k0, k1, row0, rows, n0, out, slot, aux, lds);
+      ffn_tile<GS, ACT, FIRST>(A, row_index, We, K, N, k0, k1, row0, rows, n0, out, slot, aux, kept, lds);
     else
-      ffn_tile<GN, ACT, FIRST>(A, row_index, We, K, N, k0, k1, row0, rows, n0, out, slot, aux, lds);
+      ffn_tile<GN, ACT, FIRST>(A, row_index, We, K, N, k0, k1, row0, rows, n0, out, slot, aux, kept, lds);
   }
 }
 
@@ -692,24 +780,26 @@ FfnWs carve_ffn(Carver& c, int max_rows, int d_ff, int dtype) {
 }
 
 
-template <int ACT>
+// KEEP: Z in microscaled 8 bits beside (bf16).
+template <int ACT, bool KEEP = false>
 void launch_ffn(const void* x, const int32_t* row_index, const int32_t* rep_offsets, int E, int d,
                 int d_ff, int dtype, const void* w1, const void* w2, int max_rows, void* y_rep,
-                const FfnWs& ws, hipStream_t s) {
+                const FfnWs& ws, hipStream_t s, const Kept8& kept = Kept8{}) {
+  constexpr int kFirst = !KEEP ? ACT : ACT == LUFFY_ACT_GELU ? kActKeepGelu : kActKeepSilu;
   void* hidden = ws.hidden;
   if (dtype == LUFFY_BF16) {
     const int grid = persistent_grid();
     launch("ffn_queue", ffn_queue_clear_kernel, 1, 64, 0, s, ws.queue, 2);
     {
-      launch("ffn1", ffn_kernel_bf16<ACT, true>, grid, FfnGemm::THREADS, 0, s, static_cast<const uint16_t*>(x),
+      launch("ffn1", ffn_kernel_bf16<kFirst, true>, grid, FfnGemm::THREADS, 0, s, static_cast<const uint16_t*>(x),
              row_index, rep_offsets, E, d, d_ff, static_cast<const uint16_t*>(w1), static_cast<uint16_t*>(hidden),
-             ws.split_slots, static_cast<uint16_t*>(nullptr), ws.queue);
+             ws.split_slots, static_cast<uint16_t*>(nullptr), ws.queue, kept);
     }
     {
       launch("ffn2", ffn_kernel_bf16<ACT, false>, grid, FfnGemm::THREADS, 0, s,
              static_cast<const uint16_t*>(hidden), nullptr, rep_offsets, E, d_ff, d,
              static_cast<const uint16_t*>(w2), static_cast<uint16_t*>(y_rep), ws.split_slots,
-             static_cast<uint16_t*>(nullptr), ws.queue + 1);
+             static_cast<uint16_t*>(nullptr), ws.queue + 1, Kept8{});
     }
     {
       launch("ffn2_reduce", ffn_split_reduce_kernel, 8 * grid, 256, 0, s, rep_offsets, E, d_ff, d, ws.split_slots,
@@ -745,6 +835,32 @@ __global__ __launch_bounds__(256) void gather_rows_kernel(const int32_t* __restr
     const uint4* src = reinterpret_cast<const uint4*>(x + static_cast<size_t>(row_index[r]) * d);
     uint4* dst = reinterpret_cast<uint4*>(xg + static_cast<size_t>(r) * d);
     for (int c = lane; c < d / 8; c += 64) dst[c] = src[c];
+  }
+}
+
+// The same from rows in microscaled 8 bits (their values are bf16 numbers);
+// row_index may be null.
+__global__ __launch_bounds__(256) void gather_rows_mx8_kernel(const int32_t* __restrict__ rep_offsets, int E, int d,
+                                                              Kept8 x, const int32_t* __restrict__ row_index,
+                                                              uint16_t* __restrict__ xg) {
+  const int R = rep_offsets[E];
+  const int lane = threadIdx.x & 63;
+  for (int r = blockIdx.x * 4 + (threadIdx.x >> 6); r < R; r += gridDim.x * 4) {
+    const size_t from = row_index ? row_index[r] : r;
+    for (int c = lane; c < d / 16; c += 64) {
+      const uint4 w = *reinterpret_cast<const uint4*>(x.q + from * d + 16 * c);
+      const float f = mx8_scale(x.s[(static_cast<size_t>(c >> 4) * x.rows + from) * 8 + ((c >> 1) & 7)]);
+      float a[4], b[4];
+      uint4* dst = reinterpret_cast<uint4*>(xg + static_cast<size_t>(r) * d + 16 * c);
+      mx8_unpack(w.x, f, a);
+      mx8_unpack(w.y, f, b);
+      dst[0] = make_uint4(pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]), pack_bf16x2(b[0], b[1]),
+                          pack_bf16x2(b[2], b[3]));
+      mx8_unpack(w.z, f, a);
+      mx8_unpack(w.w, f, b);
+      dst[1] = make_uint4(pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]), pack_bf16x2(b[0], b[1]),
+                          pack_bf16x2(b[2], b[3]));
+    }
   }
 }
 
@@ -843,10 +959,11 @@ struct FfnBwdWs {
   int* queue;   // kFfnQueueSets tail counters
 };
 
-FfnBwdWs carve_ffn_bwd(Carver& c, int max_rows, int E, int d, int d_ff) {
+// kept: Z comes from the forward.
+FfnBwdWs carve_ffn_bwd(Carver& c, int max_rows, int E, int d, int d_ff, bool kept = false) {
   (void)E;
   FfnBwdWs w;
-  w.z = c.take<uint16_t>(static_cast<size_t>(max_rows) * d_ff);
+  w.z = kept ? nullptr : c.take<uint16_t>(static_cast<size_t>(max_rows) * d_ff);
   w.a = c.take<uint16_t>(static_cast<size_t>(max_rows) * d_ff);
   w.dz = c.take<uint16_t>(static_cast<size_t>(max_rows) * d_ff);
   w.xg = c.take<uint16_t>(static_cast<size_t>(max_rows) * d);
@@ -855,27 +972,34 @@ FfnBwdWs carve_ffn_bwd(Carver& c, int max_rows, int E, int d, int d_ff) {
   return w;
 }
 
+// z (q not null): Z as the forward kept it, so that its product is left out; x8 (q
+// not null): the rows of x in microscaled 8 bits, in x's place.
 template <int ACT>
-void launch_ffn_bwd(const uint16_t* x, const int32_t* row_index, const int32_t* rep_offsets, int E, int d, int d_ff,
-                    const uint16_t* w1, const uint16_t* w2, int max_rows, const uint16_t* dy, uint16_t* dx,
-                    void* dw1, void* dw2, bool dw_bf16, const FfnBwdWs& ws, hipStream_t s) {
-  (void)max_rows;
+void launch_ffn_bwd(const uint16_t* x, const Kept8& x8, const int32_t* row_index, const int32_t* rep_offsets, int E,
+                    int d, int d_ff, const uint16_t* w1, const uint16_t* w2, const uint16_t* dy, uint16_t* dx,
+                    void* dw1, void* dw2, bool dw_bf16, const Kept8& z, const FfnBwdWs& ws, hipStream_t s) {
   const int grid = persistent_grid();
   const int egrid = 4 * grid;
   launch("ffn_queue", ffn_queue_clear_kernel, 1, 64, 0, s, ws.queue, 3);
-  // Z = X W1^T and A = act(Z), both from the product's epilogue (a pass of its
-  // own that read Z back took 14 us for 4021 rows of 4096)
-  constexpr int kZa = ACT == LUFFY_ACT_GELU ? kActZaGelu : kActZaSilu;
-  launch("bwd_z", ffn_kernel_bf16<kZa, true>, grid, FfnGemm::THREADS, 0, s, x, row_index, rep_offsets, E, d, d_ff, w1,
-         ws.z, ws.split_slots, ws.a, ws.queue);
   // dZ = (dY W2) act'(Z): W2 [E][d][d_ff] read K-major (k = output row o)
-  constexpr int kDz = ACT == LUFFY_ACT_GELU ? kActDzGelu : kActDzSilu;
-  launch("bwd_da", ffn_kernel_bf16<kDz, true, true>, grid, FfnGemm::THREADS, 0, s, dy, nullptr, rep_offsets, E, d,
-         d_ff, w2, ws.dz, ws.split_slots, ws.z, ws.queue + 1);
+  if (z.q) {
+    constexpr int kDz = ACT == LUFFY_ACT_GELU ? kActDz8Gelu : kActDz8Silu;
+    launch("bwd_da", ffn_kernel_bf16<kDz, true, true>, grid, FfnGemm::THREADS, 0, s, dy, nullptr, rep_offsets, E, d,
+           d_ff, w2, ws.dz, ws.split_slots, ws.a, ws.queue + 1, z);
+  } else {
+    // Z = X W1^T and A = act(Z), both from the product's epilogue (a pass of its
+    // own that read Z back took 14 us for 4021 rows of 4096)
+    constexpr int kZa = ACT == LUFFY_ACT_GELU ? kActZaGelu : kActZaSilu;
+    launch("bwd_z", ffn_kernel_bf16<kZa, true>, grid, FfnGemm::THREADS, 0, s, x, row_index, rep_offsets, E, d, d_ff,
+           w1, ws.z, ws.split_slots, ws.a, ws.queue, z);
+    constexpr int kDz = ACT == LUFFY_ACT_GELU ? kActDzGelu : kActDzSilu;
+    launch("bwd_da", ffn_kernel_bf16<kDz, true, true>, grid, FfnGemm::THREADS, 0, s, dy, nullptr, rep_offsets, E, d,
+           d_ff, w2, ws.dz, ws.split_slots, ws.z, ws.queue + 1, z);
+  }
   // dX = dZ W1: W1 [E][d_ff][d] read K-major, split over K as the forward's second product
   launch("bwd_dx", ffn_kernel_bf16<kActNone, false, true>, grid, FfnGemm::THREADS, 0, s,
          static_cast<const uint16_t*>(ws.dz), nullptr, rep_offsets, E, d_ff, d, w1, dx, ws.split_slots,
-         static_cast<uint16_t*>(nullptr), ws.queue + 2);
+         static_cast<uint16_t*>(nullptr), ws.queue + 2, z);
   launch("bwd_dx_reduce", ffn_split_reduce_kernel, 8 * grid, 256, 0, s, rep_offsets, E, d_ff, d, ws.split_slots, dx,
          grid);
   // dW2 = dY^T A, dW1 = dZ^T X (X's rows gathered first)
@@ -883,12 +1007,43 @@ void launch_ffn_bwd(const uint16_t* x, const int32_t* row_index, const int32_t* 
   launch("bwd_dw2", wgrad, grid, WgradGemm::THREADS, 0, s, dy, static_cast<const uint16_t*>(ws.a), rep_offsets, E, d,
          d_ff, dw2);
   const uint16_t* xr = x;
-  if (row_index) {
+  if (x8.q) {
+    launch("bwd_gather", gather_rows_mx8_kernel, egrid, 256, 0, s, rep_offsets, E, d, x8, row_index, ws.xg);
+    xr = ws.xg;
+  } else if (row_index) {
     launch("bwd_gather", gather_rows_kernel, egrid, 256, 0, s, rep_offsets, E, d, x, row_index, ws.xg);
     xr = ws.xg;
   }
   launch("bwd_dw1", wgrad, grid, WgradGemm::THREADS, 0, s, static_cast<const uint16_t*>(ws.dz), xr, rep_offsets, E,
          d_ff, d, dw1);
+}
+
+// Host checks that the two forwards, and the two backwards, share.
+int ffn_check(const char* fn, int E, int d, int d_ff, int dtype, int act, int max_rows) {
+  if (E <= 0 || d <= 0 || d_ff <= 0 || max_rows <= 0)
+    return fail(LUFFY_E_INVALID, "%s: E=%d d=%d d_ff=%d max_rows=%d", fn, E, d, d_ff, max_rows);
+  if (dtype != LUFFY_F32 && dtype != LUFFY_BF16) return fail(LUFFY_E_INVALID, "%s: unknown dtype %d", fn, dtype);
+  if (act != LUFFY_ACT_GELU && act != LUFFY_ACT_SILU)
+    return fail(LUFFY_E_INVALID, "%s: unknown activation %d", fn, act);
+  if (E > kMaxExperts) return fail(LUFFY_E_UNSUPPORTED, "%s: E=%d > %d", fn, E, kMaxExperts);
+  if (d % 64 != 0 || d_ff % 64 != 0)
+    return fail(LUFFY_E_UNSUPPORTED, "%s: d=%d d_ff=%d must be multiples of 64", fn, d, d_ff);
+  if (d > 32768 || d_ff > 32768)
+    return fail(LUFFY_E_UNSUPPORTED, "%s: d=%d d_ff=%d must be at most 32768", fn, d, d_ff);
+  if (static_cast<long long>(max_rows) * d_ff * elem_bytes(dtype) > 0xFFFF0000ll ||
+      static_cast<long long>(d) * d_ff * elem_bytes(dtype) > 0xFFFF0000ll)
+    return fail(LUFFY_E_UNSUPPORTED, "%s: hidden activations or one expert's weights exceed 4 GiB - 64 KiB", fn);
+  return LUFFY_OK;
+}
+
+bool kept_aligned(const void* q, const void* s) {
+  return !(reinterpret_cast<uintptr_t>(q) & 15u) && !(reinterpret_cast<uintptr_t>(s) & 7u);
+}
+
+bool aligned16(std::initializer_list<const void*> ps) {
+  uintptr_t bits = 0;
+  for (const void* p : ps) bits |= reinterpret_cast<uintptr_t>(p);
+  return (bits & 15u) == 0;
 }
 
 }  // namespace
@@ -983,11 +1138,78 @@ extern "C" int luffy_expert_ffn_backward(const void* x, const int32_t* row_index
   const auto* dyb = static_cast<const uint16_t*>(dy_rep);
   auto* dxb = static_cast<uint16_t*>(dx_rep);
   if (act == LUFFY_ACT_GELU)
-    launch_ffn_bwd<LUFFY_ACT_GELU>(xb, row_index, rep_offsets, E, d, d_ff, w1b, w2b, max_rows, dyb, dxb, dw1, dw2,
-                                   dw_dtype == LUFFY_BF16, ws, s);
+    launch_ffn_bwd<LUFFY_ACT_GELU>(xb, Kept8{}, row_index, rep_offsets, E, d, d_ff, w1b, w2b, dyb, dxb, dw1, dw2,
+                                   dw_dtype == LUFFY_BF16, Kept8{}, ws, s);
   else
-    launch_ffn_bwd<LUFFY_ACT_SILU>(xb, row_index, rep_offsets, E, d, d_ff, w1b, w2b, max_rows, dyb, dxb, dw1, dw2,
-                                   dw_dtype == LUFFY_BF16, ws, s);
+    launch_ffn_bwd<LUFFY_ACT_SILU>(xb, Kept8{}, row_index, rep_offsets, E, d, d_ff, w1b, w2b, dyb, dxb, dw1, dw2,
+                                   dw_dtype == LUFFY_BF16, Kept8{}, ws, s);
   return check_launch("luffy_expert_ffn_backward");
 }
 
+
+extern "C" int luffy_expert_ffn_keep(const void* x, const int32_t* row_index, const int32_t* rep_offsets, int E, int d,
+                                     int d_ff, const void* w1, const void* w2, int act, int max_rows, void* zq,
+                                     void* zs, void* y_rep, void* workspace, size_t workspace_bytes, void* stream) {
+  const char* fn = "luffy_expert_ffn_keep";
+  if (!x || !rep_offsets || !w1 || !w2 || !zq || !zs || !y_rep)
+    return fail(LUFFY_E_INVALID, "%s: null pointer argument", fn);
+  const int st = ffn_check(fn, E, d, d_ff, LUFFY_BF16, act, max_rows);
+  if (st != LUFFY_OK) return st;
+  if (!kept_aligned(zq, zs) || !aligned16({x, w1, w2, y_rep}))
+    return fail(LUFFY_E_INVALID, "%s: zs must be 8-byte, the other matrices 16-byte aligned", fn);
+  const size_t need = luffy_expert_ffn_workspace_size(max_rows, E, d_ff, LUFFY_BF16);
+  if (workspace_bytes < need || !workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u))
+    return fail(LUFFY_E_WORKSPACE, "%s: workspace needs %zu bytes, 256-aligned", fn, need);
+  Carver c(workspace);
+  const FfnWs ws = carve_ffn(c, max_rows, d_ff, LUFFY_BF16);
+  const Kept8 kept{static_cast<uint8_t*>(zq), static_cast<uint8_t*>(zs), max_rows};
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (act == LUFFY_ACT_GELU)
+    launch_ffn<LUFFY_ACT_GELU, true>(x, row_index, rep_offsets, E, d, d_ff, LUFFY_BF16, w1, w2, max_rows, y_rep, ws, s,
+                                     kept);
+  else
+    launch_ffn<LUFFY_ACT_SILU, true>(x, row_index, rep_offsets, E, d, d_ff, LUFFY_BF16, w1, w2, max_rows, y_rep, ws, s,
+                                     kept);
+  return check_launch(fn);
+}
+
+extern "C" size_t luffy_expert_ffn_backward_kept_workspace_size(int max_rows, int E, int d, int d_ff) {
+  if (max_rows <= 0 || E <= 0 || d <= 0 || d_ff <= 0) return 0;
+  Carver c(nullptr);
+  carve_ffn_bwd(c, max_rows, E, d, d_ff, true);
+  return c.size();
+}
+
+extern "C" int luffy_expert_ffn_backward_kept(const void* x, const void* x_scale, int x_rows, const int32_t* row_index,
+                                              const int32_t* rep_offsets, int E, int d, int d_ff, const void* w1,
+                                              const void* w2, int act, int max_rows, const void* zq, const void* zs,
+                                              const void* dy_rep, void* dx_rep, void* dw1, void* dw2, int dw_dtype,
+                                              void* workspace, size_t workspace_bytes, void* stream) {
+  const char* fn = "luffy_expert_ffn_backward_kept";
+  if (!x || !rep_offsets || !w1 || !w2 || !zq || !zs || !dy_rep || !dx_rep || !dw1 || !dw2)
+    return fail(LUFFY_E_INVALID, "%s: null pointer argument", fn);
+  if (dw_dtype != LUFFY_F32 && dw_dtype != LUFFY_BF16)
+    return fail(LUFFY_E_INVALID, "%s: unknown weight-gradient dtype %d", fn, dw_dtype);
+  if (x_scale && x_rows <= 0) return fail(LUFFY_E_INVALID, "%s: x_rows=%d of a microscaled x", fn, x_rows);
+  const int st = ffn_check(fn, E, d, d_ff, LUFFY_BF16, act, max_rows);
+  if (st != LUFFY_OK) return st;
+  if (!kept_aligned(zq, zs) || !kept_aligned(x, x_scale) || !aligned16({w1, w2, dy_rep, dx_rep, dw1, dw2}))
+    return fail(LUFFY_E_INVALID, "%s: scales must be 8-byte, the other matrices 16-byte aligned", fn);
+  // K-major reads of the activations run up to 63 rows past an expert's last
+  if ((static_cast<long long>(max_rows) + 64) * (d > d_ff ? d : d_ff) * 2 > 0xFFFF0000ll)
+    return fail(LUFFY_E_UNSUPPORTED, "%s: an operand exceeds 4 GiB - 64 KiB", fn);
+  const size_t need = luffy_expert_ffn_backward_kept_workspace_size(max_rows, E, d, d_ff);
+  if (workspace_bytes < need || !workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u))
+    return fail(LUFFY_E_WORKSPACE, "%s: workspace needs %zu bytes, 256-aligned", fn, need);
+  Carver c(workspace);
+  const FfnBwdWs ws = carve_ffn_bwd(c, max_rows, E, d, d_ff, true);
+  const auto bytes = [](const void* p) { return static_cast<uint8_t*>(const_cast<void*>(p)); };
+  const Kept8 z{bytes(zq), bytes(zs), max_rows}, x8 = x_scale ? Kept8{bytes(x), bytes(x_scale), x_rows} : Kept8{};
+  const auto* w1b = static_cast<const uint16_t*>(w1);
+  const auto* w2b = static_cast<const uint16_t*>(w2);
+  auto* launch_act = act == LUFFY_ACT_GELU ? launch_ffn_bwd<LUFFY_ACT_GELU> : launch_ffn_bwd<LUFFY_ACT_SILU>;
+  launch_act(static_cast<const uint16_t*>(x), x8, row_index, rep_offsets, E, d, d_ff, w1b, w2b,
+             static_cast<const uint16_t*>(dy_rep), static_cast<uint16_t*>(dx_rep), dw1, dw2, dw_dtype == LUFFY_BF16, z,
+             ws, static_cast<hipStream_t>(stream));
+  return check_launch(fn);
+}
