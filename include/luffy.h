@@ -31,7 +31,9 @@
  *  - Outputs must not alias inputs.  Integer outputs are deterministic: the
  *    same inputs give bit-identical indices on every run.
  *  - Supported sizes: d and d_ff multiples of 64 and at most 32768,
- *    1 <= E <= 64, k in {1, 2}, T*k < 2^31 (luffy_condense: T*k <= 2^24),
+ *    1 <= E <= 64, k in {1, 2} (luffy_route_scored, luffy_condense,
+ *    luffy_combine_many and its backward: 1 <= k <= 8), T*k < 2^31
+ *    (luffy_condense: T*k <= 2^24),
  *    every activation matrix and every expert's weight matrix smaller than
  *    4 GiB - 64 KiB.  Other sizes return LUFFY_E_UNSUPPORTED where the call
  *    can see them (x of luffy_expert_ffn, read through row_index, is the
@@ -357,6 +359,11 @@ int luffy_combine(const void* y_rep, const int32_t* rep_row,
                   const int32_t* slot_pos, const float* topk_gate,
                   int T, int k, int d, int dtype, void* y, void* stream);
 
+/* luffy_combine_many - luffy_combine for 1 <= k <= 8 slots a token, as
+ * luffy_route_scored leaves them. */
+int luffy_combine_many(const void* y_rep, const int32_t* rep_row, const int32_t* slot_pos, const float* topk_gate, int T,
+                       int k, int d, int dtype, void* y, void* stream);
+
 /* ------------------------------------------------------------------------
  * Backward of the condensed layer.  The paper trains the layer but does not
  * say how a gradient passes a condensed token; these calls differentiate the
@@ -386,6 +393,12 @@ int luffy_combine_backward(const void* dy, const void* y_rep, const int32_t* rep
                            const int32_t* rep_offsets, int E, int T, int k, int d, int dtype,
                            int max_rows, void* dy_rep, float* dgate,
                            void* workspace, size_t workspace_bytes, void* stream);
+
+/* luffy_combine_many_backward - the same for luffy_combine_many. */
+int luffy_combine_many_backward(const void* dy, const void* y_rep, const int32_t* rep_row, const int32_t* perm_token,
+                                const int32_t* slot_pos, const float* topk_gate, const int32_t* offsets,
+                                const int32_t* rep_offsets, int E, int T, int k, int d, int dtype, int max_rows,
+                                void* dy_rep, float* dgate, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
  * luffy_expert_ffn_backward - gradients of luffy_expert_ffn (Sec. 2.1: an
@@ -617,7 +630,10 @@ int luffy_adaptive_threshold(double l_ini, double l_prev, double* h_out);
  * ffn2_reduce, combine; backward: cbwd_group, cbwd_rows, cbwd_gate,
  * bwd_z, bwd_da, bwd_dx, bwd_dx_reduce, bwd_gather, bwd_dw2,
  * bwd_dw1; serving: mx4_quantize, mx4_dequantize, mx4_matmul, mx4_ffn1,
- * mx4_ffn2, few_gate, few_ffn1, few_ffn2.
+ * mx4_ffn2, few_gate, few_ffn1, few_ffn2; a block: block_norm,
+ * block_norm_backward, block_norm_reduce, scored_gate, scored_settle,
+ * scored_dlogits, scored_dx, scored_dw, scored_dw_reduce, mx8_quantize,
+ * mx8_dequantize.
  * ---------------------------------------------------------------------- */
 int luffy_profile_kernel(const char* name);
 int luffy_profile_read(double* total_ms, int* launches);

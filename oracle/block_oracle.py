@@ -195,4 +195,50 @@ def ffn_backward_kept(x_rows, z, offsets, w1, w2, act, dy):
     return dx, dw1, dw2
 
 
+# ------------------------------------------------------------ a whole block
+def block_forward(p, dec, cfg):
+    """o of a block with its decisions held fixed.  p: x, w_gate, b_gate, w1, w2,
+    w_pre, b_pre, w_post, b_post, gate (None where there is none); dec: idx,
+    slot_pos, rep_row, rep_of_pos, rep_token, rep_offsets; cfg: norm, eps,
+    res_scale, score, renormalise, scale, act.  Returns (o, what the backward
+    needs)."""
+    n = dict(norm=cfg["norm"], eps=cfg["eps"])
+    u = pre_norm(p["x"], w_pre=p["w_pre"], b_pre=p["b_pre"], **n)
+    l = u @ p["w_gate"].T + p["b_gate"]
+    g = gates(l, dec["idx"], cfg["score"], cfg["renormalise"], cfg["scale"])
+    off = dec["rep_offsets"]
+    R = int(off[-1])
+    z = np.zeros((R, p["w1"].shape[1]))
+    y_rep = np.zeros((R, u.shape[1]))
+    for e in range(len(off) - 1):
+        r = slice(int(off[e]), int(off[e + 1]))
+        z[r] = u[dec["rep_token"][r]] @ p["w1"][e].T
+        y_rep[r] = activation(z[r], cfg["act"]) @ p["w2"][e].T
+    kept = dec["slot_pos"] >= 0
+    row = np.where(kept, dec["rep_row"][np.maximum(dec["slot_pos"], 0)], 0)
+    y = (np.where(kept, g, 0.0)[..., None] * y_rep[row]).sum(1) if R else np.zeros_like(u)
+    o = block_norm(p["x"], y, res_scale=cfg["res_scale"], w_post=p["w_post"], b_post=p["b_post"], gate=p["gate"], **n)
+    return o, dict(u=u, l=l, g=g, z=z, y_rep=y_rep, y=y, o=o, row=row, kept=kept)
+
+
+def block_backward(p, dec, cfg, s, dout, dlogits=None):
+    """Gradients of block_forward (a dict: dx, dw_gate, ...) from what it left."""
+    n = dict(norm=cfg["norm"], eps=cfg["eps"])
+    out = block_norm_backward(s["y"], s["o"], dout, None, res_scale=cfg["res_scale"], w_post=p["w_post"],
+                              b_post=p["b_post"], gate=p["gate"], **n)
+    stream, dy = out.pop("dx"), out.pop("dy")
+    dg = np.where(s["kept"], (dy[:, None] * s["y_rep"][s["row"]]).sum(2), 0.0)
+    dy_rep = np.zeros_like(s["y_rep"])
+    for j in range(dg.shape[1]):
+        np.add.at(dy_rep, s["row"][s["kept"][:, j], j], (s["g"][:, j, None] * dy)[s["kept"][:, j]])
+    dx_rep, out["dw1"], out["dw2"] = ffn_backward_kept(s["u"][dec["rep_token"]], s["z"], dec["rep_offsets"], p["w1"],
+                                                       p["w2"], cfg["act"], dy_rep)
+    du, out["dw_gate"], out["db_gate"] = route_backward(
+        s["u"], p["w_gate"], s["l"], dec["idx"], dg, cfg["score"], cfg["renormalise"], cfg["scale"], dlogits, dx_rep,
+        dec["slot_pos"], dec["rep_of_pos"], dec["rep_row"])
+    pre = block_norm_backward(None, p["x"], stream, du, norm=cfg["norm"], eps=cfg["eps"], w_pre=p["w_pre"])
+    out.update(dx=pre["dx"], dw_pre=pre["dw_pre"], db_pre=pre["db_pre"])
+    return out
+
+
 __all__ = [n for n in dir() if not n.startswith("_") and n not in ("annotations", "math", "np")]

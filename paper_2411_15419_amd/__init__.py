@@ -30,7 +30,7 @@ __all__ = [
     "luffy_block_norm", "luffy_block_norm_backward", "block_norm_backward_workspace_size",
     "luffy_route_scored", "luffy_route_scored_backward", "route_scored_backward_workspace_size",
     "luffy_mx8_quantize", "luffy_mx8_dequantize", "luffy_expert_ffn_keep", "luffy_expert_ffn_backward_kept",
-    "expert_ffn_backward_kept_workspace_size",
+    "expert_ffn_backward_kept_workspace_size", "luffy_combine_many", "luffy_combine_many_backward", "MoEBlock",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libluffy.so")
@@ -72,6 +72,9 @@ _SIGS = {
     "luffy_expert_ffn": (_c_int, [_vp, _vp, _vp, _c_int, _c_int, _c_int, _c_int, _vp, _vp,
                                   _c_int, _c_int, _vp, _vp, _c_size, _vp]),
     "luffy_combine": (_c_int, [_vp, _vp, _vp, _vp, _c_int, _c_int, _c_int, _c_int, _vp, _vp]),
+    "luffy_combine_many": (_c_int, [_vp, _vp, _vp, _vp, _c_int, _c_int, _c_int, _c_int, _vp, _vp]),
+    "luffy_combine_many_backward": (_c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _c_int, _c_int, _c_int,
+                                             _c_int, _c_int, _c_int, _vp, _vp, _vp, _c_size, _vp]),
     "luffy_combine_backward_workspace_size": (_c_size, [_c_int, _c_int, _c_int]),
     "luffy_combine_backward": (_c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _c_int, _c_int, _c_int,
                                         _c_int, _c_int, _c_int, _vp, _vp, _vp, _c_size, _vp]),
@@ -720,6 +723,51 @@ def luffy_route_scored_backward(x, w_gate, score, logits, topk_idx, dgate, dx, d
         _stream(stream)), what)
 
 
+def luffy_combine_many(y_rep, rep_row, slot_pos, topk_gate, y, stream=None):
+    """luffy_combine for up to 8 slots a token."""
+    what = "luffy_combine_many"
+    T, k = slot_pos.shape
+    i32 = torch.int32
+    if y.dim() != 2 or y_rep.dim() != 2 or y_rep.dtype != y.dtype or y_rep.shape[1] != y.shape[1]:
+        raise LuffyError(f"{what}: y_rep {list(y_rep.shape)} and y {list(y.shape)} must be rows of one width and dtype")
+    d = y.shape[1]
+    _fits(what, "y", y, (T, d), y.dtype)
+    _fits(what, "slot_pos", slot_pos, (T, k), i32)
+    _fits(what, "topk_gate", topk_gate, (T, k), torch.float32)
+    _fits(what, "rep_row", rep_row, (T * k,), i32)
+    dt = _dtype_code(y)
+    y_rep, rep_row, slot_pos, topk_gate, y = _device_ptrs(what, y_rep, rep_row, slot_pos, topk_gate, y)
+    _check(load_library().luffy_combine_many(y_rep, rep_row, slot_pos, topk_gate, T, k, d, dt, y, _stream(stream)),
+           what)
+
+
+def luffy_combine_many_backward(dy, y_rep, rep_row, perm_token, slot_pos, topk_gate, offsets, rep_offsets, dy_rep,
+                                dgate, workspace, stream=None):
+    """luffy_combine_backward for up to 8 slots a token."""
+    what = "luffy_combine_many_backward"
+    T, k = slot_pos.shape
+    i32 = torch.int32
+    if dy.dim() != 2 or y_rep.dim() != 2 or y_rep.shape[1] != dy.shape[1]:
+        raise LuffyError(f"{what}: dy {list(dy.shape)} and y_rep {list(y_rep.shape)} must be rows of one width")
+    d, E, max_rows = dy.shape[1], offsets.numel() - 1, y_rep.shape[0]
+    _fits(what, "dy", dy, (T, d), y_rep.dtype)
+    _fits(what, "dy_rep", dy_rep, y_rep.shape, y_rep.dtype)
+    _fits(what, "slot_pos", slot_pos, (T, k), i32)
+    for name, t in (("rep_row", rep_row), ("perm_token", perm_token)):
+        _fits(what, name, t, (T * k,), i32)
+    for name, t in (("topk_gate", topk_gate), ("dgate", dgate)):
+        _fits(what, name, t, (T, k), torch.float32)
+    for name, t in (("offsets", offsets), ("rep_offsets", rep_offsets)):
+        _fits(what, name, t, (E + 1,), i32)
+    dt, ws_bytes = _dtype_code(dy), workspace.numel() * workspace.element_size()
+    (dy, y_rep, rep_row, perm_token, slot_pos, topk_gate, offsets, rep_offsets, dy_rep, dgate,
+     workspace) = _device_ptrs(what, dy, y_rep, rep_row, perm_token, slot_pos, topk_gate, offsets, rep_offsets, dy_rep,
+                               dgate, workspace)
+    _check(load_library().luffy_combine_many_backward(
+        dy, y_rep, rep_row, perm_token, slot_pos, topk_gate, offsets, rep_offsets, E, T, k, d, dt, max_rows, dy_rep,
+        dgate, workspace, ws_bytes, _stream(stream)), what)
+
+
 def adaptive_threshold(l_ini: float, l_prev: float) -> float:
     """h_t of Sec. 5.2 Eq. 2 from the first and the previous loss
     (luffy_adaptive_threshold)."""
@@ -975,6 +1023,145 @@ class ServingLayer(MoELayer):
                       self.step_gate[:n], y, self.ws_step, w1_scale=self.w1_scale, w2_scale=self.w2_scale,
                       stream=stream)
         return y
+
+
+class MoEBlock(MoELayer):
+    """A layer that learns, with what stands around it (bf16):
+        u = N(x; w_pre, b_pre),  y = the condensed layer of u,
+        o = res_scale x + gate N(y; w_post, b_post)
+    with the scored router (up to 8 experts a token), and between the forward and
+    the backward no more of the experts than their first product in microscaled 8
+    bits, and of u the same (keep8).
+
+    A block's last pass can be the next one's first: with `following` a call writes
+    following.u beside o (one read of the stream), and following is then called
+    with normed=True.  Buffers are allocated once; a block's outputs and gradients
+    are valid until its next call."""
+
+    def __init__(self, w_gate, b_gate, w1, w2, *, w_pre, b_pre=None, w_post=None, b_post=None, gate=None,
+                 res_scale: float = 1.0, norm: str = "rms", eps: float = 1e-6, score: str = "softmax", balance=None,
+                 groups: int = 1, top_groups: int = 1, group_best: int = 1, renormalise: bool = True,
+                 scale: float = 1.0, keep8: bool = True, **layer):
+        super().__init__(w_gate, b_gate, w1, w2, **layer)
+        if self.dtype != torch.bfloat16:
+            raise LuffyError("MoEBlock: the expert FFN backward is bf16 only")
+        if self.history and self.k > 2:
+            raise LuffyError("MoEBlock: historical similarity takes k <= 2")
+        self.w_pre, self.b_pre, self.w_post, self.b_post, self.gate = w_pre, b_pre, w_post, b_post, gate
+        self.res_scale, self.norm, self.eps = res_scale, norm, eps
+        self.score, self.balance, self.renormalise, self.scale, self.keep8 = score, balance, renormalise, scale, keep8
+        self.groups = dict(groups=groups, top_groups=top_groups, group_best=group_best)
+        T, S, E, d, d_ff, dev = self.T, self.T * self.k, self.E, self.d, self.d_ff, w1.device
+        bf = dict(dtype=torch.bfloat16, device=dev)
+
+        def mx8(rows, cols):
+            return (torch.empty(rows, cols, dtype=torch.int8, device=dev),
+                    torch.empty((cols + 255) // 256, rows, 8, dtype=torch.uint8, device=dev))
+
+        self.logits = torch.empty(T, E, dtype=torch.float32, device=dev)
+        self.u, self.o = torch.empty(T, d, **bf), torch.empty(T, d, **bf)
+        self.zq, self.zs = mx8(S, d_ff)
+        if keep8:
+            self.uq, self.us = mx8(T, d)
+        if self.buf.x_rep is not None:
+            raise LuffyError("MoEBlock: gather_x_rep is of no use here")
+
+    def route(self, x, stream=None):
+        b = self.buf
+        luffy_route_scored(x, self.w_gate, self.b_gate, self.k, self.score, self.cf, b.topk_idx, b.topk_gate,
+                           self.logits, b.slot_pos, b.perm_token, b.offsets, b.ws_route, balance=self.balance,
+                           renormalise=self.renormalise, scale=self.scale, inv_norm=b.inv_norm, stream=stream,
+                           **self.groups)
+
+    def expert_ffn(self, x, stream=None):
+        b = self.buf
+        luffy_expert_ffn_keep(x, b.rep_token, b.rep_offsets, self.w1, self.w2, self.act, self.T * self.k, self.zq,
+                              self.zs, b.y_rep, b.ws_ffn, stream)
+
+    def combine(self, stream=None):
+        b = self.buf
+        luffy_combine_many(b.y_rep, b.rep_row, b.slot_pos, b.topk_gate, b.y, stream)
+
+    def __call__(self, x, stream=None, threshold=None, hist_in=None, *, normed: bool = False, following=None):
+        """o [T, d] for the stream x.  normed: self.u holds N(x) already (the call
+        before this one had this block as its `following`)."""
+        kw = dict(norm=self.norm, eps=self.eps, stream=stream)
+        if x.shape != (self.T, self.d) or x.dtype != self.dtype:
+            raise LuffyError(f"x must be [{self.T}, {self.d}] {self.dtype}")
+        if following is not None and (following.norm, following.eps) != (self.norm, self.eps):
+            raise LuffyError("MoEBlock: blocks that share a pass must have the same norm and eps")
+        self.normed = normed
+        if not normed:
+            luffy_block_norm(x, None, None, self.u, w_pre=self.w_pre, b_pre=self.b_pre, **kw)
+        super().__call__(self.u, stream, threshold, hist_in)
+        if self.keep8:
+            luffy_mx8_quantize(self.u, self.uq, self.us, stream)
+        luffy_block_norm(x, self.buf.y, self.o, following.u if following else None, res_scale=self.res_scale,
+                         w_post=self.w_post, b_post=self.b_post, gate=self.gate,
+                         w_pre=following.w_pre if following else None, b_pre=following.b_pre if following else None,
+                         **kw)
+        return self.o
+
+    def _gradients(self, dw_dtype):
+        """Buffers of the backward, made on the first call."""
+        if getattr(self, "_bwd", None) is not None and self._bwd["dw1"].dtype == dw_dtype:
+            return self._bwd
+        T, S, E, d, d_ff, dev = self.T, self.T * self.k, self.E, self.d, self.d_ff, self.w1.device
+        f32 = dict(dtype=torch.float32, device=dev)
+
+        def vec(w):
+            return None if w is None else torch.empty(d, **f32)
+
+        rows = lambda n: torch.empty(n, d, dtype=torch.bfloat16, device=dev)  # noqa: E731
+        self._bwd = dict(
+            dx=rows(T), dstream=rows(T), dy=rows(T), du=rows(T), dy_rep=rows(S), dx_rep=rows(S),
+            dlayer=torch.empty(T, self.k, **f32), dw_gate=torch.empty(E, d, **f32), db_gate=torch.empty(E, **f32),
+            dw1=torch.empty(E, d_ff, d, dtype=dw_dtype, device=dev),
+            dw2=torch.empty(E, d, d_ff, dtype=dw_dtype, device=dev),
+            dgate=None if self.gate is None else torch.empty_like(self.gate), dw_post=vec(self.w_post),
+            db_post=vec(self.b_post), dw_pre=vec(self.w_pre), db_pre=vec(self.b_pre),
+            ws_n=_workspace(block_norm_backward_workspace_size(T, d), dev),
+            ws_c=_workspace(combine_backward_workspace_size(T, self.k, S), dev),
+            ws_f=_workspace(expert_ffn_backward_kept_workspace_size(S, E, d, d_ff), dev),
+            ws_r=_workspace(route_scored_backward_workspace_size(T, d, E), dev))
+        return self._bwd
+
+    def backward(self, x, dout, stream=None, dw_dtype=torch.float32, *, dlogits=None, following=None):
+        """Gradients of the last call for dout = dL/do (bf16 [T, d]) and, where an
+        auxiliary loss has one, dlogits (float32 [T, E]); the condensation and the
+        choices are held fixed.  With the call's `following` its backward comes
+        first, and dout is what it returned.  Returns (dx, gradients): a dict of
+        dw1, dw2 (dw_dtype), dw_gate, db_gate, and dgate, dw_post, db_post, dw_pre,
+        db_pre as far as the block has them; a block called with normed=True
+        leaves dx and its dw_pre, db_pre to the block before it (dx is then the
+        stream's gradient without the norm's share)."""
+        b, g = self.buf, self._gradients(dw_dtype)
+        kw = dict(norm=self.norm, eps=self.eps, stream=stream)
+        S = self.T * self.k
+        nxt = following._bwd if following is not None else {}
+        luffy_block_norm_backward(b.y, self.o, dout, nxt.get("du"), g["dstream"], g["dy"], g["ws_n"],
+                                  res_scale=self.res_scale, w_post=self.w_post, b_post=self.b_post, gate=self.gate,
+                                  w_pre=following.w_pre if following else None, dgate=g["dgate"],
+                                  dw_post=g["dw_post"], db_post=g["db_post"], dw_pre=nxt.get("dw_pre"),
+                                  db_pre=nxt.get("db_pre"), **kw)
+        luffy_combine_many_backward(g["dy"], b.y_rep, b.rep_row, b.perm_token, b.slot_pos, b.topk_gate, b.offsets,
+                                    b.rep_offsets, g["dy_rep"], g["dlayer"], g["ws_c"], stream)
+        u, us = (self.uq, self.us) if self.keep8 else (self.u, None)
+        luffy_expert_ffn_backward_kept(u, us, b.rep_token, b.rep_offsets, self.w1, self.w2, self.act, S, self.zq,
+                                       self.zs, g["dy_rep"], g["dx_rep"], g["dw1"], g["dw2"], g["ws_f"], stream)
+        if self.keep8:
+            luffy_mx8_dequantize(self.uq, self.us, self.u, stream)
+        luffy_route_scored_backward(self.u, self.w_gate, self.score, self.logits, b.topk_idx, g["dlayer"], g["du"],
+                                    g["dw_gate"], g["db_gate"], g["ws_r"], renormalise=self.renormalise,
+                                    scale=self.scale, dlogits=dlogits, dx_rep=g["dx_rep"], slot_pos=b.slot_pos,
+                                    rep_of_pos=b.rep_of_pos, rep_row=b.rep_row, stream=stream)
+        dx = g["dstream"]
+        if not self.normed:
+            dx = g["dx"]
+            luffy_block_norm_backward(None, x, g["dstream"], g["du"], dx, None, g["ws_n"], w_pre=self.w_pre,
+                                      dw_pre=g["dw_pre"], db_pre=g["db_pre"], **kw)
+        names = ("dw1", "dw2", "dw_gate", "db_gate", "dgate", "dw_post", "db_post", "dw_pre", "db_pre")
+        return dx, {n: g[n] for n in names if g[n] is not None}
 
 
 class MoEStack:

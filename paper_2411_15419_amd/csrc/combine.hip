@@ -17,9 +17,9 @@ namespace {
 // the host against T*k rows).
 constexpr uint32_t kRange = 0xFFFF0000u;
 
-// K: slots per token (1 or 2); U: 16-byte chunks per lane per pass (2 when
-// two passes' worth of chunks cover a row, else 4), so no load is issued for
-// a source or a chunk that cannot exist.
+// K: slots per token (1 to 8); U: 16-byte chunks per lane per pass (2 when
+// two passes' worth of chunks cover a row or with more than two slots, else 4), so
+// no load is issued for a source or a chunk that cannot exist.
 template <bool BF16, int K, int U>
 __global__ __launch_bounds__(256) void combine_kernel(const void* __restrict__ y_rep,
                                                       const int32_t* __restrict__ rep_row,
@@ -36,9 +36,12 @@ __global__ __launch_bounds__(256) void combine_kernel(const void* __restrict__ y
   const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(y_rep),
                                                                        static_cast<short>(0),
                                                                        static_cast<int>(kRange), 0x00020000);
-  uint32_t rbase[2] = {kRange, kRange};
-  float g[2] = {0.f, 0.f};
+  uint32_t rbase[K];
+  float g[K];
+#pragma unroll
   for (int j = 0; j < k; ++j) {
+    rbase[j] = kRange;
+    g[j] = 0.f;
     const int p = slot_pos[static_cast<size_t>(t) * k + j];
     if (p >= 0) {
       rbase[j] = static_cast<uint32_t>(rep_row[p]) * static_cast<uint32_t>(d) * ES;
@@ -278,7 +281,13 @@ __global__ __launch_bounds__(256) void cbwd_rows_kernel(const void* __restrict__
         const int mm = min(m + u, m1 - 1);
         const int p = list[mm];
         t[u] = perm_token[p];
-        const int j = (K == 2 && slot_pos[static_cast<size_t>(t[u]) * K] != p) ? 1 : 0;
+        int j = 0;   // the token's slot at position p
+        if constexpr (K == 2) {
+          j = slot_pos[static_cast<size_t>(t[u]) * K] != p ? 1 : 0;
+        } else {
+#pragma unroll
+          for (int i = 1; i < K; ++i) j = slot_pos[static_cast<size_t>(t[u]) * K + i] == p ? i : j;
+        }
         g[u] = m + u < m1 ? gate[static_cast<size_t>(t[u]) * K + j] : 0.f;
       }
       if (col) {
@@ -377,19 +386,20 @@ __global__ __launch_bounds__(256) void cbwd_gate_kernel(const void* __restrict__
 
 using namespace luffy;
 
-extern "C" int luffy_combine(const void* y_rep, const int32_t* rep_row,
-                             const int32_t* slot_pos, const float* topk_gate,
-                             int T, int k, int d, int dtype, void* y, void* stream) {
+namespace {
+
+int combine_run(const char* fn, int most_k, const void* y_rep, const int32_t* rep_row, const int32_t* slot_pos,
+                const float* topk_gate, int T, int k, int d, int dtype, void* y, void* stream) {
   if (!y_rep || !rep_row || !slot_pos || !topk_gate || !y)
-    return fail(LUFFY_E_INVALID, "luffy_combine: null pointer argument");
-  if (T <= 0 || d <= 0) return fail(LUFFY_E_INVALID, "luffy_combine: T=%d d=%d", T, d);
-  if (k != 1 && k != 2) return fail(LUFFY_E_INVALID, "luffy_combine: k=%d must be 1 or 2", k);
+    return fail(LUFFY_E_INVALID, "%s: null pointer argument", fn);
+  if (T <= 0 || d <= 0) return fail(LUFFY_E_INVALID, "%s: T=%d d=%d", fn, T, d);
+  if (k < 1 || k > most_k) return fail(LUFFY_E_INVALID, "%s: k=%d must be 1 to %d", fn, k, most_k);
   if (dtype != LUFFY_F32 && dtype != LUFFY_BF16)
-    return fail(LUFFY_E_INVALID, "luffy_combine: unknown dtype %d", dtype);
-  if (d % 64 != 0) return fail(LUFFY_E_UNSUPPORTED, "luffy_combine: d=%d not a multiple of 64", d);
+    return fail(LUFFY_E_INVALID, "%s: unknown dtype %d", fn, dtype);
+  if (d % 64 != 0) return fail(LUFFY_E_UNSUPPORTED, "%s: d=%d not a multiple of 64", fn, d);
   if (static_cast<double>(T) * k * d * (dtype == LUFFY_BF16 ? 2 : 4) >= static_cast<double>(kRange))
-    return fail(LUFFY_E_UNSUPPORTED, "luffy_combine: y_rep of up to T*k=%lld rows of d=%d must span < 4 GiB - 64 KiB",
-                static_cast<long long>(T) * k, d);
+    return fail(LUFFY_E_UNSUPPORTED, "%s: y_rep of up to T*k=%lld rows of d=%d must span < 4 GiB - 64 KiB",
+                fn, static_cast<long long>(T) * k, d);
   hipStream_t s = static_cast<hipStream_t>(stream);
   // Top-2 (two source rows a token) takes the column-sliced kernel when a
   // row's 16-byte chunks split into eight slices of 2^n (n <= 6) or of a
@@ -410,21 +420,44 @@ extern "C" int luffy_combine(const void* y_rep, const int32_t* rep_row,
     if (dtype == LUFFY_BF16) LUFFY_COMBINE_S(true, 2, 4);
     else LUFFY_COMBINE_S(false, 2, 4);
 #undef LUFFY_COMBINE_S
-    return check_launch("luffy_combine");
+    return check_launch(fn);
   }
   const int blocks = (T + 3) / 4;
   const bool two = d * (dtype == LUFFY_BF16 ? 2 : 4) <= 2 * 64 * 16;   // two chunks per lane cover a row
 #define LUFFY_COMBINE(BF, K_, U_) launch("combine", combine_kernel<BF, K_, U_>, blocks, 256, 0, s, y_rep, rep_row, \
                                          slot_pos, topk_gate, T, d, y)
-  if (dtype == LUFFY_BF16) {
+#define LUFFY_COMBINE_K(K_) \
+  do { if (dtype == LUFFY_BF16) LUFFY_COMBINE(true, K_, 2); else LUFFY_COMBINE(false, K_, 2); } while (0)
+  if (k > 2) {
+    if (k == 3) LUFFY_COMBINE_K(3);
+    else if (k == 4) LUFFY_COMBINE_K(4);
+    else if (k == 5) LUFFY_COMBINE_K(5);
+    else if (k == 6) LUFFY_COMBINE_K(6);
+    else if (k == 7) LUFFY_COMBINE_K(7);
+    else LUFFY_COMBINE_K(8);
+  } else if (dtype == LUFFY_BF16) {
     if (k == 1) { if (two) LUFFY_COMBINE(true, 1, 2); else LUFFY_COMBINE(true, 1, 4); }
     else { if (two) LUFFY_COMBINE(true, 2, 2); else LUFFY_COMBINE(true, 2, 4); }
   } else {
     if (k == 1) { if (two) LUFFY_COMBINE(false, 1, 2); else LUFFY_COMBINE(false, 1, 4); }
     else { if (two) LUFFY_COMBINE(false, 2, 2); else LUFFY_COMBINE(false, 2, 4); }
   }
+#undef LUFFY_COMBINE_K
 #undef LUFFY_COMBINE
-  return check_launch("luffy_combine");
+  return check_launch(fn);
+}
+
+}  // namespace
+
+extern "C" int luffy_combine(const void* y_rep, const int32_t* rep_row,
+                             const int32_t* slot_pos, const float* topk_gate,
+                             int T, int k, int d, int dtype, void* y, void* stream) {
+  return combine_run("luffy_combine", 2, y_rep, rep_row, slot_pos, topk_gate, T, k, d, dtype, y, stream);
+}
+
+extern "C" int luffy_combine_many(const void* y_rep, const int32_t* rep_row, const int32_t* slot_pos,
+                                  const float* topk_gate, int T, int k, int d, int dtype, void* y, void* stream) {
+  return combine_run("luffy_combine_many", 8, y_rep, rep_row, slot_pos, topk_gate, T, k, d, dtype, y, stream);
 }
 
 struct CbwdWs {
@@ -447,26 +480,26 @@ extern "C" size_t luffy_combine_backward_workspace_size(int T, int k, int max_ro
   return c.size();
 }
 
-extern "C" int luffy_combine_backward(const void* dy, const void* y_rep, const int32_t* rep_row,
-                                      const int32_t* perm_token, const int32_t* slot_pos,
-                                      const float* topk_gate, const int32_t* offsets,
-                                      const int32_t* rep_offsets, int E, int T, int k, int d, int dtype,
-                                      int max_rows, void* dy_rep, float* dgate, void* workspace,
-                                      size_t workspace_bytes, void* stream) {
+namespace {
+
+int combine_backward_run(const char* fn, int most_k, const void* dy, const void* y_rep, const int32_t* rep_row, const int32_t* perm_token,
+                         const int32_t* slot_pos, const float* topk_gate, const int32_t* offsets,
+                         const int32_t* rep_offsets, int E, int T, int k, int d, int dtype, int max_rows, void* dy_rep,
+                         float* dgate, void* workspace, size_t workspace_bytes, void* stream) {
   if (!dy || !y_rep || !rep_row || !perm_token || !slot_pos || !topk_gate || !offsets || !rep_offsets ||
       !dy_rep || !dgate)
-    return fail(LUFFY_E_INVALID, "luffy_combine_backward: null pointer argument");
+    return fail(LUFFY_E_INVALID, "%s: null pointer argument", fn);
   if (T <= 0 || d <= 0 || E <= 0 || max_rows <= 0)
-    return fail(LUFFY_E_INVALID, "luffy_combine_backward: T=%d d=%d E=%d max_rows=%d", T, d, E, max_rows);
-  if (k != 1 && k != 2) return fail(LUFFY_E_INVALID, "luffy_combine_backward: k=%d must be 1 or 2", k);
+    return fail(LUFFY_E_INVALID, "%s: T=%d d=%d E=%d max_rows=%d", fn, T, d, E, max_rows);
+  if (k < 1 || k > most_k) return fail(LUFFY_E_INVALID, "%s: k=%d must be 1 to %d", fn, k, most_k);
   if (dtype != LUFFY_F32 && dtype != LUFFY_BF16)
-    return fail(LUFFY_E_INVALID, "luffy_combine_backward: unknown dtype %d", dtype);
-  if (d % 64 != 0) return fail(LUFFY_E_UNSUPPORTED, "luffy_combine_backward: d=%d not a multiple of 64", d);
+    return fail(LUFFY_E_INVALID, "%s: unknown dtype %d", fn, dtype);
+  if (d % 64 != 0) return fail(LUFFY_E_UNSUPPORTED, "%s: d=%d not a multiple of 64", fn, d);
   if (static_cast<long long>(T) * k >= (1ll << 31))
-    return fail(LUFFY_E_UNSUPPORTED, "luffy_combine_backward: T*k >= 2^31");
+    return fail(LUFFY_E_UNSUPPORTED, "%s: T*k >= 2^31", fn);
   const size_t need = luffy_combine_backward_workspace_size(T, k, max_rows);
   if (workspace_bytes < need || !workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u))
-    return fail(LUFFY_E_WORKSPACE, "luffy_combine_backward: workspace needs %zu bytes, 256-aligned", need);
+    return fail(LUFFY_E_WORKSPACE, "%s: workspace needs %zu bytes, 256-aligned", fn, need);
   hipStream_t s = static_cast<hipStream_t>(stream);
   Carver c(workspace);
   const CbwdWs ws = carve_cbwd(c, max_rows, static_cast<long long>(T) * k);
@@ -491,9 +524,35 @@ extern "C" int luffy_combine_backward(const void* dy, const void* y_rep, const i
     launch("cbwd_gate", cbwd_gate_kernel<BF, K_>, blocks, 256, 0, s, dy, y_rep, rep_row, slot_pos, max_rows,   \
            T, d, dgate);                                                                                       \
   } while (0)
-  if (dtype == LUFFY_BF16) { if (k == 1) LUFFY_CBWD(true, 1); else LUFFY_CBWD(true, 2); }
-  else { if (k == 1) LUFFY_CBWD(false, 1); else LUFFY_CBWD(false, 2); }
+#define LUFFY_CBWD_K(K_) \
+  do { if (dtype == LUFFY_BF16) LUFFY_CBWD(true, K_); else LUFFY_CBWD(false, K_); } while (0)
+  if (k == 1) LUFFY_CBWD_K(1);
+  else if (k == 2) LUFFY_CBWD_K(2);
+  else if (k == 3) LUFFY_CBWD_K(3);
+  else if (k == 4) LUFFY_CBWD_K(4);
+  else if (k == 5) LUFFY_CBWD_K(5);
+  else if (k == 6) LUFFY_CBWD_K(6);
+  else if (k == 7) LUFFY_CBWD_K(7);
+  else LUFFY_CBWD_K(8);
+#undef LUFFY_CBWD_K
 #undef LUFFY_CBWD
-  return check_launch("luffy_combine_backward");
+  return check_launch(fn);
 }
 
+}  // namespace
+
+extern "C" int luffy_combine_backward(const void* dy, const void* y_rep, const int32_t* rep_row, const int32_t* perm_token,
+                         const int32_t* slot_pos, const float* topk_gate, const int32_t* offsets,
+                         const int32_t* rep_offsets, int E, int T, int k, int d, int dtype, int max_rows, void* dy_rep,
+                         float* dgate, void* workspace, size_t workspace_bytes, void* stream) {
+  return combine_backward_run("luffy_combine_backward", 2, dy, y_rep, rep_row, perm_token, slot_pos, topk_gate, offsets,
+                              rep_offsets, E, T, k, d, dtype, max_rows, dy_rep, dgate, workspace, workspace_bytes, stream);
+}
+
+extern "C" int luffy_combine_many_backward(const void* dy, const void* y_rep, const int32_t* rep_row, const int32_t* perm_token,
+                         const int32_t* slot_pos, const float* topk_gate, const int32_t* offsets,
+                         const int32_t* rep_offsets, int E, int T, int k, int d, int dtype, int max_rows, void* dy_rep,
+                         float* dgate, void* workspace, size_t workspace_bytes, void* stream) {
+  return combine_backward_run("luffy_combine_many_backward", 8, dy, y_rep, rep_row, perm_token, slot_pos, topk_gate, offsets,
+                              rep_offsets, E, T, k, d, dtype, max_rows, dy_rep, dgate, workspace, workspace_bytes, stream);
+}

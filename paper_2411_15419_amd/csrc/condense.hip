@@ -3139,14 +3139,14 @@ using namespace luffy;
 
 namespace {
 
-int condense_check(const char* fn, const void* x, int T, int d, int dtype, const int32_t* perm_token,
+int condense_check(const char* fn, int most_k, const void* x, int T, int d, int dtype, const int32_t* perm_token,
                    const int32_t* offsets, int E, int k, int max_bucket, float threshold, const int32_t* rep_of_pos,
                    const int32_t* rep_row, const int32_t* rep_offsets, const int32_t* rep_token) {
   if (!x || !perm_token || !offsets || !rep_of_pos || !rep_row || !rep_offsets || !rep_token)
     return fail(LUFFY_E_INVALID, "%s: null pointer argument", fn);
   if (T <= 0 || d <= 0 || E <= 0 || max_bucket < 0)
     return fail(LUFFY_E_INVALID, "%s: T=%d d=%d E=%d max_bucket=%d", fn, T, d, E, max_bucket);
-  if (k != 1 && k != 2) return fail(LUFFY_E_INVALID, "%s: k=%d must be 1 or 2", fn, k);
+  if (k < 1 || k > most_k) return fail(LUFFY_E_INVALID, "%s: k=%d must be 1 to %d", fn, k, most_k);
   if (dtype != LUFFY_F32 && dtype != LUFFY_BF16) return fail(LUFFY_E_INVALID, "%s: unknown dtype %d", fn, dtype);
   if (threshold != threshold) return fail(LUFFY_E_INVALID, "%s: threshold is NaN", fn);
   if (E > kMaxExperts) return fail(LUFFY_E_UNSUPPORTED, "%s: E=%d > %d", fn, E, kMaxExperts);
@@ -3335,7 +3335,7 @@ extern "C" int luffy_condense(const void* x, int T, int d, int dtype,
                               int32_t* rep_offsets, int32_t* rep_token,
                               void* x_rep, int32_t* degree, const float* inv_norm,
                               void* workspace, size_t workspace_bytes, void* stream) {
-  const int st = condense_check("luffy_condense", x, T, d, dtype, perm_token, offsets, E, k, max_bucket, threshold,
+  const int st = condense_check("luffy_condense", 8, x, T, d, dtype, perm_token, offsets, E, k, max_bucket, threshold,
                                 rep_of_pos, rep_row, rep_offsets, rep_token);
   if (st != LUFFY_OK) return st;
   const size_t need = luffy_condense_workspace_size(T, d, E, k, max_bucket);
@@ -3380,7 +3380,7 @@ extern "C" int luffy_condense_history(const void* x, int T, int d, int dtype,
                                       unsigned long long* stats,
                                       void* workspace, size_t workspace_bytes, void* stream) {
   const char* fn = "luffy_condense_history";
-  const int st = condense_check(fn, x, T, d, dtype, perm_token, offsets, E, k, max_bucket, threshold, rep_of_pos,
+  const int st = condense_check(fn, 2, x, T, d, dtype, perm_token, offsets, E, k, max_bucket, threshold, rep_of_pos,
                                 rep_row, rep_offsets, rep_token);
   if (st != LUFFY_OK) return st;
   if (hist_out && !slot_pos) return fail(LUFFY_E_INVALID, "%s: hist_out needs slot_pos", fn);

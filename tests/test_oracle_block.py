@@ -119,3 +119,31 @@ def test_kept_ffn_gradients(act):
     check(lambda a: loss(a, w1, w2), x, dx, rng)
     check(lambda a: loss(x, a, w2), w1, dw1, rng)
     check(lambda a: loss(x, w1, a), w2, dw2, rng)
+
+
+@pytest.mark.parametrize("norm,score,renorm", [("rms", "sigmoid", True), ("layer", "softmax", False)])
+def test_block_gradients(norm, score, renorm):
+    rng = np.random.default_rng(11)
+    T, d, E, k, f = 6, 8, 4, 3, 10
+    p = dict(x=rng.standard_normal((T, d)), w_gate=0.3 * rng.standard_normal((E, d)), b_gate=rng.standard_normal(E),
+             w1=rng.standard_normal((E, f, d)), w2=rng.standard_normal((E, d, f)), w_pre=1 + 0.1 * rng.standard_normal(d),
+             b_pre=0.1 * rng.standard_normal(d), w_post=1 + 0.1 * rng.standard_normal(d),
+             b_post=0.1 * rng.standard_normal(d), gate=rng.standard_normal(d))
+    cfg = dict(norm=norm, eps=1e-3, res_scale=0.8, score=score, renormalise=renorm, scale=1.5, act="gelu")
+    u = B.pre_norm(p["x"], norm=norm, eps=1e-3, w_pre=p["w_pre"], b_pre=p["b_pre"])
+    idx = B.choose(u @ p["w_gate"].T + p["b_gate"], k, score)
+    slot_pos, perm, off = B.buckets(idx, E, 0.9)
+    rep = rng.random(len(perm)) < 0.6
+    rep[off[:-1][off[:-1] < len(perm)]] = True
+    rep_of = np.maximum.accumulate(np.where(rep, np.arange(len(perm)), -1))
+    dec = dict(idx=idx, slot_pos=slot_pos, rep_of_pos=rep_of, rep_row=(np.cumsum(rep) - 1)[rep_of],
+               rep_token=perm[rep], rep_offsets=np.concatenate([[0], np.cumsum(rep)])[off])
+    dout, dl = rng.standard_normal((T, d)), 0.1 * rng.standard_normal((T, E))
+
+    def loss(p):
+        o, s = B.block_forward(p, dec, cfg)
+        return (dout * o).sum() + (dl * s["l"]).sum()
+
+    g = B.block_backward(p, dec, cfg, B.block_forward(p, dec, cfg)[1], dout, dl)
+    for name in p:
+        check(lambda a: loss(dict(p, **{name: a})), p[name], g["d" + name], rng)
