@@ -156,7 +156,7 @@ int luffy_route_noalloc(const void* x, int T, int d, int dtype,
  *           chosen only where nothing else is left), not +infinity
  *   topk_gate [T, k] scale * s, or scale * s / (sum of the k chosen s) with
  *           renormalise
- *   logits  [T, E] float or NULL: l, for luffy_route_scored_backward
+ *   logits  [T, E] float: l, for luffy_route_scored_backward
  * Choices are those of exact logits: float32 sums decide where their error bound
  * allows, the other tokens are decided in float64.  Everything else (capacity,
  * slot_pos, perm_token, offsets, inv_norm) as for luffy_route; workspace:
@@ -631,7 +631,7 @@ int luffy_adaptive_threshold(double l_ini, double l_prev, double* h_out);
  * bwd_z, bwd_da, bwd_dx, bwd_dx_reduce, bwd_gather, bwd_dw2,
  * bwd_dw1; serving: mx4_quantize, mx4_dequantize, mx4_matmul, mx4_ffn1,
  * mx4_ffn2, few_gate, few_ffn1, few_ffn2; a block: block_norm,
- * block_norm_backward, block_norm_reduce, scored_gate, scored_settle,
+ * block_norm_backward, block_norm_reduce, scored_gate, scored_choose,
  * scored_dlogits, scored_dx, scored_dw, scored_dw_reduce, mx8_quantize,
  * mx8_dequantize.
  * ---------------------------------------------------------------------- */

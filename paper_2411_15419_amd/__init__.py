@@ -658,8 +658,8 @@ def luffy_route_scored(x, w_gate, b_gate, k, score, capacity_factor, topk_idx, t
                        scale=1.0, inv_norm=None, stream=None):
     """luffy_route with "softmax" or "sigmoid" scores, a bias for balance
     (float32 [E], in the choice alone), the experts of the top_groups best of
-    `groups` groups, and up to 8 experts a token.  logits (float32 [T, E] or None)
-    are what luffy_route_scored_backward needs."""
+    `groups` groups, and up to 8 experts a token.  logits (float32 [T, E]) are what
+    luffy_route_scored_backward needs."""
     what = "luffy_route_scored"
     T, d, E = _router_shapes(what, x, w_gate)
     f32, i32 = torch.float32, torch.int32

@@ -3,12 +3,11 @@
 // token.
 //
 // Forward kernels:
-//   scored_gate    logits on MFMA (float32 sums), scores and a first choice; a token
-//                  with a deciding gap within the sums' error bound is marked (its
-//                  experts stored as -1 - e)
-//   scored_settle  decides the marked tokens in float64 from exact products, ranks
-//                  every slot among its chunk's slots of the same expert, and leaves
-//                  the chunks' counts
+//   scored_gate    logits by float32 sums on MFMA, and a bound on their error
+//   scored_choose  scores and choices; a token with a deciding gap within the bound is
+//                  decided in float64 from exact products; ranks every slot among its
+//                  chunk's slots of the same expert and leaves the chunks' counts
+//                  (64 tokens or fewer: the buckets too)
 //   slot_scan, slot_scatter  (route.hip) bucket offsets and positions
 #include <algorithm>
 #include <cmath>
@@ -21,7 +20,8 @@ namespace luffy {
 namespace {
 
 constexpr int kMaxChoices = 8, kMaxGroups = 16;
-constexpr int kSettleTok = 64;   // tokens of a scored_settle block and histogram chunk
+constexpr int kChooseTok = 64, kChooseWaves = 4;   // of a scored_choose block; a histogram chunk is its tokens
+constexpr int kAgainExperts = 4;                   // logits that a wave takes again together
 constexpr float kLog2e = 1.44269504088896341f;
 
 struct ScoreArgs {
@@ -30,24 +30,20 @@ struct ScoreArgs {
   float scale;
 };
 
-template <int N>
-__device__ __forceinline__ uint32_t ror16(uint32_t x) {   // by N lanes inside each row of 16
-  return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), 0x120 + N, 0xF, 0xF, false));
+template <int DPP>
+__device__ __forceinline__ uint32_t dpp(uint32_t x) {
+  return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), DPP, 0xF, 0xF, false));
 }
 template <int N>
-__device__ __forceinline__ float ror16f(float x) { return __uint_as_float(ror16<N>(__float_as_uint(x))); }
+__device__ __forceinline__ float ror16f(float x) {   // by N lanes inside each row of 16
+  return __uint_as_float(dpp<0x120 + N>(__float_as_uint(x)));
+}
 // Every lane of a row of 16 ends with the row's maximum or sum.
 __device__ __forceinline__ uint32_t max16(uint32_t x) {
-  x = max(x, ror16<8>(x));
-  x = max(x, ror16<4>(x));
-  x = max(x, ror16<2>(x));
-  return max(x, ror16<1>(x));
-}
-__device__ __forceinline__ float max16f(float x) {
-  x = fmaxf(x, ror16f<8>(x));
-  x = fmaxf(x, ror16f<4>(x));
-  x = fmaxf(x, ror16f<2>(x));
-  return fmaxf(x, ror16f<1>(x));
+  x = max(x, dpp<0x128>(x));
+  x = max(x, dpp<0x124>(x));
+  x = max(x, dpp<0x122>(x));
+  return max(x, dpp<0x121>(x));
 }
 __device__ __forceinline__ float sum16(float x) {
   x += ror16f<8>(x);
@@ -55,152 +51,200 @@ __device__ __forceinline__ float sum16(float x) {
   x += ror16f<2>(x);
   return x + ror16f<1>(x);
 }
-// The two largest of a row, a >= b in every lane.
-__device__ __forceinline__ void best2_16(float& a, float& b) {
-  auto merge = [&](float c, float e) {
-    b = fmaxf(fminf(a, c), fmaxf(b, e));
-    a = fmaxf(a, c);
-  };
-  merge(ror16f<8>(a), ror16f<8>(b));
-  merge(ror16f<4>(a), ror16f<4>(b));
-  merge(ror16f<2>(a), ror16f<2>(b));
-  merge(ror16f<1>(a), ror16f<1>(b));
+// The two largest, a >= b, of these lanes' and of those that a DPP control exchanges
+// them with.
+template <int DPP>
+__device__ __forceinline__ void best2_step(uint32_t& a, uint32_t& b) {
+  const uint32_t c = dpp<DPP>(a), e = dpp<DPP>(b);
+  b = max(min(a, c), max(b, e));
+  a = max(a, c);
 }
 
-// Order-preserving key of a value with its expert in the low six bits: among
-// values equal in their top 26 bits the lower expert has the larger key.  What is
-// dropped is less than 2^-17 of the value.
-__device__ __forceinline__ uint32_t choice_key(float v, int e) {
+// Order-preserving key of a value (integer maxima fold into their exchanges, float
+// ones do not).  Every number's key is above 0; NaN counts as -infinity.
+__device__ __forceinline__ uint32_t order_key(float v) {
+  if (!(v == v)) v = -INFINITY;
   const uint32_t u = __float_as_uint(v);
-  const uint32_t o = (u & 0x80000000u) ? ~u : (u | 0x80000000u);
-  return (o & ~63u) | static_cast<uint32_t>(63 - e);
+  return u ^ (static_cast<uint32_t>(static_cast<int32_t>(u) >> 31) | 0x80000000u);
 }
-__device__ __forceinline__ float key_value(uint32_t key) {
-  if (key == 0u) return -INFINITY;   // no expert
-  const uint32_t o = key & ~63u;
-  return __uint_as_float((o & 0x80000000u) ? (o & 0x7FFFFFFFu) : ~o);
+__device__ __forceinline__ float key_value(uint32_t key) {   // (0: -infinity's neighbour, a NaN)
+  return __uint_as_float(key ^ (static_cast<uint32_t>(static_cast<int32_t>(~key) >> 31) | 0x80000000u));
 }
+// The value of a key whose low bits `mask` hold something else: off by less than
+// (mask + 1) 2^-23 of itself, infinities as they are.
+__device__ __forceinline__ float key_value(uint32_t key, uint32_t mask) {
+  return key_value(key & 0x80000000u ? key & ~mask : key | mask);
+}
+__device__ __forceinline__ float max16f(float x) { return key_value(max16(order_key(x))); }
 
-// Whether a > b in truth, each known to `rel` of itself and `abs` besides.  A b of
-// -infinity (an expert that is masked out) is below every other a, unless abs says
-// that the numbers left float32's range.
-__device__ __forceinline__ bool apart(float a, float b, float rel, float abs) {
-  if (b == -INFINITY && a > -INFINITY) return abs < INFINITY;
-  return a - b > fmaf(rel, fabsf(a) + fabsf(b), 2.0f * abs);
+// Whether a >= b, each known to `rel` of itself and `abs` besides, may be the other way
+// round.  A b of -infinity (an expert that is masked out) is below every other a, unless
+// abs says that the numbers left float32's range.
+__device__ __forceinline__ bool uncertain(float a, float b, float rel, float abs) {
+  if (b == -INFINITY) return !(abs < INFINITY);
+  return !(a - b > fmaf(rel, fabsf(a) + fabsf(b), 2.0f * abs));
 }
 
 // 1 / (1 + e^-l) times e^-shift, shift <= 0: no overflow for any l.
 __device__ __forceinline__ float sigmoid_shifted(float l, float shift) {
-  return __builtin_amdgcn_exp2f((fminf(l, 0.f) - shift) * kLog2e) /
-         (1.0f + __builtin_amdgcn_exp2f(-fabsf(l) * kLog2e));
+  return __builtin_amdgcn_exp2f((fminf(l, 0.f) - shift) * kLog2e) *
+         __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-fabsf(l) * kLog2e));
+}
+__device__ __forceinline__ float sigmoid(float l) {
+  const float e = __builtin_amdgcn_exp2f(-fabsf(l) * kLog2e);
+  return (l < 0.f ? e : 1.0f) * __builtin_amdgcn_rcpf(1.0f + e);
 }
 
-// Choice of one token by the 16 lanes of a row, lane m with the logits l[j] of
-// experts 16 j + m (those past E are ignored).  dl bounds the logits' error.  Lane
-// i < k ends with the i-th expert and its gate; `marked` is set for the row where a
-// deciding gap may be of either sign:
+// Choices of R tokens by the 16 lanes of a row, lane m with the logits l[r][j] of
+// experts 16 j + m (those past E are ignored).  dl bounds a token's logits' error.
+// Lane i < k ends with the i-th expert and its gate; `marked` is set for the row where
+// a deciding gap may be of either sign:
 //   logits         2 dl
 //   sigmoid + bias a score moves by at most dl / 4, its evaluation and the sum by
 //                  less than 2^-20 (1 + |c|)
 //   softmax + bias by at most 2 dl of itself (its own exponential and the sum of
 //                  all), evaluation as above
-// and 2^-17 of either value for the keys; the sum of a group's two best moves by
-// twice that.
-template <int NEB>
-__device__ __forceinline__ void choose16(const float (&l)[NEB], const float (&bal)[NEB], const int (&grp)[NEB],
-                                         const ScoreArgs& a, float dl, int& expert, float& gate, bool& marked) {
+// and 2^-17 (2^-19) of either value for the six (four) low bits of a key that hold the
+// expert (group), the lower one being the larger key; the sum of a group's two best
+// moves by twice that.
+//   A lane sorts its experts once; then the row's largest head is the next choice, and
+// its lane goes on to its next.  The steps are chains of exchanges, and the code is
+// fetched once a block, cold: both want little of it.  (Float maxima, a search through
+// all registers for every choice, gaps tested one by one: 5000 instructions for four
+// tokens of 64 experts instead of TODO, and TODO us.)
+template <int NEB, int R>
+__device__ __forceinline__ void choose16(const float (&l)[R][NEB], const float (&bal)[NEB], const int (&grp)[NEB],
+                                         const ScoreArgs& a, const float (&dl)[R], int (&expert)[R],
+                                         float (&gate)[R], bool (&marked)[R]) {
   const int lane = threadIdx.x & 63, m = lane & 15, row = lane & 48;
   const bool sig = a.score == LUFFY_SCORE_SIGMOID, biased = a.balance != nullptr;
   const bool grouped = a.top_groups < a.groups;
-  float top = -INFINITY, inv_z = 0.f;
-  if (!sig) {
-    float z = 0.f;
+  const bool by_score = grouped && !biased && a.best == 2;   // what groups go by
 #pragma unroll
-    for (int j = 0; j < NEB; ++j) top = fmaxf(top, 16 * j + m < a.E ? l[j] : -INFINITY);
-    top = max16f(top);
+  for (int r = 0; r < R; ++r) {
+    float s[NEB], top = 0.f, inv_z = 0.f;
+    uint32_t key[NEB];
+    if (!sig) {
+      uint32_t most = 0;
+      float z = 0.f;
 #pragma unroll
-    for (int j = 0; j < NEB; ++j)
-      z += 16 * j + m < a.E ? __builtin_amdgcn_exp2f((l[j] - top) * kLog2e) : 0.f;
-    inv_z = 1.0f / sum16(z);
-  }
-  auto score = [&](float v) {
-    return sig ? sigmoid_shifted(v, 0.f) : __builtin_amdgcn_exp2f((v - top) * kLog2e) * inv_z;
-  };
-  const float ds = sig ? 0.25f * dl + 0x1p-21f : fmaf(2.0f * inv_z, dl, 0x1p-21f);   // (inv_z: the largest score)
-  float c[NEB];
-#pragma unroll
-  for (int j = 0; j < NEB; ++j) {
-    c[j] = biased ? score(l[j]) + bal[j] : l[j];
-    if (c[j] != c[j]) c[j] = -INFINITY;   // no number: chosen last
-  }
-  const float dc = biased ? ds : dl;
-  marked = false;
-  uint32_t kept = ~0u;   // groups
-  if (grouped) {
-    const bool by_score = !biased && a.best == 2;
-    const float dg = (a.best == 2 ? 2.0f : 1.0f) * (by_score ? ds : dc);
-    float value = -INFINITY;   // lane g: group g's
-    for (int g = 0; g < a.groups; ++g) {
-      float b1 = -INFINITY, b2 = -INFINITY;
+      for (int j = 0; j < NEB; ++j) most = max(most, 16 * j + m < a.E ? order_key(l[r][j]) : 0u);
+      top = key_value(max16(most));
 #pragma unroll
       for (int j = 0; j < NEB; ++j) {
-        float v = by_score ? score(l[j]) : c[j];
-        if (!(v == v) || grp[j] != g || 16 * j + m >= a.E) v = -INFINITY;
-        b2 = fmaxf(b2, fminf(b1, v));
-        b1 = fmaxf(b1, v);
+        s[j] = __builtin_amdgcn_exp2f((l[r][j] - top) * kLog2e);
+        z += 16 * j + m < a.E ? s[j] : 0.f;
       }
-      best2_16(b1, b2);
-      if (m == g) value = a.best == 2 && a.group_size > 1 ? b1 + b2 : b1;
+      inv_z = __builtin_amdgcn_rcpf(sum16(z));
+#pragma unroll
+      for (int j = 0; j < NEB; ++j) s[j] *= inv_z;
+    } else if (biased || by_score) {
+#pragma unroll
+      for (int j = 0; j < NEB; ++j) s[j] = sigmoid(l[r][j]);
     }
-    bool open = m < a.groups;
-    float last = 0.f;
-    kept = 0;
-    for (int r = 0; r < a.top_groups; ++r) {
-      last = max16f(open ? value : -INFINITY);
-      const uint32_t at = static_cast<uint32_t>(__ballot(open && value == last) >> row) & 0xFFFFu;
-      const int g = __ffs(static_cast<int>(at)) - 1;
-      kept |= 1u << g;
-      if (m == g) open = false;
+    const float ds = sig ? fmaf(0.25f, dl[r], 0x1p-21f) : fmaf(2.0f * inv_z, dl[r], 0x1p-21f);   // (inv_z: the largest score)
+    const float dc = biased ? ds : dl[r];
+#pragma unroll
+    for (int j = 0; j < NEB; ++j) key[j] = 16 * j + m < a.E ? order_key(biased ? s[j] + bal[j] : l[r][j]) : 0u;
+    bool bad = false;
+    if (grouped) {
+      // every lane: its experts' groups' values, with the group in the low bits
+      const bool two = a.best == 2 && a.group_size > 1;
+      const int gs = a.group_size;
+      uint32_t gk[NEB], u[NEB];
+#pragma unroll
+      for (int j = 0; j < NEB; ++j) {
+        u[j] = by_score && 16 * j + m < a.E ? order_key(s[j]) : key[j];
+        gk[j] = 0;
+      }
+      auto value_key = [&](uint32_t b1, uint32_t b2, int g) {
+        const uint32_t v = two ? order_key(key_value(b1) + key_value(b2)) : b1;
+        return (v & ~15u) | static_cast<uint32_t>(15 - g);
+      };
+      if (gs <= 16 && (gs & (gs - 1)) == 0) {
+        // a group is gs neighbouring lanes of one register
+#pragma unroll
+        for (int j = 0; j < NEB; ++j) {
+          uint32_t b1 = u[j], b2 = 0;
+          if (gs >= 2) best2_step<0xB1>(b1, b2);     // quad_perm [1, 0, 3, 2]
+          if (gs >= 4) best2_step<0x4E>(b1, b2);     // quad_perm [2, 3, 0, 1]
+          if (gs >= 8) best2_step<0x141>(b1, b2);    // row_half_mirror
+          if (gs >= 16) best2_step<0x140>(b1, b2);   // row_mirror
+          if (16 * j + m < a.E) gk[j] = value_key(b1, b2, grp[j]);
+        }
+      } else {
+        for (int g = 0; g < a.groups; ++g) {
+          uint32_t b1 = 0, b2 = 0;
+#pragma unroll
+          for (int j = 0; j < NEB; ++j) {
+            const uint32_t v = grp[j] == g ? u[j] : 0u;
+            b2 = max(b2, min(b1, v));
+            b1 = max(b1, v);
+          }
+          best2_step<0x128>(b1, b2);
+          best2_step<0x124>(b1, b2);
+          best2_step<0x122>(b1, b2);
+          best2_step<0x121>(b1, b2);
+          const uint32_t v = value_key(b1, b2, g);
+#pragma unroll
+          for (int j = 0; j < NEB; ++j)
+            if (grp[j] == g && 16 * j + m < a.E) gk[j] = v;
+        }
+      }
+      uint32_t bound = ~0u, last = ~0u;   // the i-th group's key, and the one before
+      for (int i = 0; i <= a.top_groups; ++i) {
+        uint32_t best = 0;
+        last = bound;
+#pragma unroll
+        for (int j = 0; j < NEB; ++j) best = max(best, gk[j] < bound ? gk[j] : 0u);
+        bound = max16(best);
+      }
+#pragma unroll
+      for (int j = 0; j < NEB; ++j)
+        if (gk[j] < last) key[j] = 0;
+      const float dg = (a.best == 2 ? 2.0f : 1.0f) * (by_score ? ds : dc);
+      bad = uncertain(key_value(last, 15u), key_value(bound, 15u), 0x1p-18f, dg);
     }
-    const float next = max16f(open ? value : -INFINITY);
-    marked = !apart(last, next, 0x1p-21f, dg);
-  }
-  uint32_t key[NEB];
+    // the lane's experts, largest key first
 #pragma unroll
-  for (int j = 0; j < NEB; ++j) {
-    const int e = 16 * j + m;
-    key[j] = e < a.E && ((kept >> grp[j]) & 1u) ? choice_key(c[j], e) : 0u;
-  }
-  uint32_t bound = ~0u;
-  float before = 0.f;
-  expert = 0;
-  for (int i = 0; i <= a.k; ++i) {
-    uint32_t best = 0;
+    for (int j = 0; j < NEB; ++j) key[j] = key[j] ? (key[j] & ~63u) | static_cast<uint32_t>(63 - 16 * j - m) : 0u;
 #pragma unroll
-    for (int j = 0; j < NEB; ++j) best = max(best, key[j] < bound ? key[j] : 0u);
-    best = max16(best);
-    const float v = key_value(best);
-    if (i > 0 && best != 0u) marked = marked || !apart(before, v, 0x1p-17f, dc);
-    if (i < a.k && m == i) expert = 63 - static_cast<int>(best & 63u);
-    bound = best;
-    before = v;
-  }
-  // gates, from the chosen experts' logits
-  float own = 0.f;
+    for (int i = 0; i + 1 < NEB; ++i)
 #pragma unroll
-  for (int j = 0; j < NEB; ++j) {
-    const float v = __shfl(l[j], row | (expert & 15), 64);
-    if ((expert >> 4) == j) own = v;
-  }
-  const bool mine = m < a.k;
-  if (a.renormalise) {
-    const float most = max16f(mine ? own : -INFINITY);
-    const float s = !mine ? 0.f
-                          : sig ? sigmoid_shifted(own, fminf(most, 0.f))
-                                : __builtin_amdgcn_exp2f((own - most) * kLog2e);
-    gate = a.scale * (s / sum16(s));
-  } else {
-    gate = a.scale * score(own);
+      for (int j = 0; j + 1 < NEB - i; ++j) {
+        const uint32_t hi = max(key[j], key[j + 1]);
+        key[j + 1] = min(key[j], key[j + 1]);
+        key[j] = hi;
+      }
+    uint32_t own = 0;   // lane i: the i-th choice's key; lane k: the first that is left out
+    for (int i = 0; i <= a.k; ++i) {
+      const uint32_t best = max16(key[0]);
+      own = m == i ? best : own;
+      const bool taken = key[0] == best;   // (none is left: zeros move up)
+#pragma unroll
+      for (int j = 0; j + 1 < NEB; ++j) key[j] = taken ? key[j + 1] : key[j];
+      key[NEB - 1] = taken ? 0u : key[NEB - 1];
+    }
+    const uint32_t next = dpp<0x101>(own);   // row_shl: lane i + 1's
+    bad = bad || (m < a.k && next && uncertain(key_value(own, 63u), key_value(next, 63u), 0x1p-17f, dc));
+    marked[r] = max16(bad ? 1u : 0u) != 0;
+    expert[r] = 63 - static_cast<int>(own & 63u);
+    // gates, from the chosen experts' logits
+    float lx = 0.f;
+#pragma unroll
+    for (int j = 0; j < NEB; ++j) {
+      const float v = __shfl(l[r][j], row | (expert[r] & 15), 64);
+      if ((expert[r] >> 4) == j) lx = v;
+    }
+    if (a.renormalise) {
+      const bool mine = m < a.k;
+      const float most = key_value(max16(mine ? order_key(lx) : 0u));
+      const float p = !mine ? 0.f
+                            : sig ? sigmoid_shifted(lx, fminf(most, 0.f)) : __builtin_amdgcn_exp2f((lx - most) * kLog2e);
+      gate[r] = a.scale * (p * __builtin_amdgcn_rcpf(sum16(p)));
+    } else {
+      gate[r] = a.scale * (sig ? sigmoid(lx) : __builtin_amdgcn_exp2f((lx - top) * kLog2e) * inv_z);
+    }
   }
 }
 
@@ -210,12 +254,12 @@ __device__ __forceinline__ void choose16(const float (&l)[NEB], const float (&ba
 // fragments (the diagonals of their own Grams): with n MFMA sums in a row and their
 // few joins the error of a logit is at most (n + 16) 2^-24 |x| |w| (every rounding
 // is relative to the absolute sum of the products, which is at most |x| |w|), the
-// norms being a little off covered by a factor of 1.01.
+// norms being a little off covered by a factor of 1.01.  The bound goes to
+// bound[t k], a token's first gate, for scored_choose.
 template <bool BF16, int A>
 __global__ __launch_bounds__(256) void scored_gate_kernel(const void* __restrict__ xv, const void* __restrict__ wv,
-                                                          int T, int d, ScoreArgs a, int32_t* __restrict__ topk_idx,
-                                                          float* __restrict__ topk_gate, float* __restrict__ logits,
-                                                          float* __restrict__ inv_norm) {
+                                                          int T, int d, ScoreArgs a, float* __restrict__ logits,
+                                                          float* __restrict__ bound, float* __restrict__ inv_norm) {
   constexpr int TOK = 16 * A, LD = TOK + 4;
   __shared__ __attribute__((aligned(16))) float part[4][kMaxExperts][LD];
   __shared__ float xsq[4][TOK], wsq[4][kMaxExperts];
@@ -307,46 +351,163 @@ __global__ __launch_bounds__(256) void scored_gate_kernel(const void* __restrict
         if (j < neb) *reinterpret_cast<f32x4*>(&part[w][16 * j + m][16 * i + 4 * q]) = acc[i][j];
   }
   __syncthreads();
-  float bias[4], bal[4], wmost = 0.f;
-  int grp[4];
+  // sixteen lanes a token, lane m experts 16 j + m
+  float bias[4], wmost = 0.f, bmost = 0.f;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const int e = 16 * j + m;
     const bool in = e < E;
     bias[j] = in && a.bias ? a.bias[e] : 0.f;
-    bal[j] = in && a.balance ? a.balance[e] : 0.f;
-    grp[j] = in && a.top_groups < a.groups ? e / a.group_size : 0;
+    bmost = fmaxf(bmost, fabsf(bias[j]));
     const float sq = in ? ((wsq[0][e] + wsq[1][e]) + wsq[2][e]) + wsq[3][e] : 0.f;
     wmost = sq > wmost || sq != sq ? sq : wmost;   // NaN stays
   }
   // (a NaN norm marks every token: fmaxf would drop it)
   wmost = __any(wmost != wmost) ? NAN : max16f(wmost);
+  bmost = max16f(bmost);
   for (int it = w; it < TOK / 4; it += 4) {
     const int tl = 4 * it + q, t = t0 + tl;
+    if (t >= T) continue;
     const float ss = ((xsq[0][tl] + xsq[1][tl]) + xsq[2][tl]) + xsq[3][tl];
-    const float dl = 1.01f * static_cast<float>(per * (BF16 ? 1 : 4) + 16) * 0x1p-24f * sqrtf(ss) * sqrtf(wmost);
-    float l[4], most = 0.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int e = min(16 * j + m, E - 1);
-      l[j] = ((part[0][e][tl] + part[1][e][tl]) + part[2][e][tl]) + part[3][e][tl] + bias[j];
-      most = fmaxf(most, fabsf(bias[j]));
+      const int e = 16 * j + m;
+      if (e < E)
+        logits[static_cast<size_t>(t) * E + e] =
+            ((part[0][e][tl] + part[1][e][tl]) + part[2][e][tl]) + part[3][e][tl] + bias[j];
     }
-    int expert;
-    float gate;
-    bool marked;
-    choose16(l, bal, grp, a, fmaf(0x1p-23f, max16f(most), dl), expert, gate, marked);
-    if (t >= T) continue;
-    if (logits) {
+    if (m == 0) {
+      bound[static_cast<size_t>(t) * a.k] =
+          fmaf(0x1p-23f, bmost,
+               1.01f * static_cast<float>(per * (BF16 ? 1 : 4) + 16) * 0x1p-24f * sqrtf(ss) * sqrtf(wmost));
+      if (inv_norm) inv_norm[t] = ss > 0.f ? 1.0f / sqrtf(ss) : 0.f;
+    }
+  }
+}
+
+// bf16 logits for W of at most kStreamLds bytes and many tokens: persistent blocks
+// hold W in LDS, and every wave takes 16 tokens over the whole of d, 2 NB K steps of
+// loads in flight: 8 with 16 waves a block, 16 with up to eight, which have the
+// registers for them (about 128 KB a CU either way).  The sums of eight steps are added up apart, so that the
+// error bound has 8 + d / 256 roundings and not d / 32.
+constexpr int kStreamLds = 128 * 1024, kStreamWaves = 16;
+
+inline bool stream_ok(int dtype, int E, int d) {
+  return dtype == LUFFY_BF16 && static_cast<long long>(E) * d * 2 <= kStreamLds;
+}
+
+template <int NEB, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void scored_gate_stream_kernel(
+    const uint16_t* __restrict__ X, const uint16_t* __restrict__ W, int T, int d, ScoreArgs a,
+    float* __restrict__ logits, float* __restrict__ bound, float* __restrict__ inv_norm) {
+  // row e's 16-byte chunk c at e * d/8 + (c ^ (e & 7)): the 16 rows that a fragment
+  // read touches fall on distinct banks; then the rows' squared norms
+  __shared__ __attribute__((aligned(16))) uint8_t lds[kStreamLds + kMaxExperts * 4];
+  uint4* wl = reinterpret_cast<uint4*>(lds);
+  float* wsq = reinterpret_cast<float*>(lds + kStreamLds);
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, waves = blockDim.x >> 6;
+  const int m = lane & 15, q = lane >> 4, E = a.E;
+  const int cpr = d >> 3;
+  constexpr int NB = WAVES > 8 ? 4 : 8;
+  const int nsteps = d >> 5, nchunks = (T + 15) >> 4;
+  Pack16 x[2][NB];
+  auto load = [&](int ch, int s0, Pack16 (&xx)[NB]) {
+    // two steps take 128 bytes of a row: step 2 p has values 64 p + 16 q .. + 7 in
+    // lane group q, step 2 p + 1 the eight after them (the sum may take the values
+    // in any order), so that both loads of a lane are of one line
+    const uint16_t* arow = X + static_cast<size_t>(min(ch * 16 + m, T - 1)) * d + 16 * q;
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (16 * j + m < E) logits[static_cast<size_t>(t) * E + 16 * j + m] = l[j];
+    for (int u = 0; u < NB; ++u)   // (nsteps and s0 are even)
+      xx[u].u4 = s0 + u < nsteps ? *reinterpret_cast<const uint4*>(arow + 32 * (s0 + (u & ~1)) + 8 * (u & 1))
+                                 : make_uint4(0, 0, 0, 0);
+  };
+  int ch = blockIdx.x * waves + w;
+  load(min(ch, nchunks - 1), 0, x[0]);   // on its way while W is staged
+  for (int e = w; e < E; e += waves) {
+    float s = 0.f;
+    for (int c = lane; c < cpr; c += 64) {
+      Pack16 v;
+      v.u4 = reinterpret_cast<const uint4*>(W)[static_cast<size_t>(e) * cpr + c];
+      wl[e * cpr + (c ^ (e & 7))] = v.u4;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) s = fmaf(bf16_to_f32(v.h[u]), bf16_to_f32(v.h[u]), s);
     }
-    if (m < a.k) {
-      topk_idx[static_cast<size_t>(t) * a.k + m] = marked ? -1 - expert : expert;
-      topk_gate[static_cast<size_t>(t) * a.k + m] = gate;
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) s += __shfl_xor(s, o, 64);
+    if (lane == 0) wsq[e] = s;
+  }
+  int brow[NEB];
+  float bias[NEB], bmost = 0.f;
+#pragma unroll
+  for (int j = 0; j < NEB; ++j) {
+    const int e = 16 * j + m, er = min(e, E - 1);
+    brow[j] = er * cpr + ((2 * q) ^ (er & 7));   // (the odd step's chunk: its lowest bit flipped)
+    bias[j] = e < E && a.bias ? a.bias[e] : 0.f;
+    bmost = fmaxf(bmost, fabsf(bias[j]));
+  }
+  __syncthreads();
+  float wmost = 0.f;
+#pragma unroll
+  for (int j = 0; j < NEB; ++j) {
+    const float sq = wsq[min(16 * j + m, E - 1)];
+    wmost = sq > wmost || sq != sq ? sq : wmost;
+  }
+  // (a NaN norm marks every token: fmaxf would drop it)
+  wmost = __any(wmost != wmost) ? NAN : max16f(wmost);
+  const float rel = 1.01f * static_cast<float>(8 + (nsteps + 7) / 8 + 16) * 0x1p-24f * sqrtf(wmost);
+  const float add = 0x1p-23f * max16f(bmost);
+  for (; ch < nchunks; ch += gridDim.x * waves) {
+    const int t0 = ch * 16;
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    f32x4 tot[NEB], acc[NEB], sq = zero;
+#pragma unroll
+    for (int j = 0; j < NEB; ++j) tot[j] = zero;
+    auto compute = [&](int s0, const Pack16 (&xx)[NB], bool first) {
+#pragma unroll
+      for (int u = 0; u < NB; ++u) {
+        if (s0 + u >= nsteps) break;
+        const int c8 = 4 * (s0 + (u & ~1));
+#pragma unroll
+        for (int j = 0; j < NEB; ++j) {
+          Pack16 b;
+          b.u4 = wl[(brow[j] ^ (u & 1)) + c8];
+          acc[j] = mfma16x16x32(xx[u].v, b.v, first && u == 0 ? zero : acc[j]);
+        }
+        sq = mfma16x16x32(xx[u].v, xx[u].v, sq);
+      }
+    };
+    for (int s0 = 0; s0 < nsteps; s0 += 2 * NB) {
+      if (s0 + NB < nsteps) load(ch, s0 + NB, x[1]);
+      compute(s0, x[0], true);
+      if (NB == 8) {
+#pragma unroll
+        for (int j = 0; j < NEB; ++j) tot[j] += acc[j];
+      }
+      // the next batch, at the end the next chunk's first
+      const bool more = s0 + 2 * NB < nsteps;
+      load(more ? ch : min(ch + static_cast<int>(gridDim.x) * waves, nchunks - 1), more ? s0 + 2 * NB : 0, x[0]);
+      if (s0 + NB < nsteps) compute(s0 + NB, x[1], NB == 8);
+      if (NB == 4 || s0 + NB < nsteps) {
+#pragma unroll
+        for (int j = 0; j < NEB; ++j) tot[j] += acc[j];
+      }
     }
-    if (inv_norm && m == 0) inv_norm[t] = ss > 0.f ? 1.0f / sqrtf(ss) : 0.f;
+    // register i of tot[j]: token 4 q + i, expert 16 j + m; of the squares, element
+    // (4 q + i, 4 q + i) is in lane 4 q + i of row q
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int t = t0 + 4 * q + i;
+      const float ss = __shfl(sq[i], (lane & 48) + 4 * q + i, 64);
+      if (t < T) {
+#pragma unroll
+        for (int j = 0; j < NEB; ++j)
+          if (16 * j + m < E) logits[static_cast<size_t>(t) * E + 16 * j + m] = tot[j][i] + bias[j];
+        if (m == 0) {
+          bound[static_cast<size_t>(t) * a.k] = fmaf(rel, sqrtf(ss), add);
+          if (inv_norm) inv_norm[t] = ss > 0.f ? 1.0f / sqrtf(ss) : 0.f;
+        }
+      }
+    }
   }
 }
 
@@ -361,117 +522,308 @@ __device__ __forceinline__ double wave_max64(double v) {
   return v;
 }
 
-// A block's kSettleTok tokens: the marked ones are decided from float64 logits of
-// exact products (the waves share the experts, then wave 0 has one a lane), and
+// kChooseTok tokens a block: choices by the 16 lanes of a row, four tokens a wave at
+// a time; then those whose float32 logits do not tell are decided in float64, and
 // waves rank the slots of a choice each.
-template <bool BF16>
-__global__ __launch_bounds__(256) void scored_settle_kernel(const void* __restrict__ xv, const void* __restrict__ wv,
-                                                            int T, int d, ScoreArgs a, int32_t* __restrict__ topk_idx,
-                                                            float* __restrict__ topk_gate, float* __restrict__ logits,
-                                                            int32_t* __restrict__ slot_rank,
-                                                            int32_t* __restrict__ hist, int* __restrict__ scan_done) {
+//   Of an undecided token the logits that another one (or, in a group, another
+// group's value) is too close to are taken again from exact products, usually two;
+// the others are far enough from every other as they are.  Under a softmax with a
+// bias every score moves with the sum of all, and where float32 sums left their range
+// no logit tells anything: then all are.  The waves share these products.
+//   T <= kChooseTok: the one block has every slot, and lays out the buckets as well.
+template <bool BF16, int NEB>
+__global__ __launch_bounds__(kChooseWaves * 64) void scored_choose_kernel(
+    const void* __restrict__ xv, const void* __restrict__ wv, int T, int d, ScoreArgs a, int C,
+    int32_t* __restrict__ topk_idx, float* __restrict__ topk_gate, float* __restrict__ logits,
+    int32_t* __restrict__ slot_pos, int32_t* __restrict__ hist, int* __restrict__ scan_done,
+    int32_t* __restrict__ perm_token, int32_t* __restrict__ offsets) {
   using Elem = std::conditional_t<BF16, uint16_t, float>;
-  constexpr int VL = 16 / sizeof(Elem);
-  __shared__ int choice[kMaxChoices][kSettleTok];
-  __shared__ double lg[kMaxExperts], val[kMaxExperts], gval[kMaxGroups];
-  __shared__ int cnt[4][kMaxExperts];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int ch = blockIdx.x, t0 = ch * kSettleTok, E = a.E, k = a.k, nch = gridDim.x;
+  constexpr int VL = 16 / sizeof(Elem), NE = kAgainExperts, ITEMS = 16, ROWS = kChooseTok / 4 / kChooseWaves;
+  __shared__ int choice[kMaxChoices][kChooseTok];
+  __shared__ int cnt[kMaxChoices][kMaxExperts];
+  __shared__ float bounds[kChooseTok];
+  __shared__ bool marks[kChooseTok];
+  __shared__ int first[kMaxExperts];              // (one chunk) an expert's first position
+  __shared__ uint64_t agains[kChooseTok];         // of the n-th marked token: the logits to take again
+  __shared__ double lg[kChooseTok][kMaxExperts];  // its logits
+  __shared__ double vals[kChooseWaves][kMaxExperts], gvals[kChooseWaves][kMaxGroups];
+  __shared__ double sums[kChooseWaves][ITEMS][NE];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, m = lane & 15, q = lane >> 4;
+  const int ch = blockIdx.x, t0 = ch * kChooseTok, E = a.E, k = a.k, nch = gridDim.x;
+  const bool sig = a.score == LUFFY_SCORE_SIGMOID, grouped = a.top_groups < a.groups;
   if (ch == 0 && threadIdx.x == 0) *scan_done = 0;   // armed for slot_scan
-  for (int i = threadIdx.x; i < kSettleTok * k; i += 256) {
-    const int tl = i / k, j = i - tl * k;
-    choice[j][tl] = t0 + tl < T ? topk_idx[static_cast<size_t>(t0) * k + i] : 0;
+  {
+    float bal[NEB], l[ROWS][NEB], dl[ROWS];
+    int grp[NEB];
+#pragma unroll
+    for (int j = 0; j < NEB; ++j) {
+      const int e = 16 * j + m;
+      bal[j] = e < E && a.balance ? a.balance[e] : 0.f;
+      grp[j] = e < E && grouped ? e / a.group_size : 0;
+    }
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+      const size_t t = min(t0 + 4 * (w + kChooseWaves * i) + q, T - 1);
+#pragma unroll
+      for (int j = 0; j < NEB; ++j) l[i][j] = logits[t * E + min(16 * j + m, E - 1)];
+      dl[i] = topk_gate[t * k];
+    }
+    int expert[ROWS];
+    float gate[ROWS];
+    bool marked[ROWS];
+    choose16(l, bal, grp, a, dl, expert, gate, marked);
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+      const int tl = 4 * (w + kChooseWaves * i) + q, t = t0 + tl;
+      if (m < k) {
+        choice[m][tl] = expert[i];
+        if (t < T && !marked[i]) {
+          topk_idx[static_cast<size_t>(t) * k + m] = expert[i];
+          topk_gate[static_cast<size_t>(t) * k + m] = gate[i];
+        }
+      }
+      if (m == 0) {
+        marks[tl] = marked[i] && t < T;
+        bounds[tl] = dl[i];
+      }
+    }
   }
   __syncthreads();
-  uint64_t open = __ballot(choice[0][lane] < 0);   // the same in every wave
-  while (open) {
-    const int tl = __ffsll(static_cast<long long>(open)) - 1;
-    open &= open - 1;
-    const size_t t = t0 + tl;
-    const Elem* x = static_cast<const Elem*>(xv) + t * d;
-    for (int e = w; e < E; e += 4) {
-      const Elem* we = static_cast<const Elem*>(wv) + static_cast<size_t>(e) * d;
-      double s = 0.0;
-      for (int c = lane * VL; c < d; c += 64 * VL) {
-        Pack16 xa, wa;
-        xa.u4 = *reinterpret_cast<const uint4*>(x + c);
-        wa.u4 = *reinterpret_cast<const uint4*>(we + c);
+  const uint64_t open = __ballot(marks[lane]);   // the same in every wave
+  const int marked = __popcll(open);
+  if (marked) {
+    auto nth = [&](int n) {   // the n-th marked token
+      uint64_t left = open;
+      for (; n > 0; --n) left &= left - 1;
+      return __ffsll(static_cast<long long>(left)) - 1;
+    };
+    const bool in = lane < E;
+    const uint64_t full = E == 64 ? ~0ull : (1ull << E) - 1;
+    const bool by_score = !a.balance && a.best == 2;   // what groups go by
+    const float bal = a.balance && in ? a.balance[lane] : 0.f;
+    double* val = vals[w];
+    double* gval = gvals[w];
+    // values of the groups, in lane g, from those of the experts in the lanes
+    auto group_values = [&](double v) {
+      __builtin_amdgcn_wave_barrier();
+      val[lane] = in && v == v ? v : -INFINITY;
+      __builtin_amdgcn_wave_barrier();
+      double b1 = -INFINITY, b2 = -INFINITY;
+      if (lane < a.groups) {
+        for (int u = 0; u < a.group_size; ++u) {
+          const double e = val[lane * a.group_size + u];
+          b2 = fmax(b2, fmin(b1, e));
+          b1 = fmax(b1, e);
+        }
+        gval[lane] = a.best == 2 && a.group_size > 1 ? b1 + b2 : b1;
+      }
+      __builtin_amdgcn_wave_barrier();
+      return a.best == 2 && a.group_size > 1 ? b1 + b2 : b1;
+    };
+    // which logits to take again
+    for (int n = w; n < marked; n += kChooseWaves) {
+      const int tl = nth(n);
+      const float lf = in ? logits[static_cast<size_t>(t0 + tl) * E + lane] : -INFINITY, dl = bounds[tl];
+      uint64_t again = full;
+      if (dl < 0x1p-6f && !__any(in && !(fabsf(lf) < INFINITY))) {
+        float top = 0.f, z = 1.f;
+        if (!sig) {
+          top = lf;
 #pragma unroll
-        for (int u = 0; u < VL; ++u) {
-          if constexpr (BF16)
-            s = fma(static_cast<double>(bf16_to_f32(xa.h[u])), static_cast<double>(bf16_to_f32(wa.h[u])), s);
-          else
-            s = fma(static_cast<double>(xa.f[u]), static_cast<double>(wa.f[u]), s);
+          for (int o = 32; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+          z = in ? expf(lf - top) : 0.f;
+#pragma unroll
+          for (int o = 32; o >= 1; o >>= 1) z += __shfl_xor(z, o, 64);
+        }
+        const float s = sig ? sigmoid_shifted(lf, 0.f) : expf(lf - top) / z;
+        const float ds = sig ? 0.25f * dl + 0x1p-20f : fmaf(2.0f / z, dl, 0x1p-20f);
+        const float c = a.balance ? s + bal : lf, dc = a.balance ? ds : dl;
+        // experts too close to one of the first choice's (an expert that is close to
+        // none of those is not among the k best, or surely so and in its place)
+        float size = in && c > -INFINITY ? fabsf(c) : 0.f;
+#pragma unroll
+        for (int o = 32; o >= 1; o >>= 1) size = fmaxf(size, __shfl_xor(size, o, 64));
+        const float close = fmaf(0x1p-15f, size, 2.0f * dc);
+        again = 0;
+        for (int j = 0; j < k; ++j) {
+          const int e = __builtin_amdgcn_readfirstlane(choice[j][tl]);
+          const float v = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(c), e));
+          const uint64_t near = __ballot(in && lane != e && fabsf(c - v) <= close);
+          if (near) again |= near | (1ull << e);
+        }
+        if (grouped) {
+          const double g = group_values(by_score ? s : c);
+          const double dg = 2.0 * (a.best == 2 ? 2.0 : 1.0) * (by_score ? ds : dc);
+          bool hard = false;
+          for (int h = 0; h < a.groups; ++h)
+            hard = hard || (lane < a.groups && h != lane &&
+                            !(fabs(g - gval[h]) > dg + 0x1p-20 * (fabs(g) + fabs(gval[h]))) &&
+                            !(g == -INFINITY && gval[h] == -INFINITY));
+          const uint64_t groups = __ballot(hard);
+          again |= __ballot(in && ((groups >> (in ? lane / a.group_size : 0)) & 1ull));
         }
       }
-      s = wave_sum64(s);
-      if (lane == 0) lg[e] = s + (a.bias ? static_cast<double>(a.bias[e]) : 0.0);
+      lg[n][lane] = lf;
+      if (lane == 0) agains[n] = again;
     }
     __syncthreads();
-    if (w == 0) {
-      const bool in = lane < E, sig = a.score == LUFFY_SCORE_SIGMOID;
-      const double l = in ? lg[lane] : -INFINITY;
-      double s;
-      if (sig) {
-        s = 1.0 / (1.0 + exp(-l));
-      } else {
-        const double top = wave_max64(l), p = in ? exp(l - top) : 0.0;
-        s = p / wave_sum64(p);
-      }
-      double c = a.balance ? s + (in ? static_cast<double>(a.balance[lane]) : 0.0) : l;
-      if (!(c == c) || !in) c = -INFINITY;
-      bool allowed = in;
-      if (a.top_groups < a.groups) {
-        val[lane] = !a.balance && a.best == 2 ? (s == s && in ? s : -INFINITY) : c;
-        __builtin_amdgcn_wave_barrier();
-        double g = -INFINITY;
-        if (lane < a.groups) {
-          double b1 = -INFINITY, b2 = -INFINITY;
-          for (int u = 0; u < a.group_size; ++u) {
-            const double v = val[lane * a.group_size + u];
-            b2 = fmax(b2, fmin(b1, v));
-            b1 = fmax(b1, v);
+    for (int pass = 0; pass < 2; ++pass) {
+      // their products, NE experts of a token at a time, ITEMS such sums between two
+      // barriers; where there are few, the waves take a quarter of d each
+      int items = 0;
+      for (int n = 0; n < marked; ++n) items += (__popcll(agains[n]) + NE - 1) / NE;
+      if (!items) break;   // (the second pass: none was left)
+      const bool split = items < 2 * kChooseWaves;
+      const int quarter = ((d / VL + kChooseWaves - 1) / kChooseWaves) * VL;
+      const int c_lo = split ? w * quarter : 0, c_hi = split ? min(d, c_lo + quarter) : d;
+      for (int base = 0; base < items; base += ITEMS) {
+        int item = 0;
+        for (int n = 0; n < marked; ++n) {
+          for (uint64_t todo = agains[n]; todo; ++item) {
+            int ec[NE];
+#pragma unroll
+            for (int j = 0; j < NE; ++j) {
+              ec[j] = todo ? __ffsll(static_cast<long long>(todo)) - 1 : ec[0];
+              todo &= todo - 1;
+            }
+            if (item < base || item >= base + ITEMS || (!split && item % kChooseWaves != w)) continue;
+            const Elem* x = static_cast<const Elem*>(xv) + static_cast<size_t>(t0 + nth(n)) * d;
+            double s[NE];
+#pragma unroll
+            for (int j = 0; j < NE; ++j) s[j] = 0.0;
+            for (int c = c_lo + lane * VL; c < c_hi; c += 64 * VL) {
+              Pack16 xa, wa[NE];
+              xa.u4 = *reinterpret_cast<const uint4*>(x + c);
+#pragma unroll
+              for (int j = 0; j < NE; ++j)
+                wa[j].u4 =
+                    *reinterpret_cast<const uint4*>(static_cast<const Elem*>(wv) + static_cast<size_t>(ec[j]) * d + c);
+#pragma unroll
+              for (int u = 0; u < VL; ++u) {
+                double xd;
+                if constexpr (BF16) xd = static_cast<double>(bf16_to_f32(xa.h[u]));
+                else xd = static_cast<double>(xa.f[u]);
+#pragma unroll
+                for (int j = 0; j < NE; ++j) {
+                  if constexpr (BF16) s[j] = fma(xd, static_cast<double>(bf16_to_f32(wa[j].h[u])), s[j]);
+                  else s[j] = fma(xd, static_cast<double>(wa[j].f[u]), s[j]);
+                }
+              }
+            }
+            // four sums over the wave: halves keep two each, quarters one
+            static_assert(NE == 4, "four sums a wave");
+            const bool h5 = lane & 32, h4 = lane & 16;
+            const double p0 = (h5 ? s[2] : s[0]) + __shfl_xor(h5 ? s[0] : s[2], 32, 64);
+            const double p1 = (h5 ? s[3] : s[1]) + __shfl_xor(h5 ? s[1] : s[3], 32, 64);
+            double sum = (h4 ? p1 : p0) + __shfl_xor(h4 ? p0 : p1, 16, 64);
+#pragma unroll
+            for (int o = 8; o >= 1; o >>= 1) sum += __shfl_xor(sum, o, 64);
+            if ((lane & 15) == 0) sums[split ? w : 0][item - base][lane >> 4] = sum;
           }
-          g = a.best == 2 && a.group_size > 1 ? b1 + b2 : b1;
-          gval[lane] = g;
         }
+        __syncthreads();
+        // a sum's four quarters, a thread each: the expert and the token again by the
+        // same walk
+        int at = 0;
+        for (int n = 0; n < marked; ++n) {
+          const uint64_t mask = agains[n];
+          const int below = __popcll(mask & lanemask_lt());   // of this lane's expert
+          const int mine = at + below / NE;
+          if (w == 0 && ((mask >> lane) & 1ull) && mine >= base && mine < base + ITEMS) {
+            double s = sums[0][mine - base][below % NE];
+            for (int v = 1; split && v < kChooseWaves; ++v) s += sums[v][mine - base][below % NE];
+            lg[n][lane] = s + (a.bias ? static_cast<double>(a.bias[lane]) : 0.0);
+          }
+          at += (__popcll(mask) + NE - 1) / NE;
+        }
+        __syncthreads();
+      }
+      // the decisions
+      for (int n = w; n < marked; n += kChooseWaves) {
+        if (pass == 1 && !agains[n]) continue;
+        const int tl = nth(n);
+        const size_t t = t0 + tl;
+        const double l = lg[n][lane];   // (-infinity past E)
+        double s = 0.0;
+        if (a.balance || (grouped && by_score)) {
+          if (sig) {
+            s = 1.0 / (1.0 + exp(-l));
+          } else {
+            const double top = wave_max64(l), p = in ? exp(l - top) : 0.0;
+            s = p / wave_sum64(p);
+          }
+        }
+        double c = a.balance ? s + static_cast<double>(bal) : l;
+        if (!(c == c) || !in) c = -INFINITY;
+        // under a softmax with a bias the other logits still move the scores by their
+        // sum: by as much of themselves
+        const bool moves = pass == 0 && !sig && a.balance && agains[n] != full;
+        const double part = moves ? 1.01 * bounds[tl] + 1e-12 : 0.0, s_most = moves ? wave_max64(s) : 0.0;
+        bool loose = false;
+        bool allowed = in;
+        if (grouped) {
+          const double g = group_values(by_score ? s : c);
+          int rank = kMaxGroups;
+          if (lane < a.groups) {
+            rank = 0;
+            for (int h = 0; h < a.groups; ++h) {
+              rank += gval[h] > g || (gval[h] == g && h < lane);
+              loose = loose || (moves && h != lane && fabs(gval[h] - g) <= 2.0 * s_most * part);
+            }
+          }
+          const uint64_t kept = __ballot(rank < a.top_groups);
+          allowed = in && ((kept >> (in ? lane / a.group_size : 0)) & 1ull);
+        }
+        // the k best are among the first choice and what was taken again
+        uint64_t first_choice = 0;
+        for (int j = 0; j < k; ++j) first_choice |= 1ull << __builtin_amdgcn_readfirstlane(choice[j][tl]);
+        const uint64_t may = __ballot(allowed) & (first_choice | agains[n]);
         __builtin_amdgcn_wave_barrier();
-        int rank = kMaxGroups;
-        if (lane < a.groups) {
-          rank = 0;
-          for (int h = 0; h < a.groups; ++h) rank += gval[h] > g || (gval[h] == g && h < lane);
+        val[lane] = c;
+        __builtin_amdgcn_wave_barrier();
+        int rank = 0;
+        for (uint64_t left = may; left; left &= left - 1) {
+          const int e = __ffsll(static_cast<long long>(left)) - 1;
+          const double v = val[e];
+          rank += v > c || (v == c && e < lane);
+          if (moves) {
+            const double se = __shfl(s, e, 64);
+            loose = loose || (((may >> lane) & 1ull) && e != lane && fabs(v - c) <= fabs(se - s) * part + 1e-14);
+          }
         }
-        const uint64_t kept = __ballot(rank < a.top_groups);
-        allowed = in && ((kept >> (in ? lane / a.group_size : 0)) & 1ull);
+        const bool chosen = ((may >> lane) & 1ull) && rank < k;
+        const bool all = __any(loose);
+        if (lane == 0) agains[n] = all ? full : 0ull;   // none: done
+        if (all) continue;
+        // gates by choose16's formulas, in float32
+        const float lx = static_cast<float>(l);
+        float top = (a.renormalise ? chosen : in) ? lx : -INFINITY;
+#pragma unroll
+        for (int o = 32; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+        float p = !in ? 0.f : sig ? sigmoid_shifted(lx, a.renormalise ? fminf(top, 0.f) : 0.f) : expf(lx - top);
+        float sum = a.renormalise && !chosen ? 0.f : p;
+#pragma unroll
+        for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o, 64);
+        if (a.renormalise || !sig) p /= sum;
+        if (chosen) {
+          choice[rank][tl] = lane;
+          topk_idx[t * k + rank] = lane;
+          topk_gate[t * k + rank] = a.scale * p;
+        }
+        if (in) logits[t * E + lane] = lx;
       }
-      __builtin_amdgcn_wave_barrier();
-      val[lane] = c;
-      const uint64_t may = __ballot(allowed);
-      __builtin_amdgcn_wave_barrier();
-      int rank = 0;
-      for (int e = 0; e < E; ++e)
-        rank += ((may >> e) & 1ull) && (val[e] > c || (val[e] == c && e < lane));
-      const bool chosen = allowed && rank < k;
-      double gate = s;
-      if (a.renormalise) {
-        const double most = wave_max64(chosen ? l : -INFINITY);
-        const double shift = sig ? fmin(most, 0.0) : most;
-        const double p = !chosen ? 0.0 : sig ? exp(fmin(l, 0.0) - shift) / (1.0 + exp(-fabs(l))) : exp(l - shift);
-        gate = p / wave_sum64(p);
-      }
-      if (chosen) {
-        choice[rank][tl] = lane;
-        topk_idx[t * k + rank] = lane;
-        topk_gate[t * k + rank] = static_cast<float>(static_cast<double>(a.scale) * gate);
-      }
-      if (logits && in) logits[t * E + lane] = static_cast<float>(l);
+      __syncthreads();
     }
-    __syncthreads();
   }
   // stable ranks among the chunk's slots of the same expert: the lanes that hold
   // it, by ballots on its bits
   const bool valid = t0 + lane < T;
-  for (int j = w; j < k; j += 4) {
+  constexpr int PER = kMaxChoices / kChooseWaves;
+  int ranks[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int j = w + i * kChooseWaves;
+    if (j >= k) break;
     const int e = choice[j][lane];
     const int key = valid ? e : 127;
     uint64_t same = ~0ull;
@@ -481,14 +833,48 @@ __global__ __launch_bounds__(256) void scored_settle_kernel(const void* __restri
       const uint64_t bb = __ballot(bit);
       same &= bit ? bb : ~bb;
     }
-    const int rank = __popcll(same & lanemask_lt());
-    cnt[w][lane] = 0;
+    ranks[i] = __popcll(same & lanemask_lt());
+    cnt[j][lane] = 0;
     __builtin_amdgcn_wave_barrier();
-    if (valid && rank == 0) cnt[w][e] = __popcll(same);
+    if (valid && ranks[i] == 0) cnt[j][e] = __popcll(same);
     __builtin_amdgcn_wave_barrier();
-    if (lane < E) hist[static_cast<size_t>(lane) * k * nch + static_cast<size_t>(j) * nch + ch] = cnt[w][lane];
-    if (valid) slot_rank[static_cast<size_t>(t0 + lane) * k + j] = rank;
-    __builtin_amdgcn_wave_barrier();
+    if (nch > 1) {
+      if (lane < E) hist[static_cast<size_t>(lane) * k * nch + static_cast<size_t>(j) * nch + ch] = cnt[j][lane];
+      if (valid) slot_pos[static_cast<size_t>(t0 + lane) * k + j] = ranks[i];
+    }
+  }
+  if (nch > 1) return;
+  __syncthreads();
+  // the only chunk: an expert a lane, its slots before choice j in cnt[j]
+  int total = 0;
+  if (w == 0) {
+    for (int j = 0; j < k; ++j) {
+      const int n = cnt[j][lane];
+      cnt[j][lane] = total;
+      total += n;
+    }
+    if (C > 0 && total > C) total = C;
+    if (lane >= E) total = 0;
+    int incl = total;
+#pragma unroll
+    for (int sh = 1; sh < 64; sh <<= 1) {
+      const int u = __shfl_up(incl, sh, 64);
+      if (lane >= sh) incl += u;
+    }
+    if (lane < E) offsets[lane] = incl - total;
+    if (lane == E - 1) offsets[E] = incl;
+    first[lane] = incl - total;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int j = w + i * kChooseWaves;
+    if (j >= k) break;
+    if (!valid) continue;
+    const int e = choice[j][lane], at = cnt[j][e] + ranks[i];
+    const bool kept = C <= 0 || at < C;
+    slot_pos[static_cast<size_t>(lane) * k + j] = kept ? first[e] + at : -1;
+    if (kept) perm_token[first[e] + at] = lane;
   }
 }
 
@@ -728,7 +1114,7 @@ extern "C" int luffy_route_scored(const void* x, int T, int d, int dtype, const 
                                   int32_t* offsets, float* inv_norm, void* workspace, size_t workspace_bytes,
                                   void* stream) {
   const char* fn = "luffy_route_scored";
-  if (!x || !w_gate || !topk_idx || !topk_gate || !slot_pos || !perm_token || !offsets)
+  if (!x || !w_gate || !topk_idx || !topk_gate || !logits || !slot_pos || !perm_token || !offsets)
     return fail(LUFFY_E_INVALID, "%s: null pointer argument", fn);
   const int st = scored_check(fn, T, d, dtype, E, k, score, scale);
   if (st != LUFFY_OK) return st;
@@ -749,18 +1135,42 @@ extern "C" int luffy_route_scored(const void* x, int T, int d, int dtype, const 
   Carver c(workspace);
   const RouteWs ws = carve_route(c, T, E, k);
   const ScoreArgs a{b_gate, balance, E, k, score, groups, E / groups, top_groups, group_best, renormalise != 0, scale};
-#define LUFFY_SCORED(BF, A)                                                                                         \
-  launch("scored_gate", scored_gate_kernel<BF, A>, (T + 16 * A - 1) / (16 * A), 256, 0, s, x, w_gate, T, d, a, topk_idx, \
-         topk_gate, logits, inv_norm)
+#define LUFFY_SCORED(BF, A)                                                                                             \
+  launch("scored_gate", scored_gate_kernel<BF, A>, (T + 16 * A - 1) / (16 * A), 256, 0, s, x, w_gate, T, d, a, logits, \
+         topk_gate, inv_norm)
   const bool bf16 = dtype == LUFFY_BF16;
-  if (T >= 32768) { if (bf16) LUFFY_SCORED(true, 4); else LUFFY_SCORED(false, 4); }
-  else if (T >= 8192) { if (bf16) LUFFY_SCORED(true, 2); else LUFFY_SCORED(false, 2); }
-  else { if (bf16) LUFFY_SCORED(true, 1); else LUFFY_SCORED(false, 1); }
+  const int chunks = (T + 15) / 16, cus = persistent_grid();
+  if (stream_ok(dtype, E, d) && chunks >= 4 * cus) {
+    const int waves = std::min(kStreamWaves, (chunks + cus - 1) / cus);
+#define LUFFY_SCORED_S(NEB)                                                                                         \
+  launch("scored_gate", waves > 8 ? scored_gate_stream_kernel<NEB, 16> : scored_gate_stream_kernel<NEB, 8>, cus,    \
+         64 * waves, 0, s, static_cast<const uint16_t*>(x), static_cast<const uint16_t*>(w_gate), T, d, a, logits,  \
+         topk_gate, inv_norm)
+    if (E <= 16) LUFFY_SCORED_S(1);
+    else if (E <= 32) LUFFY_SCORED_S(2);
+    else if (E <= 48) LUFFY_SCORED_S(3);
+    else LUFFY_SCORED_S(4);
+#undef LUFFY_SCORED_S
+  } else if (T >= 32768) {
+    if (bf16) LUFFY_SCORED(true, 4); else LUFFY_SCORED(false, 4);
+  } else if (T >= 8192) {
+    if (bf16) LUFFY_SCORED(true, 2); else LUFFY_SCORED(false, 2);
+  } else {
+    if (bf16) LUFFY_SCORED(true, 1); else LUFFY_SCORED(false, 1);
+  }
 #undef LUFFY_SCORED
-  launch("scored_settle", bf16 ? scored_settle_kernel<true> : scored_settle_kernel<false>,
-         (T + kSettleTok - 1) / kSettleTok, 256, 0, s, x, w_gate, T, d, a, topk_idx, topk_gate, logits, slot_pos,
-         ws.hist, ws.done);
-  route_buckets_enqueue(topk_idx, T, E, k, capacity_factor, kSettleTok, slot_pos, perm_token, offsets, ws, s);
+  const int blocks = (T + kChooseTok - 1) / kChooseTok, C = capacity_slots(T, k, E, capacity_factor);
+#define LUFFY_CHOOSE(NEB)                                                                                           \
+  launch("scored_choose", bf16 ? scored_choose_kernel<true, NEB> : scored_choose_kernel<false, NEB>, blocks,        \
+         kChooseWaves * 64, 0, s, x, w_gate, T, d, a, C, topk_idx, topk_gate, logits, slot_pos, ws.hist, ws.done,   \
+         perm_token, offsets)
+  if (E <= 16) LUFFY_CHOOSE(1);
+  else if (E <= 32) LUFFY_CHOOSE(2);
+  else if (E <= 48) LUFFY_CHOOSE(3);
+  else LUFFY_CHOOSE(4);
+#undef LUFFY_CHOOSE
+  if (blocks > 1)
+    route_buckets_enqueue(topk_idx, T, E, k, capacity_factor, kChooseTok, slot_pos, perm_token, offsets, ws, s);
   return check_launch(fn);
 }
 

@@ -87,7 +87,7 @@ ROUTE = ("x T d dtype w_gate b_gate E k score balance groups top_groups group_be
 def test_route_scored_refusals(lib):
     call = caller(lib.luffy_route_scored, ROUTE, T=8, d=64, dtype=1, E=16, k=4, score=1, groups=4, top_groups=2,
                   group_best=2, renormalise=1, scale=1.0, cf=0.0, bytes=1 << 20, stream=None)
-    for n in ("x", "w_gate", "topk_idx", "topk_gate", "slot_pos", "perm_token", "offsets"):
+    for n in ("x", "w_gate", "topk_idx", "topk_gate", "logits", "slot_pos", "perm_token", "offsets"):
         assert call(**{n: None}) == INVALID, n
     for n in ("T", "d", "E"):
         assert call(**{n: 0}) == INVALID
