@@ -14,6 +14,7 @@
 #include <type_traits>
 
 #include "act.h"
+#include "ffn.h"
 #include "gemm_core.h"
 #include "luffy_common.h"
 #include "mx8.h"
@@ -1047,6 +1048,12 @@ bool aligned16(std::initializer_list<const void*> ps) {
 }
 
 }  // namespace
+
+void row_product_enqueue(const char* name, const uint16_t* P, const uint16_t* Q, const int32_t* rows, int parts, int M,
+                         int N, float* out, hipStream_t s) {
+  launch(name, wgrad_kernel<false>, persistent_grid(), WgradGemm::THREADS, 0, s, P, Q, rows, parts, M, N, out);
+}
+
 }  // namespace luffy
 
 using namespace luffy;

@@ -7,12 +7,13 @@
 //   scored_choose  scores and choices; a token with a deciding gap within the bound is
 //                  decided in float64 from exact products; ranks every slot among its
 //                  chunk's slots of the same expert and leaves the chunks' counts
-//                  (64 tokens or fewer: the buckets too)
+//                  (one chunk of tokens: the buckets too)
 //   slot_scan, slot_scatter  (route.hip) bucket offsets and positions
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
 
+#include "ffn.h"
 #include "luffy_common.h"
 #include "route.h"
 
@@ -20,7 +21,7 @@ namespace luffy {
 namespace {
 
 constexpr int kMaxChoices = 8, kMaxGroups = 16;
-constexpr int kChooseTok = 64, kChooseWaves = 4;   // of a scored_choose block; a histogram chunk is its tokens
+constexpr int kChooseTok = 32, kChooseWaves = 4;   // of a scored_choose block; a histogram chunk is its tokens
 constexpr int kAgainExperts = 4;                   // logits that a wave takes again together
 constexpr float kLog2e = 1.44269504088896341f;
 
@@ -553,7 +554,7 @@ __global__ __launch_bounds__(kChooseWaves * 64) void scored_choose_kernel(
   const bool sig = a.score == LUFFY_SCORE_SIGMOID, grouped = a.top_groups < a.groups;
   if (ch == 0 && threadIdx.x == 0) *scan_done = 0;   // armed for slot_scan
   {
-    float bal[NEB], l[ROWS][NEB], dl[ROWS];
+    float bal[NEB], l[1][NEB], dl[1], ahead[NEB], dl_ahead;
     int grp[NEB];
 #pragma unroll
     for (int j = 0; j < NEB; ++j) {
@@ -561,35 +562,40 @@ __global__ __launch_bounds__(kChooseWaves * 64) void scored_choose_kernel(
       bal[j] = e < E && a.balance ? a.balance[e] : 0.f;
       grp[j] = e < E && grouped ? e / a.group_size : 0;
     }
-#pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
+    auto load = [&](int i) {
       const size_t t = min(t0 + 4 * (w + kChooseWaves * i) + q, T - 1);
 #pragma unroll
-      for (int j = 0; j < NEB; ++j) l[i][j] = logits[t * E + min(16 * j + m, E - 1)];
-      dl[i] = topk_gate[t * k];
-    }
-    int expert[ROWS];
-    float gate[ROWS];
-    bool marked[ROWS];
-    choose16(l, bal, grp, a, dl, expert, gate, marked);
-#pragma unroll
+      for (int j = 0; j < NEB; ++j) ahead[j] = logits[t * E + min(16 * j + m, E - 1)];
+      dl_ahead = topk_gate[t * k];
+    };
+    load(0);
+    // (not unrolled: the code is fetched once a block, cold)
+#pragma unroll 1
     for (int i = 0; i < ROWS; ++i) {
       const int tl = 4 * (w + kChooseWaves * i) + q, t = t0 + tl;
+#pragma unroll
+      for (int j = 0; j < NEB; ++j) l[0][j] = ahead[j];
+      dl[0] = dl_ahead;
+      if (i + 1 < ROWS) load(i + 1);
+      int expert[1];
+      float gate[1];
+      bool marked[1];
+      choose16(l, bal, grp, a, dl, expert, gate, marked);
       if (m < k) {
-        choice[m][tl] = expert[i];
-        if (t < T && !marked[i]) {
-          topk_idx[static_cast<size_t>(t) * k + m] = expert[i];
-          topk_gate[static_cast<size_t>(t) * k + m] = gate[i];
+        choice[m][tl] = expert[0];
+        if (t < T && !marked[0]) {
+          topk_idx[static_cast<size_t>(t) * k + m] = expert[0];
+          topk_gate[static_cast<size_t>(t) * k + m] = gate[0];
         }
       }
       if (m == 0) {
-        marks[tl] = marked[i] && t < T;
-        bounds[tl] = dl[i];
+        marks[tl] = marked[0] && t < T;
+        bounds[tl] = dl[0];
       }
     }
   }
   __syncthreads();
-  const uint64_t open = __ballot(marks[lane]);   // the same in every wave
+  const uint64_t open = __ballot(lane < kChooseTok && marks[lane % kChooseTok]);   // the same in every wave
   const int marked = __popcll(open);
   if (marked) {
     auto nth = [&](int n) {   // the n-th marked token
@@ -817,14 +823,14 @@ __global__ __launch_bounds__(kChooseWaves * 64) void scored_choose_kernel(
   }
   // stable ranks among the chunk's slots of the same expert: the lanes that hold
   // it, by ballots on its bits
-  const bool valid = t0 + lane < T;
+  const bool valid = lane < kChooseTok && t0 + lane < T;
   constexpr int PER = kMaxChoices / kChooseWaves;
   int ranks[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const int j = w + i * kChooseWaves;
     if (j >= k) break;
-    const int e = choice[j][lane];
+    const int e = choice[j][lane % kChooseTok];
     const int key = valid ? e : 127;
     uint64_t same = ~0ull;
 #pragma unroll
@@ -871,7 +877,7 @@ __global__ __launch_bounds__(kChooseWaves * 64) void scored_choose_kernel(
     const int j = w + i * kChooseWaves;
     if (j >= k) break;
     if (!valid) continue;
-    const int e = choice[j][lane], at = cnt[j][e] + ranks[i];
+    const int e = choice[j][lane % kChooseTok], at = cnt[j][e] + ranks[i];
     const bool kept = C <= 0 || at < C;
     slot_pos[static_cast<size_t>(lane) * k + j] = kept ? first[e] + at : -1;
     if (kept) perm_token[first[e] + at] = lane;
@@ -885,59 +891,152 @@ __global__ __launch_bounds__(kChooseWaves * 64) void scored_choose_kernel(
 //                      sigmoid scores; 0 for experts not chosen
 //   sigmoid            dl_j = scale dg_j s_j (1 - s_j)
 //   softmax            dl_e = s_e (ds_e - sum_i ds_i s_i), ds_j = scale dg_j
-// plus what the caller adds.  A wave a token, an expert a lane.
-__global__ __launch_bounds__(256) void scored_dlogits_kernel(const float* __restrict__ logits,
-                                                             const int32_t* __restrict__ topk_idx,
-                                                             const float* __restrict__ dgate,
-                                                             const float* __restrict__ extra, int T, ScoreArgs a,
-                                                             float* __restrict__ dl) {
-  const int lane = threadIdx.x & 63, E = a.E, k = a.k;
-  const bool sig = a.score == LUFFY_SCORE_SIGMOID, in = lane < E;
-  for (long long t = static_cast<long long>(blockIdx.x) * 4 + (threadIdx.x >> 6); t < T;
-       t += static_cast<long long>(gridDim.x) * 4) {
-    const float l = in ? logits[t * E + lane] : -INFINITY;
-    float dg = 0.f;   // of this lane's expert, 0 if it was not chosen
-    bool chosen = false;
-    for (int j = 0; j < k; ++j)
-      if (topk_idx[t * k + j] == lane) {
-        dg += dgate[t * k + j];
-        chosen = true;
-      }
-    auto wave_sum = [](float v) {
-#pragma unroll
-      for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
-      return v;
-    };
-    auto wave_max = [](float v) {
-#pragma unroll
-      for (int o = 32; o >= 1; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-      return v;
-    };
-    float g;
-    if (a.renormalise) {
-      const float most = wave_max(chosen ? l : -INFINITY), shift = sig ? fminf(most, 0.f) : most;
-      const float p = !chosen ? 0.f : sig ? expf(fminf(l, 0.f) - shift) / (1.0f + expf(-fabsf(l))) : expf(l - shift);
-      const float r = p / wave_sum(p), mean = wave_sum(dg * r);
-      g = chosen ? a.scale * r * (dg - mean) : 0.f;
-      if (sig && chosen) g *= 1.0f / (1.0f + expf(l));
-    } else if (sig) {
-      const float e = expf(-fabsf(l));
-      g = chosen ? a.scale * dg * e / ((1.0f + e) * (1.0f + e)) : 0.f;
+// plus what the caller adds.  Sixteen lanes a token, four experts a lane (4 m ..).
+//   dl leaves as three bf16 parts (their sum has dl's 24 bits): part p of expert e in
+// column p E + e of the rows that scored_dw's product takes.
+// db: a lane's sums over its tokens, added up over the block, in a fixed order.
+constexpr int kDlThreads = 256;
+
+template <bool EVEN>   // E is a multiple of 4
+__global__ __launch_bounds__(kDlThreads) void scored_dlogits_kernel(
+    const float* __restrict__ logits, const int32_t* __restrict__ topk_idx, const float* __restrict__ dgate,
+    const float* __restrict__ extra, int T, ScoreArgs a, int ld, uint16_t* __restrict__ dl, int parts, int per,
+    int32_t* __restrict__ part_rows, float* __restrict__ part_b) {
+  __shared__ float sums[kDlThreads / 16][kMaxExperts];
+  const int m = threadIdx.x & 15, E = a.E, k = a.k;
+  const bool sig = a.score == LUFFY_SCORE_SIGMOID;
+  if (blockIdx.x == 0 && threadIdx.x <= parts) part_rows[threadIdx.x] = min(T, static_cast<int>(threadIdx.x) * per);
+  float db[4] = {0.f, 0.f, 0.f, 0.f};
+  for (long long t0 = static_cast<long long>(blockIdx.x) * (kDlThreads / 16); t0 < T;
+       t0 += static_cast<long long>(gridDim.x) * (kDlThreads / 16)) {
+    const long long tt = t0 + threadIdx.x / 16;
+    const bool valid = tt < T;
+    const size_t t = valid ? tt : T - 1;
+    float l[4], ex[4] = {0.f, 0.f, 0.f, 0.f};
+    if constexpr (EVEN) {
+      const float4 v = 4 * m < E ? *reinterpret_cast<const float4*>(logits + t * E + 4 * m)
+                                 : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+      l[0] = v.x; l[1] = v.y; l[2] = v.z; l[3] = v.w;
     } else {
-      const float top = wave_max(l);
-      const float p = in ? expf(l - top) : 0.f;
-      const float s = p / wave_sum(p), mean = wave_sum(dg * s);
-      g = s * a.scale * (dg - mean);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) l[u] = 4 * m + u < E ? logits[t * E + 4 * m + u] : -INFINITY;
     }
-    if (in) dl[t * E + lane] = g + (extra ? extra[t * E + lane] : 0.f);
+    if (extra)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) ex[u] = 4 * m + u < E ? extra[t * E + 4 * m + u] : 0.f;
+    // lane j < k: the token's j-th choice
+    const int idx = m < k ? topk_idx[t * k + m] : -1;
+    const float dgj = m < k ? dgate[t * k + m] : 0.f;
+    float dg[4] = {0.f, 0.f, 0.f, 0.f};   // of this lane's experts, 0 if not chosen
+    bool chosen[4] = {false, false, false, false};
+    auto take = [&](uint32_t e, uint32_t g) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (static_cast<int>(e) == 4 * m + u) {
+          dg[u] += __uint_as_float(g);
+          chosen[u] = true;
+        }
+    };
+    const uint32_t iu = static_cast<uint32_t>(idx), gu = __float_as_uint(dgj);
+    // (row_newbcast: lane j of each row; lanes from k on hold no expert)
+    take(dpp<0x150>(iu), dpp<0x150>(gu));
+    take(dpp<0x151>(iu), dpp<0x151>(gu));
+    if (k > 2) {
+      take(dpp<0x152>(iu), dpp<0x152>(gu));
+      take(dpp<0x153>(iu), dpp<0x153>(gu));
+    }
+    if (k > 4) {
+      take(dpp<0x154>(iu), dpp<0x154>(gu));
+      take(dpp<0x155>(iu), dpp<0x155>(gu));
+      take(dpp<0x156>(iu), dpp<0x156>(gu));
+      take(dpp<0x157>(iu), dpp<0x157>(gu));
+    }
+    float g[4];
+    if (a.renormalise) {
+      float top = -INFINITY;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) top = fmaxf(top, chosen[u] ? l[u] : -INFINITY);
+      top = max16f(top);
+      const float shift = sig ? fminf(top, 0.f) : top;
+      float p[4], sum = 0.f, dot = 0.f;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        p[u] = !chosen[u] ? 0.f : sig ? sigmoid_shifted(l[u], shift) : __builtin_amdgcn_exp2f((l[u] - shift) * kLog2e);
+        sum += p[u];
+        dot = fmaf(p[u], dg[u], dot);
+      }
+      const float inv = 1.0f / sum16(sum), mean = sum16(dot) * inv;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        g[u] = chosen[u] ? a.scale * (p[u] * inv) * (dg[u] - mean) : 0.f;
+        if (sig && chosen[u]) g[u] *= sigmoid(-l[u]);
+      }
+    } else if (sig) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) g[u] = chosen[u] ? a.scale * dg[u] * (sigmoid(l[u]) * sigmoid(-l[u])) : 0.f;
+    } else {
+      float top = fmaxf(fmaxf(l[0], l[1]), fmaxf(l[2], l[3]));
+      top = max16f(top);
+      float p[4], sum = 0.f, dot = 0.f;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        p[u] = __builtin_amdgcn_exp2f((l[u] - top) * kLog2e);
+        sum += p[u];
+        dot = fmaf(p[u], dg[u], dot);
+      }
+      const float inv = 1.0f / sum16(sum), mean = sum16(dot) * inv;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) g[u] = a.scale * (p[u] * inv) * (dg[u] - mean);
+    }
+    if (!valid) continue;
+    uint16_t part[3][4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      float v = 4 * m + u < E ? g[u] + ex[u] : 0.f;
+      db[u] += v;
+#pragma unroll
+      for (int q = 0; q < 3; ++q) {
+        const uint32_t b = pack_bf16x2(v, 0.f) & 0xFFFFu;
+        part[q][u] = static_cast<uint16_t>(b);
+        v -= __uint_as_float(b << 16);
+      }
+    }
+    uint16_t* out = dl + t * ld + 4 * m;
+#pragma unroll
+    for (int q = 0; q < 3; ++q) {
+      if constexpr (EVEN) {
+        if (4 * m < E)
+          *reinterpret_cast<uint2*>(out + q * E) =
+              make_uint2(part[q][0] | static_cast<uint32_t>(part[q][1]) << 16,
+                         part[q][2] | static_cast<uint32_t>(part[q][3]) << 16);
+      } else {
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (4 * m + u < E) out[q * E + u] = part[q][u];
+      }
+    }
   }
+#pragma unroll
+  for (int u = 0; u < 4; ++u) sums[threadIdx.x / 16][4 * m + u] = db[u];
+  __syncthreads();
+  if (threadIdx.x < E) {
+    float s = 0.f;
+    for (int i = 0; i < kDlThreads / 16; ++i) s += sums[i][threadIdx.x];
+    part_b[static_cast<size_t>(blockIdx.x) * E + threadIdx.x] = s;
+  }
+}
+
+// dl from its three parts.
+__device__ __forceinline__ float dl_value(const uint16_t* p, int E) {
+  return (bf16_to_f32(p[0]) + bf16_to_f32(p[E])) + bf16_to_f32(p[2 * E]);
 }
 
 // dx of a token a wave: its experts' rows of W by dl, and the representatives'
 // rows of dx_rep that are this token's.
 template <bool BF16>
-__global__ __launch_bounds__(256) void scored_dx_kernel(const void* __restrict__ wv, const float* __restrict__ dl,
-                                                        int T, int d, int E, int k, const void* __restrict__ dx_rep,
+__global__ __launch_bounds__(256) void scored_dx_kernel(const void* __restrict__ wv, const uint16_t* __restrict__ dl,
+                                                        int ld, int T, int d, int E, int k,
+                                                        const void* __restrict__ dx_rep,
                                                         const int32_t* __restrict__ slot_pos,
                                                         const int32_t* __restrict__ rep_of_pos,
                                                         const int32_t* __restrict__ rep_row, void* __restrict__ dx) {
@@ -955,13 +1054,14 @@ __global__ __launch_bounds__(256) void scored_dx_kernel(const void* __restrict__
   };
   for (long long t = static_cast<long long>(blockIdx.x) * 4 + (threadIdx.x >> 6); t < T;
        t += static_cast<long long>(gridDim.x) * 4) {
-    const float g = lane < E ? dl[t * E + lane] : 0.f;
+    const float g = lane < E ? dl_value(dl + t * ld + lane, E) : 0.f;
     const uint64_t used = __ballot(g != 0.f);
     int row = -1;
     if (dx_rep && lane < k) {
       const int p = slot_pos[t * k + lane];
       if (p >= 0 && rep_of_pos[p] == p) row = rep_row[p];
     }
+    // (the lanes past d go along with the last columns)
     for (int c = lane * VL; c < (d + 64 * VL - 1) / (64 * VL) * (64 * VL); c += 64 * VL) {
       const int cc = min(c, d - VL);
       float acc[VL], f[VL];
@@ -995,38 +1095,30 @@ __global__ __launch_bounds__(256) void scored_dx_kernel(const void* __restrict__
 
 constexpr int kDwTok = 64, kDwCols = 64;
 
-// Part of dW = dl^T x and db: 64 columns by the tokens of part blockIdx.y, every
-// expert; 64 tokens at a time in LDS, 16 experts a wave, a column a lane.
-template <bool BF16>
-__global__ __launch_bounds__(256) void scored_dw_kernel(const void* __restrict__ xv, const float* __restrict__ dl,
-                                                        int T, int d, int E, int per, float* __restrict__ part_w,
-                                                        float* __restrict__ part_b) {
-  using Elem = std::conditional_t<BF16, uint16_t, float>;
-  constexpr int VL = 16 / sizeof(Elem);
+// float32 rows: part of dW = dl^T x, 64 columns by the tokens of part blockIdx.y,
+// every expert; 64 tokens at a time in LDS, 16 experts a wave, a column a lane.
+// (bf16 rows go through the FFN's weight-gradient product, ffn.h.)
+__global__ __launch_bounds__(256) void scored_dw_kernel(const float* __restrict__ xv, const uint16_t* __restrict__ dl,
+                                                        int ld, int T, int d, int E, int per,
+                                                        float* __restrict__ part_w) {
   __shared__ __attribute__((aligned(16))) float xs[kDwTok][kDwCols], gs[kDwTok][kMaxExperts];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int c0 = blockIdx.x * kDwCols;
   const int t_lo = blockIdx.y * per, t_hi = min(T, t_lo + per);
-  float acc[16], db = 0.f;
+  float acc[16];
 #pragma unroll
   for (int u = 0; u < 16; ++u) acc[u] = 0.f;
   for (int t0 = t_lo; t0 < t_hi; t0 += kDwTok) {
     __syncthreads();
-    for (int i = threadIdx.x; i < kDwTok * kDwCols / VL; i += 256) {
-      const int tl = i / (kDwCols / VL), c = i % (kDwCols / VL) * VL;
-      Pack16 v;
-      v.u4 = make_uint4(0, 0, 0, 0);
-      if (t0 + tl < t_hi)
-        v.u4 = *reinterpret_cast<const uint4*>(static_cast<const Elem*>(xv) + static_cast<size_t>(t0 + tl) * d + c0 + c);
-#pragma unroll
-      for (int u = 0; u < VL; ++u) {
-        if constexpr (BF16) xs[tl][c + u] = bf16_to_f32(v.h[u]);
-        else xs[tl][c + u] = v.f[u];
-      }
+    for (int i = threadIdx.x; i < kDwTok * kDwCols / 4; i += 256) {
+      const int tl = i / (kDwCols / 4), c = i % (kDwCols / 4) * 4;
+      *reinterpret_cast<float4*>(&xs[tl][c]) =
+          t0 + tl < t_hi ? *reinterpret_cast<const float4*>(xv + static_cast<size_t>(t0 + tl) * d + c0 + c)
+                         : make_float4(0.f, 0.f, 0.f, 0.f);
     }
     for (int i = threadIdx.x; i < kDwTok * kMaxExperts; i += 256) {
       const int tl = i / kMaxExperts, e = i % kMaxExperts;
-      gs[tl][e] = t0 + tl < t_hi && e < E ? dl[static_cast<size_t>(t0 + tl) * E + e] : 0.f;
+      gs[tl][e] = t0 + tl < t_hi && e < E ? dl_value(dl + static_cast<size_t>(t0 + tl) * ld + e, E) : 0.f;
     }
     __syncthreads();
     for (int tl = 0; tl < kDwTok; ++tl) {
@@ -1040,49 +1132,99 @@ __global__ __launch_bounds__(256) void scored_dw_kernel(const void* __restrict__
         acc[4 * u + 2] = fmaf(g.z, x, acc[4 * u + 2]);
         acc[4 * u + 3] = fmaf(g.w, x, acc[4 * u + 3]);
       }
-      if (w == 0) db += gs[tl][lane];
     }
   }
 #pragma unroll
   for (int u = 0; u < 16; ++u)
     if (16 * w + u < E) part_w[(static_cast<size_t>(blockIdx.y) * E + 16 * w + u) * d + c0 + lane] = acc[u];
-  if (blockIdx.x == 0 && w == 0 && lane < E) part_b[static_cast<size_t>(blockIdx.y) * E + lane] = db;
 }
 
-// out[i] = sum over parts, in order.
-__global__ __launch_bounds__(256) void scored_dw_reduce_kernel(const float* __restrict__ part_w,
+// dw = sum over the parts, of bf16 rows over dl's three as well (rows e, E + e, 2 E + e
+// of a part of `rows` rows): 256 values a block, a wave a sixteenth of
+// the parts (its loads are in flight together).  The
+// last block: db over the blocks of scored_dlogits.  In a fixed order.
+template <int SPLITS>
+__global__ __launch_bounds__(1024) void scored_dw_reduce_kernel(const float* __restrict__ part_w,
                                                                const float* __restrict__ part_b, int parts,
-                                                               long long n, int E, float* __restrict__ dw,
-                                                               float* __restrict__ db) {
-  const long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
-  if (i < n) {
-    float s = 0.f;
-    for (int p = 0; p < parts; ++p) s += part_w[p * n + i];
-    dw[i] = s;
+                                                               int b_parts, int rows, int d, int E,
+                                                               float* __restrict__ dw, float* __restrict__ db) {
+  __shared__ float4 lds[16][64];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  const bool tail = blockIdx.x + 1 == gridDim.x;
+  const long long at = static_cast<long long>(blockIdx.x) * 256 + 4 * lane;   // (E d is a multiple of 64)
+  const bool in = !tail && at < static_cast<long long>(E) * d;
+  if (tail) {
+    if (!db) return;
+#pragma unroll 8
+    for (int p = w; p < b_parts; p += 16) s.x += lane < E ? part_b[static_cast<size_t>(p) * E + lane] : 0.f;
+  } else if (in) {
+    const int e = static_cast<int>(at / d), c = static_cast<int>(at - static_cast<long long>(e) * d);
+#pragma unroll 4
+    for (int p = w; p < parts; p += 16)
+#pragma unroll
+      for (int q = 0; q < SPLITS; ++q) {
+        const float4 v = *reinterpret_cast<const float4*>(part_w + (static_cast<size_t>(p) * rows + q * E + e) * d + c);
+        s.x += v.x;
+        s.y += v.y;
+        s.z += v.z;
+        s.w += v.w;
+      }
   }
-  if (db && i < E) {
-    float s = 0.f;
-    for (int p = 0; p < parts; ++p) s += part_b[static_cast<size_t>(p) * E + i];
-    db[i] = s;
+  lds[w][lane] = s;
+  __syncthreads();
+  if (w > 0) return;
+#pragma unroll
+  for (int v = 1; v < 16; ++v) {
+    const float4 o = lds[v][lane];
+    s.x += o.x;
+    s.y += o.y;
+    s.z += o.z;
+    s.w += o.w;
+  }
+  if (tail) {
+    if (lane < E) db[lane] = s.x;
+  } else if (in) {
+    *reinterpret_cast<float4*>(dw + at) = s;
   }
 }
 
 struct ScoredBwdWs {
-  float *dl, *part_w, *part_b;
+  uint16_t* dl;         // [T][ld]
+  int32_t* part_rows;   // [parts + 1]
+  float *part_w, *part_b;
 };
 
-// Parts of T in dW's sums: about a thousand blocks.
-int dw_parts(int T, int d) {
-  const int most = std::max(1, 1024 / std::max(1, d / kDwCols));
-  return std::max(1, std::min((T + kDwTok - 1) / kDwTok, most));
+// What the backward's sizes follow from.
+struct ScoredBwdPlan {
+  int ld;          // columns of dl's rows: 3 E, rounded up as the product wants
+  int parts, per;  // parts of T in dW's sums, and the tokens of one
+  int rows;        // rows of a part's sums
+  int b_parts;     // blocks of scored_dlogits
+};
+
+ScoredBwdPlan scored_bwd_plan(int T, int d, int E, bool bf16) {
+  ScoredBwdPlan p;
+  p.ld = (3 * E + 63) / 64 * 64;
+  // bf16: 256 x 256 tiles, about one a CU, of at least 256 tokens; float32: about a
+  // thousand blocks
+  const int tiles = (d + 255) / 256;
+  const int most = bf16 ? std::min(64, std::max(1, 256 / tiles)) : std::max(1, 1024 / std::max(1, d / kDwCols));
+  const int least = bf16 ? 256 : kDwTok;
+  p.parts = std::max(1, std::min((T + least - 1) / least, most));
+  p.per = ((T + p.parts - 1) / p.parts + kDwTok - 1) / kDwTok * kDwTok;
+  p.rows = bf16 ? p.ld : E;
+  p.b_parts = std::max(1, std::min((T + 15) / 16, 1024));
+  return p;
 }
 
-ScoredBwdWs carve_scored_bwd(Carver& c, int T, int d, int E) {
+ScoredBwdWs carve_scored_bwd(Carver& c, int T, int d, int E, bool bf16) {
+  const ScoredBwdPlan p = scored_bwd_plan(T, d, E, bf16);
   ScoredBwdWs w;
-  const size_t parts = dw_parts(T, d);
-  w.dl = c.take<float>(static_cast<size_t>(T) * E);
-  w.part_w = c.take<float>(parts * E * d);
-  w.part_b = c.take<float>(parts * E);
+  w.dl = c.take<uint16_t>(static_cast<size_t>(T) * p.ld);
+  w.part_rows = c.take<int32_t>(p.parts + 1);
+  w.part_w = c.take<float>(static_cast<size_t>(p.parts) * p.rows * d);
+  w.part_b = c.take<float>(static_cast<size_t>(p.b_parts) * E);
   return w;
 }
 
@@ -1176,9 +1318,13 @@ extern "C" int luffy_route_scored(const void* x, int T, int d, int dtype, const 
 
 extern "C" size_t luffy_route_scored_backward_workspace_size(int T, int d, int E) {
   if (T <= 0 || d <= 0 || E <= 0) return 0;
-  Carver c(nullptr);
-  carve_scored_bwd(c, T, d, E);
-  return c.size();
+  size_t most = 0;
+  for (const bool bf16 : {false, true}) {
+    Carver c(nullptr);
+    carve_scored_bwd(c, T, d, E, bf16);
+    most = std::max(most, c.size());
+  }
+  return most;
 }
 
 extern "C" int luffy_route_scored_backward(const void* x, int T, int d, int dtype, const void* w_gate, int E, int k,
@@ -1203,18 +1349,25 @@ extern "C" int luffy_route_scored_backward(const void* x, int T, int d, int dtyp
     return fail(LUFFY_E_WORKSPACE, "%s: workspace needs %zu bytes, 256-aligned", fn, need);
   hipStream_t s = static_cast<hipStream_t>(stream);
   Carver c(workspace);
-  const ScoredBwdWs ws = carve_scored_bwd(c, T, d, E);
-  const ScoreArgs a{nullptr, nullptr, E, k, score, 1, E, 1, 1, renormalise != 0, scale};
   const bool bf16 = dtype == LUFFY_BF16;
+  const ScoredBwdPlan p = scored_bwd_plan(T, d, E, bf16);
+  const ScoredBwdWs ws = carve_scored_bwd(c, T, d, E, bf16);
+  const ScoreArgs a{nullptr, nullptr, E, k, score, 1, E, 1, 1, renormalise != 0, scale};
+  launch("scored_dlogits", E % 4 == 0 ? scored_dlogits_kernel<true> : scored_dlogits_kernel<false>, p.b_parts,
+         kDlThreads, 0, s, logits, topk_idx, dgate, dlogits, T, a, p.ld, ws.dl, p.parts, p.per, ws.part_rows,
+         ws.part_b);
   const int waves = std::max(1, std::min((T + 3) / 4, 16 * persistent_grid()));
-  const int parts = dw_parts(T, d), per = ((T + parts - 1) / parts + kDwTok - 1) / kDwTok * kDwTok;
+  launch("scored_dx", bf16 ? scored_dx_kernel<true> : scored_dx_kernel<false>, waves, 256, 0, s, w_gate, ws.dl, p.ld, T,
+         d, E, k, dx_rep, slot_pos, rep_of_pos, rep_row, dx);
+  if (bf16)
+    row_product_enqueue("scored_dw", ws.dl, static_cast<const uint16_t*>(x), ws.part_rows, p.parts, p.ld, d, ws.part_w,
+                        s);
+  else
+    launch("scored_dw", scored_dw_kernel, dim3(d / kDwCols, p.parts), 256, 0, s, static_cast<const float*>(x), ws.dl,
+           p.ld, T, d, E, p.per, ws.part_w);
   const long long n = static_cast<long long>(E) * d;
-  launch("scored_dlogits", scored_dlogits_kernel, waves, 256, 0, s, logits, topk_idx, dgate, dlogits, T, a, ws.dl);
-  launch("scored_dx", bf16 ? scored_dx_kernel<true> : scored_dx_kernel<false>, waves, 256, 0, s, w_gate, ws.dl, T, d, E,
-         k, dx_rep, slot_pos, rep_of_pos, rep_row, dx);
-  launch("scored_dw", bf16 ? scored_dw_kernel<true> : scored_dw_kernel<false>, dim3(d / kDwCols, parts), 256, 0, s, x,
-         ws.dl, T, d, E, per, ws.part_w, ws.part_b);
-  launch("scored_dw_reduce", scored_dw_reduce_kernel, static_cast<int>((n + 255) / 256), 256, 0, s, ws.part_w,
-         ws.part_b, parts, n, E, dw_gate, db_gate);
+  launch("scored_dw_reduce", bf16 ? scored_dw_reduce_kernel<3> : scored_dw_reduce_kernel<1>,
+         static_cast<int>((n + 255) / 256) + 1, 1024, 0, s, ws.part_w, ws.part_b, p.parts, p.b_parts, p.rows, d, E, dw_gate,
+         db_gate);
   return check_launch(fn);
 }
