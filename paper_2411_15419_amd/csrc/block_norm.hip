@@ -80,20 +80,44 @@ __device__ __forceinline__ void store8(float* p, const float (&f)[8]) {
 }
 
 // Sums over a team's lanes; every lane ends with the same sums.  WAVES = 1: the
-// team is lt <= 64 consecutive lanes (a power of two).  WAVES > 1: the whole
-// block, by way of LDS; `turn` takes the rounds of a row through three buffers,
-// so that a buffer is written again only after a barrier that follows its reads.
+// team is lt <= 64 consecutive lanes (a power of two).  WAVES > 1: by way of LDS, all
+// teams of the block together; `turn` takes the rounds of a row through three
+// buffers, so that a buffer is written again only after a barrier that follows its
+// reads.
+template <int DPP, int ROWS = 0xF>
+__device__ __forceinline__ float dpp_f32(float x) {
+  return __uint_as_float(static_cast<uint32_t>(
+      __builtin_amdgcn_update_dpp(0, static_cast<int>(__float_as_uint(x)), DPP, ROWS, 0xF, false)));
+}
 template <int WAVES, int N>
 __device__ __forceinline__ void team_sum(float (&v)[N], int lt, float (*lds)[16][4], int& turn) {
+  // inside rows of 16 lanes
 #pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) {
-    if (WAVES == 1 && o >= lt) continue;
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], o, 64);
+  for (int i = 0; i < N; ++i) {
+    v[i] += dpp_f32<0xB1>(v[i]);    // quad_perm [1, 0, 3, 2]
+    v[i] += dpp_f32<0x4E>(v[i]);    // quad_perm [2, 3, 0, 1]
+    v[i] += dpp_f32<0x141>(v[i]);   // row_half_mirror
+    if (WAVES > 1 || lt > 8) v[i] += dpp_f32<0x140>(v[i]);   // row_mirror
   }
-  if constexpr (WAVES > 1) {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    if (lane == 0) {
+  if (WAVES == 1 && lt <= 16) return;
+  if (WAVES == 1 && lt == 32) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], 16, 64);
+    return;
+  }
+  // the rows' sums to the last lane
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    v[i] += dpp_f32<0x142, 0xA>(v[i]);   // row_bcast:15 to rows 1 and 3
+    v[i] += dpp_f32<0x143, 0xC>(v[i]);   // row_bcast:31 to rows 2 and 3
+  }
+  if constexpr (WAVES == 1) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      v[i] = __uint_as_float(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(__float_as_uint(v[i])), 63)));
+  } else {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, first = w / WAVES * WAVES;
+    if (lane == 63) {
 #pragma unroll
       for (int i = 0; i < N; ++i) lds[turn][w][i] = v[i];
     }
@@ -102,7 +126,7 @@ __device__ __forceinline__ void team_sum(float (&v)[N], int lt, float (*lds)[16]
     for (int i = 0; i < N; ++i) {
       float s = 0.f;
 #pragma unroll
-      for (int j = 0; j < WAVES; ++j) s += lds[turn][j][i];
+      for (int j = 0; j < WAVES; ++j) s += lds[turn][first + j][i];
       v[i] = s;
     }
     turn = turn == 2 ? 0 : turn + 1;
@@ -242,6 +266,11 @@ __global__ __launch_bounds__(WAVES > 1 ? WAVES * 64 : 256) void block_norm_kerne
 // and adds them up in registers, a block's teams are added in LDS, and the
 // blocks' sums go through the workspace to block_norm_reduce_kernel, all in a
 // fixed order.
+//   Eight waves a block, one block a CU (no spills, and few sums to add up at the
+// end); bf16 rows are fetched while the rows before them are worked on, and a lane
+// holds its columns' weights.  16384 x 4096 bf16: 227 us and 9 us for the sums, 3.4
+// TB/s in all (a large copy: 4.9); 272 and 25 us with two blocks a CU, nothing in
+// flight and row sums by ds_bpermute.
 constexpr int kSums = 5;   // w_pre, b_pre, w_post, b_post, gate
 
 struct NormBwdArgs {
@@ -255,49 +284,90 @@ struct NormBwdArgs {
   float* sum[kSums];   // results; a null one is not wanted
 };
 
-template <bool BF16, int CH, int WAVES>
-__global__ __launch_bounds__(WAVES > 1 ? WAVES * 64 : 512) void block_norm_backward_kernel(NormBwdArgs a, int lt_log2,
-                                                                                         float* __restrict__ part) {
-  constexpr int kThreads = WAVES > 1 ? WAVES * 64 : 512;
+// BIAS: db_pre or db_post is wanted.
+template <bool BF16, int CH, int WAVES, bool BIAS>
+__global__ __launch_bounds__(WAVES == 16 ? 1024 : 512) void block_norm_backward_kernel(NormBwdArgs a, int lt_log2,
+                                                                                       float* __restrict__ part) {
+  constexpr int kThreads = WAVES == 16 ? 1024 : 512;
+  constexpr bool AHEAD = BF16 && WAVES < 16;
   __shared__ float lds[3][16][4];
   int turn = 0;
-  const int lt = WAVES > 1 ? kThreads : 1 << lt_log2;
-  const int teams = WAVES > 1 ? 1 : kThreads >> lt_log2;
-  const int sub = WAVES > 1 ? threadIdx.x : threadIdx.x & (lt - 1);
-  const int team = WAVES > 1 ? 0 : threadIdx.x >> lt_log2;
+  const int lt = WAVES > 1 ? WAVES * 64 : 1 << lt_log2;
+  const int teams = WAVES > 1 ? kThreads / (WAVES * 64) : kThreads >> lt_log2;
+  const int team = WAVES > 1 ? threadIdx.x / (WAVES * 64) : threadIdx.x >> lt_log2;
+  const int sub = WAVES > 1 ? threadIdx.x % (WAVES * 64) : threadIdx.x & (lt - 1);
   const int chunks = a.d >> 3;
   const float inv_d = 1.0f / static_cast<float>(a.d);
-  float acc[kSums][CH][8];
+  float acc[kSums][CH][8];   // (without BIAS two of them are not touched)
 #pragma unroll
   for (int p = 0; p < kSums; ++p)
 #pragma unroll
     for (int i = 0; i < CH; ++i)
 #pragma unroll
       for (int j = 0; j < 8; ++j) acc[p][i][j] = 0.f;
-  for (long long t0 = static_cast<long long>(blockIdx.x) * teams; t0 < a.T;
-       t0 += static_cast<long long>(gridDim.x) * teams) {
-    const long long tt = t0 + team;
-    if (tt >= a.T) break;   // a whole team: its sums are its own
-    const size_t row = static_cast<size_t>(tt) * a.d;
+  struct Rows {
     Chunk<BF16> y[CH], o[CH], g[CH], dn[CH], du[CH];
+  };
+  // (a team past the last row has zeros, and stores nothing)
+  auto load = [&](long long tt, Rows& r) {
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
       const int c = sub + i * lt;
-      y[i].zero();
-      o[i].zero();
-      g[i].zero();
-      dn[i].zero();
-      du[i].zero();
-      if (c < chunks) {
-        if (a.y) y[i].load(a.y, row + 8 * c);
-        if (a.dout) dn[i].load(a.dout, row + 8 * c);
+      r.y[i].zero();
+      r.o[i].zero();
+      r.g[i].zero();
+      r.dn[i].zero();
+      r.du[i].zero();
+      if (tt < a.T && c < chunks) {
+        const size_t at = static_cast<size_t>(tt) * a.d + 8 * c;
+        if (a.y) r.y[i].load(a.y, at);
+        if (a.dout) r.dn[i].load(a.dout, at);
         if (a.du) {
-          o[i].load(a.o, row + 8 * c);
-          du[i].load(a.du, row + 8 * c);
+          r.o[i].load(a.o, at);
+          r.du[i].load(a.du, at);
         }
-        if (a.gate_kind == LUFFY_GATE_TOKEN) g[i].load(a.gate, row + 8 * c);
+        if (a.gate_kind == LUFFY_GATE_TOKEN) r.g[i].load(a.gate, at);
       }
     }
+  };
+  // a lane's columns are the same in every row: their weights stay in registers
+  // where there is one chunk of them
+  constexpr bool HOLD = CH == 1 && WAVES < 16;
+  float held[3][8];   // w_pre, w_post, a channel gate
+  if constexpr (HOLD) {
+    const int c = 8 * min(sub, chunks - 1);
+    if (a.du) load8(a.w_pre + c, held[0]);
+    if (a.w_post) load8(a.w_post + c, held[1]);
+    if (a.gate_kind == LUFFY_GATE_CHANNEL) load8(static_cast<const float*>(a.gate) + c, held[2]);
+  }
+  auto weights = [&](int which, const float* from, int c, float (&w)[8]) {
+    if constexpr (HOLD) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] = held[which][j];
+    } else {
+      load8(from + 8 * c, w);
+    }
+  };
+  const long long step = static_cast<long long>(gridDim.x) * teams;
+  long long t0 = static_cast<long long>(blockIdx.x) * teams;
+  Rows cur, ahead;
+  if constexpr (AHEAD) load(t0 + team, ahead);
+  for (; t0 < a.T; t0 += step) {
+    const long long tt = t0 + team;
+    if constexpr (AHEAD) {
+      cur = ahead;
+      load(tt + step, ahead);
+    } else {
+      load(tt, cur);
+    }
+    const bool valid = tt < a.T;
+    if (WAVES == 1 && !valid) break;   // a whole team: its sums are its own
+    const size_t row = static_cast<size_t>(valid ? tt : 0) * a.d;
+    const auto& y = cur.y;
+    const auto& o = cur.o;
+    const auto& g = cur.g;
+    const auto& dn = cur.dn;
+    const auto& du = cur.du;
     float mo = 0.f, my = 0.f;
     if (a.layer) {
       float s[2] = {0.f, 0.f};
@@ -325,7 +395,7 @@ __global__ __launch_bounds__(WAVES > 1 ? WAVES * 64 : 512) void block_norm_backw
         float f[8], q[8], w[8];
         o[i].get(f);
         du[i].get(q);
-        load8(a.w_pre + 8 * c, w);
+        weights(0, a.w_pre, c, w);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const float dev = f[j] - mo;
@@ -356,12 +426,12 @@ __global__ __launch_bounds__(WAVES > 1 ? WAVES * 64 : 512) void block_norm_backw
         float f[8], q[8], w[8];
         o[i].get(f);
         du[i].get(q);
-        load8(a.w_pre + 8 * c, w);
+        weights(0, a.w_pre, c, w);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const float oh = (f[j] - mo) * ro;
-          acc[0][i][j] = fmaf(q[j], oh, acc[0][i][j]);
-          acc[1][i][j] += q[j];
+          if (valid) acc[0][i][j] = fmaf(q[j], oh, acc[0][i][j]);
+          if (BIAS) acc[1][i][j] += q[j];
           dt[j] += ro * (fmaf(q[j], w[j], -qm) - oh * qo);
         }
       }
@@ -370,7 +440,7 @@ __global__ __launch_bounds__(WAVES > 1 ? WAVES * 64 : 512) void block_norm_backw
       for (int j = 0; j < 8; ++j) v[j] = a.res_scale * dt[j];
       Chunk<BF16> st;
       st.set(v);
-      st.store(a.dx, row + 8 * c);
+      if (valid) st.store(a.dx, row + 8 * c);
       if (!a.y) continue;
       float yh[8];
       y[i].get(v);
@@ -379,7 +449,7 @@ __global__ __launch_bounds__(WAVES > 1 ? WAVES * 64 : 512) void block_norm_backw
       float w[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
       if (a.w_post) {
         float b[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        load8(a.w_post + 8 * c, w);
+        weights(1, a.w_post, c, w);
         if (a.b_post) load8(a.b_post + 8 * c, b);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = fmaf(yh[j], w[j], b[j]);
@@ -387,7 +457,7 @@ __global__ __launch_bounds__(WAVES > 1 ? WAVES * 64 : 512) void block_norm_backw
       if (a.gate_kind != LUFFY_GATE_NONE) {
         float gf[8], dg[8];
         if (a.gate_kind == LUFFY_GATE_TOKEN) g[i].get(gf);
-        else load8(static_cast<const float*>(a.gate) + 8 * c, gf);
+        else weights(2, static_cast<const float*>(a.gate), c, gf);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           dg[j] = dt[j] * v[j];
@@ -395,17 +465,18 @@ __global__ __launch_bounds__(WAVES > 1 ? WAVES * 64 : 512) void block_norm_backw
         }
         if (a.gate_kind == LUFFY_GATE_TOKEN) {
           st.set(dg);
-          if (a.dgate) st.store(a.dgate, row + 8 * c);
+          if (valid && a.dgate) st.store(a.dgate, row + 8 * c);
         } else {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) acc[4][i][j] += dg[j];
+          for (int j = 0; j < 8; ++j)
+            if (valid) acc[4][i][j] += dg[j];
         }
       }
       if (a.w_post) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          acc[2][i][j] = fmaf(dt[j], yh[j], acc[2][i][j]);
-          acc[3][i][j] += dt[j];
+          if (valid) acc[2][i][j] = fmaf(dt[j], yh[j], acc[2][i][j]);
+          if (BIAS && valid) acc[3][i][j] += dt[j];
           dt[j] *= w[j];
           ps[0] = fmaf(dt[j], yh[j], ps[0]);
           ps[1] += dt[j];
@@ -429,16 +500,16 @@ __global__ __launch_bounds__(WAVES > 1 ? WAVES * 64 : 512) void block_norm_backw
       }
       Chunk<BF16> st;
       st.set(pf);
-      st.store(a.dy, row + 8 * c);
+      if (valid) st.store(a.dy, row + 8 * c);
     }
   }
   // sums over rows: the block's teams in LDS, one sum of kSums at a time
-  __shared__ __attribute__((aligned(16))) float cols[WAVES > 1 ? 1 : kThreads * 8 * CH];
+  __shared__ __attribute__((aligned(16))) float cols[kThreads == WAVES * 64 ? 1 : kThreads * 8 * CH];
 #pragma unroll
   for (int p = 0; p < kSums; ++p) {
     if (!a.sum[p]) continue;
     float* dst = gridDim.x > 1 ? part + (static_cast<size_t>(blockIdx.x) * kSums + p) * a.d : a.sum[p];
-    if constexpr (WAVES > 1) {
+    if constexpr (kThreads == WAVES * 64) {
 #pragma unroll
       for (int i = 0; i < CH; ++i)
         if (sub + i * lt < chunks) store8(dst + 8 * (sub + i * lt), acc[p][i]);
@@ -456,22 +527,23 @@ __global__ __launch_bounds__(WAVES > 1 ? WAVES * 64 : 512) void block_norm_backw
   }
 }
 
-// Sums of the blocks' parts: 64 columns of one sum a block, a wave an eighth of
-// the parts.
-__global__ __launch_bounds__(512) void block_norm_reduce_kernel(const float* __restrict__ part, int blocks, int d,
-                                                                NormBwdArgs a) {
-  __shared__ float lds[8][64];
+// Sums of the blocks' parts: 64 columns of one sum a block, a wave a sixteenth of
+// the parts (its loads are in flight together).
+__global__ __launch_bounds__(1024) void block_norm_reduce_kernel(const float* __restrict__ part, int blocks, int d,
+                                                                 NormBwdArgs a) {
+  __shared__ float lds[16][64];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int p = blockIdx.y, c = blockIdx.x * 64 + lane;   // d is a multiple of 64
   float* out = p == 0 ? a.sum[0] : p == 1 ? a.sum[1] : p == 2 ? a.sum[2] : p == 3 ? a.sum[3] : a.sum[4];
   if (!out) return;
   float s = 0.f;
-  for (int b = w; b < blocks; b += 8) s += part[(static_cast<size_t>(b) * kSums + p) * d + c];
+#pragma unroll 16
+  for (int b = w; b < blocks; b += 16) s += part[(static_cast<size_t>(b) * kSums + p) * d + c];
   lds[w][lane] = s;
   __syncthreads();
   if (w == 0) {
 #pragma unroll
-    for (int j = 1; j < 8; ++j) s += lds[j][lane];
+    for (int j = 1; j < 16; ++j) s += lds[j][lane];
     out[c] = s;
   }
 }
@@ -507,32 +579,56 @@ void launch_norm(const NormArgs& a, hipStream_t s) {
 #undef LUFFY_NORM
 }
 
-// Blocks of the backward: each leaves kSums rows of d sums to be added up.
-int bwd_blocks(int T, int d) {
-  constexpr int most = 256;   // the workspace is sized without a device
-  if (d <= 512) return norm_blocks(T, 512 >> team_log2(d, 1), most);
-  if (d <= 1024) return norm_blocks(T, 8, most);
-  return norm_blocks(T, 1, d <= 4096 ? 2 * most : most);
+// A team of the backward and the blocks of the grid (each leaves kSums rows of d sums
+// to be added up).  One chunk a lane, or two, which halves the waves that wait for
+// each other: from 16 rows a team on (bf16, us, one | two chunks: 65536 x 1024 209 |
+// 201, 32768 x 2048 213 | 201, 16384 x 4096 237 | 227; 8192 x 1024 36 | 40; float32
+// 3001 x 1088 33 | 36).
+struct BwdShape {
+  int chunks, waves, blocks;
+};
+
+BwdShape bwd_shape(int T, int d, bool bf16) {
+  constexpr int most = 256;   // blocks: the workspace is sized without a device
+  auto waves = [&](int per) {
+    int w = 1;
+    while (w < 8 && w * per < d) w *= 2;
+    return w;
+  };
+  if (d > 8192) return {d <= 16384 ? 2 : 4, 16, norm_blocks(T, 1, most)};
+  if (d > 4096) return {2, 8, norm_blocks(T, 1, most)};
+  if (d <= 512) return {1, 1, norm_blocks(T, 512 >> team_log2(d, 1), most)};
+  const int teams = 8 / waves(1024);
+  if (bf16 && T >= 16 * most * teams) return {2, waves(1024), norm_blocks(T, teams, most)};
+  return {1, waves(512), norm_blocks(T, 8 / waves(512), most)};
 }
 
-template <bool BF16>
+template <bool BF16, bool BIAS>
 void launch_norm_backward(const NormBwdArgs& a, float* part, hipStream_t s) {
-  const int blocks = bwd_blocks(a.T, a.d);
-#define LUFFY_NORM_B(CH, WAVES)                                                                               \
-  launch("block_norm_backward", block_norm_backward_kernel<BF16, CH, WAVES>, blocks, WAVES > 1 ? WAVES * 64 : 512, \
-         0, s, a, team_log2(a.d, CH), part)
-  if (a.d <= 512) LUFFY_NORM_B(1, 1);
-  else if (a.d <= 1024) LUFFY_NORM_B(2, 1);
-  else if (a.d <= 2048) LUFFY_NORM_B(1, 4);
-  else if (a.d <= 4096) LUFFY_NORM_B(1, 8);
-  else if (a.d <= 8192) LUFFY_NORM_B(1, 16);
-  else if (a.d <= 16384) LUFFY_NORM_B(2, 16);
-  else LUFFY_NORM_B(4, 16);
+  const BwdShape sh = bwd_shape(a.T, a.d, BF16);
+  const int blocks = sh.blocks;
+#define LUFFY_NORM_B(CH, WAVES)                                                                           \
+  launch("block_norm_backward", block_norm_backward_kernel<BF16, CH, WAVES, BIAS>, blocks,                \
+         WAVES == 16 ? 1024 : 512, 0, s, a, team_log2(a.d, CH), part)
+  if (sh.waves == 16) {
+    if (sh.chunks == 2) LUFFY_NORM_B(2, 16); else LUFFY_NORM_B(4, 16);
+  } else if (sh.chunks == 1) {
+    if (sh.waves == 1) LUFFY_NORM_B(1, 1);
+    else if (sh.waves == 2) LUFFY_NORM_B(1, 2);
+    else if (sh.waves == 4) LUFFY_NORM_B(1, 4);
+    else LUFFY_NORM_B(1, 8);
+  } else if (sh.waves == 8) {
+    LUFFY_NORM_B(2, 8);
+  } else if constexpr (BF16) {
+    if (sh.waves == 1) LUFFY_NORM_B(2, 1);
+    else if (sh.waves == 2) LUFFY_NORM_B(2, 2);
+    else LUFFY_NORM_B(2, 4);
+  }
 #undef LUFFY_NORM_B
   bool any = false;
   for (float* p : a.sum) any = any || p;
   if (any && blocks > 1)
-    launch("block_norm_reduce", block_norm_reduce_kernel, dim3(a.d / 64, kSums), 512, 0, s,
+    launch("block_norm_reduce", block_norm_reduce_kernel, dim3(a.d / 64, kSums), 1024, 0, s,
            static_cast<const float*>(part), blocks, a.d, a);
 }
 
@@ -591,7 +687,7 @@ extern "C" int luffy_block_norm(const void* x, const void* y, int T, int d, int 
 extern "C" size_t luffy_block_norm_backward_workspace_size(int T, int d) {
   if (T <= 0 || d <= 0) return 0;
   Carver c(nullptr);
-  c.take<float>(static_cast<size_t>(bwd_blocks(T, d)) * kSums * d);
+  c.take<float>(static_cast<size_t>(std::max(bwd_shape(T, d, true).blocks, bwd_shape(T, d, false).blocks)) * kSums * d);
   return c.size();
 }
 
@@ -623,7 +719,9 @@ extern "C" int luffy_block_norm_backward(const void* y, const void* o, int T, in
   a.sum[2] = dw_post;
   a.sum[3] = db_post;
   a.sum[4] = gate_kind == LUFFY_GATE_CHANNEL ? static_cast<float*>(dgate) : nullptr;
-  if (dtype == LUFFY_BF16) launch_norm_backward<true>(a, static_cast<float*>(workspace), static_cast<hipStream_t>(stream));
-  else launch_norm_backward<false>(a, static_cast<float*>(workspace), static_cast<hipStream_t>(stream));
+  const bool bias = db_pre || db_post;
+  auto* run = dtype == LUFFY_BF16 ? (bias ? launch_norm_backward<true, true> : launch_norm_backward<true, false>)
+                                  : (bias ? launch_norm_backward<false, true> : launch_norm_backward<false, false>);
+  run(a, static_cast<float*>(workspace), static_cast<hipStream_t>(stream));
   return check_launch(fn);
 }
