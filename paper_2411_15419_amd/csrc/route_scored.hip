@@ -96,10 +96,11 @@ __device__ __forceinline__ float sigmoid(float l) {
   return (l < 0.f ? e : 1.0f) * __builtin_amdgcn_rcpf(1.0f + e);
 }
 
-// Choices of R tokens by the 16 lanes of a row, lane m with the logits l[r][j] of
-// experts 16 j + m (those past E are ignored).  dl bounds a token's logits' error.
-// Lane i < k ends with the i-th expert and its gate; `marked` is set for the row where
-// a deciding gap may be of either sign:
+// Choice of one token by the 16 lanes of a row, lane m with the logits l[j] of
+// experts 16 j + m (those past E are ignored).  dl bounds the logits' error.  Lane i <
+// k ends with the i-th expert and its gate; key[j] is not 0 for the experts of the kept
+// groups; `marked` is set for the row where a deciding gap may be of either sign (bit 0:
+// between experts, bit 1: between groups):
 //   logits         2 dl
 //   sigmoid + bias a score moves by at most dl / 4, its evaluation and the sum by
 //                  less than 2^-20 (1 + |c|)
@@ -109,143 +110,138 @@ __device__ __forceinline__ float sigmoid(float l) {
 // expert (group), the lower one being the larger key; the sum of a group's two best
 // moves by twice that.
 //   A lane sorts its experts once; then the row's largest head is the next choice, and
-// its lane goes on to its next.  The steps are chains of exchanges, and the code is
-// fetched once a block, cold: both want little of it.  (Float maxima, a search through
-// all registers for every choice, gaps tested one by one: 5000 instructions for four
-// tokens of 64 experts instead of TODO, and TODO us.)
-template <int NEB, int R>
-__device__ __forceinline__ void choose16(const float (&l)[R][NEB], const float (&bal)[NEB], const int (&grp)[NEB],
-                                         const ScoreArgs& a, const float (&dl)[R], int (&expert)[R],
-                                         float (&gate)[R], bool (&marked)[R]) {
+// its lane goes on to its next: the steps are one chain of exchanges, and its length is
+// the time.
+template <int NEB, bool SIG, bool GROUPED>
+__device__ __forceinline__ void choose16(const float (&l)[NEB], const float (&bal)[NEB], const int (&grp)[NEB],
+                                         const ScoreArgs& a, float dl, int& expert, float& gate, uint32_t (&key)[NEB],
+                                         uint32_t& marked) {
   const int lane = threadIdx.x & 63, m = lane & 15, row = lane & 48;
-  const bool sig = a.score == LUFFY_SCORE_SIGMOID, biased = a.balance != nullptr;
-  const bool grouped = a.top_groups < a.groups;
+  constexpr bool sig = SIG, grouped = GROUPED;
+  const bool biased = a.balance != nullptr;
   const bool by_score = grouped && !biased && a.best == 2;   // what groups go by
+  float s[NEB], top = 0.f, inv_z = 0.f;
+  if constexpr (!sig) {
+    uint32_t most = 0;
+    float z = 0.f;
 #pragma unroll
-  for (int r = 0; r < R; ++r) {
-    float s[NEB], top = 0.f, inv_z = 0.f;
-    uint32_t key[NEB];
-    if (!sig) {
-      uint32_t most = 0;
-      float z = 0.f;
-#pragma unroll
-      for (int j = 0; j < NEB; ++j) most = max(most, 16 * j + m < a.E ? order_key(l[r][j]) : 0u);
-      top = key_value(max16(most));
-#pragma unroll
-      for (int j = 0; j < NEB; ++j) {
-        s[j] = __builtin_amdgcn_exp2f((l[r][j] - top) * kLog2e);
-        z += 16 * j + m < a.E ? s[j] : 0.f;
-      }
-      inv_z = __builtin_amdgcn_rcpf(sum16(z));
-#pragma unroll
-      for (int j = 0; j < NEB; ++j) s[j] *= inv_z;
-    } else if (biased || by_score) {
-#pragma unroll
-      for (int j = 0; j < NEB; ++j) s[j] = sigmoid(l[r][j]);
-    }
-    const float ds = sig ? fmaf(0.25f, dl[r], 0x1p-21f) : fmaf(2.0f * inv_z, dl[r], 0x1p-21f);   // (inv_z: the largest score)
-    const float dc = biased ? ds : dl[r];
-#pragma unroll
-    for (int j = 0; j < NEB; ++j) key[j] = 16 * j + m < a.E ? order_key(biased ? s[j] + bal[j] : l[r][j]) : 0u;
-    bool bad = false;
-    if (grouped) {
-      // every lane: its experts' groups' values, with the group in the low bits
-      const bool two = a.best == 2 && a.group_size > 1;
-      const int gs = a.group_size;
-      uint32_t gk[NEB], u[NEB];
-#pragma unroll
-      for (int j = 0; j < NEB; ++j) {
-        u[j] = by_score && 16 * j + m < a.E ? order_key(s[j]) : key[j];
-        gk[j] = 0;
-      }
-      auto value_key = [&](uint32_t b1, uint32_t b2, int g) {
-        const uint32_t v = two ? order_key(key_value(b1) + key_value(b2)) : b1;
-        return (v & ~15u) | static_cast<uint32_t>(15 - g);
-      };
-      if (gs <= 16 && (gs & (gs - 1)) == 0) {
-        // a group is gs neighbouring lanes of one register
-#pragma unroll
-        for (int j = 0; j < NEB; ++j) {
-          uint32_t b1 = u[j], b2 = 0;
-          if (gs >= 2) best2_step<0xB1>(b1, b2);     // quad_perm [1, 0, 3, 2]
-          if (gs >= 4) best2_step<0x4E>(b1, b2);     // quad_perm [2, 3, 0, 1]
-          if (gs >= 8) best2_step<0x141>(b1, b2);    // row_half_mirror
-          if (gs >= 16) best2_step<0x140>(b1, b2);   // row_mirror
-          if (16 * j + m < a.E) gk[j] = value_key(b1, b2, grp[j]);
-        }
-      } else {
-        for (int g = 0; g < a.groups; ++g) {
-          uint32_t b1 = 0, b2 = 0;
-#pragma unroll
-          for (int j = 0; j < NEB; ++j) {
-            const uint32_t v = grp[j] == g ? u[j] : 0u;
-            b2 = max(b2, min(b1, v));
-            b1 = max(b1, v);
-          }
-          best2_step<0x128>(b1, b2);
-          best2_step<0x124>(b1, b2);
-          best2_step<0x122>(b1, b2);
-          best2_step<0x121>(b1, b2);
-          const uint32_t v = value_key(b1, b2, g);
-#pragma unroll
-          for (int j = 0; j < NEB; ++j)
-            if (grp[j] == g && 16 * j + m < a.E) gk[j] = v;
-        }
-      }
-      uint32_t bound = ~0u, last = ~0u;   // the i-th group's key, and the one before
-      for (int i = 0; i <= a.top_groups; ++i) {
-        uint32_t best = 0;
-        last = bound;
-#pragma unroll
-        for (int j = 0; j < NEB; ++j) best = max(best, gk[j] < bound ? gk[j] : 0u);
-        bound = max16(best);
-      }
-#pragma unroll
-      for (int j = 0; j < NEB; ++j)
-        if (gk[j] < last) key[j] = 0;
-      const float dg = (a.best == 2 ? 2.0f : 1.0f) * (by_score ? ds : dc);
-      bad = uncertain(key_value(last, 15u), key_value(bound, 15u), 0x1p-18f, dg);
-    }
-    // the lane's experts, largest key first
-#pragma unroll
-    for (int j = 0; j < NEB; ++j) key[j] = key[j] ? (key[j] & ~63u) | static_cast<uint32_t>(63 - 16 * j - m) : 0u;
-#pragma unroll
-    for (int i = 0; i + 1 < NEB; ++i)
-#pragma unroll
-      for (int j = 0; j + 1 < NEB - i; ++j) {
-        const uint32_t hi = max(key[j], key[j + 1]);
-        key[j + 1] = min(key[j], key[j + 1]);
-        key[j] = hi;
-      }
-    uint32_t own = 0;   // lane i: the i-th choice's key; lane k: the first that is left out
-    for (int i = 0; i <= a.k; ++i) {
-      const uint32_t best = max16(key[0]);
-      own = m == i ? best : own;
-      const bool taken = key[0] == best;   // (none is left: zeros move up)
-#pragma unroll
-      for (int j = 0; j + 1 < NEB; ++j) key[j] = taken ? key[j + 1] : key[j];
-      key[NEB - 1] = taken ? 0u : key[NEB - 1];
-    }
-    const uint32_t next = dpp<0x101>(own);   // row_shl: lane i + 1's
-    bad = bad || (m < a.k && next && uncertain(key_value(own, 63u), key_value(next, 63u), 0x1p-17f, dc));
-    marked[r] = max16(bad ? 1u : 0u) != 0;
-    expert[r] = 63 - static_cast<int>(own & 63u);
-    // gates, from the chosen experts' logits
-    float lx = 0.f;
+    for (int j = 0; j < NEB; ++j) most = max(most, 16 * j + m < a.E ? order_key(l[j]) : 0u);
+    top = key_value(max16(most));
 #pragma unroll
     for (int j = 0; j < NEB; ++j) {
-      const float v = __shfl(l[r][j], row | (expert[r] & 15), 64);
-      if ((expert[r] >> 4) == j) lx = v;
+      s[j] = __builtin_amdgcn_exp2f((l[j] - top) * kLog2e);
+      z += 16 * j + m < a.E ? s[j] : 0.f;
     }
-    if (a.renormalise) {
-      const bool mine = m < a.k;
-      const float most = key_value(max16(mine ? order_key(lx) : 0u));
-      const float p = !mine ? 0.f
-                            : sig ? sigmoid_shifted(lx, fminf(most, 0.f)) : __builtin_amdgcn_exp2f((lx - most) * kLog2e);
-      gate[r] = a.scale * (p * __builtin_amdgcn_rcpf(sum16(p)));
+    inv_z = __builtin_amdgcn_rcpf(sum16(z));
+#pragma unroll
+    for (int j = 0; j < NEB; ++j) s[j] *= inv_z;
+  } else if (biased || by_score) {
+#pragma unroll
+    for (int j = 0; j < NEB; ++j) s[j] = sigmoid(l[j]);
+  }
+  const float ds = sig ? fmaf(0.25f, dl, 0x1p-21f) : fmaf(2.0f * inv_z, dl, 0x1p-21f);   // (inv_z: the largest score)
+  const float dc = biased ? ds : dl;
+#pragma unroll
+  for (int j = 0; j < NEB; ++j) key[j] = 16 * j + m < a.E ? order_key(biased ? s[j] + bal[j] : l[j]) : 0u;
+  uint32_t bad = 0;
+  if constexpr (grouped) {
+    // every lane: its experts' groups' values, with the group in the low bits
+    const bool two = a.best == 2 && a.group_size > 1;
+    const int gs = a.group_size;
+    uint32_t gk[NEB], u[NEB];
+#pragma unroll
+    for (int j = 0; j < NEB; ++j) {
+      u[j] = by_score && 16 * j + m < a.E ? order_key(s[j]) : key[j];
+      gk[j] = 0;
+    }
+    auto value_key = [&](uint32_t b1, uint32_t b2, int g) {
+      const uint32_t v = two ? order_key(key_value(b1) + key_value(b2)) : b1;
+      return (v & ~15u) | static_cast<uint32_t>(15 - g);
+    };
+    if (gs <= 16 && (gs & (gs - 1)) == 0) {
+      // a group is gs neighbouring lanes of one register
+#pragma unroll
+      for (int j = 0; j < NEB; ++j) {
+        uint32_t b1 = u[j], b2 = 0;
+        if (gs >= 2) best2_step<0xB1>(b1, b2);     // quad_perm [1, 0, 3, 2]
+        if (gs >= 4) best2_step<0x4E>(b1, b2);     // quad_perm [2, 3, 0, 1]
+        if (gs >= 8) best2_step<0x141>(b1, b2);    // row_half_mirror
+        if (gs >= 16) best2_step<0x140>(b1, b2);   // row_mirror
+        if (16 * j + m < a.E) gk[j] = value_key(b1, b2, grp[j]);
+      }
     } else {
-      gate[r] = a.scale * (sig ? sigmoid(lx) : __builtin_amdgcn_exp2f((lx - top) * kLog2e) * inv_z);
+      for (int g = 0; g < a.groups; ++g) {
+        uint32_t b1 = 0, b2 = 0;
+#pragma unroll
+        for (int j = 0; j < NEB; ++j) {
+          const uint32_t v = grp[j] == g ? u[j] : 0u;
+          b2 = max(b2, min(b1, v));
+          b1 = max(b1, v);
+        }
+        best2_step<0x128>(b1, b2);
+        best2_step<0x124>(b1, b2);
+        best2_step<0x122>(b1, b2);
+        best2_step<0x121>(b1, b2);
+        const uint32_t v = value_key(b1, b2, g);
+#pragma unroll
+        for (int j = 0; j < NEB; ++j)
+          if (grp[j] == g && 16 * j + m < a.E) gk[j] = v;
+      }
     }
+    uint32_t bound = ~0u, last = ~0u;   // the i-th group's key, and the one before
+    for (int i = 0; i <= a.top_groups; ++i) {
+      uint32_t best = 0;
+      last = bound;
+#pragma unroll
+      for (int j = 0; j < NEB; ++j) best = max(best, gk[j] < bound ? gk[j] : 0u);
+      bound = max16(best);
+    }
+#pragma unroll
+    for (int j = 0; j < NEB; ++j)
+      if (gk[j] < last) key[j] = 0;
+    const float dg = (a.best == 2 ? 2.0f : 1.0f) * (by_score ? ds : dc);
+    bad = uncertain(key_value(last, 15u), key_value(bound, 15u), 0x1p-18f, dg) ? 2u : 0u;
+  }
+  // the lane's experts, largest key first
+  uint32_t head[NEB];
+#pragma unroll
+  for (int j = 0; j < NEB; ++j) head[j] = key[j] ? (key[j] & ~63u) | static_cast<uint32_t>(63 - 16 * j - m) : 0u;
+#pragma unroll
+  for (int i = 0; i + 1 < NEB; ++i)
+#pragma unroll
+    for (int j = 0; j + 1 < NEB - i; ++j) {
+      const uint32_t hi = max(head[j], head[j + 1]);
+      head[j + 1] = min(head[j], head[j + 1]);
+      head[j] = hi;
+    }
+  uint32_t own = 0;   // lane i: the i-th choice's key; lane k: the first that is left out
+  for (int i = 0; i <= a.k; ++i) {
+    const uint32_t best = max16(head[0]);
+    own = m == i ? best : own;
+    const bool taken = head[0] == best;   // (none is left: zeros move up)
+#pragma unroll
+    for (int j = 0; j + 1 < NEB; ++j) head[j] = taken ? head[j + 1] : head[j];
+    head[NEB - 1] = taken ? 0u : head[NEB - 1];
+  }
+  const uint32_t next = dpp<0x101>(own);   // row_shl: lane i + 1's
+  bad |= m < a.k && next && uncertain(key_value(own, 63u), key_value(next, 63u), 0x1p-17f, dc) ? 1u : 0u;
+  marked = max16(bad);   // (a group's bit is in every lane)
+  expert = 63 - static_cast<int>(own & 63u);
+  // gates, from the chosen experts' logits
+  float lx = 0.f;
+#pragma unroll
+  for (int j = 0; j < NEB; ++j) {
+    const float v = __shfl(l[j], row | (expert & 15), 64);
+    if ((expert >> 4) == j) lx = v;
+  }
+  if (a.renormalise) {
+    const bool mine = m < a.k;
+    const float most = key_value(max16(mine ? order_key(lx) : 0u));
+    const float p = !mine ? 0.f
+                          : sig ? sigmoid_shifted(lx, fminf(most, 0.f)) : __builtin_amdgcn_exp2f((lx - most) * kLog2e);
+    gate = a.scale * (p * __builtin_amdgcn_rcpf(sum16(p)));
+  } else {
+    gate = a.scale * (sig ? sigmoid(lx) : __builtin_amdgcn_exp2f((lx - top) * kLog2e) * inv_z);
   }
 }
 
@@ -523,38 +519,90 @@ __device__ __forceinline__ double wave_max64(double v) {
   return v;
 }
 
+// Sums over the wave, and the largest (NaN counts as -infinity), in every lane.
+__device__ __forceinline__ float wave_sum(float v) {
+  v = sum16(v);
+  v += __uint_as_float(static_cast<uint32_t>(
+      __builtin_amdgcn_update_dpp(0, static_cast<int>(__float_as_uint(v)), 0x142, 0xA, 0xF, false)));   // row_bcast:15
+  v += __uint_as_float(static_cast<uint32_t>(
+      __builtin_amdgcn_update_dpp(0, static_cast<int>(__float_as_uint(v)), 0x143, 0xC, 0xF, false)));   // row_bcast:31
+  return __uint_as_float(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(__float_as_uint(v)), 63)));
+}
+__device__ __forceinline__ float wave_max(float v) {
+  uint32_t u = max16(order_key(v));
+  u = max(u, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(u), 0x142, 0xA, 0xF, false)));
+  u = max(u, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(u), 0x143, 0xC, 0xF, false)));
+  return key_value(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(u), 63)));
+}
+__device__ __forceinline__ double lane_value(double v, int from) {   // from: the same in every lane
+  const uint64_t u = __double_as_longlong(v);
+  const uint32_t lo = __builtin_amdgcn_readlane(static_cast<uint32_t>(u), from);
+  const uint32_t hi = __builtin_amdgcn_readlane(static_cast<uint32_t>(u >> 32), from);
+  return __longlong_as_double(static_cast<long long>((static_cast<uint64_t>(hi) << 32) | lo));
+}
+
+// A lane's share of the float64 products of the row at `row` with the experts ec, over
+// columns c_lo .. c_hi - 1.
+template <class Elem>
+__device__ __forceinline__ void products64(const void* __restrict__ xv, const void* __restrict__ wv, size_t row, int d,
+                                           const int (&ec)[kAgainExperts], int c_lo, int c_hi,
+                                           double (&s)[kAgainExperts]) {
+  constexpr int VL = 16 / sizeof(Elem), NE = kAgainExperts;
+  const Elem* x = static_cast<const Elem*>(xv) + row;
+#pragma unroll
+  for (int j = 0; j < NE; ++j) s[j] = 0.0;
+  for (int c = c_lo + (threadIdx.x & 63) * VL; c < c_hi; c += 64 * VL) {
+    Pack16 xa, wa[NE];
+    xa.u4 = *reinterpret_cast<const uint4*>(x + c);
+#pragma unroll
+    for (int j = 0; j < NE; ++j)
+      wa[j].u4 = *reinterpret_cast<const uint4*>(static_cast<const Elem*>(wv) + static_cast<size_t>(ec[j]) * d + c);
+    auto value = [](const Pack16& p, int u) {
+      if constexpr (VL == 8) return static_cast<double>(bf16_to_f32(p.h[u]));
+      else return static_cast<double>(p.f[u]);
+    };
+#pragma unroll
+    for (int u = 0; u < VL; ++u) {
+      const double xd = value(xa, u);
+#pragma unroll
+      for (int j = 0; j < NE; ++j) s[j] = fma(xd, value(wa[j], u), s[j]);
+    }
+  }
+}
+
 // kChooseTok tokens a block: choices by the 16 lanes of a row, four tokens a wave at
 // a time; then those whose float32 logits do not tell are decided in float64, and
 // waves rank the slots of a choice each.
 //   Of an undecided token the logits that another one (or, in a group, another
 // group's value) is too close to are taken again from exact products, usually two;
-// the others are far enough from every other as they are.  Under a softmax with a
-// bias every score moves with the sum of all, and where float32 sums left their range
-// no logit tells anything: then all are.  The waves share these products.
+// the others are far enough from every other as they are.  All are where float32 sums
+// left their range, and in a second pass where other groups are kept than at first and
+// their experts are close too, or where under a softmax with a bias the other logits'
+// part in the sum still could turn a choice.  The waves share these products.
 //   T <= kChooseTok: the one block has every slot, and lays out the buckets as well.
-template <bool BF16, int NEB>
+template <int NEB, bool SIG, bool GROUPED>
 __global__ __launch_bounds__(kChooseWaves * 64) void scored_choose_kernel(
-    const void* __restrict__ xv, const void* __restrict__ wv, int T, int d, ScoreArgs a, int C,
+    const void* __restrict__ xv, const void* __restrict__ wv, bool bf16, int T, int d, ScoreArgs a, int C,
     int32_t* __restrict__ topk_idx, float* __restrict__ topk_gate, float* __restrict__ logits,
     int32_t* __restrict__ slot_pos, int32_t* __restrict__ hist, int* __restrict__ scan_done,
     int32_t* __restrict__ perm_token, int32_t* __restrict__ offsets) {
-  using Elem = std::conditional_t<BF16, uint16_t, float>;
-  constexpr int VL = 16 / sizeof(Elem), NE = kAgainExperts, ITEMS = 16, ROWS = kChooseTok / 4 / kChooseWaves;
+  constexpr int NE = kAgainExperts, ITEMS = 16, ROWS = kChooseTok / 4 / kChooseWaves;
   __shared__ int choice[kMaxChoices][kChooseTok];
   __shared__ int cnt[kMaxChoices][kMaxExperts];
   __shared__ float bounds[kChooseTok];
-  __shared__ bool marks[kChooseTok];
+  __shared__ uint32_t marks[kChooseTok];
+  __shared__ uint64_t kepts[kChooseTok];          // experts of a marked token's kept groups
   __shared__ int first[kMaxExperts];              // (one chunk) an expert's first position
   __shared__ uint64_t agains[kChooseTok];         // of the n-th marked token: the logits to take again
-  __shared__ double lg[kChooseTok][kMaxExperts];  // its logits
+  __shared__ double lg[kChooseTok][kMaxExperts];  // a marked token's logits
   __shared__ double vals[kChooseWaves][kMaxExperts], gvals[kChooseWaves][kMaxGroups];
   __shared__ double sums[kChooseWaves][ITEMS][NE];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, m = lane & 15, q = lane >> 4;
   const int ch = blockIdx.x, t0 = ch * kChooseTok, E = a.E, k = a.k, nch = gridDim.x;
-  const bool sig = a.score == LUFFY_SCORE_SIGMOID, grouped = a.top_groups < a.groups;
+  constexpr bool sig = SIG, grouped = GROUPED;
   if (ch == 0 && threadIdx.x == 0) *scan_done = 0;   // armed for slot_scan
   {
-    float bal[NEB], l[1][NEB], dl[1], ahead[NEB], dl_ahead;
+    float bal[NEB], l[NEB], dl, ahead[NEB], dl_ahead;
     int grp[NEB];
 #pragma unroll
     for (int j = 0; j < NEB; ++j) {
@@ -574,28 +622,38 @@ __global__ __launch_bounds__(kChooseWaves * 64) void scored_choose_kernel(
     for (int i = 0; i < ROWS; ++i) {
       const int tl = 4 * (w + kChooseWaves * i) + q, t = t0 + tl;
 #pragma unroll
-      for (int j = 0; j < NEB; ++j) l[0][j] = ahead[j];
-      dl[0] = dl_ahead;
+      for (int j = 0; j < NEB; ++j) l[j] = ahead[j];
+      dl = dl_ahead;
       if (i + 1 < ROWS) load(i + 1);
-      int expert[1];
-      float gate[1];
-      bool marked[1];
-      choose16(l, bal, grp, a, dl, expert, gate, marked);
+      int expert;
+      float gate;
+      uint32_t key[NEB], marked;
+      choose16<NEB, SIG, GROUPED>(l, bal, grp, a, dl, expert, gate, key, marked);
+      if (t >= T) marked = 0;
       if (m < k) {
-        choice[m][tl] = expert[0];
-        if (t < T && !marked[0]) {
-          topk_idx[static_cast<size_t>(t) * k + m] = expert[0];
-          topk_gate[static_cast<size_t>(t) * k + m] = gate[0];
+        choice[m][tl] = expert;
+        if (t < T && !marked) {
+          topk_idx[static_cast<size_t>(t) * k + m] = expert;
+          topk_gate[static_cast<size_t>(t) * k + m] = gate;
         }
       }
       if (m == 0) {
-        marks[tl] = marked[0] && t < T;
-        bounds[tl] = dl[0];
+        marks[tl] = marked;
+        bounds[tl] = dl;
+      }
+      if (__any(marked)) {
+        uint64_t kept = 0;
+#pragma unroll
+        for (int j = 0; j < NEB; ++j) {
+          kept |= ((__ballot(key[j] != 0) >> (lane & 48)) & 0xFFFFull) << (16 * j);
+          lg[tl][16 * j + m] = 16 * j + m < E ? l[j] : -INFINITY;
+        }
+        if (m == 0) kepts[tl] = kept;
       }
     }
   }
   __syncthreads();
-  const uint64_t open = __ballot(lane < kChooseTok && marks[lane % kChooseTok]);   // the same in every wave
+  const uint64_t open = __ballot(lane < kChooseTok && marks[lane % kChooseTok] != 0);   // the same in every wave
   const int marked = __popcll(open);
   if (marked) {
     auto nth = [&](int n) {   // the n-th marked token
@@ -629,27 +687,23 @@ __global__ __launch_bounds__(kChooseWaves * 64) void scored_choose_kernel(
     // which logits to take again
     for (int n = w; n < marked; n += kChooseWaves) {
       const int tl = nth(n);
-      const float lf = in ? logits[static_cast<size_t>(t0 + tl) * E + lane] : -INFINITY, dl = bounds[tl];
+      const float lf = in ? static_cast<float>(lg[tl][lane % (16 * NEB)]) : -INFINITY, dl = bounds[tl];
       uint64_t again = full;
       if (dl < 0x1p-6f && !__any(in && !(fabsf(lf) < INFINITY))) {
-        float top = 0.f, z = 1.f;
-        if (!sig) {
-          top = lf;
-#pragma unroll
-          for (int o = 32; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-          z = in ? expf(lf - top) : 0.f;
-#pragma unroll
-          for (int o = 32; o >= 1; o >>= 1) z += __shfl_xor(z, o, 64);
+        float top = 0.f, z = 1.f, s = 0.f, ds = 0.f;
+        if constexpr (!sig) {
+          top = wave_max(lf);
+          z = wave_sum(in ? __builtin_amdgcn_exp2f((lf - top) * kLog2e) : 0.f);
+          s = __builtin_amdgcn_exp2f((lf - top) * kLog2e) / z;
+          ds = fmaf(2.0f / z, dl, 0x1p-20f);
+        } else {
+          s = sigmoid(lf);
+          ds = fmaf(0.25f, dl, 0x1p-20f);
         }
-        const float s = sig ? sigmoid_shifted(lf, 0.f) : expf(lf - top) / z;
-        const float ds = sig ? 0.25f * dl + 0x1p-20f : fmaf(2.0f / z, dl, 0x1p-20f);
         const float c = a.balance ? s + bal : lf, dc = a.balance ? ds : dl;
         // experts too close to one of the first choice's (an expert that is close to
         // none of those is not among the k best, or surely so and in its place)
-        float size = in && c > -INFINITY ? fabsf(c) : 0.f;
-#pragma unroll
-        for (int o = 32; o >= 1; o >>= 1) size = fmaxf(size, __shfl_xor(size, o, 64));
-        const float close = fmaf(0x1p-15f, size, 2.0f * dc);
+        const float close = fmaf(0x1p-15f, wave_max(in && c > -INFINITY ? fabsf(c) : 0.f), 2.0f * dc);
         again = 0;
         for (int j = 0; j < k; ++j) {
           const int e = __builtin_amdgcn_readfirstlane(choice[j][tl]);
@@ -657,19 +711,18 @@ __global__ __launch_bounds__(kChooseWaves * 64) void scored_choose_kernel(
           const uint64_t near = __ballot(in && lane != e && fabsf(c - v) <= close);
           if (near) again |= near | (1ull << e);
         }
-        if (grouped) {
+        if (grouped && (marks[tl] & 2u)) {
           const double g = group_values(by_score ? s : c);
           const double dg = 2.0 * (a.best == 2 ? 2.0 : 1.0) * (by_score ? ds : dc);
           bool hard = false;
           for (int h = 0; h < a.groups; ++h)
             hard = hard || (lane < a.groups && h != lane &&
-                            !(fabs(g - gval[h]) > dg + 0x1p-20 * (fabs(g) + fabs(gval[h]))) &&
+                            !(fabs(g - gval[h]) > dg + 0x1p-17 * (fabs(g) + fabs(gval[h]))) &&
                             !(g == -INFINITY && gval[h] == -INFINITY));
           const uint64_t groups = __ballot(hard);
           again |= __ballot(in && ((groups >> (in ? lane / a.group_size : 0)) & 1ull));
         }
       }
-      lg[n][lane] = lf;
       if (lane == 0) agains[n] = again;
     }
     __syncthreads();
@@ -680,7 +733,7 @@ __global__ __launch_bounds__(kChooseWaves * 64) void scored_choose_kernel(
       for (int n = 0; n < marked; ++n) items += (__popcll(agains[n]) + NE - 1) / NE;
       if (!items) break;   // (the second pass: none was left)
       const bool split = items < 2 * kChooseWaves;
-      const int quarter = ((d / VL + kChooseWaves - 1) / kChooseWaves) * VL;
+      const int quarter = (d / 8 + kChooseWaves - 1) / kChooseWaves * 8;
       const int c_lo = split ? w * quarter : 0, c_hi = split ? min(d, c_lo + quarter) : d;
       for (int base = 0; base < items; base += ITEMS) {
         int item = 0;
@@ -693,29 +746,10 @@ __global__ __launch_bounds__(kChooseWaves * 64) void scored_choose_kernel(
               todo &= todo - 1;
             }
             if (item < base || item >= base + ITEMS || (!split && item % kChooseWaves != w)) continue;
-            const Elem* x = static_cast<const Elem*>(xv) + static_cast<size_t>(t0 + nth(n)) * d;
             double s[NE];
-#pragma unroll
-            for (int j = 0; j < NE; ++j) s[j] = 0.0;
-            for (int c = c_lo + lane * VL; c < c_hi; c += 64 * VL) {
-              Pack16 xa, wa[NE];
-              xa.u4 = *reinterpret_cast<const uint4*>(x + c);
-#pragma unroll
-              for (int j = 0; j < NE; ++j)
-                wa[j].u4 =
-                    *reinterpret_cast<const uint4*>(static_cast<const Elem*>(wv) + static_cast<size_t>(ec[j]) * d + c);
-#pragma unroll
-              for (int u = 0; u < VL; ++u) {
-                double xd;
-                if constexpr (BF16) xd = static_cast<double>(bf16_to_f32(xa.h[u]));
-                else xd = static_cast<double>(xa.f[u]);
-#pragma unroll
-                for (int j = 0; j < NE; ++j) {
-                  if constexpr (BF16) s[j] = fma(xd, static_cast<double>(bf16_to_f32(wa[j].h[u])), s[j]);
-                  else s[j] = fma(xd, static_cast<double>(wa[j].f[u]), s[j]);
-                }
-              }
-            }
+            const size_t row = static_cast<size_t>(t0 + nth(n)) * d;
+            if (bf16) products64<uint16_t>(xv, wv, row, d, ec, c_lo, c_hi, s);
+            else products64<float>(xv, wv, row, d, ec, c_lo, c_hi, s);
             // four sums over the wave: halves keep two each, quarters one
             static_assert(NE == 4, "four sums a wave");
             const bool h5 = lane & 32, h4 = lane & 16;
@@ -738,7 +772,7 @@ __global__ __launch_bounds__(kChooseWaves * 64) void scored_choose_kernel(
           if (w == 0 && ((mask >> lane) & 1ull) && mine >= base && mine < base + ITEMS) {
             double s = sums[0][mine - base][below % NE];
             for (int v = 1; split && v < kChooseWaves; ++v) s += sums[v][mine - base][below % NE];
-            lg[n][lane] = s + (a.bias ? static_cast<double>(a.bias[lane]) : 0.0);
+            lg[nth(n)][lane] = s + (a.bias ? static_cast<double>(a.bias[lane]) : 0.0);
           }
           at += (__popcll(mask) + NE - 1) / NE;
         }
@@ -749,7 +783,7 @@ __global__ __launch_bounds__(kChooseWaves * 64) void scored_choose_kernel(
         if (pass == 1 && !agains[n]) continue;
         const int tl = nth(n);
         const size_t t = t0 + tl;
-        const double l = lg[n][lane];   // (-infinity past E)
+        const double l = in ? lg[tl][lane] : -INFINITY;
         double s = 0.0;
         if (a.balance || (grouped && by_score)) {
           if (sig) {
@@ -766,8 +800,8 @@ __global__ __launch_bounds__(kChooseWaves * 64) void scored_choose_kernel(
         const bool moves = pass == 0 && !sig && a.balance && agains[n] != full;
         const double part = moves ? 1.01 * bounds[tl] + 1e-12 : 0.0, s_most = moves ? wave_max64(s) : 0.0;
         bool loose = false;
-        bool allowed = in;
-        if (grouped) {
+        uint64_t allowed = kepts[tl];
+        if (grouped && ((marks[tl] & 2u) || agains[n] == full)) {
           const double g = group_values(by_score ? s : c);
           int rank = kMaxGroups;
           if (lane < a.groups) {
@@ -778,39 +812,51 @@ __global__ __launch_bounds__(kChooseWaves * 64) void scored_choose_kernel(
             }
           }
           const uint64_t kept = __ballot(rank < a.top_groups);
-          allowed = in && ((kept >> (in ? lane / a.group_size : 0)) & 1ull);
+          allowed = __ballot(in && ((kept >> (in ? lane / a.group_size : 0)) & 1ull));
         }
-        // the k best are among the first choice and what was taken again
-        uint64_t first_choice = 0;
-        for (int j = 0; j < k; ++j) first_choice |= 1ull << __builtin_amdgcn_readfirstlane(choice[j][tl]);
-        const uint64_t may = __ballot(allowed) & (first_choice | agains[n]);
-        __builtin_amdgcn_wave_barrier();
-        val[lane] = c;
-        __builtin_amdgcn_wave_barrier();
+        // the k best are among the first choice and what was taken again; where other
+        // groups are kept than at first, anywhere in them
+        const bool turned = allowed != kepts[tl] && agains[n] != full;
+        uint64_t may = allowed;
+        if (!turned) {
+          uint64_t first_choice = 0;
+          for (int j = 0; j < k; ++j) first_choice |= 1ull << __builtin_amdgcn_readfirstlane(choice[j][tl]);
+          may &= first_choice | agains[n];
+        }
         int rank = 0;
         for (uint64_t left = may; left; left &= left - 1) {
-          const int e = __ffsll(static_cast<long long>(left)) - 1;
-          const double v = val[e];
+          const int e = __builtin_amdgcn_readfirstlane(__ffsll(static_cast<long long>(left)) - 1);
+          const double v = lane_value(c, e);
           rank += v > c || (v == c && e < lane);
-          if (moves) {
-            const double se = __shfl(s, e, 64);
-            loose = loose || (((may >> lane) & 1ull) && e != lane && fabs(v - c) <= fabs(se - s) * part + 1e-14);
-          }
+          if (moves)
+            loose = loose || (((may >> lane) & 1ull) && e != lane &&
+                              fabs(v - c) <= fabs(lane_value(s, e) - s) * part + 1e-14);
         }
         const bool chosen = ((may >> lane) & 1ull) && rank < k;
+        if (turned) {   // gaps to float32 logits: are they wide enough?
+          const double dl = bounds[tl], gap = 2.0 * (!a.balance ? dl : sig ? 0.25 * dl : 2.0 * dl) + 1e-12;
+          for (uint64_t left = may; left; left &= left - 1) {
+            const int e = __builtin_amdgcn_readfirstlane(__ffsll(static_cast<long long>(left)) - 1);
+            const bool exact = (agains[n] >> e) & (agains[n] >> lane) & 1ull;
+            loose = loose || (chosen && e != lane && !exact && fabs(lane_value(c, e) - c) <= gap);
+          }
+        }
         const bool all = __any(loose);
         if (lane == 0) agains[n] = all ? full : 0ull;   // none: done
         if (all) continue;
         // gates by choose16's formulas, in float32
         const float lx = static_cast<float>(l);
-        float top = (a.renormalise ? chosen : in) ? lx : -INFINITY;
-#pragma unroll
-        for (int o = 32; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-        float p = !in ? 0.f : sig ? sigmoid_shifted(lx, a.renormalise ? fminf(top, 0.f) : 0.f) : expf(lx - top);
-        float sum = a.renormalise && !chosen ? 0.f : p;
-#pragma unroll
-        for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o, 64);
-        if (a.renormalise || !sig) p /= sum;
+        const bool of = a.renormalise ? chosen : in;   // what the sum goes over
+        float p = 0.f;
+        if constexpr (sig) {
+          const float shift = a.renormalise ? fminf(wave_max(of ? lx : -INFINITY), 0.f) : 0.f;
+          p = in ? sigmoid_shifted(lx, shift) : 0.f;
+          if (a.renormalise) p /= wave_sum(of ? p : 0.f);
+        } else {
+          const float top = wave_max(of ? lx : -INFINITY);
+          p = of ? __builtin_amdgcn_exp2f((lx - top) * kLog2e) : 0.f;
+          p /= wave_sum(p);
+        }
         if (chosen) {
           choice[rank][tl] = lane;
           topk_idx[t * k + rank] = lane;
@@ -1303,9 +1349,12 @@ extern "C" int luffy_route_scored(const void* x, int T, int d, int dtype, const 
 #undef LUFFY_SCORED
   const int blocks = (T + kChooseTok - 1) / kChooseTok, C = capacity_slots(T, k, E, capacity_factor);
 #define LUFFY_CHOOSE(NEB)                                                                                           \
-  launch("scored_choose", bf16 ? scored_choose_kernel<true, NEB> : scored_choose_kernel<false, NEB>, blocks,        \
-         kChooseWaves * 64, 0, s, x, w_gate, T, d, a, C, topk_idx, topk_gate, logits, slot_pos, ws.hist, ws.done,   \
-         perm_token, offsets)
+  launch("scored_choose",                                                                                           \
+         sig ? (grouped ? scored_choose_kernel<NEB, true, true> : scored_choose_kernel<NEB, true, false>)           \
+             : (grouped ? scored_choose_kernel<NEB, false, true> : scored_choose_kernel<NEB, false, false>),        \
+         blocks, kChooseWaves * 64, 0, s, x, w_gate, bf16, T, d, a, C, topk_idx, topk_gate, logits, slot_pos,       \
+         ws.hist, ws.done, perm_token, offsets)
+  const bool sig = score == LUFFY_SCORE_SIGMOID, grouped = top_groups < groups;
   if (E <= 16) LUFFY_CHOOSE(1);
   else if (E <= 32) LUFFY_CHOOSE(2);
   else if (E <= 48) LUFFY_CHOOSE(3);

@@ -136,6 +136,33 @@ def test_close_calls(dtype, score, bal, groups):
     r.check(r.run())
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [5, 300])
+def test_groups_that_turn(dtype, T):
+    """Float32 sums tie two groups, the exact ones keep the other: it has fewer good
+    experts, and those that take their places are near to none of the first choice."""
+    r = Router(31, dtype, T, 2048, 16, 4, "softmax", False, 4, 2, 1)
+    x, w = np.zeros((T, 2048)), np.zeros((16, 2048))
+    x[:, 0], x[:, 128], x[:, 256], x[:, 300] = 64, 1, 64, 1
+    w[:, 0], w[:, 256] = 16, -16                          # 1024 - 1024
+    w[4:8, 128] = 2.0 ** -15                              # lost beside 1024 in float32
+    w[:, 300] = [5, 4, 3, 2, 5, -1, -2, -3, 6, 1.5, 0.5, 0.25, -5, -6, -7, -8]
+    x[::3, 300] = 0.5                                     # the same at another scale
+    r.x, r.w, r.b = tensor(x, dtype), tensor(w, dtype), tensor(np.zeros(16))
+    idx = r.check(r.run())
+    assert (idx == [8, 4, 9, 10]).all()
+    w[10], w[9] = w[9], 0                                 # now 8's group has a tie as well: 9 and 10
+    w[9, 300], w[9, 128] = 1.5, 2.0 ** -15
+    w[10, 0], w[10, 256], w[9, 0], w[9, 256] = 16, -16, 16, -16
+    r.w = tensor(w, dtype)
+    idx = r.check(r.run())
+    assert (idx[1::3] == [8, 4, 9, 10]).all()
+    w[[9, 10]] = w[[10, 9]]
+    r.w = tensor(w, dtype)
+    idx = r.check(r.run())
+    assert (idx[1::3] == [8, 4, 10, 9]).all()
+
+
 def test_cancelling_rows():
     """Sums of large products that cancel: the logits are small beside |x| |w|."""
     r = Router(8, "bf16", 192, 1024, 16, 4, "sigmoid", True)
@@ -200,7 +227,8 @@ def test_huge_values():
 
 @pytest.mark.parametrize("dtype,T,d,E,k", [("bf16", 20011, 256, 16, 4), ("bf16", 33000, 128, 64, 8),
                                             ("f32", 9001, 64, 24, 3), ("bf16", 16400, 1088, 60, 2),
-                                            ("bf16", 40003, 2048, 32, 4)])
+                                            ("bf16", 40003, 2048, 32, 4), ("bf16", 17003, 64, 40, 5),
+                                            ("bf16", 66000, 320, 45, 8)])
 def test_many_tokens(dtype, T, d, E, k):
     """Every kernel size; the choices against a stable sort of 64-bit scores."""
     import torch
