@@ -173,6 +173,8 @@ int luffy_route_noalloc(const void* x, int T, int d, int dtype,
  *      layer's input.  dx_rep NULL: the router's share alone
  * Sums are float32, dx is rounded once.  An index in topk_idx outside 0..E-1 is
  * ignored.  x, w_gate, dx_rep, dx and dw_gate 16-byte aligned.
+ * Both: d a multiple of 64, at most 32768; T at most 2^28, T * k below 2^31; the
+ * backward's bf16 x at most 64 times 4 GiB.
  * ---------------------------------------------------------------------- */
 int luffy_route_scored(const void* x, int T, int d, int dtype, const void* w_gate, const float* b_gate, int E, int k,
                        int score, const float* balance, int groups, int top_groups, int group_best, int renormalise,
@@ -433,7 +435,8 @@ int luffy_expert_ffn_backward(const void* x, const int32_t* row_index, const int
  *   values  q [rows, cols] int8; scales s [ceil(cols/256), rows, 8] uint8: those of
  *           256 consecutive columns of a row side by side, 0 past the last column
  *           (luffy_mx4_scale_bytes(1, rows, cols) bytes)
- * cols is a multiple of 32, at most 32768; x and q 16-byte, s 8-byte aligned.
+ * cols is a multiple of 32, at most 32768, rows * cols at most 2^36; x and q
+ * 16-byte, s 8-byte aligned.
  *
  * luffy_mx8_quantize - rounds x [rows, cols] (float32 or bf16).  With m the largest
  * |value| of a block its scale is 2^(floor(log2 m) - 6) (at least 2^-127), so that
@@ -483,8 +486,8 @@ int luffy_expert_ffn_backward_kept(const void* x, const void* x_scale, int x_row
  *   w_post NULL: y_t itself in N's place; b_post, b_pre NULL: zeros
  *   gate   by gate_kind: none (NULL), float32 [d], or [T, d] dtype
  *   w_pre, u  both NULL: o alone (behind a last layer)
- * d a multiple of 64, at most 32768; every pointer 16-byte aligned.  Sums are
- * float32.  With eps = 0 a row without variance gives NaN.
+ * d a multiple of 64, at most 32768, T at most 2^30; every pointer 16-byte
+ * aligned.  Sums are float32.  With eps = 0 a row without variance gives NaN.
  *
  * luffy_block_norm_backward - its gradients, for dout = dL/do (from the rest of
  * the stream; NULL: zeros) and du = dL/du (NULL: zeros; one of the two is

@@ -465,14 +465,17 @@ def _fits(what, name, t, shape, dtype):
 def _device_ptrs(what, *tensors):
     """Pointers of contiguous tensors on the current device (None stays None):
     the launch goes to the current device's stream."""
-    device = torch.cuda.current_device() if any(t is not None and t.is_cuda for t in tensors) else -1
-    out = []
+    device, out = None, []
     for t in tensors:
         if t is not None:
-            if not t.is_cuda:
-                raise LuffyError(f"{what}: tensor must be on the GPU")
-            if t.get_device() != device:
-                raise LuffyError(f"{what}: tensor on device {t.get_device()}, the current one is {device}")
+            at = t.get_device()   # -1: not on a GPU
+            if at != device:
+                if at < 0:
+                    raise LuffyError(f"{what}: tensor must be on the GPU")
+                if device is None:
+                    device = torch.cuda.current_device()
+                if at != device:
+                    raise LuffyError(f"{what}: tensor on device {at}, the current one is {device}")
             if not t.is_contiguous():
                 raise LuffyError(f"{what}: tensor must be contiguous")
             t = t.data_ptr()
@@ -501,12 +504,15 @@ def luffy_block_norm(x, y, o, u, *, norm="rms", eps=1e-6, res_scale=1.0, w_post=
     what = "luffy_block_norm"
     if x.dim() != 2:
         raise LuffyError(f"{what}: x must be [T, d], got {list(x.shape)}")
-    T, d = x.shape
+    shape, dtype, f32 = x.shape, x.dtype, torch.float32
+    T, d = shape
     for name, t in (("y", y), ("o", o), ("u", u)):
-        _fits(what, name, t, x.shape, x.dtype)
+        if t is not None:
+            _fits(what, name, t, shape, dtype)
     for name, t in (("w_post", w_post), ("b_post", b_post), ("w_pre", w_pre), ("b_pre", b_pre)):
-        _fits(what, name, t, (d,), torch.float32)
-    kind = _block_gate(what, gate, T, d, x.dtype)
+        if t is not None:
+            _fits(what, name, t, (d,), f32)
+    kind = _block_gate(what, gate, T, d, dtype)
     dt = _dtype_code(x)
     x, y, w_post, b_post, gate, w_pre, b_pre, o, u = _device_ptrs(what, x, y, w_post, b_post, gate, w_pre, b_pre, o, u)
     _check(load_library().luffy_block_norm(x, y, T, d, dt, _named(_NORMS, norm, what, "norm"), eps, w_post, b_post, gate,

@@ -649,6 +649,7 @@ int norm_check(const char* fn, int T, int d, int dtype, int norm, float eps, flo
   if (b_post && !w_post) return fail(LUFFY_E_INVALID, "%s: b_post without w_post", fn);
   if (d % 64 != 0) return fail(LUFFY_E_UNSUPPORTED, "%s: d=%d not a multiple of 64", fn, d);
   if (d > kNormMaxD) return fail(LUFFY_E_UNSUPPORTED, "%s: d=%d > %d", fn, d, kNormMaxD);
+  if (T > (1 << 30)) return fail(LUFFY_E_UNSUPPORTED, "%s: T=%d > 2^30", fn, T);
   return LUFFY_OK;
 }
 

@@ -97,20 +97,23 @@ __global__ __launch_bounds__(kThreads) void mx8_dequantize_kernel(const uint8_t*
   }
 }
 
+long long mx8_blocks(int rows, int cols) {
+  const long long per = kThreads * kUnroll;
+  return (static_cast<long long>(rows) * (cols / 8) + per - 1) / per;
+}
+constexpr long long kMaxBlocks = (1ll << 36) / 8 / (kThreads * kUnroll);   // (a grid has fewer than 2^32 threads)
+
 int mx8_check(const char* fn, const void* x, const void* q, const void* s, int rows, int cols, int dtype) {
   if (!x || !q || !s) return fail(LUFFY_E_INVALID, "%s: null pointer argument", fn);
   if (rows <= 0 || cols <= 0) return fail(LUFFY_E_INVALID, "%s: rows=%d cols=%d must be positive", fn, rows, cols);
   if (dtype != LUFFY_F32 && dtype != LUFFY_BF16) return fail(LUFFY_E_INVALID, "%s: unknown dtype %d", fn, dtype);
   if (cols % 32 != 0) return fail(LUFFY_E_UNSUPPORTED, "%s: cols=%d not a multiple of 32", fn, cols);
   if (cols > 32768) return fail(LUFFY_E_UNSUPPORTED, "%s: cols=%d > 32768", fn, cols);
+  if (mx8_blocks(rows, cols) > kMaxBlocks)
+    return fail(LUFFY_E_UNSUPPORTED, "%s: %d x %d is more than 2^36 values", fn, rows, cols);
   if (((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(q)) & 15u) || (reinterpret_cast<uintptr_t>(s) & 7u))
     return fail(LUFFY_E_INVALID, "%s: x and q must be 16-byte, s 8-byte aligned", fn);
   return LUFFY_OK;
-}
-
-int mx8_blocks(int rows, int cols) {
-  const long long per = kThreads * kUnroll;
-  return static_cast<int>((static_cast<long long>(rows) * (cols / 8) + per - 1) / per);
 }
 
 }  // namespace
@@ -122,7 +125,7 @@ extern "C" int luffy_mx8_quantize(const void* x, int rows, int cols, int dtype, 
   const int st = mx8_check("luffy_mx8_quantize", x, q, s, rows, cols, dtype);
   if (st != LUFFY_OK) return st;
   launch("mx8_quantize", dtype == LUFFY_F32 ? mx8_quantize_kernel<true> : mx8_quantize_kernel<false>,
-         mx8_blocks(rows, cols), kThreads, 0, static_cast<hipStream_t>(stream), x, rows, cols, static_cast<uint8_t*>(q),
+         static_cast<int>(mx8_blocks(rows, cols)), kThreads, 0, static_cast<hipStream_t>(stream), x, rows, cols, static_cast<uint8_t*>(q),
          static_cast<uint8_t*>(s));
   return check_launch("luffy_mx8_quantize");
 }
@@ -131,7 +134,7 @@ extern "C" int luffy_mx8_dequantize(const void* q, const void* s, int rows, int 
   const int st = mx8_check("luffy_mx8_dequantize", x, q, s, rows, cols, dtype);
   if (st != LUFFY_OK) return st;
   launch("mx8_dequantize", dtype == LUFFY_F32 ? mx8_dequantize_kernel<true> : mx8_dequantize_kernel<false>,
-         mx8_blocks(rows, cols), kThreads, 0, static_cast<hipStream_t>(stream), static_cast<const uint8_t*>(q),
+         static_cast<int>(mx8_blocks(rows, cols)), kThreads, 0, static_cast<hipStream_t>(stream), static_cast<const uint8_t*>(q),
          static_cast<const uint8_t*>(s), rows, cols, x);
   return check_launch("luffy_mx8_dequantize");
 }

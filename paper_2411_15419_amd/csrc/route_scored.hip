@@ -1140,6 +1140,7 @@ __global__ __launch_bounds__(256) void scored_dx_kernel(const void* __restrict__
 }
 
 constexpr int kDwTok = 64, kDwCols = 64;
+constexpr int kMaxDwParts = 64;   // (the product's groups)
 
 // float32 rows: part of dW = dl^T x, 64 columns by the tokens of part blockIdx.y,
 // every expert; 64 tokens at a time in LDS, 16 experts a wave, a column a lane.
@@ -1252,12 +1253,16 @@ struct ScoredBwdPlan {
 ScoredBwdPlan scored_bwd_plan(int T, int d, int E, bool bf16) {
   ScoredBwdPlan p;
   p.ld = (3 * E + 63) / 64 * 64;
-  // bf16: 256 x 256 tiles, about one a CU, of at least 256 tokens; float32: about a
-  // thousand blocks
+  // bf16: 256 x 256 tiles, about one a CU, of at least 256 tokens, and a part's rows
+  // within a buffer resource; float32: about a thousand blocks
   const int tiles = (d + 255) / 256;
-  const int most = bf16 ? std::min(64, std::max(1, 256 / tiles)) : std::max(1, 1024 / std::max(1, d / kDwCols));
+  const int most = bf16 ? std::min(kMaxDwParts, std::max(1, 256 / tiles)) : std::max(1, 1024 / std::max(1, d / kDwCols));
   const int least = bf16 ? 256 : kDwTok;
   p.parts = std::max(1, std::min((T + least - 1) / least, most));
+  if (bf16) {
+    const long long fit = 0xFFFF0000ll / 2 / std::max(d, p.ld) - 2 * kDwTok;   // tokens
+    p.parts = std::max(p.parts, static_cast<int>(std::min<long long>((T + fit - 1) / fit, kMaxDwParts + 1)));
+  }
   p.per = ((T + p.parts - 1) / p.parts + kDwTok - 1) / kDwTok * kDwTok;
   p.rows = bf16 ? p.ld : E;
   p.b_parts = std::max(1, std::min((T + 15) / 16, 1024));
@@ -1286,7 +1291,8 @@ int scored_check(const char* fn, int T, int d, int dtype, int E, int k, int scor
   if (k > kMaxChoices) return fail(LUFFY_E_UNSUPPORTED, "%s: k=%d > %d", fn, k, kMaxChoices);
   if (d % 64 != 0) return fail(LUFFY_E_UNSUPPORTED, "%s: d=%d not a multiple of 64", fn, d);
   if (d > 32768) return fail(LUFFY_E_UNSUPPORTED, "%s: d=%d > 32768", fn, d);
-  if (static_cast<long long>(T) * k >= (1ll << 31)) return fail(LUFFY_E_UNSUPPORTED, "%s: T*k too large", fn);
+  if (T > (1 << 28) || static_cast<long long>(T) * k >= (1ll << 31))
+    return fail(LUFFY_E_UNSUPPORTED, "%s: T=%d k=%d: at most 2^28 tokens, and fewer than 2^31 slots", fn, T, k);
   return LUFFY_OK;
 }
 
@@ -1393,6 +1399,8 @@ extern "C" int luffy_route_scored_backward(const void* x, int T, int d, int dtyp
   for (const void* p : {x, w_gate, dx_rep, static_cast<const void*>(dx), static_cast<const void*>(dw_gate)})
     bits |= reinterpret_cast<uintptr_t>(p);
   if (bits & 15u) return fail(LUFFY_E_INVALID, "%s: x, w_gate, dx_rep, dx and dw_gate must be 16-byte aligned", fn);
+  if (dtype == LUFFY_BF16 && scored_bwd_plan(T, d, E, true).parts > kMaxDwParts)
+    return fail(LUFFY_E_UNSUPPORTED, "%s: %d rows of %d exceed 64 parts of 4 GiB", fn, T, d);
   const size_t need = luffy_route_scored_backward_workspace_size(T, d, E);
   if (workspace_bytes < need || !workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u))
     return fail(LUFFY_E_WORKSPACE, "%s: workspace needs %zu bytes, 256-aligned", fn, need);

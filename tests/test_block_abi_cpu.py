@@ -78,6 +78,7 @@ def test_block_norm_backward_refusals(lib):
               "dw_pre", "db_pre"):
         assert call(**{n: ODD}) == INVALID, n
     assert call(bytes=need - 1) == WORKSPACE and call(workspace=ODD) == WORKSPACE and call(workspace=None) == WORKSPACE
+    assert call(T=2 ** 30 + 1) == UNSUPPORTED and norm_call(lib)(T=2 ** 31 - 1) == UNSUPPORTED
 
 
 ROUTE = ("x T d dtype w_gate b_gate E k score balance groups top_groups group_best renormalise scale cf topk_idx "
@@ -101,6 +102,7 @@ def test_route_scored_refusals(lib):
     assert call(k=9, groups=1, top_groups=1) == UNSUPPORTED
     assert call(E=32, groups=32, top_groups=8) == UNSUPPORTED          # groups to choose from: 16 at most
     assert call(T=2 ** 30) == UNSUPPORTED and call(d=65536) == UNSUPPORTED
+    assert call(T=2 ** 28 + 1, k=1) == UNSUPPORTED                     # grids count threads in 32 bits
     assert call(x=ODD) == INVALID and call(w_gate=ODD) == INVALID
     need = lib.luffy_route_workspace_size(8, 16, 4)
     assert call(bytes=need - 1) == WORKSPACE and call(workspace=ODD) == WORKSPACE
@@ -114,6 +116,9 @@ def test_route_scored_backward_refusals(lib):
         assert call(**{n: None}) == INVALID, n
     assert call(T=-1) == INVALID and call(k=17) == INVALID and call(score=5) == INVALID and call(dtype=2) == INVALID
     assert call(E=128) == UNSUPPORTED and call(d=32) == UNSUPPORTED and call(k=9) == UNSUPPORTED
+    # 64 parts of T, each below 4 GiB
+    assert call(T=64 * 66000, d=32768) == UNSUPPORTED and call(T=64 * 65000, d=32768, bytes=16) == WORKSPACE
+    assert call(T=2 ** 28 + 1, k=1) == UNSUPPORTED
     for n in ("x", "w_gate", "dx_rep", "dx", "dw"):
         assert call(**{n: ODD}) == INVALID, n
     need = lib.luffy_route_scored_backward_workspace_size(8, 64, 16)
@@ -131,6 +136,7 @@ def test_mx8_refusals(lib, name):
     for n in ("rows", "cols"):
         assert call(**{n: 0}) == INVALID and call(**{n: -3}) == INVALID
     assert call(dtype=2) == INVALID and call(cols=48) == UNSUPPORTED and call(cols=32800) == UNSUPPORTED
+    assert call(rows=2 ** 21 + 1, cols=32768) == UNSUPPORTED and call(rows=2 ** 31 - 1, cols=64) == UNSUPPORTED
     assert call(x=ODD) == INVALID and call(q=ODD) == INVALID and call(s=BYTE) == INVALID
 
 

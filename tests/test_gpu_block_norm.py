@@ -239,3 +239,53 @@ def test_runs_repeat_bit_for_bit():
     c = Case(12, "bf16", 1500, 1024, "layer", True, "channel", True, True)
     a, b = c.backward(), c.backward()
     assert all(c.torch.equal(a[n], b[n]) for n in a)
+
+
+@pytest.mark.parametrize("T,d,norm,gate", [(8200, 2112, "layer", "channel"), (16401, 1088, "rms", "token"),
+                                           (32771, 576, "layer", "token"), (4099, 4096, "rms", "channel")])
+def test_backward_of_many_rows(T, d, norm, gate):
+    """bf16 rows in such numbers that the blocks hold two chunks a lane; against the
+    same formulas in float64 by autograd."""
+    import torch
+    import paper_2411_15419_amd as L
+    gen = torch.Generator(device="cuda").manual_seed(T)
+    rnd = lambda *s: torch.randn(*s, generator=gen, device="cuda")  # noqa: E731
+    y, x, dout, du = (rnd(T, d).bfloat16() for _ in range(4))
+    w = dict(w_post=1 + 0.1 * rnd(d), b_post=0.1 * rnd(d), w_pre=1 + 0.1 * rnd(d), b_pre=0.1 * rnd(d))
+    gate = 0.5 + 0.1 * rnd(d) if gate == "channel" else (0.5 + 0.1 * rnd(T, d)).bfloat16()
+    if norm == "rms":
+        w["b_post"] = w["b_pre"] = None
+    kw = dict(norm=norm, eps=1e-5, res_scale=0.7)
+    o, u = torch.empty_like(x), torch.empty_like(x)
+    L.luffy_block_norm(x, y, o, u, gate=gate, **w, **kw)
+
+    def N(a, wt, b):
+        c = a - a.mean(1, keepdim=True) if norm == "layer" else a
+        return c * torch.rsqrt((c * c).mean(1, keepdim=True) + 1e-5) * wt + (0.0 if b is None else b)
+
+    leaf = {n: t.double().requires_grad_() for n, t in dict(y=y, gate=gate, **w).items() if t is not None}
+    x64 = x.double().requires_grad_()
+    through = lambda n: leaf.get(n)  # noqa: E731
+    o64 = 0.7 * x64 + leaf["gate"] * N(leaf["y"], leaf["w_post"], through("b_post"))
+    stored = o64 + (o.double() - o64).detach()      # u is of o as it was stored
+    ((stored * dout.double()).sum() + (N(stored, leaf["w_pre"], through("b_pre")) * du.double()).sum()).backward()
+    got = dict(dx=torch.full_like(x, float("nan")), dy=torch.full_like(x, float("nan")),
+               dgate=torch.full_like(gate, float("nan")),
+               **{"d" + n: torch.full_like(t, float("nan")) for n, t in w.items() if t is not None})
+    ws = torch.empty(L.block_norm_backward_workspace_size(T, d), dtype=torch.uint8, device="cuda")
+    names = dict(w_post=w["w_post"], b_post=w["b_post"], gate=gate, w_pre=w["w_pre"])
+    L.luffy_block_norm_backward(y, o, dout, du, workspace=ws, **names, **kw, **got)
+    want = dict(dx=x64.grad, **{"d" + n: t.grad for n, t in leaf.items()})
+    for n, t in got.items():
+        # an entry is a sum of m terms, m the rows or one.  Over the entries, random as
+        # they are, its root mean square is sqrt(m) of a term's; a term, a product of two
+        # normal numbers, is below 32 of its own (5.6 sigma each), and m of them in
+        # absolute value below 32 sqrt(m) root mean squares of the entries.
+        m = T if t.dim() == 1 else 1
+        half = HALF["f32"] if t.dtype == torch.float32 else HALF["bf16"]
+        size = 32 * m ** 0.5 * want[n].square().mean().sqrt()
+        bound = (ROW + (m - 1) * U32) * size + 1.01 * half * want[n].abs()
+        assert bool(((t.double() - want[n]).abs() <= bound).all()), n
+    again = {n: torch.empty_like(t) for n, t in got.items()}
+    L.luffy_block_norm_backward(y, o, dout, du, workspace=ws, **names, **kw, **again)
+    assert all(torch.equal(got[n], again[n]) for n in got)

@@ -377,6 +377,36 @@ def test_gradients_of_many_tokens(dtype, T, d, E, k):
     assert all(g.torch.equal(out[n], again[n]) for n in ("dx", "dw_gate", "db_gate"))
 
 
+def test_gradients_of_rows_past_4_gib():
+    """bf16 rows of 9 GB: more parts than the chip alone asks for, each within 32-bit
+    offsets.  All rows but a few are zero, at both ends and at every part's edges."""
+    import torch
+    import paper_2411_15419_amd as L
+    T, d, E, k = 140000, 32768, 2, 1
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GB")
+    some = sorted({t for p in range(1, 8) for at in (T * p // 8, T * p // 3, T * p // 4) for t in (at - 1, at, at + 63)
+                   if 0 <= t < T} | {0, 1, T - 2, T - 1, 65535, 65536, 70015, 70016})
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    x = torch.zeros(T, d, dtype=torch.bfloat16, device="cuda")
+    x[some] = torch.randn(len(some), d, generator=gen, device="cuda").bfloat16()
+    w = torch.randn(E, d, generator=gen, device="cuda").bfloat16()
+    l = torch.randn(T, E, generator=gen, device="cuda")
+    idx, dg = l.argmax(1, keepdim=True).int(), torch.randn(T, k, generator=gen, device="cuda")
+    dx, dw = torch.full_like(x, float("nan")), torch.empty(E, d, device="cuda")
+    ws = torch.empty(L.route_scored_backward_workspace_size(T, d, E), dtype=torch.uint8, device="cuda")
+    L.luffy_route_scored_backward(x, w, "sigmoid", l, idx, dg, dx, dw, None, ws, renormalise=False)
+    s = torch.sigmoid(l.double().gather(1, idx.long()))
+    dl = torch.zeros(T, E, dtype=torch.float64, device="cuda").scatter_(1, idx.long(), dg.double() * s * (1 - s))
+    want, size = dl[some].t() @ x[some].double(), dl[some].t().abs() @ x[some].double().abs()
+    # dl to 8 roundings, and a sum of `some` terms that are not zero, in at most 64 parts
+    assert bool(((dw.double() - want).abs() <= (8 + len(some) + 64) * U32 * size).all())
+    for t in (0, 65535, 65536, 131072, T - 1):     # offsets past 32 bits
+        want = dl[t] @ w.double()
+        assert bool(((dx[t].double() - want).abs() <= 1.01 * 2.0 ** -8 * want.abs()).all())
+    assert not bool(torch.isnan(dx[::997]).any())
+
+
 def test_gradients_of_extreme_logits():
     """Scores that under- and overflow float32 when taken by themselves."""
     for score in ("softmax", "sigmoid"):
