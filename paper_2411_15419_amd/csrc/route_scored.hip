@@ -21,7 +21,7 @@ namespace luffy {
 namespace {
 
 constexpr int kMaxChoices = 8, kMaxGroups = 16;
-constexpr int kChooseTok = 32, kChooseWaves = 4;   // of a scored_choose block; a histogram chunk is its tokens
+constexpr int kChooseTok = 32, kChooseWaves = 4;   // of a scored_choose block, at most; a histogram chunk is its tokens
 constexpr int kAgainExperts = 4;                   // logits that a wave takes again together
 constexpr float kLog2e = 1.44269504088896341f;
 
@@ -253,6 +253,10 @@ __device__ __forceinline__ void choose16(const float (&l)[NEB], const float (&ba
 // is relative to the absolute sum of the products, which is at most |x| |w|), the
 // norms being a little off covered by a factor of 1.01.  The bound goes to
 // bound[t k], a token's first gate, for scored_choose.
+//   Bounded by the loads' latency where T is small (one token of 1024, 16 experts: 4
+// us), by rows from HBM and W from L2 where it is large (65536 x 4096 bf16, 64 experts:
+// 176 us, 3.0 TB/s; float32 65536 x 1024, 32: 109 us, 2.5 TB/s, bound by the float32
+// products).
 template <bool BF16, int A>
 __global__ __launch_bounds__(256) void scored_gate_kernel(const void* __restrict__ xv, const void* __restrict__ wv,
                                                           int T, int d, ScoreArgs a, float* __restrict__ logits,
@@ -385,8 +389,10 @@ __global__ __launch_bounds__(256) void scored_gate_kernel(const void* __restrict
 // bf16 logits for W of at most kStreamLds bytes and many tokens: persistent blocks
 // hold W in LDS, and every wave takes 16 tokens over the whole of d, 2 NB K steps of
 // loads in flight: 8 with 16 waves a block, 16 with up to eight, which have the
-// registers for them (about 128 KB a CU either way).  The sums of eight steps are added up apart, so that the
-// error bound has 8 + d / 256 roundings and not d / 32.
+// registers for them (about 128 KB a CU either way).  The sums of eight steps are added
+// up apart, so that the error bound has 8 + d / 256 roundings and not d / 32.
+//   Bounded by the rows' stream: 32768 x 2048, 32 experts 41 us (3.3 TB/s; a launch and
+// W's staging are 8 of them), 65536 x 1024, 16 experts 32 us (4.1 TB/s).
 constexpr int kStreamLds = 128 * 1024, kStreamWaves = 16;
 
 inline bool stream_ok(int dtype, int E, int d) {
@@ -570,7 +576,7 @@ __device__ __forceinline__ void products64(const void* __restrict__ xv, const vo
   }
 }
 
-// kChooseTok tokens a block: choices by the 16 lanes of a row, four tokens a wave at
+// tok tokens a block: choices by the 16 lanes of a row, four tokens a wave at
 // a time; then those whose float32 logits do not tell are decided in float64, and
 // waves rank the slots of a choice each.
 //   Of an undecided token the logits that another one (or, in a group, another
@@ -579,14 +585,19 @@ __device__ __forceinline__ void products64(const void* __restrict__ xv, const vo
 // left their range, and in a second pass where other groups are kept than at first and
 // their experts are close too, or where under a softmax with a bias the other logits'
 // part in the sum still could turn a choice.  The waves share these products.
-//   T <= kChooseTok: the one block has every slot, and lays out the buckets as well.
+//   Bounded by its chains, not by bytes (32768 tokens, 32 experts, k 4: 12 MB): a block
+// takes some 4 us for the first choices, and one with an undecided token 2 for which
+// logits, 2 for the products and 3 for the decision; 18.7 us in all.  The softmax, the
+// sigmoid and the groups are compiled apart (a runtime switch: 2 us more).  One block
+// per 64 tokens 23.7 us, eight waves per 32 22.9.
+//   T <= tok: the one block has every slot, and lays out the buckets as well.
 template <int NEB, bool SIG, bool GROUPED>
 __global__ __launch_bounds__(kChooseWaves * 64) void scored_choose_kernel(
-    const void* __restrict__ xv, const void* __restrict__ wv, bool bf16, int T, int d, ScoreArgs a, int C,
+    const void* __restrict__ xv, const void* __restrict__ wv, bool bf16, int T, int d, int tok, ScoreArgs a, int C,
     int32_t* __restrict__ topk_idx, float* __restrict__ topk_gate, float* __restrict__ logits,
     int32_t* __restrict__ slot_pos, int32_t* __restrict__ hist, int* __restrict__ scan_done,
     int32_t* __restrict__ perm_token, int32_t* __restrict__ offsets) {
-  constexpr int NE = kAgainExperts, ITEMS = 16, ROWS = kChooseTok / 4 / kChooseWaves;
+  constexpr int NE = kAgainExperts, ITEMS = 16;
   __shared__ int choice[kMaxChoices][kChooseTok];
   __shared__ int cnt[kMaxChoices][kMaxExperts];
   __shared__ float bounds[kChooseTok];
@@ -598,7 +609,7 @@ __global__ __launch_bounds__(kChooseWaves * 64) void scored_choose_kernel(
   __shared__ double vals[kChooseWaves][kMaxExperts], gvals[kChooseWaves][kMaxGroups];
   __shared__ double sums[kChooseWaves][ITEMS][NE];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, m = lane & 15, q = lane >> 4;
-  const int ch = blockIdx.x, t0 = ch * kChooseTok, E = a.E, k = a.k, nch = gridDim.x;
+  const int ch = blockIdx.x, t0 = ch * tok, E = a.E, k = a.k, nch = gridDim.x, rows = tok / 4 / kChooseWaves;
   constexpr bool sig = SIG, grouped = GROUPED;
   if (ch == 0 && threadIdx.x == 0) *scan_done = 0;   // armed for slot_scan
   {
@@ -619,12 +630,12 @@ __global__ __launch_bounds__(kChooseWaves * 64) void scored_choose_kernel(
     load(0);
     // (not unrolled: the code is fetched once a block, cold)
 #pragma unroll 1
-    for (int i = 0; i < ROWS; ++i) {
+    for (int i = 0; i < rows; ++i) {
       const int tl = 4 * (w + kChooseWaves * i) + q, t = t0 + tl;
 #pragma unroll
       for (int j = 0; j < NEB; ++j) l[j] = ahead[j];
       dl = dl_ahead;
-      if (i + 1 < ROWS) load(i + 1);
+      if (i + 1 < rows) load(i + 1);
       int expert;
       float gate;
       uint32_t key[NEB], marked;
@@ -653,7 +664,7 @@ __global__ __launch_bounds__(kChooseWaves * 64) void scored_choose_kernel(
     }
   }
   __syncthreads();
-  const uint64_t open = __ballot(lane < kChooseTok && marks[lane % kChooseTok] != 0);   // the same in every wave
+  const uint64_t open = __ballot(lane < tok && marks[lane % kChooseTok] != 0);   // the same in every wave
   const int marked = __popcll(open);
   if (marked) {
     auto nth = [&](int n) {   // the n-th marked token
@@ -869,7 +880,7 @@ __global__ __launch_bounds__(kChooseWaves * 64) void scored_choose_kernel(
   }
   // stable ranks among the chunk's slots of the same expert: the lanes that hold
   // it, by ballots on its bits
-  const bool valid = lane < kChooseTok && t0 + lane < T;
+  const bool valid = lane < tok && t0 + lane < T;
   constexpr int PER = kMaxChoices / kChooseWaves;
   int ranks[PER];
 #pragma unroll
@@ -941,6 +952,8 @@ __global__ __launch_bounds__(kChooseWaves * 64) void scored_choose_kernel(
 //   dl leaves as three bf16 parts (their sum has dl's 24 bits): part p of expert e in
 // column p E + e of the rows that scored_dw's product takes.
 // db: a lane's sums over its tokens, added up over the block, in a fixed order.
+//   Bounded by latency (a token is a chain of loads and row sums): 65536 tokens, 64
+// experts, k 8: 17 us for 46 MB.
 constexpr int kDlThreads = 256;
 
 template <bool EVEN>   // E is a multiple of 4
@@ -1077,8 +1090,10 @@ __device__ __forceinline__ float dl_value(const uint16_t* p, int E) {
   return (bf16_to_f32(p[0]) + bf16_to_f32(p[E])) + bf16_to_f32(p[2 * E]);
 }
 
-// dx of a token a wave: its experts' rows of W by dl, and the representatives'
-// rows of dx_rep that are this token's.
+// dx of a token a wave: its experts' rows of W by dl (from L2), and the representatives'
+// rows of dx_rep that are this token's, added in float32 and rounded once.  Bounded by
+// the gathered rows: 65536 x 1024 bf16, k 8, 196 us for 765 MB, 3.9 TB/s (a large copy
+// 4.9).  Sixteen loads in flight, held in arrays, took 151 registers and 369 us.
 template <bool BF16>
 __global__ __launch_bounds__(256) void scored_dx_kernel(const void* __restrict__ wv, const uint16_t* __restrict__ dl,
                                                         int ld, int T, int d, int E, int k,
@@ -1144,7 +1159,9 @@ constexpr int kMaxDwParts = 64;   // (the product's groups)
 
 // float32 rows: part of dW = dl^T x, 64 columns by the tokens of part blockIdx.y,
 // every expert; 64 tokens at a time in LDS, 16 experts a wave, a column a lane.
-// (bf16 rows go through the FFN's weight-gradient product, ffn.h.)
+// (bf16 rows go through the FFN's weight-gradient product, ffn.h: dl's three bf16 parts
+// are 3 E of its columns, so the sums are float32's at the matrix cores' rate.  65536 x
+// 1024, 64 experts: 44 us, where these products took 260.)
 __global__ __launch_bounds__(256) void scored_dw_kernel(const float* __restrict__ xv, const uint16_t* __restrict__ dl,
                                                         int ld, int T, int d, int E, int per,
                                                         float* __restrict__ part_w) {
@@ -1187,9 +1204,9 @@ __global__ __launch_bounds__(256) void scored_dw_kernel(const float* __restrict_
 }
 
 // dw = sum over the parts, of bf16 rows over dl's three as well (rows e, E + e, 2 E + e
-// of a part of `rows` rows): 256 values a block, a wave a sixteenth of
-// the parts (its loads are in flight together).  The
-// last block: db over the blocks of scored_dlogits.  In a fixed order.
+// of a part of `rows` rows): 256 values a block, a wave a sixteenth of the parts (its
+// loads are in flight together).  The last block: db over the blocks of scored_dlogits.
+// In a fixed order.  Bounded by the parts' 50 MB: 15 us (65536 x 1024, 64 experts).
 template <int SPLITS>
 __global__ __launch_bounds__(1024) void scored_dw_reduce_kernel(const float* __restrict__ part_w,
                                                                const float* __restrict__ part_b, int parts,
@@ -1334,7 +1351,13 @@ extern "C" int luffy_route_scored(const void* x, int T, int d, int dtype, const 
          topk_gate, inv_norm)
   const bool bf16 = dtype == LUFFY_BF16;
   const int chunks = (T + 15) / 16, cus = persistent_grid();
-  if (stream_ok(dtype, E, d) && chunks >= 4 * cus) {
+  // Streaming from eight chunks of 16 tokens a CU on: below, staging W (8 us) and the
+  // idle waves cost more than blocks that fetch it from L2 (us, streaming | blocks: 64 x
+  // 1024 at T 16384 25 | 18, 32768 25 | 31; 32 x 2048 28 | 21, 42 | 45; 16 x 1024 at 65536
+  // 32 | 45).  Blocks of 16 tokens have the most waves, of 64 fetch W least often (16, 32,
+  // 64 tokens: 2048 x 64 x 1024 11, 13, 15 us; 8192 15, 13, 17; 32768 45, 31, 31; 65536 x
+  // 64 x 4096 with 32 213, with 64 176).
+  if (stream_ok(dtype, E, d) && chunks >= 8 * cus) {
     const int waves = std::min(kStreamWaves, (chunks + cus - 1) / cus);
 #define LUFFY_SCORED_S(NEB)                                                                                         \
   launch("scored_gate", waves > 8 ? scored_gate_stream_kernel<NEB, 16> : scored_gate_stream_kernel<NEB, 8>, cus,    \
@@ -1353,12 +1376,18 @@ extern "C" int luffy_route_scored(const void* x, int T, int d, int dtype, const 
     if (bf16) LUFFY_SCORED(true, 1); else LUFFY_SCORED(false, 1);
   }
 #undef LUFFY_SCORED
-  const int blocks = (T + kChooseTok - 1) / kChooseTok, C = capacity_slots(T, k, E, capacity_factor);
+  // Tokens of a chunk: 16 make the longest chain of a block shorter while the chip has
+  // room for the blocks, 32 halve the counts that slot_scan goes through (64 experts of
+  // 1024, k 8, choices | scan in us, 16 against 32 tokens: T 2048 11.2 | 6.4 against 13.0
+  // | 6.5, 8192 17.4 | 7.1 against 19.5 | 6.5, 16384 20.2 | 8.4 against 20.2 | 7.4; 64 x
+  // 4096 at 65536 58 | 16 against 54 | 11).  As many as there are where one block does.
+  const int tok = T <= 16 || (T > kChooseTok && T <= 8192) ? 16 : kChooseTok;
+  const int blocks = (T + tok - 1) / tok, C = capacity_slots(T, k, E, capacity_factor);
 #define LUFFY_CHOOSE(NEB)                                                                                           \
   launch("scored_choose",                                                                                           \
          sig ? (grouped ? scored_choose_kernel<NEB, true, true> : scored_choose_kernel<NEB, true, false>)           \
              : (grouped ? scored_choose_kernel<NEB, false, true> : scored_choose_kernel<NEB, false, false>),        \
-         blocks, kChooseWaves * 64, 0, s, x, w_gate, bf16, T, d, a, C, topk_idx, topk_gate, logits, slot_pos,       \
+         blocks, kChooseWaves * 64, 0, s, x, w_gate, bf16, T, d, tok, a, C, topk_idx, topk_gate, logits, slot_pos,       \
          ws.hist, ws.done, perm_token, offsets)
   const bool sig = score == LUFFY_SCORE_SIGMOID, grouped = top_groups < groups;
   if (E <= 16) LUFFY_CHOOSE(1);
@@ -1367,7 +1396,7 @@ extern "C" int luffy_route_scored(const void* x, int T, int d, int dtype, const 
   else LUFFY_CHOOSE(4);
 #undef LUFFY_CHOOSE
   if (blocks > 1)
-    route_buckets_enqueue(topk_idx, T, E, k, capacity_factor, kChooseTok, slot_pos, perm_token, offsets, ws, s);
+    route_buckets_enqueue(topk_idx, T, E, k, capacity_factor, tok, slot_pos, perm_token, offsets, ws, s);
   return check_launch(fn);
 }
 
