@@ -174,6 +174,9 @@ __device__ __forceinline__ void row_stats(const Chunk<BF16> (&c)[CH], int chunks
   r = 1.0f / sqrtf(fmaf(q[0], inv_d, eps));
 }
 
+// A row a team, in registers from its loads to its stores.  Bounded by HBM: 8192 x
+// 1024 bf16, layer norms and a token gate, 17.0 us, 4.9 TB/s; 16384 x 4096 142 us, 4.7
+// TB/s (a large copy: 4.9).  One row of 4096: 3.5 us, a launch and its loads' latency.
 template <bool BF16, int CH, int WAVES>
 __global__ __launch_bounds__(WAVES > 1 ? WAVES * 64 : 256) void block_norm_kernel(NormArgs a, int lt_log2) {
   __shared__ float lds[3][16][4];
@@ -268,9 +271,10 @@ __global__ __launch_bounds__(WAVES > 1 ? WAVES * 64 : 256) void block_norm_kerne
 // fixed order.
 //   Eight waves a block, one block a CU (no spills, and few sums to add up at the
 // end); bf16 rows are fetched while the rows before them are worked on, and a lane
-// holds its columns' weights.  16384 x 4096 bf16: 227 us and 9 us for the sums, 3.4
+// holds its columns' weights.  16384 x 4096 bf16: 200 us and 7 us for the sums, 3.9
 // TB/s in all (a large copy: 4.9); 272 and 25 us with two blocks a CU, nothing in
-// flight and row sums by ds_bpermute.
+// flight and row sums by ds_bpermute.  3001 x 1088 float32 33 and 6 us: six rows a
+// team, bound by their chains of loads and row sums.
 constexpr int kSums = 5;   // w_pre, b_pre, w_post, b_post, gate
 
 struct NormBwdArgs {
@@ -561,18 +565,23 @@ int norm_blocks(int T, int teams, int most) {
   return static_cast<int>(std::max(1ll, std::min<long long>((static_cast<long long>(T) + teams - 1) / teams, most)));
 }
 
+// One chunk a lane as far as eight waves reach: more waves have more loads in flight
+// (us, against two or four chunks a lane on fewer waves: 64 x 2048 bf16 4.8 | 6.2, 8192 x
+// 2048 float32 67 | 76, 8192 x 2112 bf16 46 | 52, 4096 x 4096 38.6 | 41.8, 16384 x 4096
+// 142 | 152; 8192 x 8192 with one chunk on 16 waves 146, with two on eight 142).
 template <bool BF16>
 void launch_norm(const NormArgs& a, hipStream_t s) {
 #define LUFFY_NORM(CH, WAVES, PER)                                                                               \
   do {                                                                                                           \
     const int lg = team_log2(a.d, CH);                                                                           \
-    launch("block_norm", block_norm_kernel<BF16, CH, WAVES>, norm_blocks(a.T, WAVES > 1 ? 1 : 256 >> lg, PER * persistent_grid()), \
-           WAVES > 1 ? WAVES * 64 : 256, 0, s, a, lg);                                                           \
+    launch("block_norm", block_norm_kernel<BF16, CH, WAVES>,                                                     \
+           norm_blocks(a.T, WAVES > 1 ? 1 : 256 >> lg, PER * persistent_grid()), WAVES > 1 ? WAVES * 64 : 256,   \
+           0, s, a, lg);                                                                                         \
   } while (0)
   if (a.d <= 512) LUFFY_NORM(1, 1, 8);
-  else if (a.d <= 1024) LUFFY_NORM(2, 1, 8);
-  else if (a.d <= 2048) LUFFY_NORM(4, 1, 8);
-  else if (a.d <= 4096) LUFFY_NORM(2, 4, 8);
+  else if (a.d <= 1024) LUFFY_NORM(1, 2, 16);
+  else if (a.d <= 2048) LUFFY_NORM(1, 4, 8);
+  else if (a.d <= 4096) LUFFY_NORM(1, 8, 4);
   else if (a.d <= 8192) LUFFY_NORM(2, 8, 4);
   else if (a.d <= 16384) LUFFY_NORM(2, 16, 2);
   else LUFFY_NORM(4, 16, 2);
