@@ -584,6 +584,13 @@ def luffy_mx8_dequantize(q, s, x, stream=None):
     _check(load_library().luffy_mx8_dequantize(q, s, rows, cols, dt, x, _stream(stream)), what)
 
 
+def _rows(what, name, t):
+    """(rows, columns) of a bf16 matrix."""
+    if t.dim() != 2 or t.dtype != torch.bfloat16:
+        raise LuffyError(f"{what}: {name} must be bfloat16 [rows, cols], got {str(t.dtype)[6:]} {list(t.shape)}")
+    return t.shape
+
+
 def _ffn_shapes(what, x_rows, x_cols, row_index, rep_offsets, w1, w2, max_rows, zq, zs):
     """(E, d, d_ff), the tensors of an FFN that keeps Z checked."""
     bf, i32 = torch.bfloat16, torch.int32
@@ -608,8 +615,8 @@ def luffy_expert_ffn_keep(x, row_index, rep_offsets, w1, w2, act, max_rows, zq, 
     [ceil(d_ff/256), max_rows, 8], for luffy_expert_ffn_backward_kept.  Workspace:
     expert_ffn_workspace_size."""
     what = "luffy_expert_ffn_keep"
-    _fits(what, "x", x, x.shape, torch.bfloat16)
-    E, d, d_ff = _ffn_shapes(what, x.shape[0], x.shape[-1], row_index, rep_offsets, w1, w2, max_rows, zq, zs)
+    x_rows, x_cols = _rows(what, "x", x)
+    E, d, d_ff = _ffn_shapes(what, x_rows, x_cols, row_index, rep_offsets, w1, w2, max_rows, zq, zs)
     _fits(what, "y_rep", y_rep, (y_rep.shape[0], d), torch.bfloat16)
     if y_rep.shape[0] < max_rows:
         raise LuffyError(f"{what}: y_rep has {y_rep.shape[0]} rows of {max_rows}")
@@ -632,8 +639,7 @@ def luffy_expert_ffn_backward_kept(x, x_scale, row_index, rep_offsets, w1, w2, a
     what = "luffy_expert_ffn_backward_kept"
     bf = torch.bfloat16
     if x_scale is None:
-        _fits(what, "x", x, x.shape, bf)
-        x_rows, x_cols = x.shape
+        x_rows, x_cols = _rows(what, "x", x)
     else:
         x_rows, x_cols = _mx8_shape(what, x, x_scale)
     E, d, d_ff = _ffn_shapes(what, x_rows, x_cols, row_index, rep_offsets, w1, w2, max_rows, zq, zs)
@@ -732,6 +738,8 @@ def luffy_route_scored_backward(x, w_gate, score, logits, topk_idx, dgate, dx, d
 def luffy_combine_many(y_rep, rep_row, slot_pos, topk_gate, y, stream=None):
     """luffy_combine for up to 8 slots a token."""
     what = "luffy_combine_many"
+    if slot_pos.dim() != 2:
+        raise LuffyError(f"{what}: slot_pos must be [T, k], got {list(slot_pos.shape)}")
     T, k = slot_pos.shape
     i32 = torch.int32
     if y.dim() != 2 or y_rep.dim() != 2 or y_rep.dtype != y.dtype or y_rep.shape[1] != y.shape[1]:
@@ -751,6 +759,8 @@ def luffy_combine_many_backward(dy, y_rep, rep_row, perm_token, slot_pos, topk_g
                                 dgate, workspace, stream=None):
     """luffy_combine_backward for up to 8 slots a token."""
     what = "luffy_combine_many_backward"
+    if slot_pos.dim() != 2:
+        raise LuffyError(f"{what}: slot_pos must be [T, k], got {list(slot_pos.shape)}")
     T, k = slot_pos.shape
     i32 = torch.int32
     if dy.dim() != 2 or y_rep.dim() != 2 or y_rep.shape[1] != dy.shape[1]:
@@ -1094,9 +1104,9 @@ class MoEBlock(MoELayer):
         kw = dict(norm=self.norm, eps=self.eps, stream=stream)
         if x.shape != (self.T, self.d) or x.dtype != self.dtype:
             raise LuffyError(f"x must be [{self.T}, {self.d}] {self.dtype}")
-        if following is not None and (following.norm, following.eps) != (self.norm, self.eps):
-            raise LuffyError("MoEBlock: blocks that share a pass must have the same norm and eps")
-        self.normed = normed
+        if following is not None and (following is self or (following.norm, following.eps) != (self.norm, self.eps)):
+            raise LuffyError("MoEBlock: blocks that share a pass must be two, of the same norm and eps")
+        self.normed, self.following, self.backed = normed, following, False
         if not normed:
             luffy_block_norm(x, None, None, self.u, w_pre=self.w_pre, b_pre=self.b_pre, **kw)
         super().__call__(self.u, stream, threshold, hist_in)
@@ -1141,6 +1151,10 @@ class MoEBlock(MoELayer):
         db_pre as far as the block has them; a block called with normed=True
         leaves dx and its dw_pre, db_pre to the block before it (dx is then the
         stream's gradient without the norm's share)."""
+        if not hasattr(self, "backed") or following is not self.following:
+            raise LuffyError("MoEBlock.backward: of a call, with the `following` that the call had")
+        if following is not None and not (following.backed and following.normed):
+            raise LuffyError("MoEBlock.backward: the following block, called with normed=True, comes first")
         b, g = self.buf, self._gradients(dw_dtype)
         kw = dict(norm=self.norm, eps=self.eps, stream=stream)
         S = self.T * self.k
@@ -1166,6 +1180,7 @@ class MoEBlock(MoELayer):
             dx = g["dx"]
             luffy_block_norm_backward(None, x, g["dstream"], g["du"], dx, None, g["ws_n"], w_pre=self.w_pre,
                                       dw_pre=g["dw_pre"], db_pre=g["db_pre"], **kw)
+        self.backed = True
         names = ("dw1", "dw2", "dw_gate", "db_gate", "dgate", "dw_post", "db_post", "dw_pre", "db_pre")
         return dx, {n: g[n] for n in names if g[n] is not None}
 
@@ -1180,6 +1195,8 @@ class MoEStack:
     def __init__(self, layers):
         if not layers or any(not L.history for L in layers):
             raise LuffyError("MoEStack: every layer needs history=(S1, S2)")
+        if any(isinstance(L, MoEBlock) for L in layers):
+            raise LuffyError("MoEStack: runs layers without their norms; call MoEBlocks one after the other")
         self.layers = list(layers)
 
     def __call__(self, xs, stream=None, threshold=None, ffn=True):

@@ -482,10 +482,11 @@ extern "C" size_t luffy_combine_backward_workspace_size(int T, int k, int max_ro
 
 namespace {
 
-int combine_backward_run(const char* fn, int most_k, const void* dy, const void* y_rep, const int32_t* rep_row, const int32_t* perm_token,
-                         const int32_t* slot_pos, const float* topk_gate, const int32_t* offsets,
-                         const int32_t* rep_offsets, int E, int T, int k, int d, int dtype, int max_rows, void* dy_rep,
-                         float* dgate, void* workspace, size_t workspace_bytes, void* stream) {
+int combine_backward_run(const char* fn, int most_k, const void* dy, const void* y_rep, const int32_t* rep_row,
+                         const int32_t* perm_token, const int32_t* slot_pos, const float* topk_gate,
+                         const int32_t* offsets, const int32_t* rep_offsets, int E, int T, int k, int d, int dtype,
+                         int max_rows, void* dy_rep, float* dgate, void* workspace, size_t workspace_bytes,
+                         void* stream) {
   if (!dy || !y_rep || !rep_row || !perm_token || !slot_pos || !topk_gate || !offsets || !rep_offsets ||
       !dy_rep || !dgate)
     return fail(LUFFY_E_INVALID, "%s: null pointer argument", fn);
@@ -541,18 +542,22 @@ int combine_backward_run(const char* fn, int most_k, const void* dy, const void*
 
 }  // namespace
 
-extern "C" int luffy_combine_backward(const void* dy, const void* y_rep, const int32_t* rep_row, const int32_t* perm_token,
-                         const int32_t* slot_pos, const float* topk_gate, const int32_t* offsets,
-                         const int32_t* rep_offsets, int E, int T, int k, int d, int dtype, int max_rows, void* dy_rep,
-                         float* dgate, void* workspace, size_t workspace_bytes, void* stream) {
+extern "C" int luffy_combine_backward(const void* dy, const void* y_rep, const int32_t* rep_row,
+                                      const int32_t* perm_token, const int32_t* slot_pos, const float* topk_gate,
+                                      const int32_t* offsets, const int32_t* rep_offsets, int E, int T, int k, int d,
+                                      int dtype, int max_rows, void* dy_rep, float* dgate, void* workspace,
+                                      size_t workspace_bytes, void* stream) {
   return combine_backward_run("luffy_combine_backward", 2, dy, y_rep, rep_row, perm_token, slot_pos, topk_gate, offsets,
-                              rep_offsets, E, T, k, d, dtype, max_rows, dy_rep, dgate, workspace, workspace_bytes, stream);
+                              rep_offsets, E, T, k, d, dtype, max_rows, dy_rep, dgate, workspace, workspace_bytes,
+                              stream);
 }
 
-extern "C" int luffy_combine_many_backward(const void* dy, const void* y_rep, const int32_t* rep_row, const int32_t* perm_token,
-                         const int32_t* slot_pos, const float* topk_gate, const int32_t* offsets,
-                         const int32_t* rep_offsets, int E, int T, int k, int d, int dtype, int max_rows, void* dy_rep,
-                         float* dgate, void* workspace, size_t workspace_bytes, void* stream) {
+extern "C" int luffy_combine_many_backward(const void* dy, const void* y_rep, const int32_t* rep_row,
+                                           const int32_t* perm_token, const int32_t* slot_pos, const float* topk_gate,
+                                           const int32_t* offsets, const int32_t* rep_offsets, int E, int T, int k, int d,
+                                           int dtype, int max_rows, void* dy_rep, float* dgate, void* workspace,
+                                           size_t workspace_bytes, void* stream) {
   return combine_backward_run("luffy_combine_many_backward", 8, dy, y_rep, rep_row, perm_token, slot_pos, topk_gate, offsets,
-                              rep_offsets, E, T, k, d, dtype, max_rows, dy_rep, dgate, workspace, workspace_bytes, stream);
+                              rep_offsets, E, T, k, d, dtype, max_rows, dy_rep, dgate, workspace, workspace_bytes,
+                              stream);
 }

@@ -240,3 +240,43 @@ def test_binding_refusals():
                          (dict(x=x.float()), "x must be"), (dict(act="tanh"), "act")):
         with pytest.raises(L.LuffyError, match=what):
             L.luffy_expert_ffn_keep(**dict(f, **change))
+    for bad in (x.flatten(), x[0], x[None]):                       # one row is not as many as it has values
+        with pytest.raises(L.LuffyError, match="x must be"):
+            L.luffy_expert_ffn_keep(**dict(f, x=bad))
+        with pytest.raises(L.LuffyError, match="x must be"):
+            L.luffy_expert_ffn_backward_kept(bad, None, None, f["rep_offsets"], f["w1"], f["w2"], "gelu", T, f["zq"], s,
+                                             x, x, f["w1"], f["w2"], ws)
+    flat = r["slot_pos"].flatten()
+    with pytest.raises(L.LuffyError, match="slot_pos"):
+        L.luffy_combine_many(x, flat, flat, r["topk_gate"], x)
+    with pytest.raises(L.LuffyError, match="slot_pos"):
+        L.luffy_combine_many_backward(x, x, flat, flat, flat, r["topk_gate"], r["offsets"], r["offsets"], x,
+                                      r["topk_gate"], ws)
+
+
+def test_block_calls_in_another_order():
+    """Calls that a block's documentation rules out, before anything is enqueued."""
+    import torch
+    import paper_2411_15419_amd as L
+
+    def block(**more):
+        b = L.MoEBlock.__new__(L.MoEBlock)
+        b.__dict__.update(dict(T=4, d=64, dtype=torch.bfloat16, norm="rms", eps=1e-6, history=(0.1, 0.9)), **more)
+        return b
+    x = torch.zeros(4, 64, dtype=torch.bfloat16)
+    a, b, other = block(), block(), block()
+    for following in (a, block(norm="layer"), block(eps=1e-5)):
+        with pytest.raises(L.LuffyError, match="share a pass"):
+            a(x, following=following)
+    with pytest.raises(L.LuffyError, match="of a call"):
+        a.backward(x, x)                                           # none yet
+    a.__dict__.update(normed=False, following=b, backed=False)
+    for following in (None, other):
+        with pytest.raises(L.LuffyError, match="the call had"):
+            a.backward(x, x, following=following)
+    for state in (dict(normed=True, backed=False), dict(normed=False, backed=True)):
+        b.__dict__.update(following=None, **state)
+        with pytest.raises(L.LuffyError, match="comes first"):
+            a.backward(x, x, following=b)
+    with pytest.raises(L.LuffyError, match="norms"):
+        L.MoEStack([a, b])
