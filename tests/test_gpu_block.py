@@ -149,6 +149,26 @@ def test_chained_blocks():
         assert far(h2[n], numpy(g2[n])) < 4 * 2.0 ** -8, n
 
 
+def test_blocks_with_history():
+    """The first of a stack computes every pair: the plain block's bits.  The second
+    condenses with the first's record."""
+    import torch
+    kw = dict(T=512, d=256, E=8, k=2, d_ff=256, score="sigmoid", threshold=0.9)
+    plain, a, b = make(15, **kw), make(15, **kw, history=(0.2, 0.95)), make(16, **kw, history=(0.2, 0.95))
+    x = stream(17, 512, 256, centres=40)
+    dout = tensor(np.random.default_rng(18).standard_normal((512, 256)), "bf16")
+    want, o1 = plain(x), a(x)
+    assert torch.equal(want, o1) and torch.equal(plain.buf.rep_of_pos, a.buf.rep_of_pos)
+    o1 = o1.clone()
+    o2 = b(o1, hist_in=a.record).clone()
+    dx, g = b.backward(o1, dout)
+    ref_o, ref, dec = reference(b, o1, numpy(dout))
+    assert 0 < dec["rep_offsets"][-1] < 1024
+    assert far(o2, ref_o) < NORM and far(dx, ref["dx"]) < NORM
+    for n, v in g.items():
+        assert far(v, ref[n]) < NORM, n
+
+
 def test_captured_block():
     """Forward and backward in a graph, replayed on other inputs beside eager work."""
     import torch
