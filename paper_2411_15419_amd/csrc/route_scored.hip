@@ -3,6 +3,7 @@
 // token.
 //
 // Forward kernels:
+//   scored_small   (up to 16 tokens) all of the following in one block
 //   scored_gate    logits by float32 sums on MFMA, and a bound on their error
 //   scored_choose  scores and choices; a token with a deciding gap within the bound is
 //                  decided in float64 from exact products; ranks every slot among its
@@ -258,9 +259,8 @@ __device__ __forceinline__ void choose16(const float (&l)[NEB], const float (&ba
 // 176 us, 3.0 TB/s; float32 65536 x 1024, 32: 109 us, 2.5 TB/s, bound by the float32
 // products).
 template <bool BF16, int A>
-__global__ __launch_bounds__(256) void scored_gate_kernel(const void* __restrict__ xv, const void* __restrict__ wv,
-                                                          int T, int d, ScoreArgs a, float* __restrict__ logits,
-                                                          float* __restrict__ bound, float* __restrict__ inv_norm) {
+__device__ __forceinline__ void gate_block(const void* xv, const void* wv, int T, int d, const ScoreArgs& a,
+                                           float* logits, float* bound, float* inv_norm) {
   constexpr int TOK = 16 * A, LD = TOK + 4;
   __shared__ __attribute__((aligned(16))) float part[4][kMaxExperts][LD];
   __shared__ float xsq[4][TOK], wsq[4][kMaxExperts];
@@ -384,6 +384,13 @@ __global__ __launch_bounds__(256) void scored_gate_kernel(const void* __restrict
       if (inv_norm) inv_norm[t] = ss > 0.f ? 1.0f / sqrtf(ss) : 0.f;
     }
   }
+}
+
+template <bool BF16, int A>
+__global__ __launch_bounds__(256) void scored_gate_kernel(const void* __restrict__ xv, const void* __restrict__ wv,
+                                                          int T, int d, ScoreArgs a, float* __restrict__ logits,
+                                                          float* __restrict__ bound, float* __restrict__ inv_norm) {
+  gate_block<BF16, A>(xv, wv, T, d, a, logits, bound, inv_norm);
 }
 
 // bf16 logits for W of at most kStreamLds bytes and many tokens: persistent blocks
@@ -592,11 +599,10 @@ __device__ __forceinline__ void products64(const void* __restrict__ xv, const vo
 // per 64 tokens 23.7 us, eight waves per 32 22.9.
 //   T <= tok: the one block has every slot, and lays out the buckets as well.
 template <int NEB, bool SIG, bool GROUPED>
-__global__ __launch_bounds__(kChooseWaves * 64) void scored_choose_kernel(
-    const void* __restrict__ xv, const void* __restrict__ wv, bool bf16, int T, int d, int tok, ScoreArgs a, int C,
-    int32_t* __restrict__ topk_idx, float* __restrict__ topk_gate, float* __restrict__ logits,
-    int32_t* __restrict__ slot_pos, int32_t* __restrict__ hist, int* __restrict__ scan_done,
-    int32_t* __restrict__ perm_token, int32_t* __restrict__ offsets) {
+__device__ __forceinline__ void choose_block(const void* xv, const void* wv, bool bf16, int T, int d, int tok,
+                                             const ScoreArgs& a, int C, int32_t* topk_idx, float* topk_gate,
+                                             float* logits, int32_t* slot_pos, int32_t* hist, int* scan_done,
+                                             int32_t* perm_token, int32_t* offsets) {
   constexpr int NE = kAgainExperts, ITEMS = 16;
   __shared__ int choice[kMaxChoices][kChooseTok];
   __shared__ int cnt[kMaxChoices][kMaxExperts];
@@ -939,6 +945,33 @@ __global__ __launch_bounds__(kChooseWaves * 64) void scored_choose_kernel(
     slot_pos[static_cast<size_t>(lane) * k + j] = kept ? first[e] + at : -1;
     if (kept) perm_token[first[e] + at] = lane;
   }
+}
+
+template <int NEB, bool SIG, bool GROUPED>
+__global__ __launch_bounds__(kChooseWaves * 64) void scored_choose_kernel(
+    const void* __restrict__ xv, const void* __restrict__ wv, bool bf16, int T, int d, int tok, ScoreArgs a, int C,
+    int32_t* __restrict__ topk_idx, float* __restrict__ topk_gate, float* __restrict__ logits,
+    int32_t* __restrict__ slot_pos, int32_t* __restrict__ hist, int* __restrict__ scan_done,
+    int32_t* __restrict__ perm_token, int32_t* __restrict__ offsets) {
+  choose_block<NEB, SIG, GROUPED>(xv, wv, bf16, T, d, tok, a, C, topk_idx, topk_gate, logits, slot_pos, hist, scan_done,
+                                  perm_token, offsets);
+}
+
+// A whole call of up to 16 tokens in one launch: a block's logits, its choices and the
+// buckets.  (No pointer is __restrict__: the logits and bounds are read back.)  Bounded
+// by a launch and its chains: one token of 1024 on 16 experts 11.4 us a call, 14.4 in two
+// launches.  Larger calls would leave their tokens to one CU.
+template <bool BF16, int NEB, bool SIG, bool GROUPED>
+__global__ __launch_bounds__(256) void scored_small_kernel(const void* xv, const void* wv, int T, int d, ScoreArgs a,
+                                                           int C, int32_t* topk_idx, float* topk_gate, float* logits,
+                                                           float* inv_norm, int32_t* slot_pos, int32_t* hist,
+                                                           int* scan_done, int32_t* perm_token, int32_t* offsets) {
+  static_assert(kChooseWaves == 4, "the logits' block and the choices' are one");
+  gate_block<BF16, 1>(xv, wv, T, d, a, logits, topk_gate, inv_norm);
+  __threadfence_block();
+  __syncthreads();
+  choose_block<NEB, SIG, GROUPED>(xv, wv, BF16, T, d, 16, a, C, topk_idx, topk_gate, logits, slot_pos, hist, scan_done,
+                                  perm_token, offsets);
 }
 
 // ---------------------------------------------------------------- backward
@@ -1349,7 +1382,23 @@ extern "C" int luffy_route_scored(const void* x, int T, int d, int dtype, const 
 #define LUFFY_SCORED(BF, A)                                                                                             \
   launch("scored_gate", scored_gate_kernel<BF, A>, (T + 16 * A - 1) / (16 * A), 256, 0, s, x, w_gate, T, d, a, logits, \
          topk_gate, inv_norm)
-  const bool bf16 = dtype == LUFFY_BF16;
+  const bool bf16 = dtype == LUFFY_BF16, sig = score == LUFFY_SCORE_SIGMOID, grouped = top_groups < groups;
+  const int C = capacity_slots(T, k, E, capacity_factor);
+  if (T <= 16) {
+#define LUFFY_SMALL(BF, NEB)                                                                                        \
+  launch("scored_small",                                                                                            \
+         sig ? (grouped ? scored_small_kernel<BF, NEB, true, true> : scored_small_kernel<BF, NEB, true, false>)     \
+             : (grouped ? scored_small_kernel<BF, NEB, false, true> : scored_small_kernel<BF, NEB, false, false>),  \
+         1, 256, 0, s, x, w_gate, T, d, a, C, topk_idx, topk_gate, logits, inv_norm, slot_pos, ws.hist, ws.done,    \
+         perm_token, offsets)
+    if (E <= 16) {
+      if (bf16) LUFFY_SMALL(true, 1); else LUFFY_SMALL(false, 1);
+    } else {
+      if (bf16) LUFFY_SMALL(true, 4); else LUFFY_SMALL(false, 4);
+    }
+#undef LUFFY_SMALL
+    return check_launch(fn);
+  }
   const int chunks = (T + 15) / 16, cus = persistent_grid();
   // Streaming from eight chunks of 16 tokens a CU on: below, staging W (8 us) and the
   // idle waves cost more than blocks that fetch it from L2 (us, streaming | blocks: 64 x
@@ -1381,15 +1430,14 @@ extern "C" int luffy_route_scored(const void* x, int T, int d, int dtype, const 
   // 1024, k 8, choices | scan in us, 16 against 32 tokens: T 2048 11.2 | 6.4 against 13.0
   // | 6.5, 8192 17.4 | 7.1 against 19.5 | 6.5, 16384 20.2 | 8.4 against 20.2 | 7.4; 64 x
   // 4096 at 65536 58 | 16 against 54 | 11).  As many as there are where one block does.
-  const int tok = T <= 16 || (T > kChooseTok && T <= 8192) ? 16 : kChooseTok;
-  const int blocks = (T + tok - 1) / tok, C = capacity_slots(T, k, E, capacity_factor);
+  const int tok = T > kChooseTok && T <= 8192 ? 16 : kChooseTok;
+  const int blocks = (T + tok - 1) / tok;
 #define LUFFY_CHOOSE(NEB)                                                                                           \
   launch("scored_choose",                                                                                           \
          sig ? (grouped ? scored_choose_kernel<NEB, true, true> : scored_choose_kernel<NEB, true, false>)           \
              : (grouped ? scored_choose_kernel<NEB, false, true> : scored_choose_kernel<NEB, false, false>),        \
          blocks, kChooseWaves * 64, 0, s, x, w_gate, bf16, T, d, tok, a, C, topk_idx, topk_gate, logits, slot_pos,       \
          ws.hist, ws.done, perm_token, offsets)
-  const bool sig = score == LUFFY_SCORE_SIGMOID, grouped = top_groups < groups;
   if (E <= 16) LUFFY_CHOOSE(1);
   else if (E <= 32) LUFFY_CHOOSE(2);
   else if (E <= 48) LUFFY_CHOOSE(3);

@@ -106,6 +106,14 @@ CASES = [  # dtype, T, d, E, k, score, balance, groups, top, best, renorm, cf
     ("bf16", 257, 1088, 64, 7, "softmax", True, 2, 1, 2, True, 0.0),
     ("bf16", 90, 4096, 8, 2, "softmax", False, 4, 4, 2, True, 0.0),
     ("f32", 77, 4096, 64, 8, "softmax", True, 64, 64, 1, True, 0.0),
+    ("bf16", 16, 1088, 64, 8, "sigmoid", True, 8, 4, 2, True, 1.0),      # one block and one launch up to 16 tokens
+    ("f32", 16, 320, 40, 6, "softmax", True, 10, 3, 2, True, 0.0),
+    ("bf16", 7, 2112, 24, 4, "softmax", False, 1, 1, 1, False, 0.6),
+    ("f32", 2, 64, 16, 3, "sigmoid", False, 4, 2, 2, False, 0.0),
+    ("bf16", 15, 4096, 12, 2, "softmax", True, 3, 1, 1, True, 0.0),
+    ("f32", 9, 128, 64, 8, "sigmoid", True, 1, 1, 1, True, 0.5),
+    ("bf16", 17, 1088, 64, 8, "sigmoid", True, 8, 4, 2, True, 1.0),      # one block, two launches
+    ("bf16", 32, 256, 33, 8, "softmax", True, 3, 2, 2, True, 0.0),
 ]
 
 
@@ -161,6 +169,22 @@ def test_groups_that_turn(dtype, T):
     r.w = tensor(w, dtype)
     idx = r.check(r.run())
     assert (idx[1::3] == [8, 4, 10, 9]).all()
+
+
+@pytest.mark.parametrize("E", [16, 48])
+def test_a_token_alone_or_among_others(E):
+    """The choices, buckets and logits' bits of 16 tokens are those of one call for
+    each: the largest call in one launch, and the same rows in a larger one."""
+    import torch
+    r = Router(33, "bf16", 40, 1088, E, 4, "sigmoid", True, 8, 4, 2)
+    want = r.run()
+    x = r.x
+    for lo, hi in ((0, 16), (16, 17), (17, 31)):
+        r.x, r.T = x[lo:hi], hi - lo
+        out = r.run()
+        r.check(out)
+        for n in ("topk_idx", "logits", "topk_gate"):
+            assert torch.equal(out[n], want[n][lo:hi]), n
 
 
 def test_cancelling_rows():
