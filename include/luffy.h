@@ -435,7 +435,7 @@ int luffy_expert_ffn_backward(const void* x, const int32_t* row_index, const int
  *   values  q [rows, cols] int8; scales s [ceil(cols/256), rows, 8] uint8: those of
  *           256 consecutive columns of a row side by side, 0 past the last column
  *           (luffy_mx4_scale_bytes(1, rows, cols) bytes)
- * cols is a multiple of 32, at most 32768, rows * cols at most 2^36; x and q
+ * cols is a multiple of 32, at most 32768, rows * cols at most 2^34; x and q
  * 16-byte, s 8-byte aligned.
  *
  * luffy_mx8_quantize - rounds x [rows, cols] (float32 or bf16).  With m the largest
@@ -635,7 +635,7 @@ int luffy_adaptive_threshold(double l_ini, double l_prev, double* h_out);
  * bwd_dw1; serving: mx4_quantize, mx4_dequantize, mx4_matmul, mx4_ffn1,
  * mx4_ffn2, few_gate, few_ffn1, few_ffn2; a block: block_norm,
  * block_norm_backward, block_norm_reduce, scored_gate, scored_choose,
- * scored_small, scored_dlogits, scored_dx, scored_dw, scored_dw_reduce, mx8_quantize,
+ * scored_both, scored_dlogits, scored_dx, scored_dw, scored_dw_reduce, mx8_quantize,
  * mx8_dequantize.
  * ---------------------------------------------------------------------- */
 int luffy_profile_kernel(const char* name);

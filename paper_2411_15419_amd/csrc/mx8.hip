@@ -8,23 +8,27 @@
 namespace luffy {
 namespace {
 
-constexpr int kThreads = 256, kUnroll = 4;   // eight values a thread and step
+// Eight values a thread and step; two steps, for float32 results one (us, with one, two
+// and four steps: 65536 x 2048 bf16 to 8 bits 83, 85, 92, back 71, 66, 67; 16384 x 4096
+// float32 to 8 bits 80, 82, 83, back 58, 79, 84; 3001 x 1088 float32 7.3, 7.3, 8.7 and
+// 8.3, 7.6, 8.0).
+constexpr int kThreads = 256, kQuantizeSteps = 2;
+constexpr int dequantize_steps(bool f32) { return f32 ? 1 : 2; }
 
 // Eight values a thread; a block's four threads find its largest absolute value,
 // the first of them stores the scale (and the zeros past the last column).  Bound by
-// HBM: 65536 x 2048 bf16 88 us, 4.7 TB/s; back to bf16 66 us, 6.2 TB/s (the values are
-// still in the last-level cache in part).  Four units a thread, loads and stores of
-// whole lines.
+// HBM: 65536 x 2048 bf16 85 us, 4.8 TB/s; back to bf16 66 us, 6.2 TB/s (the values are
+// still in the last-level cache in part).  Loads and stores are whole lines.
 template <bool F32>
 __global__ __launch_bounds__(kThreads) void mx8_quantize_kernel(const void* __restrict__ x, int rows, int cols,
                                                                 uint8_t* __restrict__ q, uint8_t* __restrict__ s) {
   const int units = cols / 8;
   const long long limit = static_cast<long long>(rows) * units;
-  const long long base = static_cast<long long>(blockIdx.x) * (kThreads * kUnroll);
+  const long long base = static_cast<long long>(blockIdx.x) * (kThreads * kQuantizeSteps);
   const long long row0 = base / units;
   const int first = static_cast<int>(base - row0 * units);
 #pragma unroll
-  for (int i = 0; i < kUnroll; ++i) {
+  for (int i = 0; i < kQuantizeSteps; ++i) {
     const int at = i * kThreads + threadIdx.x;
     const bool in = base + at < limit;   // (the same for a block's four threads)
     const unsigned u = static_cast<unsigned>(first + at);
@@ -70,13 +74,14 @@ template <bool F32>
 __global__ __launch_bounds__(kThreads) void mx8_dequantize_kernel(const uint8_t* __restrict__ q,
                                                                   const uint8_t* __restrict__ s, int rows, int cols,
                                                                   void* __restrict__ x) {
+  constexpr int kSteps = dequantize_steps(F32);
   const int units = cols / 8;
   const long long limit = static_cast<long long>(rows) * units;
-  const long long base = static_cast<long long>(blockIdx.x) * (kThreads * kUnroll);
+  const long long base = static_cast<long long>(blockIdx.x) * (kThreads * kSteps);
   const long long row0 = base / units;
   const int first = static_cast<int>(base - row0 * units);
 #pragma unroll
-  for (int i = 0; i < kUnroll; ++i) {
+  for (int i = 0; i < kSteps; ++i) {
     const int at = i * kThreads + threadIdx.x;
     if (base + at >= limit) continue;
     const unsigned u = static_cast<unsigned>(first + at);
@@ -100,11 +105,11 @@ __global__ __launch_bounds__(kThreads) void mx8_dequantize_kernel(const uint8_t*
   }
 }
 
-long long mx8_blocks(int rows, int cols) {
-  const long long per = kThreads * kUnroll;
+long long mx8_blocks(int rows, int cols, int steps) {
+  const long long per = kThreads * steps;
   return (static_cast<long long>(rows) * (cols / 8) + per - 1) / per;
 }
-constexpr long long kMaxBlocks = (1ll << 36) / 8 / (kThreads * kUnroll);   // (a grid has fewer than 2^32 threads)
+constexpr long long kMaxValues = 1ll << 34;   // (a grid has fewer than 2^32 threads)
 
 int mx8_check(const char* fn, const void* x, const void* q, const void* s, int rows, int cols, int dtype) {
   if (!x || !q || !s) return fail(LUFFY_E_INVALID, "%s: null pointer argument", fn);
@@ -112,9 +117,10 @@ int mx8_check(const char* fn, const void* x, const void* q, const void* s, int r
   if (dtype != LUFFY_F32 && dtype != LUFFY_BF16) return fail(LUFFY_E_INVALID, "%s: unknown dtype %d", fn, dtype);
   if (cols % 32 != 0) return fail(LUFFY_E_UNSUPPORTED, "%s: cols=%d not a multiple of 32", fn, cols);
   if (cols > 32768) return fail(LUFFY_E_UNSUPPORTED, "%s: cols=%d > 32768", fn, cols);
-  if (mx8_blocks(rows, cols) > kMaxBlocks)
-    return fail(LUFFY_E_UNSUPPORTED, "%s: %d x %d is more than 2^36 values", fn, rows, cols);
-  if (((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(q)) & 15u) || (reinterpret_cast<uintptr_t>(s) & 7u))
+  if (static_cast<long long>(rows) * cols > kMaxValues)
+    return fail(LUFFY_E_UNSUPPORTED, "%s: %d x %d is more than 2^34 values", fn, rows, cols);
+  const uintptr_t bits = reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(q);
+  if ((bits & 15u) || (reinterpret_cast<uintptr_t>(s) & 7u))
     return fail(LUFFY_E_INVALID, "%s: x and q must be 16-byte, s 8-byte aligned", fn);
   return LUFFY_OK;
 }
@@ -127,17 +133,20 @@ using namespace luffy;
 extern "C" int luffy_mx8_quantize(const void* x, int rows, int cols, int dtype, void* q, void* s, void* stream) {
   const int st = mx8_check("luffy_mx8_quantize", x, q, s, rows, cols, dtype);
   if (st != LUFFY_OK) return st;
-  launch("mx8_quantize", dtype == LUFFY_F32 ? mx8_quantize_kernel<true> : mx8_quantize_kernel<false>,
-         static_cast<int>(mx8_blocks(rows, cols)), kThreads, 0, static_cast<hipStream_t>(stream), x, rows, cols, static_cast<uint8_t*>(q),
-         static_cast<uint8_t*>(s));
+  const bool f32 = dtype == LUFFY_F32;
+  launch("mx8_quantize", f32 ? mx8_quantize_kernel<true> : mx8_quantize_kernel<false>,
+         static_cast<int>(mx8_blocks(rows, cols, kQuantizeSteps)), kThreads, 0, static_cast<hipStream_t>(stream), x,
+         rows, cols, static_cast<uint8_t*>(q), static_cast<uint8_t*>(s));
   return check_launch("luffy_mx8_quantize");
 }
 
-extern "C" int luffy_mx8_dequantize(const void* q, const void* s, int rows, int cols, int dtype, void* x, void* stream) {
+extern "C" int luffy_mx8_dequantize(const void* q, const void* s, int rows, int cols, int dtype, void* x,
+                                    void* stream) {
   const int st = mx8_check("luffy_mx8_dequantize", x, q, s, rows, cols, dtype);
   if (st != LUFFY_OK) return st;
-  launch("mx8_dequantize", dtype == LUFFY_F32 ? mx8_dequantize_kernel<true> : mx8_dequantize_kernel<false>,
-         static_cast<int>(mx8_blocks(rows, cols)), kThreads, 0, static_cast<hipStream_t>(stream), static_cast<const uint8_t*>(q),
-         static_cast<const uint8_t*>(s), rows, cols, x);
+  const bool f32 = dtype == LUFFY_F32;
+  launch("mx8_dequantize", f32 ? mx8_dequantize_kernel<true> : mx8_dequantize_kernel<false>,
+         static_cast<int>(mx8_blocks(rows, cols, dequantize_steps(f32))), kThreads, 0,
+         static_cast<hipStream_t>(stream), static_cast<const uint8_t*>(q), static_cast<const uint8_t*>(s), rows, cols, x);
   return check_launch("luffy_mx8_dequantize");
 }

@@ -3,7 +3,7 @@
 // token.
 //
 // Forward kernels:
-//   scored_small   (up to 16 tokens) all of the following in one block
+//   scored_both    (small calls) scored_gate and scored_choose, 16 tokens a block
 //   scored_gate    logits by float32 sums on MFMA, and a bound on their error
 //   scored_choose  scores and choices; a token with a deciding gap within the bound is
 //                  decided in float64 from exact products; ranks every slot among its
@@ -957,12 +957,11 @@ __global__ __launch_bounds__(kChooseWaves * 64) void scored_choose_kernel(
                                   perm_token, offsets);
 }
 
-// A whole call of up to 16 tokens in one launch: a block's logits, its choices and the
-// buckets.  (No pointer is __restrict__: the logits and bounds are read back.)  Bounded
-// by a launch and its chains: one token of 1024 on 16 experts 11.4 us a call, 14.4 in two
-// launches.  Larger calls would leave their tokens to one CU.
+// Both in one launch, 16 tokens a block (up to 16: the buckets as well).  No pointer is
+// __restrict__: the logits and bounds are read back.  Bounded by a launch and its chains:
+// one token of 1024 on 16 experts 11.4 us a call, 14.4 in two launches.
 template <bool BF16, int NEB, bool SIG, bool GROUPED>
-__global__ __launch_bounds__(256) void scored_small_kernel(const void* xv, const void* wv, int T, int d, ScoreArgs a,
+__global__ __launch_bounds__(256) void scored_both_kernel(const void* xv, const void* wv, int T, int d, ScoreArgs a,
                                                            int C, int32_t* topk_idx, float* topk_gate, float* logits,
                                                            float* inv_norm, int32_t* slot_pos, int32_t* hist,
                                                            int* scan_done, int32_t* perm_token, int32_t* offsets) {
@@ -1384,22 +1383,28 @@ extern "C" int luffy_route_scored(const void* x, int T, int d, int dtype, const 
          topk_gate, inv_norm)
   const bool bf16 = dtype == LUFFY_BF16, sig = score == LUFFY_SCORE_SIGMOID, grouped = top_groups < groups;
   const int C = capacity_slots(T, k, E, capacity_factor);
-  if (T <= 16) {
-#define LUFFY_SMALL(BF, NEB)                                                                                        \
-  launch("scored_small",                                                                                            \
-         sig ? (grouped ? scored_small_kernel<BF, NEB, true, true> : scored_small_kernel<BF, NEB, true, false>)     \
-             : (grouped ? scored_small_kernel<BF, NEB, false, true> : scored_small_kernel<BF, NEB, false, false>),  \
-         1, 256, 0, s, x, w_gate, T, d, a, C, topk_idx, topk_gate, logits, inv_norm, slot_pos, ws.hist, ws.done,    \
-         perm_token, offsets)
+  // One launch where every block has a CU of its own, and where it is not two chunks
+  // instead of a whole call in one (us a call in a graph, one | two launches: 64 x 1024, 64
+  // experts 19.1 | 20.2, 1024 x 4096 46.3 | 48.0, 4096 x 1024 30.1 | 32.0, float32 40.9 |
+  // 42.7; 8192 x 2048, 32 experts 34.3 | 33.7; from the host a launch less is 2.5 us more).
+  const int chunks = (T + 15) / 16, cus = persistent_grid();
+  if (T <= 16 || (T > kChooseTok && chunks <= cus)) {
+#define LUFFY_BOTH(BF, NEB)                                                                                        \
+  launch("scored_both",                                                                                            \
+         sig ? (grouped ? scored_both_kernel<BF, NEB, true, true> : scored_both_kernel<BF, NEB, true, false>)     \
+             : (grouped ? scored_both_kernel<BF, NEB, false, true> : scored_both_kernel<BF, NEB, false, false>),  \
+         chunks, 256, 0, s, x, w_gate, T, d, a, C, topk_idx, topk_gate, logits, inv_norm, slot_pos, ws.hist,        \
+         ws.done, perm_token, offsets)
     if (E <= 16) {
-      if (bf16) LUFFY_SMALL(true, 1); else LUFFY_SMALL(false, 1);
+      if (bf16) LUFFY_BOTH(true, 1); else LUFFY_BOTH(false, 1);
     } else {
-      if (bf16) LUFFY_SMALL(true, 4); else LUFFY_SMALL(false, 4);
+      if (bf16) LUFFY_BOTH(true, 4); else LUFFY_BOTH(false, 4);
     }
-#undef LUFFY_SMALL
+#undef LUFFY_BOTH
+    if (chunks > 1)
+      route_buckets_enqueue(topk_idx, T, E, k, capacity_factor, 16, slot_pos, perm_token, offsets, ws, s);
     return check_launch(fn);
   }
-  const int chunks = (T + 15) / 16, cus = persistent_grid();
   // Streaming from eight chunks of 16 tokens a CU on: below, staging W (8 us) and the
   // idle waves cost more than blocks that fetch it from L2 (us, streaming | blocks: 64 x
   // 1024 at T 16384 25 | 18, 32768 25 | 31; 32 x 2048 28 | 21, 42 | 45; 16 x 1024 at 65536

@@ -136,7 +136,7 @@ def test_mx8_refusals(lib, name):
     for n in ("rows", "cols"):
         assert call(**{n: 0}) == INVALID and call(**{n: -3}) == INVALID
     assert call(dtype=2) == INVALID and call(cols=48) == UNSUPPORTED and call(cols=32800) == UNSUPPORTED
-    assert call(rows=2 ** 21 + 1, cols=32768) == UNSUPPORTED and call(rows=2 ** 31 - 1, cols=64) == UNSUPPORTED
+    assert call(rows=2 ** 19 + 1, cols=32768) == UNSUPPORTED and call(rows=2 ** 31 - 1, cols=64) == UNSUPPORTED
     assert call(x=ODD) == INVALID and call(q=ODD) == INVALID and call(s=BYTE) == INVALID
 
 
