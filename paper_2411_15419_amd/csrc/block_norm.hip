@@ -175,7 +175,7 @@ __device__ __forceinline__ void row_stats(const Chunk<BF16> (&c)[CH], int chunks
 }
 
 // A row a team, in registers from its loads to its stores.  Bounded by HBM: 8192 x
-// 1024 bf16, layer norms and a token gate, 17.0 us, 4.9 TB/s; 16384 x 4096 142 us, 4.7
+// 1024 bf16, layer norms and a token gate, 16.7 us, 5.0 TB/s; 16384 x 4096 129 us, 5.2
 // TB/s (a large copy: 4.9).  One row of 4096: 3.5 us, a launch and its loads' latency.
 template <bool BF16, int CH, int WAVES>
 __global__ __launch_bounds__(WAVES > 1 ? WAVES * 64 : 256) void block_norm_kernel(NormArgs a, int lt_log2) {
@@ -269,11 +269,11 @@ __global__ __launch_bounds__(WAVES > 1 ? WAVES * 64 : 256) void block_norm_kerne
 // and adds them up in registers, a block's teams are added in LDS, and the
 // blocks' sums go through the workspace to block_norm_reduce_kernel, all in a
 // fixed order.
-//   Eight waves a block, one block a CU (no spills, and few sums to add up at the
-// end); bf16 rows are fetched while the rows before them are worked on, and a lane
+//   Eight to twelve waves a block, one block a CU (its registers, and few sums to add up
+// at the end); bf16 rows are fetched while the rows before them are worked on, and a lane
 // holds its columns' weights.  16384 x 4096 bf16: 200 us and 7 us for the sums, 3.9
 // TB/s in all (a large copy: 4.9); 272 and 25 us with two blocks a CU, nothing in
-// flight and row sums by ds_bpermute.  3001 x 1088 float32 33 and 6 us: six rows a
+// flight and row sums by ds_bpermute.  3001 x 1088 float32 31 and 6 us: four rows a
 // team, bound by their chains of loads and row sums.
 constexpr int kSums = 5;   // w_pre, b_pre, w_post, b_post, gate
 
@@ -288,11 +288,17 @@ struct NormBwdArgs {
   float* sum[kSums];   // results; a null one is not wanted
 };
 
+// Threads of a block: as many whole teams as about eight waves hold, twelve where
+// fewer would be one team.
+constexpr int bwd_threads(int waves) {
+  return 64 * (waves == 16 ? 16 : waves == 3 ? 9 : waves == 5 ? 10 : waves == 6 ? 12 : waves == 7 ? 7 : 8);
+}
+
 // BIAS: db_pre or db_post is wanted.
 template <bool BF16, int CH, int WAVES, bool BIAS>
-__global__ __launch_bounds__(WAVES == 16 ? 1024 : 512) void block_norm_backward_kernel(NormBwdArgs a, int lt_log2,
-                                                                                       float* __restrict__ part) {
-  constexpr int kThreads = WAVES == 16 ? 1024 : 512;
+__global__ __launch_bounds__(bwd_threads(WAVES)) void block_norm_backward_kernel(NormBwdArgs a, int lt_log2,
+                                                                                 float* __restrict__ part) {
+  constexpr int kThreads = bwd_threads(WAVES);
   constexpr bool AHEAD = BF16 && WAVES < 16;
   __shared__ float lds[3][16][4];
   int turn = 0;
@@ -565,73 +571,89 @@ int norm_blocks(int T, int teams, int most) {
   return static_cast<int>(std::max(1ll, std::min<long long>((static_cast<long long>(T) + teams - 1) / teams, most)));
 }
 
-// One chunk a lane as far as eight waves reach: more waves have more loads in flight
-// (us, against two or four chunks a lane on fewer waves: 64 x 2048 bf16 4.8 | 6.2, 8192 x
-// 2048 float32 67 | 76, 8192 x 2112 bf16 46 | 52, 4096 x 4096 38.6 | 41.8, 16384 x 4096
-// 142 | 152; 8192 x 8192 with one chunk on 16 waves 146, with two on eight 142).
+// As many waves as a row's chunks fill, one chunk a lane up to 4096 columns, two to 16384:
+// more waves have more loads in flight (us, against two or four chunks a lane on fewer
+// waves: 64 x 2048 bf16 4.8 | 6.2, 8192 x 2048 float32 67 | 76, 4096 x 4096 38.6 | 41.8;
+// 8192 x 8192 with one chunk on 16 waves 146, with two on eight 142).  A team takes one
+// row: blocks that stay for the next ones wait for theirs (16384 x 4096 128 | 139, 65536 x
+// 1024 129 | 142, 8192 x 2112 42 | 51); a grid has fewer than 2^32 threads, so past 2^20
+// blocks they do.
 template <bool BF16>
 void launch_norm(const NormArgs& a, hipStream_t s) {
-#define LUFFY_NORM(CH, WAVES, PER)                                                                               \
+#define LUFFY_NORM(CH, WAVES)                                                                                    \
   do {                                                                                                           \
     const int lg = team_log2(a.d, CH);                                                                           \
     launch("block_norm", block_norm_kernel<BF16, CH, WAVES>,                                                     \
-           norm_blocks(a.T, WAVES > 1 ? 1 : 256 >> lg, PER * persistent_grid()), WAVES > 1 ? WAVES * 64 : 256,   \
-           0, s, a, lg);                                                                                         \
+           norm_blocks(a.T, WAVES > 1 ? 1 : 256 >> lg, 1 << 20), WAVES > 1 ? WAVES * 64 : 256, 0, s, a, lg);     \
   } while (0)
-  if (a.d <= 512) LUFFY_NORM(1, 1, 8);
-  else if (a.d <= 1024) LUFFY_NORM(1, 2, 16);
-  else if (a.d <= 2048) LUFFY_NORM(1, 4, 8);
-  else if (a.d <= 4096) LUFFY_NORM(1, 8, 4);
-  else if (a.d <= 8192) LUFFY_NORM(2, 8, 4);
-  else if (a.d <= 16384) LUFFY_NORM(2, 16, 2);
-  else LUFFY_NORM(4, 16, 2);
+  switch (a.d <= 4096 ? (a.d + 511) / 512 : a.d <= 8192 ? (a.d + 1023) / 1024 + 8 : 0) {
+    case 1: LUFFY_NORM(1, 1); break;
+    case 2: LUFFY_NORM(1, 2); break;
+    case 3: LUFFY_NORM(1, 3); break;
+    case 4: LUFFY_NORM(1, 4); break;
+    case 5: LUFFY_NORM(1, 5); break;
+    case 6: LUFFY_NORM(1, 6); break;
+    case 7: LUFFY_NORM(1, 7); break;
+    case 8: LUFFY_NORM(1, 8); break;
+    case 13: LUFFY_NORM(2, 5); break;
+    case 14: LUFFY_NORM(2, 6); break;
+    case 15: LUFFY_NORM(2, 7); break;
+    case 16: LUFFY_NORM(2, 8); break;
+    default:
+      if (a.d <= 16384) LUFFY_NORM(2, 16);
+      else LUFFY_NORM(4, 16);
+  }
 #undef LUFFY_NORM
 }
 
 // A team of the backward and the blocks of the grid (each leaves kSums rows of d sums
-// to be added up).  One chunk a lane, or two, which halves the waves that wait for
-// each other: from 16 rows a team on (bf16, us, one | two chunks: 65536 x 1024 209 |
-// 201, 32768 x 2048 213 | 201, 16384 x 4096 237 | 227; 8192 x 1024 36 | 40; float32
-// 3001 x 1088 33 | 36).
+// to be added up).  One chunk a lane on as many waves as a row fills; or two, which halves
+// the waves that wait for each other, from 16 rows a team on, where they fill three
+// quarters of the lanes (bf16, us, one | two chunks: 65536 x 1024 207 | 202, 32768 x 2048
+// 211 | 199, 16384 x 4096 217 | 199, 8192 x 3520 105 | 99; 8192 x 2880 75 | 90, 8192 x
+// 2112 68 | 82, 32768 x 1088 148 | 160; 8192 x 1024 36 | 40; float32 3001 x 1088 33 | 36),
+// and, up to 1024 columns, where no bias gradient takes the registers (65536 x 1024 257 |
+// 290).
 struct BwdShape {
   int chunks, waves, blocks;
 };
 
-BwdShape bwd_shape(int T, int d, bool bf16) {
+BwdShape bwd_shape(int T, int d, bool bf16, bool bias) {
   constexpr int most = 256;   // blocks: the workspace is sized without a device
-  auto waves = [&](int per) {
-    int w = 1;
-    while (w < 8 && w * per < d) w *= 2;
-    return w;
-  };
   if (d > 8192) return {d <= 16384 ? 2 : 4, 16, norm_blocks(T, 1, most)};
   if (d > 4096) return {2, 8, norm_blocks(T, 1, most)};
   if (d <= 512) return {1, 1, norm_blocks(T, 512 >> team_log2(d, 1), most)};
-  const int teams = 8 / waves(1024);
-  if (bf16 && T >= 16 * most * teams) return {2, waves(1024), norm_blocks(T, teams, most)};
-  return {1, waves(512), norm_blocks(T, 8 / waves(512), most)};
+  const int two = d <= 1024 ? 1 : d <= 2048 ? 2 : 4, teams = 8 / two;
+  if (bf16 && T >= 16 * most * teams && 4 * d > 3 * 1024 * two && !(bias && two == 1))
+    return {2, two, norm_blocks(T, teams, most)};
+  const int one = (d + 511) / 512;
+  return {1, one, norm_blocks(T, bwd_threads(one) / 64 / one, most)};
 }
 
 template <bool BF16, bool BIAS>
 void launch_norm_backward(const NormBwdArgs& a, float* part, hipStream_t s) {
-  const BwdShape sh = bwd_shape(a.T, a.d, BF16);
+  const BwdShape sh = bwd_shape(a.T, a.d, BF16, BIAS);
   const int blocks = sh.blocks;
 #define LUFFY_NORM_B(CH, WAVES)                                                                           \
   launch("block_norm_backward", block_norm_backward_kernel<BF16, CH, WAVES, BIAS>, blocks,                \
-         WAVES == 16 ? 1024 : 512, 0, s, a, team_log2(a.d, CH), part)
+         bwd_threads(WAVES), 0, s, a, team_log2(a.d, CH), part)
   if (sh.waves == 16) {
     if (sh.chunks == 2) LUFFY_NORM_B(2, 16); else LUFFY_NORM_B(4, 16);
   } else if (sh.chunks == 1) {
     if (sh.waves == 1) LUFFY_NORM_B(1, 1);
     else if (sh.waves == 2) LUFFY_NORM_B(1, 2);
+    else if (sh.waves == 3) LUFFY_NORM_B(1, 3);
     else if (sh.waves == 4) LUFFY_NORM_B(1, 4);
+    else if (sh.waves == 5) LUFFY_NORM_B(1, 5);
+    else if (sh.waves == 6) LUFFY_NORM_B(1, 6);
+    else if (sh.waves == 7) LUFFY_NORM_B(1, 7);
     else LUFFY_NORM_B(1, 8);
   } else if (sh.waves == 8) {
     LUFFY_NORM_B(2, 8);
   } else if constexpr (BF16) {
-    if (sh.waves == 1) LUFFY_NORM_B(2, 1);
+    if (sh.waves == 4) LUFFY_NORM_B(2, 4);
     else if (sh.waves == 2) LUFFY_NORM_B(2, 2);
-    else LUFFY_NORM_B(2, 4);
+    else if constexpr (!BIAS) LUFFY_NORM_B(2, 1);
   }
 #undef LUFFY_NORM_B
   bool any = false;
@@ -697,7 +719,10 @@ extern "C" int luffy_block_norm(const void* x, const void* y, int T, int d, int 
 extern "C" size_t luffy_block_norm_backward_workspace_size(int T, int d) {
   if (T <= 0 || d <= 0) return 0;
   Carver c(nullptr);
-  c.take<float>(static_cast<size_t>(std::max(bwd_shape(T, d, true).blocks, bwd_shape(T, d, false).blocks)) * kSums * d);
+  int blocks = 0;   // of any type and any gradients
+  for (const bool bf16 : {false, true})
+    for (const bool bias : {false, true}) blocks = std::max(blocks, bwd_shape(T, d, bf16, bias).blocks);
+  c.take<float>(static_cast<size_t>(blocks) * kSums * d);
   return c.size();
 }
 

@@ -171,6 +171,24 @@ def test_many_rows(T, d):
     c.check_backward(c.backward())
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [1536, 1600, 2560, 2624, 3008, 3136, 3584, 3648, 4608, 5120, 5184, 6144, 6208, 7232])
+@pytest.mark.parametrize("norm", ["rms", "layer"])
+def test_teams_of_any_number_of_waves(norm, d, dtype):
+    """Rows on three, five, six and seven waves, of all lanes or not, more of them than
+    a block has teams."""
+    c = Case(d, dtype, 7, d, norm, True, "channel", True, norm == "layer")
+    c.check_forward(*c.forward())
+    c.check_backward(c.backward())
+
+
+@pytest.mark.parametrize("T,d", [(1600, 1152), (1100, 2176), (1050, 2880)])
+def test_more_rows_than_teams_of_odd_waves(T, d):
+    c = Case(12, "bf16", T, d, "layer", True, "token", True, True)
+    c.check_forward(*c.forward())
+    c.check_backward(c.backward())
+
+
 def test_u_is_that_of_the_stored_stream():
     """u of a call with y and u of a call that is given o alone: the same bits."""
     import paper_2411_15419_amd as L
@@ -242,10 +260,13 @@ def test_runs_repeat_bit_for_bit():
 
 
 @pytest.mark.parametrize("T,d,norm,gate", [(8200, 2112, "layer", "channel"), (16401, 1088, "rms", "token"),
-                                           (32771, 576, "layer", "token"), (4099, 4096, "rms", "channel")])
+                                           (32771, 576, "layer", "token"), (4099, 4096, "rms", "channel"),
+                                           (32775, 896, "rms", "token"), (32775, 896, "layer", "channel"),
+                                           (16389, 1856, "layer", "token"), (8203, 3904, "layer", "channel"),
+                                           (8203, 3904, "rms", "token"), (16399, 2048, "rms", "channel")])
 def test_backward_of_many_rows(T, d, norm, gate):
-    """bf16 rows in such numbers that the blocks hold two chunks a lane; against the
-    same formulas in float64 by autograd."""
+    """bf16 rows in such numbers that the blocks hold two chunks a lane, where those fill
+    the lanes; against the same formulas in float64 by autograd."""
     import torch
     import paper_2411_15419_amd as L
     gen = torch.Generator(device="cuda").manual_seed(T)
