@@ -166,9 +166,10 @@ def _p(t: Optional[torch.Tensor]):
 
 def _stream(stream) -> Optional[int]:
     # the current stream's handle without a Stream object: 0.3 us instead of
-    # 2.7, of about 7 for a whole call
+    # 2.7, of about 7 for a whole call (the tensors' checks came before: the
+    # device is initialised)
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return stream.cuda_stream
 
 
@@ -473,7 +474,7 @@ def _device_ptrs(what, *tensors):
                 if at < 0:
                     raise LuffyError(f"{what}: tensor must be on the GPU")
                 if device is None:
-                    device = torch.cuda.current_device()
+                    device = torch._C._cuda_getDevice()
                 if at != device:
                     raise LuffyError(f"{what}: tensor on device {at}, the current one is {device}")
             if not t.is_contiguous():
@@ -507,11 +508,12 @@ def luffy_block_norm(x, y, o, u, *, norm="rms", eps=1e-6, res_scale=1.0, w_post=
     shape, dtype, f32 = x.shape, x.dtype, torch.float32
     T, d = shape
     for name, t in (("y", y), ("o", o), ("u", u)):
-        if t is not None:
+        if t is not None and (t.shape != shape or t.dtype != dtype):
             _fits(what, name, t, shape, dtype)
+    columns = (d,)
     for name, t in (("w_post", w_post), ("b_post", b_post), ("w_pre", w_pre), ("b_pre", b_pre)):
-        if t is not None:
-            _fits(what, name, t, (d,), f32)
+        if t is not None and (t.shape != columns or t.dtype != f32):
+            _fits(what, name, t, columns, f32)
     kind = _block_gate(what, gate, T, d, dtype)
     dt = _dtype_code(x)
     x, y, w_post, b_post, gate, w_pre, b_pre, o, u = _device_ptrs(what, x, y, w_post, b_post, gate, w_pre, b_pre, o, u)

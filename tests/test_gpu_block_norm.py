@@ -189,6 +189,25 @@ def test_more_rows_than_teams_of_odd_waves(T, d):
     c.check_backward(c.backward())
 
 
+def test_more_rows_than_a_grid_has_blocks():
+    """Past 2^20 rows a block takes several: rows at both ends and at the seam have the
+    bits of a call of their own."""
+    import torch
+    import paper_2411_15419_amd as L
+    T, d = (1 << 20) + 7, 576
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    x, y = (torch.randn(T, d, generator=gen, device="cuda").bfloat16() for _ in range(2))
+    w = 1 + 0.1 * torch.randn(d, generator=gen, device="cuda")
+    o, u = torch.full_like(x, float("nan")), torch.full_like(x, float("nan"))
+    kw = dict(norm="layer", res_scale=0.5, w_post=w, w_pre=w, gate=w)
+    L.luffy_block_norm(x, y, o, u, **kw)
+    some = [0, 1, 12345, (1 << 20) - 1, 1 << 20, (1 << 20) + 1, T - 1]
+    o2, u2 = torch.empty(len(some), d, dtype=x.dtype, device="cuda"), torch.empty(len(some), d, dtype=x.dtype, device="cuda")
+    L.luffy_block_norm(x[some], y[some], o2, u2, **kw)
+    assert torch.equal(o[some], o2) and torch.equal(u[some], u2)
+    assert not bool(torch.isnan(u).any())
+
+
 def test_u_is_that_of_the_stored_stream():
     """u of a call with y and u of a call that is given o alone: the same bits."""
     import paper_2411_15419_amd as L
