@@ -1122,13 +1122,14 @@ __device__ __forceinline__ float dl_value(const uint16_t* p, int E) {
   return (bf16_to_f32(p[0]) + bf16_to_f32(p[E])) + bf16_to_f32(p[2 * E]);
 }
 
-// dx of a token a wave: its experts' rows of W by dl (from L2), and the representatives'
-// rows of dx_rep that are this token's, added in float32 and rounded once.  Bounded by
-// the gathered rows: 65536 x 1024 bf16, k 8, 196 us for 765 MB, 3.9 TB/s (a large copy
-// 4.9).  Sixteen loads in flight, held in arrays, took 151 registers and 369 us.
+// dx of a token (or of some of its columns) a wave: its experts' rows of W by dl (from
+// L2), and the representatives' rows of dx_rep that are this token's, added in float32
+// and rounded once.  Bounded by the gathered rows: 65536 x 1024 bf16, k 8, 196 us for 765
+// MB, 3.9 TB/s (a large copy 4.9).  Sixteen loads in flight, held in arrays, took 151
+// registers and 369 us.
 template <bool BF16>
 __global__ __launch_bounds__(256) void scored_dx_kernel(const void* __restrict__ wv, const uint16_t* __restrict__ dl,
-                                                        int ld, int T, int d, int E, int k,
+                                                        int ld, int T, int d, int E, int k, int slices,
                                                         const void* __restrict__ dx_rep,
                                                         const int32_t* __restrict__ slot_pos,
                                                         const int32_t* __restrict__ rep_of_pos,
@@ -1145,8 +1146,10 @@ __global__ __launch_bounds__(256) void scored_dx_kernel(const void* __restrict__
       else f[u] = v.f[u];
     }
   };
-  for (long long t = static_cast<long long>(blockIdx.x) * 4 + (threadIdx.x >> 6); t < T;
-       t += static_cast<long long>(gridDim.x) * 4) {
+  for (long long i = static_cast<long long>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+       i < static_cast<long long>(T) * slices; i += static_cast<long long>(gridDim.x) * 4) {
+    const long long t = slices == 1 ? i : i / slices;
+    const int slice = static_cast<int>(i - t * slices);
     const float g = lane < E ? dl_value(dl + t * ld + lane, E) : 0.f;
     const uint64_t used = __ballot(g != 0.f);
     int row = -1;
@@ -1155,7 +1158,7 @@ __global__ __launch_bounds__(256) void scored_dx_kernel(const void* __restrict__
       if (p >= 0 && rep_of_pos[p] == p) row = rep_row[p];
     }
     // (the lanes past d go along with the last columns)
-    for (int c = lane * VL; c < (d + 64 * VL - 1) / (64 * VL) * (64 * VL); c += 64 * VL) {
+    for (int c = (64 * slice + lane) * VL; c < (d + 64 * VL - 1) / (64 * VL) * (64 * VL); c += 64 * VL * slices) {
       const int cc = min(c, d - VL);
       float acc[VL], f[VL];
 #pragma unroll
@@ -1302,11 +1305,13 @@ struct ScoredBwdPlan {
 ScoredBwdPlan scored_bwd_plan(int T, int d, int E, bool bf16) {
   ScoredBwdPlan p;
   p.ld = (3 * E + 63) / 64 * 64;
-  // bf16: 256 x 256 tiles, about one a CU, of at least 256 tokens, and a part's rows
-  // within a buffer resource; float32: about a thousand blocks
+  // bf16: 256 x 256 tiles, about one a CU, of at least 128 tokens (product + sums in us
+  // with 64, 128, 256: 761 x 3008, 32 experts 18.9, 18.2, 19.7; 4096 x 1024, 64 experts
+  // 25.9, 23.4, 22.7; 2048 x 4096, 16 experts 19.0, 19.5, 21.2), and a part's rows within
+  // a buffer resource; float32: about a thousand blocks
   const int tiles = (d + 255) / 256;
   const int most = bf16 ? std::min(kMaxDwParts, std::max(1, 256 / tiles)) : std::max(1, 1024 / std::max(1, d / kDwCols));
-  const int least = bf16 ? 256 : kDwTok;
+  const int least = bf16 ? 128 : kDwTok;
   p.parts = std::max(1, std::min((T + least - 1) / least, most));
   if (bf16) {
     const long long fit = 0xFFFF0000ll / 2 / std::max(d, p.ld) - 2 * kDwTok;   // tokens
@@ -1495,9 +1500,15 @@ extern "C" int luffy_route_scored_backward(const void* x, int T, int d, int dtyp
   launch("scored_dlogits", E % 4 == 0 ? scored_dlogits_kernel<true> : scored_dlogits_kernel<false>, p.b_parts,
          kDlThreads, 0, s, logits, topk_idx, dgate, dlogits, T, a, p.ld, ws.dl, p.parts, p.per, ws.part_rows,
          ws.part_b);
-  const int waves = std::max(1, std::min((T + 3) / 4, 16 * persistent_grid()));
-  launch("scored_dx", bf16 ? scored_dx_kernel<true> : scored_dx_kernel<false>, waves, 256, 0, s, w_gate, ws.dl, p.ld, T,
-         d, E, k, dx_rep, slot_pos, rep_of_pos, rep_row, dx);
+  // a row is shared by waves where there are fewer tokens than the chip holds waves (us,
+  // with a wave a row | shared: 761 x 3008, 32 experts, k 8 32 | 11; float32 405 x 2176 19
+  // | 7; 1498 x 1216 12 | 8; twice as many waves are no faster)
+  const int cols = 64 * 16 / elem_bytes(dtype), cus = persistent_grid();
+  const int slices = std::max(1, std::min((d + cols - 1) / cols, 32 * cus / T));
+  const long long items = static_cast<long long>(T) * slices;
+  const int blocks = static_cast<int>(std::min<long long>((items + 3) / 4, 16 * cus));
+  launch("scored_dx", bf16 ? scored_dx_kernel<true> : scored_dx_kernel<false>, blocks, 256, 0, s, w_gate, ws.dl, p.ld,
+         T, d, E, k, slices, dx_rep, slot_pos, rep_of_pos, rep_row, dx);
   if (bf16)
     row_product_enqueue("scored_dw", ws.dl, static_cast<const uint16_t*>(x), ws.part_rows, p.parts, p.ld, d, ws.part_w,
                         s);
