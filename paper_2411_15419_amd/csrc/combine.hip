@@ -224,31 +224,68 @@ __global__ __launch_bounds__(256) void cbwd_group_kernel(const int32_t* __restri
   }
 }
 
-// start[r] = sum of cnt[r'] for r' < r over the R rows in use; one block of
-// 1024 threads, each scanning a contiguous run of rows.
-__global__ __launch_bounds__(1024) void cbwd_scan_kernel(const int32_t* __restrict__ rep_offsets, int E,
-                                                         int max_rows, const int* __restrict__ cnt,
-                                                         int* __restrict__ start) {
-  __shared__ int part[1024];
-  const int R = min(rep_offsets[E], max_rows);
-  const int per = (R + 1023) / 1024;
-  const int b = threadIdx.x * per, e = min(b + per, R);
-  int sum = 0;
-  for (int i = b; i < e; ++i) sum += cnt[i];
-  part[threadIdx.x] = sum;
+// start[r] = sum of cnt[r'] for r' < r over the R rows in use, start[R] their sum.  A
+// block scans kScanRows rows, four a thread, on top of the blocks before it, whose sums
+// (more than one block: from cbwd_sums_kernel) it adds up itself.  524288 rows: the
+// grouping's five launches take 21 us, 868 with one block and a run of rows a thread.
+constexpr int kScanRows = 4096;
+
+__device__ __forceinline__ int4 load_counts(const int* __restrict__ cnt, int i, int R) {
+  if (i + 3 < R) return *reinterpret_cast<const int4*>(cnt + i);
+  return make_int4(i < R ? cnt[i] : 0, i + 1 < R ? cnt[i + 1] : 0, i + 2 < R ? cnt[i + 2] : 0, 0);
+}
+// The sum of the block's values, in every thread.
+__device__ __forceinline__ int block_sum(int v, int (&part)[16]) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
   __syncthreads();
-  for (int o = 1; o < 1024; o <<= 1) {
-    const int v = threadIdx.x >= o ? part[threadIdx.x - o] : 0;
-    __syncthreads();
-    part[threadIdx.x] += v;
-    __syncthreads();
+  int s = 0;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) s += part[w];
+  __syncthreads();
+  return s;
+}
+
+__global__ __launch_bounds__(1024) void cbwd_sums_kernel(const int32_t* __restrict__ rep_offsets, int E, int max_rows,
+                                                         const int* __restrict__ cnt, int* __restrict__ sums) {
+  __shared__ int part[16];
+  const int4 c = load_counts(cnt, blockIdx.x * kScanRows + 4 * threadIdx.x, min(rep_offsets[E], max_rows));
+  const int s = block_sum(c.x + c.y + c.z + c.w, part);
+  if (threadIdx.x == 0) sums[blockIdx.x] = s;
+}
+
+__global__ __launch_bounds__(1024) void cbwd_scan_kernel(const int32_t* __restrict__ rep_offsets, int E, int max_rows,
+                                                         const int* __restrict__ cnt, const int* __restrict__ sums,
+                                                         int* __restrict__ start) {
+  __shared__ int part[16];
+  const int R = min(rep_offsets[E], max_rows), b = blockIdx.x;
+  if (b > 0 && b * kScanRows >= R) return;
+  int before = 0;
+  for (int i = threadIdx.x; i < b; i += 1024) before += sums[i];
+  before = block_sum(before, part);
+  const int i = b * kScanRows + 4 * threadIdx.x, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int4 c = load_counts(cnt, i, R);
+  const int own = c.x + c.y + c.z + c.w;
+  int incl = own;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int u = __shfl_up(incl, o, 64);
+    if (lane >= o) incl += u;
   }
-  int run = part[threadIdx.x] - sum;   // exclusive prefix of this thread's run
-  for (int i = b; i < e; ++i) {
-    start[i] = run;
-    run += cnt[i];
+  if (lane == 63) part[w] = incl;
+  __syncthreads();
+  int run = before + incl - own, all = before;
+#pragma unroll
+  for (int v = 0; v < 16; ++v) {
+    if (v < w) run += part[v];
+    all += part[v];
   }
-  if (threadIdx.x == 1023) start[R] = part[1023];
+  const int s[4] = {run, run + c.x, run + c.x + c.y, run + c.x + c.y + c.z};
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (i + j < R) start[i + j] = s[j];
+  if (threadIdx.x == 0 && R <= (b + 1) * kScanRows) start[R] = all;
 }
 
 // One wave per (representative r, 512-column chunk): lane l holds columns
@@ -461,7 +498,7 @@ extern "C" int luffy_combine_many(const void* y_rep, const int32_t* rep_row, con
 }
 
 struct CbwdWs {
-  int *cnt, *start, *cursor, *list;
+  int *cnt, *start, *cursor, *list, *sums;
 };
 
 CbwdWs carve_cbwd(Carver& c, int max_rows, long long slots) {
@@ -470,6 +507,7 @@ CbwdWs carve_cbwd(Carver& c, int max_rows, long long slots) {
   w.start = c.take<int>(static_cast<size_t>(max_rows) + 1);
   w.cursor = c.take<int>(static_cast<size_t>(max_rows));
   w.list = c.take<int>(static_cast<size_t>(slots));
+  w.sums = c.take<int>(static_cast<size_t>((max_rows - 1) / kScanRows + 1));
   return w;
 }
 
@@ -510,8 +548,12 @@ int combine_backward_run(const char* fn, int most_k, const void* dy, const void*
   launch("cbwd_group", cbwd_clear_kernel, rblocks, 256, 0, s, rep_offsets, E, max_rows, ws.cnt, ws.cursor);
   launch("cbwd_group", cbwd_group_kernel<false>, sblocks, 256, 0, s, rep_row, offsets, E, max_rows, ws.cnt,
          static_cast<const int*>(ws.start), ws.cursor, ws.list);
-  launch("cbwd_group", cbwd_scan_kernel, 1, 1024, 0, s, rep_offsets, E, max_rows, static_cast<const int*>(ws.cnt),
-         ws.start);
+  const int scans = (max_rows - 1) / kScanRows + 1;
+  if (scans > 1)
+    launch("cbwd_group", cbwd_sums_kernel, scans, 1024, 0, s, rep_offsets, E, max_rows, static_cast<const int*>(ws.cnt),
+           ws.sums);
+  launch("cbwd_group", cbwd_scan_kernel, scans, 1024, 0, s, rep_offsets, E, max_rows, static_cast<const int*>(ws.cnt),
+         static_cast<const int*>(ws.sums), ws.start);
   launch("cbwd_group", cbwd_group_kernel<true>, sblocks, 256, 0, s, rep_row, offsets, E, max_rows, ws.cnt,
          static_cast<const int*>(ws.start), ws.cursor, ws.list);
   const long long row_waves = static_cast<long long>(max_rows) * ((d + 511) / 512);

@@ -274,3 +274,39 @@ def test_condense_with_many_choices(dtype):
     assert 0 < R < S
     assert np.array_equal(row[:S].cpu().numpy(), np.asarray(ref.rep_row)[:S])
     assert np.array_equal(tok[:R].cpu().numpy(), np.asarray(ref.rep_token)[:R])
+
+
+@pytest.mark.parametrize("T,k,R,rows", [(1, 1, 1, 20000), (2048, 3, 4095, 4095), (2048, 3, 4096, 4096), (3000, 4, 4097, 9000),
+                                        (5000, 5, 8192, 8192), (5000, 8, 20001, 40000), (3, 2, 0, 5000)])
+def test_combine_many_backward_of_many_representatives(T, k, R, rows):
+    """More representatives than a block counts, numbers around its edges, and room for
+    more rows than there are slots."""
+    import torch
+    import paper_2411_15419_amd as L
+    gen = torch.Generator(device="cuda").manual_seed(R)
+    S, d = T * k if R else 0, 64
+    i32 = dict(dtype=torch.int32, device="cuda")
+    slot_pos = torch.randperm(T * k, generator=gen, device="cuda").to(torch.int32).view(T, k) if R else torch.full((T, k), -1, **i32)
+    tok = torch.zeros(T * k, **i32)
+    if R:
+        tok[slot_pos.flatten().long()] = torch.arange(T, **i32).repeat_interleave(k)
+    rep_row = torch.cat([torch.arange(R, **i32), torch.randint(0, max(R, 1), (T * k - R,), generator=gen, **i32)])
+    off, ro = torch.tensor([0, S], **i32), torch.tensor([0, R], **i32)
+    dy, gate = torch.randn(T, d, generator=gen, device="cuda"), torch.rand(T, k, generator=gen, device="cuda")
+    y_rep = torch.randn(rows, d, generator=gen, device="cuda")
+    dy_rep, dgate = torch.full_like(y_rep, -9.0), torch.empty_like(gate)
+    ws = torch.empty(L.combine_backward_workspace_size(T, k, rows), dtype=torch.uint8, device="cuda")
+    for _ in range(2):
+        L.luffy_combine_many_backward(dy, y_rep, rep_row, tok, slot_pos, gate, off, ro, dy_rep, dgate, ws)
+    assert bool((dy_rep[R:] == -9.0).all())
+    if not R:
+        assert not bool(dgate.any())
+        return
+    at = rep_row[slot_pos.long()].long()
+    terms = gate.double()[..., None] * dy.double()[:, None]
+    want = torch.zeros(R, d, dtype=torch.float64, device="cuda").index_add_(0, at.flatten(), terms.view(-1, d))
+    size = torch.zeros_like(want).index_add_(0, at.flatten(), terms.abs().view(-1, d))
+    most = int(torch.bincount(at.flatten()).max())
+    assert bool(((dy_rep[:R].double() - want).abs() <= (most + 1) * 2.0 ** -24 * size).all())
+    dots = dy.double()[:, None] * y_rep.double()[at]
+    assert bool(((dgate.double() - dots.sum(2)).abs() <= d * 2.0 ** -24 * dots.abs().sum(2)).all())
