@@ -194,7 +194,7 @@ __global__ __launch_bounds__(256) void combine_sliced_kernel(const void* __restr
 // Row sums through a member list: the kept positions are grouped by
 // representative (counts, an exclusive scan, then a fill with one cursor
 // per representative; the order inside a group is not fixed), and one wave
-// per (representative, 512-column chunk) adds gate * dy[t] of its members
+// per (representative, 512 or 1024 columns) adds gate * dy[t] of its members
 // in registers, four members' rows in flight at a time, and stores the row.
 
 // counts[r] = cursor[r] = 0 for the R rows in use.
@@ -288,10 +288,14 @@ __global__ __launch_bounds__(1024) void cbwd_scan_kernel(const int32_t* __restri
   if (threadIdx.x == 0 && R <= (b + 1) * kScanRows) start[R] = all;
 }
 
-// One wave per (representative r, 512-column chunk): lane l holds columns
-// c0 + 8l .. c0 + 8l + 7 (bf16: one 16-byte load per member row; float32:
-// two).
-template <bool BF16, int K>
+// One wave per (representative r, 512 U columns): lane l holds columns c0 + 8l .. c0 +
+// 8l + 7 of each 512 (bf16: one 16-byte load per member row; float32: two).  Four members
+// at a time; lane 16 u + i looks whether the u-th one is its token's slot i, and has that
+// slot's gate.  The chain (member, token, slots) is a group's latency, so that groups of
+// one are bound by it: 65536 tokens of 1024 bf16 with 8 slots each, no two alike, 481 us
+// for 2.1 GB; 660 with the slots looked up one after the other, 512 columns a wave and the
+// last member's row read four times.
+template <bool BF16, int K, int U>
 __global__ __launch_bounds__(256) void cbwd_rows_kernel(const void* __restrict__ dy,
                                                         const int32_t* __restrict__ perm_token,
                                                         const int32_t* __restrict__ slot_pos,
@@ -299,71 +303,87 @@ __global__ __launch_bounds__(256) void cbwd_rows_kernel(const void* __restrict__
                                                         const int32_t* __restrict__ rep_offsets, int E, int d,
                                                         int max_rows, const int* __restrict__ start,
                                                         const int* __restrict__ list, void* __restrict__ dy_rep) {
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63, who = lane >> 4, slot = lane & 15;
   const int R = min(rep_offsets[E], max_rows);
-  const int nc = (d + 511) / 512;
+  const int nc = (d + 512 * U - 1) / (512 * U);
   const long long items = static_cast<long long>(R) * nc;
   for (long long it = (static_cast<long long>(blockIdx.x) * 256 + threadIdx.x) >> 6; it < items;
        it += static_cast<long long>(gridDim.x) * 4) {
     const int r = static_cast<int>(it / nc);
-    const int c = static_cast<int>(it - static_cast<long long>(r) * nc) * 512 + lane * 8;
-    const bool col = c < d;
-    const int m0 = start[r], m1 = start[r + 1];
-    float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const int c0 = static_cast<int>(it - static_cast<long long>(r) * nc) * (512 * U) + lane * 8;
+    const int m0 = __builtin_amdgcn_readfirstlane(start[r]), m1 = __builtin_amdgcn_readfirstlane(start[r + 1]);
+    float acc[U][8];
+#pragma unroll
+    for (int v = 0; v < U; ++v)
+#pragma unroll
+      for (int h = 0; h < 8; ++h) acc[v][h] = 0.f;
     for (int m = m0; m < m1; m += 4) {
-      int t[4];
-      float g[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int mm = min(m + u, m1 - 1);
-        const int p = list[mm];
-        t[u] = perm_token[p];
-        int j = 0;   // the token's slot at position p
-        if constexpr (K == 2) {
-          j = slot_pos[static_cast<size_t>(t[u]) * K] != p ? 1 : 0;
-        } else {
-#pragma unroll
-          for (int i = 1; i < K; ++i) j = slot_pos[static_cast<size_t>(t[u]) * K + i] == p ? i : j;
-        }
-        g[u] = m + u < m1 ? gate[static_cast<size_t>(t[u]) * K + j] : 0.f;
+      const int p = list[min(m + who, m1 - 1)], tok = perm_token[p];
+      int at = 0;
+      float gt = 0.f;
+      if (slot < K) {
+        at = K > 1 ? slot_pos[static_cast<size_t>(tok) * K + slot] : p;
+        gt = gate[static_cast<size_t>(tok) * K + slot];
       }
-      if (col) {
+      const uint64_t hits = __ballot(slot < K && at == p);
+      struct Row {
+        Pack16 q[U][BF16 ? 1 : 2];
+      };
+      int tu[4];
+      float g[4];
+      auto load = [&](int u, Row& row) {
+        tu[u] = __builtin_amdgcn_readlane(tok, 16 * u);
+        const uint32_t of = static_cast<uint32_t>(hits >> (16 * u)) & 0xFFFFu;
+        g[u] = __uint_as_float(
+            __builtin_amdgcn_readlane(__float_as_uint(gt), 16 * u + (of ? __builtin_ctz(of) : 0)));
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int v = 0; v < U; ++v) {
+          const size_t c = static_cast<size_t>(tu[u]) * d + min(c0 + 512 * v, d - 8);
           if constexpr (BF16) {
-            const uint4 q = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(dy) +
-                                                            static_cast<size_t>(t[u]) * d + c);
-            const uint32_t wv[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-            for (int h = 0; h < 4; ++h) {
-              acc[2 * h] = fmaf(g[u], __uint_as_float(wv[h] << 16), acc[2 * h]);
-              acc[2 * h + 1] = fmaf(g[u], __uint_as_float(wv[h] & 0xFFFF0000u), acc[2 * h + 1]);
-            }
+            row.q[v][0].u4 = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(dy) + c);
           } else {
-            const float4* src = reinterpret_cast<const float4*>(static_cast<const float*>(dy) +
-                                                                static_cast<size_t>(t[u]) * d + c);
-            const float4 a = src[0], b = src[1];
-            acc[0] = fmaf(g[u], a.x, acc[0]);
-            acc[1] = fmaf(g[u], a.y, acc[1]);
-            acc[2] = fmaf(g[u], a.z, acc[2]);
-            acc[3] = fmaf(g[u], a.w, acc[3]);
-            acc[4] = fmaf(g[u], b.x, acc[4]);
-            acc[5] = fmaf(g[u], b.y, acc[5]);
-            acc[6] = fmaf(g[u], b.z, acc[6]);
-            acc[7] = fmaf(g[u], b.w, acc[7]);
+            row.q[v][0].u4 = *reinterpret_cast<const uint4*>(static_cast<const float*>(dy) + c);
+            row.q[v][1].u4 = *reinterpret_cast<const uint4*>(static_cast<const float*>(dy) + c + 4);
           }
         }
+      };
+      auto add = [&](int u, const Row& row) {
+#pragma unroll
+        for (int v = 0; v < U; ++v)
+#pragma unroll
+          for (int h = 0; h < 8; ++h) {
+            if constexpr (BF16) acc[v][h] = fmaf(g[u], bf16_to_f32(row.q[v][0].h[h]), acc[v][h]);
+            else acc[v][h] = fmaf(g[u], row.q[v][h / 4].f[h % 4], acc[v][h]);
+          }
+      };
+      Row row[4];
+      if (m + 4 <= m1) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) load(u, row[u]);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) add(u, row[u]);
+      } else {
+#pragma unroll
+        for (int u = 0; u < 3; ++u)
+          if (m + u < m1) load(u, row[u]);
+#pragma unroll
+        for (int u = 0; u < 3; ++u)
+          if (m + u < m1) add(u, row[u]);
       }
     }
-    if (col) {
+#pragma unroll
+    for (int v = 0; v < U; ++v) {
+      const int c = c0 + 512 * v;
+      if (c >= d) continue;
+      const float* f = acc[v];
       if constexpr (BF16) {
         *reinterpret_cast<uint4*>(static_cast<uint16_t*>(dy_rep) + static_cast<size_t>(r) * d + c) =
-            make_uint4(pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3]), pack_bf16x2(acc[4], acc[5]),
-                       pack_bf16x2(acc[6], acc[7]));
+            make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]),
+                       pack_bf16x2(f[6], f[7]));
       } else {
         float4* dst = reinterpret_cast<float4*>(static_cast<float*>(dy_rep) + static_cast<size_t>(r) * d + c);
-        dst[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
-        dst[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
+        dst[0] = make_float4(f[0], f[1], f[2], f[3]);
+        dst[1] = make_float4(f[4], f[5], f[6], f[7]);
       }
     }
   }
@@ -556,14 +576,15 @@ int combine_backward_run(const char* fn, int most_k, const void* dy, const void*
          static_cast<const int*>(ws.sums), ws.start);
   launch("cbwd_group", cbwd_group_kernel<true>, sblocks, 256, 0, s, rep_row, offsets, E, max_rows, ws.cnt,
          static_cast<const int*>(ws.start), ws.cursor, ws.list);
-  const long long row_waves = static_cast<long long>(max_rows) * ((d + 511) / 512);
+  const int row_cols = d > 512 ? 1024 : 512;
+  const long long row_waves = static_cast<long long>(max_rows) * ((d + row_cols - 1) / row_cols);
   const int row_blocks = static_cast<int>(std::max(1ll, std::min((row_waves + 3) / 4, 8192ll)));
   const int blocks = (T + 3) / 4;
 #define LUFFY_CBWD(BF, K_)                                                                                     \
   do {                                                                                                         \
-    launch("cbwd_rows", cbwd_rows_kernel<BF, K_>, row_blocks, 256, 0, s, dy, perm_token, slot_pos, topk_gate,  \
-           rep_offsets, E, d, max_rows, static_cast<const int*>(ws.start), static_cast<const int*>(ws.list),   \
-           dy_rep);                                                                                            \
+    launch("cbwd_rows", d > 512 ? cbwd_rows_kernel<BF, K_, 2> : cbwd_rows_kernel<BF, K_, 1>, row_blocks, 256,  \
+           0, s, dy, perm_token, slot_pos, topk_gate, rep_offsets, E, d, max_rows,                             \
+           static_cast<const int*>(ws.start), static_cast<const int*>(ws.list), dy_rep);                       \
     launch("cbwd_gate", cbwd_gate_kernel<BF, K_>, blocks, 256, 0, s, dy, y_rep, rep_row, slot_pos, max_rows,   \
            T, d, dgate);                                                                                       \
   } while (0)
