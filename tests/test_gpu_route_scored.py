@@ -226,6 +226,34 @@ def test_numbers_that_are_none():
     assert not bool((idx == 3).any())
 
 
+@pytest.mark.parametrize("T,d,E", [(33000, 128, 64), (9000, 192, 24), (66000, 64, 12)])
+def test_numbers_that_are_none_among_many(T, d, E):
+    """The same in the larger calls' kernels, and an expert whose weights are none: it is
+    chosen by no token, the other choices are those of a call without it."""
+    import torch
+    r = Router(34, "bf16", T, d, E, 4, "sigmoid", True, 4, 2, 2)
+    clean = r.run()
+    bad = [0, 17, T // 2, T - 1]
+    r.x[bad[0], 7], r.x[bad[1], 0], r.x[bad[2]], r.x[bad[3], d - 1] = (float("nan"), float("inf"), float("-inf"),
+                                                                        float("nan"))
+    out = r.run()
+    keep = torch.ones(T, dtype=torch.bool, device="cuda")
+    keep[bad] = False
+    for name in ("topk_idx", "topk_gate", "logits"):
+        assert bool((out[name][keep] == clean[name][keep]).all())
+    chosen = out["topk_idx"][bad].long()
+    assert bool(((chosen >= 0) & (chosen < E)).all())
+    assert all(len(set(row)) == 4 for row in chosen.tolist())
+    counts = torch.bincount(out["topk_idx"].flatten().long(), minlength=E)
+    assert torch.equal(torch.diff(out["offsets"].long()), counts)
+    r = Router(35, "bf16", T, d, E, 3, "softmax", False)
+    r.w[5, 3] = float("nan")
+    idx = r.run()["topk_idx"].long()
+    l = r.x.double() @ torch.nan_to_num(r.w.double()).t() + r.b.double()
+    l[:, 5] = -torch.inf
+    assert torch.equal(idx, torch.sort(l, dim=1, descending=True, stable=True).indices[:, :3])
+
+
 def test_masked_experts():
     """balance -infinity: chosen only where nothing else is left."""
     r = Router(12, "bf16", 50, 128, 16, 4, "sigmoid", True, 4, 2, 2)
