@@ -635,7 +635,7 @@ int luffy_adaptive_threshold(double l_ini, double l_prev, double* h_out);
  * bwd_dw1; serving: mx4_quantize, mx4_dequantize, mx4_matmul, mx4_ffn1,
  * mx4_ffn2, few_gate, few_ffn1, few_ffn2; a block: block_norm,
  * block_norm_backward, block_norm_reduce, scored_gate, scored_choose,
- * scored_both, scored_dlogits, scored_dx, scored_dw, scored_dw_reduce, mx8_quantize,
+ * scored_both, slot_place, scored_dlogits, scored_dx, scored_dw, scored_dw_reduce, mx8_quantize,
  * mx8_dequantize.
  * ---------------------------------------------------------------------- */
 int luffy_profile_kernel(const char* name);

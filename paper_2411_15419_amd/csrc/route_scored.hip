@@ -9,7 +9,8 @@
 //                  decided in float64 from exact products; ranks every slot among its
 //                  chunk's slots of the same expert and leaves the chunks' counts
 //                  (one chunk of tokens: the buckets too)
-//   slot_scan, slot_scatter  (route.hip) bucket offsets and positions
+//   slot_place     bucket offsets and positions; slot_scan, slot_scatter (route.hip) where
+//                  the counts do not fit LDS
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -973,6 +974,82 @@ __global__ __launch_bounds__(256) void scored_both_kernel(const void* xv, const 
                                   perm_token, offsets);
 }
 
+// Bucket offsets, positions and tokens in one launch where the chunks' counts (layout:
+// RouteWs) fit LDS: every block scans them all by itself, a wave an expert, and takes
+// 1024 slots.  Bounded by the chain of trips to memory and the scan (us of a whole call in
+// a graph, against slot_scan and slot_scatter: 40 x 1024, 16 experts 10.4 | 14.1, 300 x
+// 1024, 64 experts 22.2 | 23.6, 3001 x 512 float32, 8 experts 18.4 | 20.5, 4090 x 1024, 16
+// experts, at the limit, 20.5 | 20.4); from the host a launch less is 2.5 more.
+constexpr int kPlaceCounts = 16384;
+
+__global__ __launch_bounds__(1024) void slot_place_kernel(const int32_t* __restrict__ topk_idx,
+                                                          const int32_t* __restrict__ hist, int T, int k, int E, int C,
+                                                          int tok, int32_t* __restrict__ slot_pos,
+                                                          int32_t* __restrict__ perm_token,
+                                                          int32_t* __restrict__ offsets) {
+  __shared__ int cnt[kPlaceCounts];
+  __shared__ int totals[kMaxExperts], first[kMaxExperts];
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const int nblk = (T + tok - 1) / tok, nch = k * nblk, n = E * nch;
+  const int s = blockIdx.x * 1024 + tid;   // (E k T / tok counts: a grid of few blocks)
+  const bool valid = s < T * k;
+  const int j = valid ? s / T : 0, t = valid ? s - j * T : 0;
+  const size_t o = static_cast<size_t>(t) * k + j;
+  const int e = topk_idx[o], rank = slot_pos[o];
+#pragma unroll 4
+  for (int i = tid; i < n; i += 1024) cnt[i] = hist[i];
+  __syncthreads();
+  for (int x = w; x < E; x += 16) {
+    int* c = cnt + x * nch;
+    int carry = 0;
+    for (int c0 = 4 * lane; c0 - 4 * lane < nch; c0 += 256) {
+      int v[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) v[u] = c0 + u < nch ? c[c0 + u] : 0;
+      const int own = (v[0] + v[1]) + (v[2] + v[3]);
+      int incl = own;
+#pragma unroll
+      for (int sh = 1; sh < 64; sh <<= 1) {
+        const int u = __shfl_up(incl, sh, 64);
+        if (lane >= sh) incl += u;
+      }
+      int run = carry + incl - own;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (c0 + u < nch) c[c0 + u] = run;
+        run += v[u];
+      }
+      carry += __builtin_amdgcn_readlane(incl, 63);
+    }
+    if (lane == 0) totals[x] = carry;
+  }
+  __syncthreads();
+  if (w == 0) {
+    int own = lane < E ? totals[lane] : 0;
+    if (C > 0 && own > C) own = C;
+    int incl = own;
+#pragma unroll
+    for (int sh = 1; sh < 64; sh <<= 1) {
+      const int u = __shfl_up(incl, sh, 64);
+      if (lane >= sh) incl += u;
+    }
+    first[lane] = incl - own;
+    if (blockIdx.x == 0) {
+      if (lane < E) offsets[lane] = incl - own;
+      if (lane == E - 1) offsets[E] = incl;
+    }
+  }
+  __syncthreads();
+  if (!valid) return;
+  const int pos = cnt[e * nch + j * nblk + t / tok] + rank;
+  if (C > 0 && pos >= C) {
+    slot_pos[o] = -1;
+  } else {
+    slot_pos[o] = first[e] + pos;
+    perm_token[first[e] + pos] = t;
+  }
+}
+
 // ---------------------------------------------------------------- backward
 // dl, the logits' gradient: with r_j = s_j / sum of the chosen (shifted as in the
 // forward, so that nothing under- or overflows)
@@ -1388,6 +1465,14 @@ extern "C" int luffy_route_scored(const void* x, int T, int d, int dtype, const 
          topk_gate, inv_norm)
   const bool bf16 = dtype == LUFFY_BF16, sig = score == LUFFY_SCORE_SIGMOID, grouped = top_groups < groups;
   const int C = capacity_slots(T, k, E, capacity_factor);
+  auto buckets = [&](int tok) {
+    const long long slots = static_cast<long long>(T) * k, nblk = (T + tok - 1) / tok;
+    if (E * k * nblk <= kPlaceCounts)
+      launch("slot_place", slot_place_kernel, static_cast<int>((slots + 1023) / 1024), 1024, 0, s, topk_idx, ws.hist, T,
+             k, E, C, tok, slot_pos, perm_token, offsets);
+    else
+      route_buckets_enqueue(topk_idx, T, E, k, capacity_factor, tok, slot_pos, perm_token, offsets, ws, s);
+  };
   // One launch where every block has a CU of its own, and where it is not two chunks
   // instead of a whole call in one (us a call in a graph, one | two launches: 64 x 1024, 64
   // experts 19.1 | 20.2, 1024 x 4096 46.3 | 48.0, 4096 x 1024 30.1 | 32.0, float32 40.9 |
@@ -1406,8 +1491,7 @@ extern "C" int luffy_route_scored(const void* x, int T, int d, int dtype, const 
       if (bf16) LUFFY_BOTH(true, 4); else LUFFY_BOTH(false, 4);
     }
 #undef LUFFY_BOTH
-    if (chunks > 1)
-      route_buckets_enqueue(topk_idx, T, E, k, capacity_factor, 16, slot_pos, perm_token, offsets, ws, s);
+    if (chunks > 1) buckets(16);
     return check_launch(fn);
   }
   // Streaming from eight chunks of 16 tokens a CU on: below, staging W (8 us) and the
@@ -1453,8 +1537,7 @@ extern "C" int luffy_route_scored(const void* x, int T, int d, int dtype, const 
   else if (E <= 48) LUFFY_CHOOSE(3);
   else LUFFY_CHOOSE(4);
 #undef LUFFY_CHOOSE
-  if (blocks > 1)
-    route_buckets_enqueue(topk_idx, T, E, k, capacity_factor, tok, slot_pos, perm_token, offsets, ws, s);
+  if (blocks > 1) buckets(tok);
   return check_launch(fn);
 }
 
