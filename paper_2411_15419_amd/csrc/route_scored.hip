@@ -88,6 +88,15 @@ __device__ __forceinline__ bool uncertain(float a, float b, float rel, float abs
   return !(a - b > fmaf(rel, fabsf(a) + fabsf(b), 2.0f * abs));
 }
 
+// The norm of a row of d values, at most, from their squares' float32 sum: squares
+// below float32's normal numbers may be missing from it, 2^-126 each, so that rows of
+// about 2^-64 and less have a sum of zero.  (Products of theirs, and sums of those, lose
+// as much each: kLost d.  A row of zeros is left with bounds far below any other's.)
+constexpr float kLost = 0x1p-124f;
+__device__ __forceinline__ float norm_most(float ss, int d) {
+  return sqrtf(fmaf(static_cast<float>(d), 0x1p-126f, ss));
+}
+
 // 1 / (1 + e^-l) times e^-shift, shift <= 0: no overflow for any l.
 __device__ __forceinline__ float sigmoid_shifted(float l, float shift) {
   return __builtin_amdgcn_exp2f((fminf(l, 0.f) - shift) * kLog2e) *
@@ -253,7 +262,7 @@ __device__ __forceinline__ void choose16(const float (&l)[NEB], const float (&ba
 // fragments (the diagonals of their own Grams): with n MFMA sums in a row and their
 // few joins the error of a logit is at most (n + 16) 2^-24 |x| |w| (every rounding
 // is relative to the absolute sum of the products, which is at most |x| |w|), the
-// norms being a little off covered by a factor of 1.01.  The bound goes to
+// norms being a little off covered by a factor of 1.01 (and norm_most).  The bound goes to
 // bound[t k], a token's first gate, for scored_choose.
 //   Bounded by the loads' latency where T is small (one token of 1024, 16 experts: 4
 // us), by rows from HBM and W from L2 where it is large (65536 x 4096 bf16, 64 experts:
@@ -380,8 +389,8 @@ __device__ __forceinline__ void gate_block(const void* xv, const void* wv, int T
     }
     if (m == 0) {
       bound[static_cast<size_t>(t) * a.k] =
-          fmaf(0x1p-23f, bmost,
-               1.01f * static_cast<float>(per * (BF16 ? 1 : 4) + 16) * 0x1p-24f * sqrtf(ss) * sqrtf(wmost));
+          fmaf(0x1p-23f, bmost, kLost * static_cast<float>(d)) +
+          1.01f * static_cast<float>(per * (BF16 ? 1 : 4) + 16) * 0x1p-24f * norm_most(ss, d) * norm_most(wmost, d);
       if (inv_norm) inv_norm[t] = ss > 0.f ? 1.0f / sqrtf(ss) : 0.f;
     }
   }
@@ -465,8 +474,8 @@ __global__ __launch_bounds__(WAVES * 64) void scored_gate_stream_kernel(
   }
   // (a NaN norm marks every token: fmaxf would drop it)
   wmost = __any(wmost != wmost) ? NAN : max16f(wmost);
-  const float rel = 1.01f * static_cast<float>(8 + (nsteps + 7) / 8 + 16) * 0x1p-24f * sqrtf(wmost);
-  const float add = 0x1p-23f * max16f(bmost);
+  const float rel = 1.01f * static_cast<float>(8 + (nsteps + 7) / 8 + 16) * 0x1p-24f * norm_most(wmost, d);
+  const float add = fmaf(0x1p-23f, max16f(bmost), kLost * static_cast<float>(d));
   for (; ch < nchunks; ch += gridDim.x * waves) {
     const int t0 = ch * 16;
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
@@ -514,7 +523,7 @@ __global__ __launch_bounds__(WAVES * 64) void scored_gate_stream_kernel(
         for (int j = 0; j < NEB; ++j)
           if (16 * j + m < E) logits[static_cast<size_t>(t) * E + 16 * j + m] = tot[j][i] + bias[j];
         if (m == 0) {
-          bound[static_cast<size_t>(t) * a.k] = fmaf(rel, sqrtf(ss), add);
+          bound[static_cast<size_t>(t) * a.k] = fmaf(rel, norm_most(ss, d), add);
           if (inv_norm) inv_norm[t] = ss > 0.f ? 1.0f / sqrtf(ss) : 0.f;
         }
       }
