@@ -1047,19 +1047,27 @@ class MoEBlock(MoELayer):
     """A layer that learns, with what stands around it (bf16):
         u = N(x; w_pre, b_pre),  y = the condensed layer of u,
         o = res_scale x + gate N(y; w_post, b_post)
-    with the scored router (up to 8 experts a token), and between the forward and
-    the backward no more of the experts than their first product in microscaled 8
-    bits, and of u the same (keep8).
+    with the scored router (up to 8 experts a token).
 
     A block's last pass can be the next one's first: with `following` a call writes
     following.u beside o (one read of the stream), and following is then called
     with normed=True.  Buffers are allocated once; a block's outputs and gradients
-    are valid until its next call."""
+    are valid until its next call.
+
+    From its call to its backward a block keeps, of T tokens and S = T k slots: the
+    experts' first product in microscaled 8 bits [S, d_ff], their outputs [S, d], y
+    and o [T, d] in bf16, the logits and the choices; and u, in bf16 of its own or,
+    with keep8, in microscaled 8 bits.  What it works with besides (u in bf16, the
+    forward's and the backward's workspaces and gradients on their way) is its own
+    too, unless it `shares` another block's: of blocks of the same sizes, called one
+    after the other on one stream, all but the first then hold none of it.  Blocks
+    that share are built with keep8 (the default with shares; the first one has to
+    ask for it), as the next block's u takes the place of theirs; of no use without."""
 
     def __init__(self, w_gate, b_gate, w1, w2, *, w_pre, b_pre=None, w_post=None, b_post=None, gate=None,
                  res_scale: float = 1.0, norm: str = "rms", eps: float = 1e-6, score: str = "softmax", balance=None,
                  groups: int = 1, top_groups: int = 1, group_best: int = 1, renormalise: bool = True,
-                 scale: float = 1.0, keep8: bool = True, **layer):
+                 scale: float = 1.0, keep8: Optional[bool] = None, shares: Optional["MoEBlock"] = None, **layer):
         super().__init__(w_gate, b_gate, w1, w2, **layer)
         if self.dtype != torch.bfloat16:
             raise LuffyError("MoEBlock: the expert FFN backward is bf16 only")
@@ -1067,7 +1075,8 @@ class MoEBlock(MoELayer):
             raise LuffyError("MoEBlock: historical similarity takes k <= 2")
         self.w_pre, self.b_pre, self.w_post, self.b_post, self.gate = w_pre, b_pre, w_post, b_post, gate
         self.res_scale, self.norm, self.eps = res_scale, norm, eps
-        self.score, self.balance, self.renormalise, self.scale, self.keep8 = score, balance, renormalise, scale, keep8
+        self.score, self.balance, self.renormalise, self.scale = score, balance, renormalise, scale
+        self.keep8 = shares is not None if keep8 is None else keep8
         self.groups = dict(groups=groups, top_groups=top_groups, group_best=group_best)
         T, S, E, d, d_ff, dev = self.T, self.T * self.k, self.E, self.d, self.d_ff, w1.device
         bf = dict(dtype=torch.bfloat16, device=dev)
@@ -1076,13 +1085,29 @@ class MoEBlock(MoELayer):
             return (torch.empty(rows, cols, dtype=torch.int8, device=dev),
                     torch.empty((cols + 255) // 256, rows, 8, dtype=torch.uint8, device=dev))
 
-        self.logits = torch.empty(T, E, dtype=torch.float32, device=dev)
-        self.u, self.o = torch.empty(T, d, **bf), torch.empty(T, d, **bf)
-        self.zq, self.zs = mx8(S, d_ff)
-        if keep8:
-            self.uq, self.us = mx8(T, d)
         if self.buf.x_rep is not None:
             raise LuffyError("MoEBlock: gather_x_rep is of no use here")
+        if shares is None:
+            # what blocks can share; the backward's part comes with its first call
+            self._work = dict(u=torch.empty(T, d, **bf))
+        else:
+            if not (shares.keep8 and self.keep8):
+                raise LuffyError("MoEBlock: blocks that share keep u in 8 bits (keep8=True)")
+            if shares._sizes() != self._sizes():
+                raise LuffyError(f"MoEBlock: blocks that share are of the same sizes, not {shares._sizes()} and "
+                                 f"{self._sizes()}")
+            self._work = shares._work
+            for name in ("ws_route", "ws_condense", "ws_ffn"):
+                setattr(self.buf, name, getattr(shares.buf, name))
+        self.u, self.o = self._work["u"], torch.empty(T, d, **bf)
+        self.logits = torch.empty(T, E, dtype=torch.float32, device=dev)
+        self.zq, self.zs = mx8(S, d_ff)
+        if self.keep8:
+            self.uq, self.us = mx8(T, d)
+
+    def _sizes(self):
+        return dict(T=self.T, k=self.k, E=self.E, d=self.d, d_ff=self.d_ff, max_bucket=self.max_bucket,
+                    history=self.history is not None, device=self.w1.device)
 
     def route(self, x, stream=None):
         b = self.buf
@@ -1131,17 +1156,19 @@ class MoEBlock(MoELayer):
             return None if w is None else torch.empty(d, **f32)
 
         rows = lambda n: torch.empty(n, d, dtype=torch.bfloat16, device=dev)  # noqa: E731
+        if "du" not in self._work:
+            self._work.update(
+                dy=rows(T), du=rows(T), dy_rep=rows(S), dx_rep=rows(S), dlayer=torch.empty(T, self.k, **f32),
+                ws_n=_workspace(block_norm_backward_workspace_size(T, d), dev),
+                ws_c=_workspace(combine_backward_workspace_size(T, self.k, S), dev),
+                ws_f=_workspace(expert_ffn_backward_kept_workspace_size(S, E, d, d_ff), dev),
+                ws_r=_workspace(route_scored_backward_workspace_size(T, d, E), dev))
         self._bwd = dict(
-            dx=rows(T), dstream=rows(T), dy=rows(T), du=rows(T), dy_rep=rows(S), dx_rep=rows(S),
-            dlayer=torch.empty(T, self.k, **f32), dw_gate=torch.empty(E, d, **f32), db_gate=torch.empty(E, **f32),
+            self._work, dx=rows(T), dstream=rows(T), dw_gate=torch.empty(E, d, **f32), db_gate=torch.empty(E, **f32),
             dw1=torch.empty(E, d_ff, d, dtype=dw_dtype, device=dev),
             dw2=torch.empty(E, d, d_ff, dtype=dw_dtype, device=dev),
             dgate=None if self.gate is None else torch.empty_like(self.gate), dw_post=vec(self.w_post),
-            db_post=vec(self.b_post), dw_pre=vec(self.w_pre), db_pre=vec(self.b_pre),
-            ws_n=_workspace(block_norm_backward_workspace_size(T, d), dev),
-            ws_c=_workspace(combine_backward_workspace_size(T, self.k, S), dev),
-            ws_f=_workspace(expert_ffn_backward_kept_workspace_size(S, E, d, d_ff), dev),
-            ws_r=_workspace(route_scored_backward_workspace_size(T, d, E), dev))
+            db_post=vec(self.b_post), dw_pre=vec(self.w_pre), db_pre=vec(self.b_pre))
         return self._bwd
 
     def backward(self, x, dout, stream=None, dw_dtype=torch.float32, *, dlogits=None, following=None):
