@@ -1052,7 +1052,8 @@ class MoEBlock(MoELayer):
     A block's last pass can be the next one's first: with `following` a call writes
     following.u beside o (one read of the stream), and following is then called
     with normed=True.  Buffers are allocated once; a block's outputs and gradients
-    are valid until its next call.
+    are valid until its next call.  A backward is of the last call, and refused where
+    what it needs has been written over since.
 
     From its call to its backward a block keeps, of T tokens and S = T k slots: the
     experts' first product in microscaled 8 bits [S, d_ff], their outputs [S, d], y
@@ -1090,13 +1091,14 @@ class MoEBlock(MoELayer):
         if shares is None:
             # what blocks can share; the backward's part comes with its first call
             self._work = dict(u=torch.empty(T, d, **bf))
+            self._now = {}   # whose u and du the buffers hold: (block, the call before it or None), a call
         else:
             if not (shares.keep8 and self.keep8):
                 raise LuffyError("MoEBlock: blocks that share keep u in 8 bits (keep8=True)")
             if shares._sizes() != self._sizes():
                 raise LuffyError(f"MoEBlock: blocks that share are of the same sizes, not {shares._sizes()} and "
                                  f"{self._sizes()}")
-            self._work = shares._work
+            self._work, self._now = shares._work, shares._now
             for name in ("ws_route", "ws_condense", "ws_ffn"):
                 setattr(self.buf, name, getattr(shares.buf, name))
         self.u, self.o = self._work["u"], torch.empty(T, d, **bf)
@@ -1133,9 +1135,15 @@ class MoEBlock(MoELayer):
             raise LuffyError(f"x must be [{self.T}, {self.d}] {self.dtype}")
         if following is not None and (following is self or (following.norm, following.eps) != (self.norm, self.eps)):
             raise LuffyError("MoEBlock: blocks that share a pass must be two, of the same norm and eps")
-        self.normed, self.following, self.backed = normed, following, False
+        made = self._now.get("u", (None, None))
+        if normed and (made[0] is not self or made[1] is None):
+            raise LuffyError("MoEBlock: normed=True, but self.u is not what a call with this block as its `following` "
+                             "has left")
+        self.normed, self.following, self.backed, self.call = normed, following, False, object()
         if not normed:
+            made = self._now["u"] = (self, None)
             luffy_block_norm(x, None, None, self.u, w_pre=self.w_pre, b_pre=self.b_pre, **kw)
+        self.made = made
         super().__call__(self.u, stream, threshold, hist_in)
         if self.keep8:
             luffy_mx8_quantize(self.u, self.uq, self.us, stream)
@@ -1143,6 +1151,8 @@ class MoEBlock(MoELayer):
                          w_post=self.w_post, b_post=self.b_post, gate=self.gate,
                          w_pre=following.w_pre if following else None, b_pre=following.b_pre if following else None,
                          **kw)
+        if following:
+            following._now["u"] = (following, self.call)
         return self.o
 
     def _gradients(self, dw_dtype):
@@ -1182,8 +1192,14 @@ class MoEBlock(MoELayer):
         stream's gradient without the norm's share)."""
         if not hasattr(self, "backed") or following is not self.following:
             raise LuffyError("MoEBlock.backward: of a call, with the `following` that the call had")
-        if following is not None and not (following.backed and following.normed):
-            raise LuffyError("MoEBlock.backward: the following block, called with normed=True, comes first")
+        if following is not None:
+            if not (following.backed and following.normed and following.made[1] is self.call):
+                raise LuffyError("MoEBlock.backward: the following block, called with normed=True behind this call, "
+                                 "comes first")
+            if following._now["du"] is not following.call:
+                raise LuffyError("MoEBlock.backward: the following block's gradient has been written over")
+        if not self.keep8 and self._now["u"] is not self.made:
+            raise LuffyError("MoEBlock.backward: u has been written over (keep8 keeps one of its own)")
         b, g = self.buf, self._gradients(dw_dtype)
         kw = dict(norm=self.norm, eps=self.eps, stream=stream)
         S = self.T * self.k
@@ -1199,7 +1215,9 @@ class MoEBlock(MoELayer):
         luffy_expert_ffn_backward_kept(u, us, b.rep_token, b.rep_offsets, self.w1, self.w2, self.act, S, self.zq,
                                        self.zs, g["dy_rep"], g["dx_rep"], g["dw1"], g["dw2"], g["ws_f"], stream)
         if self.keep8:
+            self._now["u"] = (self, None)
             luffy_mx8_dequantize(self.uq, self.us, self.u, stream)
+        self._now["du"] = self.call
         luffy_route_scored_backward(self.u, self.w_gate, self.score, self.logits, b.topk_idx, g["dlayer"], g["du"],
                                     g["dw_gate"], g["db_gate"], g["ws_r"], renormalise=self.renormalise,
                                     scale=self.scale, dlogits=dlogits, dx_rep=g["dx_rep"], slot_pos=b.slot_pos,
