@@ -8,6 +8,7 @@ fallback: without the built library every call raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from dataclasses import dataclass
@@ -835,6 +836,18 @@ KERNELS = ("gate", "slot_scan", "slot_scatter", "norm", "gram", "gram_recheck", 
            "ffn2_reduce", "combine")
 
 
+def _on(stream):
+    """What is allocated under it belongs to the stream that will use it."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+def _hold(t: torch.Tensor, raw) -> None:
+    """t's memory stays t's until the stream of this handle is through with what it
+    has been given so far."""
+    if t.is_cuda:
+        t.record_stream(torch.cuda.ExternalStream(raw, device=t.device) if raw else torch.cuda.default_stream(t.device))
+
+
 def _workspace(nbytes: int, device) -> torch.Tensor:
     # torch's caching allocator hands out 512-byte aligned blocks
     return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
@@ -959,18 +972,18 @@ class MoELayer:
             raise LuffyError("MoELayer.backward: the expert FFN backward is bf16 only")
         S = self.T * self.k
         dev = dy.device
-        if getattr(self, "_bwd", None) is None or self._bwd["dw1"].dtype != dw_dtype:
+        if getattr(self, "_bwd", None) is None:
             E, dff, d = self.w1.shape
-            self._bwd = dict(
-                dy_rep=torch.empty_like(b.y_rep),
-                dgate=torch.empty(self.T, self.k, dtype=torch.float32, device=dev),
-                dx_rep=torch.empty(S, d, dtype=self.dtype, device=dev),
-                dw1=torch.empty(E, dff, d, dtype=dw_dtype, device=dev),
-                dw2=torch.empty(E, d, dff, dtype=dw_dtype, device=dev),
-                ws_c=_workspace(combine_backward_workspace_size(self.T, self.k, S), dev),
-                ws_f=_workspace(expert_ffn_backward_workspace_size(S, E, d, dff, LUFFY_BF16), dev),
-            )
+            with _on(stream):
+                self._bwd = dict(
+                    dy_rep=torch.empty_like(b.y_rep),
+                    dgate=torch.empty(self.T, self.k, dtype=torch.float32, device=dev),
+                    dx_rep=torch.empty(S, d, dtype=self.dtype, device=dev),
+                    ws_c=_workspace(combine_backward_workspace_size(self.T, self.k, S), dev),
+                    ws_f=_workspace(expert_ffn_backward_workspace_size(S, E, d, dff, LUFFY_BF16), dev),
+                )
         g = self._bwd
+        self._weight_gradients(g, dw_dtype, stream)
         luffy_combine_backward(dy, b.y_rep, b.rep_row, b.perm_token, b.slot_pos, b.topk_gate, b.offsets,
                                b.rep_offsets, g["dy_rep"], g["dgate"], g["ws_c"], stream)
         if b.x_rep is not None:
@@ -980,6 +993,19 @@ class MoELayer:
         luffy_expert_ffn_backward(src, idx, b.rep_offsets, self.w1, self.w2, self.act, S, g["dy_rep"],
                                   g["dx_rep"], g["dw1"], g["dw2"], g["ws_f"], stream)
         return g["dgate"], g["dx_rep"], g["dw1"], g["dw2"]
+
+    def _weight_gradients(self, g, dw_dtype, stream):
+        """dw1 and dw2 of dw_dtype in the backward's buffers g; those of another type
+        go when the stream that wrote them has."""
+        at, g["stream"] = g.get("stream"), _stream(stream) if self.w1.is_cuda else stream
+        if "dw1" in g:
+            if g["dw1"].dtype == dw_dtype:
+                return
+            for name in ("dw1", "dw2"):
+                _hold(g[name], at)
+        with _on(stream):
+            for name, w in (("dw1", self.w1), ("dw2", self.w2)):
+                g[name] = torch.empty(w.shape, dtype=dw_dtype, device=w.device)
 
     def __call__(self, x, stream=None, threshold=None, hist_in=None):
         if x.shape != (self.T, self.d) or x.dtype != self.dtype:
@@ -1155,10 +1181,15 @@ class MoEBlock(MoELayer):
             following._now["u"] = (following, self.call)
         return self.o
 
-    def _gradients(self, dw_dtype):
+    def _gradients(self, dw_dtype, stream=None):
         """Buffers of the backward, made on the first call."""
-        if getattr(self, "_bwd", None) is not None and self._bwd["dw1"].dtype == dw_dtype:
-            return self._bwd
+        if getattr(self, "_bwd", None) is None:
+            with _on(stream):
+                self._bwd = self._backward_buffers()
+        self._weight_gradients(self._bwd, dw_dtype, stream)
+        return self._bwd
+
+    def _backward_buffers(self):
         T, S, E, d, d_ff, dev = self.T, self.T * self.k, self.E, self.d, self.d_ff, self.w1.device
         f32 = dict(dtype=torch.float32, device=dev)
 
@@ -1173,13 +1204,10 @@ class MoEBlock(MoELayer):
                 ws_c=_workspace(combine_backward_workspace_size(T, self.k, S), dev),
                 ws_f=_workspace(expert_ffn_backward_kept_workspace_size(S, E, d, d_ff), dev),
                 ws_r=_workspace(route_scored_backward_workspace_size(T, d, E), dev))
-        self._bwd = dict(
+        return dict(
             self._work, dx=rows(T), dstream=rows(T), dw_gate=torch.empty(E, d, **f32), db_gate=torch.empty(E, **f32),
-            dw1=torch.empty(E, d_ff, d, dtype=dw_dtype, device=dev),
-            dw2=torch.empty(E, d, d_ff, dtype=dw_dtype, device=dev),
             dgate=None if self.gate is None else torch.empty_like(self.gate), dw_post=vec(self.w_post),
             db_post=vec(self.b_post), dw_pre=vec(self.w_pre), db_pre=vec(self.b_pre))
-        return self._bwd
 
     def backward(self, x, dout, stream=None, dw_dtype=torch.float32, *, dlogits=None, following=None):
         """Gradients of the last call for dout = dL/do (bf16 [T, d]) and, where an
@@ -1200,7 +1228,7 @@ class MoEBlock(MoELayer):
                 raise LuffyError("MoEBlock.backward: the following block's gradient has been written over")
         if not self.keep8 and self._now["u"] is not self.made:
             raise LuffyError("MoEBlock.backward: u has been written over (keep8 keeps one of its own)")
-        b, g = self.buf, self._gradients(dw_dtype)
+        b, g = self.buf, self._gradients(dw_dtype, stream)
         kw = dict(norm=self.norm, eps=self.eps, stream=stream)
         S = self.T * self.k
         nxt = following._bwd if following is not None else {}
