@@ -176,7 +176,8 @@ __device__ __forceinline__ void row_stats(const Chunk<BF16> (&c)[CH], int chunks
 
 // A row a team, in registers from its loads to its stores.  Bounded by HBM: 8192 x
 // 1024 bf16, layer norms and a token gate, 16.7 us, 5.0 TB/s; 16384 x 4096 129 us, 5.2
-// TB/s (a large copy: 4.9).  One row of 4096: 3.5 us, a launch and its loads' latency.
+// TB/s (a large copy: 4.9).  One row of 4096: 2.7 us, a launch and its loads' latency.
+// (float32 rows past 16384 columns: 32 registers spill; 2048 x 32768 364 us, 3.7 TB/s.)
 template <bool BF16, int CH, int WAVES>
 __global__ __launch_bounds__(WAVES > 1 ? WAVES * 64 : 256) void block_norm_kernel(NormArgs a, int lt_log2) {
   __shared__ float lds[3][16][4];
@@ -275,6 +276,12 @@ __global__ __launch_bounds__(WAVES > 1 ? WAVES * 64 : 256) void block_norm_kerne
 // TB/s in all (a large copy: 4.9); 272 and 25 us with two blocks a CU, nothing in
 // flight and row sums by ds_bpermute.  3001 x 1088 float32 31 and 6 us: four rows a
 // team, bound by their chains of loads and row sums.
+//   Two kinds of rows have more sums a lane than registers.  Past 8192 columns 16 waves
+// have 128 a lane for up to 160 sums: 121 to 683 spill, and bytes that take 164 us take
+// 479 (4096 x 16384 bf16, rms; 204 as 8192 x 8192), 714 with biases and layer norms, as
+// float32 1070 and 1405 for 329.  bf16 rows of 1025 to 1536 and 2049 to 3072 columns with
+// bias gradients, on blocks of nine to twelve waves, spill 20 to 28 (8192 x 2880 with
+// biases and layer norms 99 us, without 75).
 constexpr int kSums = 5;   // w_pre, b_pre, w_post, b_post, gate
 
 struct NormBwdArgs {
@@ -609,7 +616,7 @@ void launch_norm(const NormArgs& a, hipStream_t s) {
 // A team of the backward and the blocks of the grid (each leaves kSums rows of d sums
 // to be added up).  One chunk a lane on as many waves as a row fills; or two, which halves
 // the waves that wait for each other, from 16 rows a team on, where they fill three
-// quarters of the lanes (bf16, us, one | two chunks: 65536 x 1024 207 | 202, 32768 x 2048
+// quarters of the lanes (bf16, no bias gradients, us, one | two chunks: 65536 x 1024 207 | 202, 32768 x 2048
 // 211 | 199, 16384 x 4096 217 | 199, 8192 x 3520 105 | 99; 8192 x 2880 75 | 90, 8192 x
 // 2112 68 | 82, 32768 x 1088 148 | 160; 8192 x 1024 36 | 40; float32 3001 x 1088 33 | 36),
 // and, up to 1024 columns, where no bias gradient takes the registers (65536 x 1024 257 |

@@ -294,7 +294,9 @@ __global__ __launch_bounds__(1024) void cbwd_scan_kernel(const int32_t* __restri
 // slot's gate.  The chain (member, token, slots) is a group's latency, so that groups of
 // one are bound by it: 65536 tokens of 1024 bf16 with 8 slots each, no two alike, 481 us
 // for 2.1 GB; 660 with the slots looked up one after the other, 512 columns a wave and the
-// last member's row read four times.
+// last member's row read four times.  Of one or two slots, the same two: 16384 x 2 slots of
+// 2048 bf16 46 | 57, float32 94 | 112 (on 140 registers), 65536 x 1 of 1024 float32 91 |
+// 123, 8192 x 2 of 1024 float32 26 | 25.
 template <bool BF16, int K, int U>
 __global__ __launch_bounds__(256) void cbwd_rows_kernel(const void* __restrict__ dy,
                                                         const int32_t* __restrict__ perm_token,

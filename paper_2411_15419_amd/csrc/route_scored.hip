@@ -620,7 +620,7 @@ __device__ __forceinline__ void products64(const void* __restrict__ xv, const vo
 // part in the sum still could turn a choice.  The waves share these products.
 //   Bounded by its chains, not by bytes (32768 tokens, 32 experts, k 4: 12 MB): a block
 // takes some 4 us for the first choices, and one with an undecided token 2 for which
-// logits, 2 for the products and 3 for the decision; 18.7 us in all.  The softmax, the
+// logits, 2 for the products and 3 for the decision; 19.8 us in all.  The softmax, the
 // sigmoid and the groups are compiled apart (a runtime switch: 2 us more).  One block
 // per 64 tokens 23.7 us, eight waves per 32 22.9.
 //   T <= tok: the one block has every slot, and lays out the buckets as well.
