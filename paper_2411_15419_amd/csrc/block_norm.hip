@@ -279,9 +279,9 @@ __global__ __launch_bounds__(WAVES > 1 ? WAVES * 64 : 256) void block_norm_kerne
 //   Two kinds of rows have more sums a lane than registers.  Past 8192 columns 16 waves
 // have 128 a lane for up to 160 sums: 121 to 683 spill, and bytes that take 164 us take
 // 479 (4096 x 16384 bf16, rms; 204 as 8192 x 8192), 714 with biases and layer norms, as
-// float32 1070 and 1405 for 329.  bf16 rows of 1025 to 1536 and 2049 to 3072 columns with
-// bias gradients, on blocks of nine to twelve waves, spill 20 to 28 (8192 x 2880 with
-// biases and layer norms 99 us, without 75).
+// float32 1070 and 1405 for 329.  bf16 rows on three, five and six waves with bias
+// gradients, on blocks of nine to twelve waves, spill 20 to 28 (8192 x 2880 with biases and
+// layer norms 99 us, without 75).
 constexpr int kSums = 5;   // w_pre, b_pre, w_post, b_post, gate
 
 struct NormBwdArgs {
